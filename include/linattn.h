@@ -88,6 +88,7 @@ extern "C" {
 #define LINATTN_E_HIP        -7   /* a HIP launch reported an error */
 #define LINATTN_E_STATE      -8   /* linattn_bwd without a state buffer, or a state buffer too small for this B */
 #define LINATTN_E_ALIAS      -9   /* an output aliases an input */
+#define LINATTN_E_VALUE     -10   /* a number is outside its range (linattn_sight) */
 
 /* feature-map kinds */
 #define LINATTN_PHI_HEDGEHOG  1   /* Eq. 5 */
@@ -224,6 +225,102 @@ int linattn_fwd_noalloc(const void* q, const void* k, const void* v, void* out,
 int linattn_bwd(const void* q, const void* k, const void* v, const void* dout,
                 void* dq, void* dk, void* dv,
                 int B, int H, int n, int d, int phi_id, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Softmax attention: the softmax branch of a layer (its output is what linattn_phi_set_blend takes as blend_in, its upstream
+ * gradient is r' * dout), and the same attention for a chunk of new tokens over a paged cache, for generation piece by piece.
+ *
+ *   s_ij = scale q_i . k_j,   lse_i = log(sum_j exp(s_ij)),   o_i = sum_j exp(s_ij - lse_i) v_j
+ *
+ * with the sums over the keys that query i sees.  H query heads share HK key heads in groups of H / HK neighbours: query
+ * head h reads key head h / (H / HK).  Which keys a query sees goes by positions; the query at position p sees key j of a
+ * sequence of len tokens if
+ *
+ *   j < len,   and right < 0 or j <= p + right,   and left < 0 or j >= p - left or j < sinks
+ *
+ * (a window of left tokens before and right tokens after it, and the first `sinks` tokens as far as they are not
+ * beyond the window's right end; right = 0 is causal, a negative number is no limit).  A row that sees nothing has out = 0 and lse = -inf.
+ * The conventions at the top of this file hold.  Numbers in device memory (lengths, counts, tables) cannot be checked on the host: the
+ * kernels bring lengths and counts into range and take a table entry that names no page of the pool for keys that are not there.
+ *
+ * Numeric domain: scores, their softmax, and all sums are fp32.  LINATTN_BF16: the probabilities, and in the backward their gradients, enter the
+ * matrix cores as bf16 (the stored type of the values they multiply, so that neither has a range of its own); with the store of the
+ * result that is two roundings of 2^-9 relative each.  LINATTN_F32 and LINATTN_BF16_F32MATH: fp32 arithmetic.  The results of a row depend on the
+ * keys that it sees and on nothing else: an infinity or NaN in a token that it does not see, or in the padding, does not reach it.  */
+typedef struct linattn_sight {
+  int left, right, sinks;
+  float scale;            /* 0: 1 / sqrt(d) */
+} linattn_sight;
+
+/* q, out, dout, dq: H heads; k, v, dk, dv: HK heads; all of n tokens, in `layout`.  Token i of a batch item has position i. */
+typedef struct linattn_window_desc {
+  int dtype;              /* LINATTN_BF16, LINATTN_F32 or LINATTN_BF16_F32MATH: type of q, k, v, out, dout, dq, dk, dv */
+  int B, H, HK, n, d;     /* H a multiple of HK, d 64 or 128 */
+  int layout;             /* LINATTN_LAYOUT_BHND or LINATTN_LAYOUT_BNHD */
+  linattn_sight sight;
+  const int* lengths;     /* optional device [B]: tokens of each item, the others are padding.  Padding is not read; its rows of out, dq, dk, dv are
+                             zeros, of lse -inf.  NULL: n each. */
+  void* workspace;        /* linattn_window_bwd only: device scratch, 256-byte aligned, not shared by calls that overlap in time */
+  size_t workspace_bytes;
+} linattn_window_desc;
+
+/* Scratch bytes linattn_window_bwd needs (the forward needs none).  Pure function of the descriptor's numbers; 0 for an invalid one. */
+size_t linattn_window_workspace_bytes(const linattn_window_desc* desc);
+
+/* Forward.  lse: optional device fp32 [B, H, n], what the backward needs and what joins results over parts of the keys.
+ * Errors: E_NULL, E_DTYPE, E_SHAPE, E_VALUE, E_ALIGN, E_ALIAS, E_HIP. */
+int linattn_window_fwd(const linattn_window_desc* desc, const void* q, const void* k, const void* v, void* out, float* lse, void* stream);
+
+/* Backward for L with dL/dout = dout, from the forward's out and lse; writes dq, dk, dv (dk and dv summed over the query heads of a group).
+ * Errors: as above, and E_WORKSPACE. */
+int linattn_window_bwd(const linattn_window_desc* desc, const void* q, const void* k, const void* v, const void* out, const float* lse,
+                       const void* dout, void* dq, void* dk, void* dv, void* stream);
+
+/* How a cache holds rows of k and v */
+#define LINATTN_CACHE_BF16 1
+#define LINATTN_CACHE_E4M3 2    /* d codes of 8 bits (e4m3, the variant without infinities) and the exponent e of a scale 2^e, per token, head and
+                                   tensor: e = the least integer with max|x| 2^-e <= 448, at least -117; stored as the byte e + 127.  The codes round to
+                                   nearest even.  Scaled codes are bf16 numbers (none is 2^128: entries
+                                   that would round to it are held as 240 2^120), so reading back rounds no further.  Infinities become NaN; the maximum is
+                                   taken over the finite entries. */
+
+/*
+ * A paged cache of B sequences: position j of sequence b is row j % page of page table[b * width + j / page] of the pool.  Rows of a
+ * page's head lie together: the pools are [pages, H, page, d], the exponents [pages, H, page].
+ * A chunk of n tokens per sequence (k, v of a write; q, out of an attention) is bf16 [B, H, n, d] or [B, n, H, d]; its token t has position
+ * lengths[b] - counts[b] + t, and tokens from counts[b] on, or with a negative position, are padding: not read, not written
+ * to the cache, their rows of out are zeros and of lse -inf.  lengths counts the chunk, before the write as after.
+ */
+typedef struct linattn_cache_desc {
+  int type;               /* LINATTN_CACHE_BF16 or LINATTN_CACHE_E4M3 */
+  int B, H, d;            /* H: heads of k and v; d 64 or 128 */
+  int page, pages;        /* tokens to a page (any number), pages of the pool */
+  int width;              /* table entries of a sequence; page * width <= 2^30 */
+  int layout;             /* of the token tensors, not of the pool */
+  void *k, *v;            /* device, 16-byte aligned */
+  unsigned char *k_exp, *v_exp;      /* device; LINATTN_CACHE_E4M3 only */
+  const int* table;       /* device [B, width]; entries outside 0 .. pages-1 stand for no page */
+  const int* lengths;     /* device [B] */
+  const int* counts;      /* optional device [B]: new tokens of each sequence.  NULL: n */
+} linattn_cache_desc;
+
+/* Put the k and v rows of a chunk into the cache; nothing else in the pool changes.  No two tokens of a call may have the same place.
+ * Errors: E_NULL, E_DTYPE, E_SHAPE, E_ALIGN, E_ALIAS, E_HIP. */
+int linattn_cache_write(const linattn_cache_desc* desc, const void* k, const void* v, int n, void* stream);
+
+/* The first n tokens of every sequence as bf16 [B, H, n, d] or [B, n, H, d]; rows behind a sequence's end, or without a page, are zeros.
+ * counts is not looked at.  Errors: as above. */
+int linattn_cache_read(const linattn_cache_desc* desc, void* k, void* v, int n, void* stream);
+
+/* Scratch bytes linattn_cache_attn needs for chunks of n tokens of H query heads: pure function of the descriptor's numbers.  0 for an invalid
+ * argument. */
+size_t linattn_cache_workspace_bytes(const linattn_cache_desc* desc, int H, int n);
+
+/* Attention of a chunk of n tokens, H query heads, over the cache (which already holds the chunk's own keys).  n = 1 is the step of
+ * generation token by token.  lse: optional device fp32 [B, H, n].  workspace: 256-byte aligned, not shared by calls that overlap in time.
+ * Errors: as above, E_VALUE, E_WORKSPACE. */
+int linattn_cache_attn(const linattn_cache_desc* desc, const linattn_sight* sight, const void* q, void* out, float* lse, int H, int n,
+                       void* workspace, size_t workspace_bytes, void* stream);
 
 /* Static description of a status code. */
 const char* linattn_strerror(int status);

@@ -13,15 +13,18 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "liblinattn.so")
 
 OK = 0
-E_NULL, E_SHAPE, E_DTYPE, E_ALIGN, E_PHI, E_WORKSPACE, E_HIP, E_STATE, E_ALIAS = range(-1, -10, -1)
+E_NULL, E_SHAPE, E_DTYPE, E_ALIGN, E_PHI, E_WORKSPACE, E_HIP, E_STATE, E_ALIAS, E_VALUE = range(-1, -11, -1)
 PHI_HEDGEHOG = 1
 PHI_RELU = 2
 BF16, F32, BF16_F32MATH = 1, 2, 3
 LAYOUT_BHND, LAYOUT_BNHD = 0, 1
 FLAG_CENTRED = 1
+CACHE_BF16, CACHE_E4M3 = 1, 2
 
 EXPORTS = ("linattn_phi_create", "linattn_phi_destroy", "linattn_workspace_bytes", "linattn_workspace_bytes_wgrads",
-           "linattn_fwd", "linattn_fwd_noalloc", "linattn_bwd", "linattn_strerror", "linattn_set_stage_events", "linattn_phi_set_blend")
+           "linattn_fwd", "linattn_fwd_noalloc", "linattn_bwd", "linattn_strerror", "linattn_set_stage_events", "linattn_phi_set_blend",
+           "linattn_window_workspace_bytes", "linattn_window_fwd", "linattn_window_bwd",
+           "linattn_cache_workspace_bytes", "linattn_cache_write", "linattn_cache_read", "linattn_cache_attn")
 
 
 class PhiDesc(ctypes.Structure):
@@ -35,6 +38,27 @@ class PhiDesc(ctypes.Structure):
         ("blend_in", ctypes.c_void_p), ("blend_r", ctypes.c_void_p), ("blend_dr", ctypes.c_void_p),
         ("state_bytes", ctypes.c_size_t),
         ("flags", ctypes.c_uint),
+    ]
+
+
+class Sight(ctypes.Structure):
+    _fields_ = [("left", ctypes.c_int), ("right", ctypes.c_int), ("sinks", ctypes.c_int), ("scale", ctypes.c_float)]
+
+
+class WindowDesc(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int), ("B", ctypes.c_int), ("H", ctypes.c_int), ("HK", ctypes.c_int), ("n", ctypes.c_int), ("d", ctypes.c_int),
+        ("layout", ctypes.c_int), ("sight", Sight), ("lengths", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
+class CacheDesc(ctypes.Structure):
+    _fields_ = [
+        ("type", ctypes.c_int), ("B", ctypes.c_int), ("H", ctypes.c_int), ("d", ctypes.c_int), ("page", ctypes.c_int), ("pages", ctypes.c_int),
+        ("width", ctypes.c_int), ("layout", ctypes.c_int), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("k_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p), ("table", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
+        ("counts", ctypes.c_void_p),
     ]
 
 
@@ -73,6 +97,21 @@ def lib() -> ctypes.CDLL:
         L.linattn_bwd.restype = ci
         L.linattn_set_stage_events.argtypes = [ctypes.POINTER(vp)]
         L.linattn_set_stage_events.restype = ci
+        wd, cd = ctypes.POINTER(WindowDesc), ctypes.POINTER(CacheDesc)
+        L.linattn_window_workspace_bytes.argtypes = [wd]
+        L.linattn_window_workspace_bytes.restype = ctypes.c_size_t
+        L.linattn_window_fwd.argtypes = [wd] + [vp] * 6
+        L.linattn_window_fwd.restype = ci
+        L.linattn_window_bwd.argtypes = [wd] + [vp] * 10
+        L.linattn_window_bwd.restype = ci
+        L.linattn_cache_workspace_bytes.argtypes = [cd, ci, ci]
+        L.linattn_cache_workspace_bytes.restype = ctypes.c_size_t
+        L.linattn_cache_write.argtypes = [cd, vp, vp, ci, vp]
+        L.linattn_cache_write.restype = ci
+        L.linattn_cache_read.argtypes = [cd, vp, vp, ci, vp]
+        L.linattn_cache_read.restype = ci
+        L.linattn_cache_attn.argtypes = [cd, ctypes.POINTER(Sight), vp, vp, vp, ci, ci, vp, ctypes.c_size_t, vp]
+        L.linattn_cache_attn.restype = ci
         L.linattn_strerror.argtypes = [ci]
         L.linattn_strerror.restype = ctypes.c_char_p
         _lib = L
@@ -153,6 +192,48 @@ def linattn_bwd(q, k, v, dout, dq, dk, dv, B, H, n, d, phi_id, stream=None, *, c
     if st != OK and check:
         raise LinattnError(st, "linattn_bwd")
     return st
+
+
+def _ref(desc):
+    return None if desc is None else ctypes.byref(desc)
+
+
+def _done(st: int, where: str, check: bool) -> int:
+    if st != OK and check:
+        raise LinattnError(st, where)
+    return st
+
+
+def linattn_window_workspace_bytes(desc) -> int:
+    return int(lib().linattn_window_workspace_bytes(_ref(desc)))
+
+
+def linattn_window_fwd(desc, q, k, v, out, lse=None, stream=None, *, check: bool = True) -> int:
+    return _done(lib().linattn_window_fwd(_ref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), _ptr(stream)),
+                 "linattn_window_fwd", check)
+
+
+def linattn_window_bwd(desc, q, k, v, out, lse, dout, dq, dk, dv, stream=None, *, check: bool = True) -> int:
+    return _done(lib().linattn_window_bwd(_ref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), _ptr(dout),
+                                          _ptr(dq), _ptr(dk), _ptr(dv), _ptr(stream)), "linattn_window_bwd", check)
+
+
+def linattn_cache_workspace_bytes(desc, H: int, n: int) -> int:
+    return int(lib().linattn_cache_workspace_bytes(_ref(desc), H, n))
+
+
+def linattn_cache_write(desc, k, v, n: int, stream=None, *, check: bool = True) -> int:
+    return _done(lib().linattn_cache_write(_ref(desc), _ptr(k), _ptr(v), n, _ptr(stream)), "linattn_cache_write", check)
+
+
+def linattn_cache_read(desc, k, v, n: int, stream=None, *, check: bool = True) -> int:
+    return _done(lib().linattn_cache_read(_ref(desc), _ptr(k), _ptr(v), n, _ptr(stream)), "linattn_cache_read", check)
+
+
+def linattn_cache_attn(desc, sight, q, out, lse, H: int, n: int, workspace=None, workspace_bytes: int = 0, stream=None, *,
+                       check: bool = True) -> int:
+    return _done(lib().linattn_cache_attn(_ref(desc), _ref(sight), _ptr(q), _ptr(out), _ptr(lse), H, n, _ptr(workspace),
+                                          workspace_bytes, _ptr(stream)), "linattn_cache_attn", check)
 
 
 def linattn_set_stage_events(events) -> int:

@@ -10,7 +10,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblinattn.so")
 PROBE_LIB = os.path.join(HERE, "libmembw_probe.so")      # bench.py's streaming-rate probe, a library of its own
 PROBE_SOURCE = "membw_probe.hip"
-SOURCES = ["api.cpp", "fwd_f32.hip", "fwd_bf16.hip", "state_reduce.hip", "bwd_bf16.hip", "bwd_bf16_stream.hip", "bwd_f32.hip", "relu_bf16.hip"]
+SOURCES = ["api.cpp", "fwd_f32.hip", "fwd_bf16.hip", "state_reduce.hip", "bwd_bf16.hip", "bwd_bf16_stream.hip", "bwd_f32.hip", "relu_bf16.hip",
+           "api_attn.cpp", "window.hip", "cache.hip"]
 # Packed-fp32 VALU forms are switched off for every device compilation.
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

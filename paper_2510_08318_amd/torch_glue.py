@@ -2,9 +2,11 @@
 
 Nothing of the operator is computed here; `Layer` owns the buffers a converted attention layer
 needs (W~_q, W~_k, state, workspace), registers them as a phi descriptor and forwards to
-linattn_fwd / linattn_bwd.
+linattn_fwd / linattn_bwd.  `window_attention`, `window_attention_backward` and `PagedCache` do the same for the softmax branch.
 """
 from __future__ import annotations
+
+import functools
 
 import numpy as np
 import torch
@@ -165,3 +167,165 @@ class Layer:
         dv = torch.empty_like(q) if dv is None else dv
         B_.linattn_bwd(q, k, v, dout, dq, dk, dv, Bq, H, n, d, self.phi_id, _current_stream())
         return dq, dk, dv
+
+
+# ---- softmax attention: a sliding window with first tokens that stay visible, and a paged cache ---------------------------
+# Scratch memory comes from torch's allocator call by call, so that calls on several streams, or captured into several graphs, share none.
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _on_device_of(fn):
+    """Runs `fn` with the device of its first tensor argument current (the library launches on the current device)."""
+    @functools.wraps(fn)
+    def call(*args, **kw):
+        t = args[0] if isinstance(args[0], torch.Tensor) else args[0].k
+        _need(t.is_cuda, "tensors must be on the GPU")
+        if t.device.index == torch.cuda.current_device():
+            return fn(*args, **kw)
+        with torch.cuda.device(t.device):
+            return fn(*args, **kw)
+    return call
+
+
+def _check_tokens(name, t, shape, dtype, device):
+    _need(t.device == device and t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous(),
+          f"{name}: expected a contiguous {dtype} tensor {tuple(shape)} on {device}")
+
+
+def _check_ints(name, t, shape, device):
+    if t is not None:
+        _check_tokens(name, t, shape, torch.int32, device)
+
+
+def _token_dims(t, layout):
+    """(B, heads, n, d) of a token tensor."""
+    _need(layout in ("bhnd", "bnhd"), "layout is 'bhnd' or 'bnhd'")
+    _need(t.dim() == 4, "expected four dimensions")
+    B, x, y, d = t.shape
+    return (B, y, x, d) if layout == "bnhd" else (B, x, y, d)
+
+
+def _token_shape(B, heads, n, d, layout):
+    return (B, n, heads, d) if layout == "bnhd" else (B, heads, n, d)
+
+
+def _window_desc(q, k, v, left, right, sinks, scale, layout, lengths, f32_math):
+    B, H, n, d = _token_dims(q, layout)
+    HK = _token_dims(k, layout)[1]
+    _need(q.dtype in (torch.bfloat16, torch.float32), "bf16 or fp32 tensors")
+    _check_tokens("q", q, q.shape, q.dtype, q.device)
+    for name, t in (("k", k), ("v", v)):
+        _check_tokens(name, t, _token_shape(B, HK, n, d, layout), q.dtype, q.device)
+    _check_ints("lengths", lengths, (B,), q.device)
+    dtype = (B_.BF16_F32MATH if f32_math else B_.BF16) if q.dtype == torch.bfloat16 else B_.F32
+    return B_.WindowDesc(dtype, B, H, HK, n, d, B_.LAYOUT_BNHD if layout == "bnhd" else B_.LAYOUT_BHND,
+                         B_.Sight(left, right, sinks, scale), B_._ptr(lengths), None, 0)
+
+
+@_on_device_of
+def window_attention(q, k, v, *, left=-1, right=-1, sinks=0, scale=0.0, layout="bhnd", lengths=None, f32_math=False, out=None, lse=None):
+    """Softmax attention in which token i sees tokens i - left .. i + right and the first `sinks` tokens (up to i + right); a negative
+    limit is none, right=0 is causal.  q [B, H, n, d] ("bhnd") or [B, n, H, d] ("bnhd"); k, v with H or a divisor of H heads.
+    lengths: int32 [B], the tokens of each item; the rest is padding.  scale: 0 for 1/sqrt(d).  f32_math: fp32 arithmetic on bf16 tensors.
+    Returns (out, lse); lse is fp32 [B, H, n]."""
+    desc = _window_desc(q, k, v, left, right, sinks, scale, layout, lengths, f32_math)
+    out = torch.empty_like(q) if out is None else out
+    lse = torch.empty((desc.B, desc.H, desc.n), dtype=torch.float32, device=q.device) if lse is None else lse
+    _check_tokens("out", out, q.shape, q.dtype, q.device)
+    _check_tokens("lse", lse, (desc.B, desc.H, desc.n), torch.float32, q.device)
+    B_.linattn_window_fwd(desc, q, k, v, out, lse, _current_stream())
+    return out, lse
+
+
+@_on_device_of
+def window_attention_backward(q, k, v, out, lse, dout, *, left=-1, right=-1, sinks=0, scale=0.0, layout="bhnd", lengths=None,
+                              f32_math=False, dq=None, dk=None, dv=None):
+    """Gradients of window_attention (same keyword arguments) for the upstream gradient dout, from its out and lse."""
+    desc = _window_desc(q, k, v, left, right, sinks, scale, layout, lengths, f32_math)
+    dq, dk, dv = [torch.empty_like(t) if g is None else g for g, t in ((dq, q), (dk, k), (dv, v))]
+    for name, t, like in (("out", out, q), ("dout", dout, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, v)):
+        _check_tokens(name, t, like.shape, q.dtype, q.device)
+    _check_tokens("lse", lse, (desc.B, desc.H, desc.n), torch.float32, q.device)
+    size = B_.linattn_window_workspace_bytes(desc)
+    work = torch.empty(size, dtype=torch.uint8, device=q.device)
+    desc.workspace, desc.workspace_bytes = B_._ptr(work), size
+    B_.linattn_window_bwd(desc, q, k, v, out, lse, dout, dq, dk, dv, _current_stream())
+    return dq, dk, dv
+
+
+class PagedCache:
+    """Keys and values of B sequences in pages of a pool (see linattn_cache_desc).  k, v: [pages, H, page, d], bfloat16 or float8_e4m3fn; k_exp,
+    v_exp (float8 only): uint8 [pages, H, page]; table: int32 [B, width]; lengths: int32 [B].  The caller owns the tensors and writes table
+    and lengths: a chunk's tokens are counted in lengths before it is written or attended to."""
+
+    def __init__(self, k, v, table, lengths, k_exp=None, v_exp=None):
+        _need(k.dim() == 4 and k.dtype in (torch.bfloat16, torch.float8_e4m3fn), "k: a bf16 or float8_e4m3fn tensor [pages, H, page, d]")
+        _need(table.dim() == 2, "table: [B, width]")
+        self.k, self.v, self.table, self.lengths, self.k_exp, self.v_exp = k, v, table, lengths, k_exp, v_exp
+        self.pages, self.H, self.page, self.d = k.shape
+        self.B, self.width = table.shape
+        quantised = k.dtype == torch.float8_e4m3fn
+        for name, t in (("k", k), ("v", v)):
+            _check_tokens(name, t, k.shape, k.dtype, k.device)
+        _check_ints("table", table, table.shape, k.device)
+        _check_ints("lengths", lengths, (self.B,), k.device)
+        _need((k_exp is not None and v_exp is not None) == quantised, "k_exp and v_exp go with float8 rows")
+        for name, t in (("k_exp", k_exp), ("v_exp", v_exp)):
+            if t is not None:
+                _check_tokens(name, t, k.shape[:3], torch.uint8, k.device)
+        self._desc = B_.CacheDesc(B_.CACHE_E4M3 if quantised else B_.CACHE_BF16, self.B, self.H, self.d, self.page, self.pages, self.width,
+                                  0, *[B_._ptr(t) for t in (k, v, k_exp, v_exp, table, lengths)], None)
+
+    @classmethod
+    def empty(cls, pages, page, H, d, B, width, *, quantised=False, device="cuda"):
+        """A pool of `pages` pages of `page` tokens, tables that name no page, lengths zero."""
+        rows = [torch.empty((pages, H, page, d), dtype=torch.float8_e4m3fn if quantised else torch.bfloat16, device=device) for _ in range(2)]
+        exps = [torch.empty((pages, H, page), dtype=torch.uint8, device=device) if quantised else None for _ in range(2)]
+        return cls(*rows, torch.full((B, width), -1, dtype=torch.int32, device=device), torch.zeros(B, dtype=torch.int32, device=device), *exps)
+
+    def _describe(self, layout, counts):
+        _check_ints("counts", counts, (self.B,), self.k.device)
+        desc = B_.CacheDesc.from_buffer_copy(self._desc)
+        desc.layout, desc.counts = B_.LAYOUT_BNHD if layout == "bnhd" else B_.LAYOUT_BHND, B_._ptr(counts)
+        return desc
+
+    @_on_device_of
+    def write(self, k, v, *, counts=None, layout="bnhd"):
+        """Put a chunk's rows into the cache.  k, v: bf16 [B, n, H, d] or [B, H, n, d]; counts: int32 [B], the new tokens of each sequence
+        (None: n), at its positions lengths - counts, ..."""
+        n = _token_dims(k, layout)[2]
+        for name, t in (("k", k), ("v", v)):
+            _check_tokens(name, t, _token_shape(self.B, self.H, n, self.d, layout), torch.bfloat16, self.k.device)
+        B_.linattn_cache_write(self._describe(layout, counts), k, v, n, _current_stream())
+
+    @_on_device_of
+    def read(self, n, *, layout="bnhd", k=None, v=None):
+        """The first n tokens of every sequence as bf16 tensors (k, v); zeros behind a sequence's end."""
+        _need(layout in ("bhnd", "bnhd"), "layout is 'bhnd' or 'bnhd'")
+        shape = _token_shape(self.B, self.H, n, self.d, layout)
+        k, v = [torch.empty(shape, dtype=torch.bfloat16, device=self.k.device) if t is None else t for t in (k, v)]
+        for name, t in (("k", k), ("v", v)):
+            _check_tokens(name, t, shape, torch.bfloat16, self.k.device)
+        B_.linattn_cache_read(self._describe(layout, None), k, v, n, _current_stream())
+        return k, v
+
+    @_on_device_of
+    def attend(self, q, *, counts=None, left=-1, right=0, sinks=0, scale=0.0, layout="bnhd", out=None, lse=None):
+        """Attention of a chunk over the cache, which holds the chunk's own keys already (write).  q: bf16 [B, n, H, d] or [B, H, n, d] with a
+        multiple of the cache's heads; left, right, sinks, scale as in window_attention, by position in the sequence.
+        Returns (out, lse); lse is fp32 [B, H, n]."""
+        B, H, n, d = _token_dims(q, layout)
+        _check_tokens("q", q, _token_shape(self.B, H, n, self.d, layout), torch.bfloat16, self.k.device)
+        out = torch.empty_like(q) if out is None else out
+        lse = torch.empty((B, H, n), dtype=torch.float32, device=q.device) if lse is None else lse
+        _check_tokens("out", out, q.shape, q.dtype, q.device)
+        _check_tokens("lse", lse, (B, H, n), torch.float32, q.device)
+        desc = self._describe(layout, counts)
+        size = B_.linattn_cache_workspace_bytes(desc, H, n)
+        work = torch.empty(size, dtype=torch.uint8, device=q.device) if size else None
+        B_.linattn_cache_attn(desc, B_.Sight(left, right, sinks, scale), q, out, lse, H, n, work, size, _current_stream())
+        return out, lse
