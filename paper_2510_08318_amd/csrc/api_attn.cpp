@@ -34,12 +34,12 @@ int check_heads(int B, int H, int HK, int n, int d, int layout) {
   if (B <= 0 || H <= 0 || HK <= 0 || n <= 0 || H % HK) return LINATTN_E_SHAPE;
   if (d != 64 && d != 128) return LINATTN_E_SHAPE;
   if (layout != LINATTN_LAYOUT_BHND && layout != LINATTN_LAYOUT_BNHD) return LINATTN_E_SHAPE;
-  if ((long long)B * H > 65535 || n > kMostTokens) return LINATTN_E_SHAPE;
+  if ((long long)B * H > 65535 || (long long)n * (H / HK) > kMostTokens) return LINATTN_E_SHAPE;
   return LINATTN_OK;
 }
 
 struct WindowSizes {
-  size_t q, k, lse, work;      // bytes of a tensor of H heads, of HK heads, of lse, of the workspace
+  size_t q, k, lse, parts, work;      // bytes of a tensor of H heads, of HK heads, of lse; where the parts start in the workspace, its size
 };
 int check_window(const linattn_window_desc* w, WindowArgs* a, WindowSizes* z) {
   if (!w) return LINATTN_E_NULL;
@@ -56,7 +56,9 @@ int check_window(const linattn_window_desc* w, WindowArgs* a, WindowSizes* z) {
   z->q = (size_t)w->B * w->H * w->n * w->d * esz;
   z->k = (size_t)w->B * w->HK * w->n * w->d * esz;
   z->lse = (size_t)w->B * w->H * w->n * sizeof(float);
-  z->work = (z->lse + 255) & ~(size_t)255;
+  z->parts = (2 * z->lse + 255) & ~(size_t)255;
+  z->work = z->parts;
+  if (w->dtype == LINATTN_BF16) z->work += (size_t)key_split(w->B * w->HK, w->H / w->HK, w->n, w->d, a->sight).parts * 2 * key_block(w->d) * w->d * sizeof(float);
   return LINATTN_OK;
 }
 
@@ -145,7 +147,9 @@ int linattn_window_bwd(const linattn_window_desc* w, const void* q, const void* 
   if (any_overlap(outs, ins)) return LINATTN_E_ALIAS;
   a.q = q; a.k = k; a.v = v; a.out = out; a.dout = dout; a.dq = dq; a.dk = dk; a.dv = dv;
   a.lse = const_cast<float*>(lse);
-  a.delta = static_cast<float*>(w->workspace);
+  a.nl = static_cast<float*>(w->workspace);
+  a.nd = a.nl + (size_t)w->B * w->H * w->n;
+  a.parts = reinterpret_cast<float*>(static_cast<char*>(w->workspace) + z.parts);
   a.stream = static_cast<hipStream_t>(stream);
   return launch_window_bwd(a, w->dtype) == hipSuccess ? LINATTN_OK : LINATTN_E_HIP;
 }

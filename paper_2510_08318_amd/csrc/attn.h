@@ -29,12 +29,47 @@ __host__ __device__ inline int clamp_length(const int* lengths, int b, int n) {
   return x < 0 ? 0 : x < n ? x : n;
 }
 
+// Rows that see at most this many keys take delta from a pass over them (window_dq_kernel).
+constexpr int kFewKeys = 256;
+
+// How the key side of the bf16 backward is dealt: blocks of key_block(d) keys, the ones that hold first tokens, which all later queries see, to sink_share
+// workgroups each, the others to `share`; the parts of a block that has several are summed afterwards.
+constexpr int kQueryTile = 64;
+constexpr int key_block(int d) { return d == 128 ? 256 : 128; }
+struct KeySplit {
+  int blocks, sink_blocks, sink_share, share;
+  long long workgroups, parts;      // parts: of the blocks that have several workgroups
+};
+inline KeySplit key_split(int heads, int G, int n, int d, const Sight& s) {
+  KeySplit r{};
+  const int kKeyBlock = key_block(d), slots = kCUs * 256 / kKeyBlock;      // resident workgroups
+  r.blocks = (n + kKeyBlock - 1) / kKeyBlock;
+  r.sink_blocks = s.left < 0 ? 0 : (int)(((long long)(s.sinks < n ? s.sinks : n) + kKeyBlock - 1) / kKeyBlock);
+  const long long all = (n + kQueryTile - 1) / kQueryTile;
+  long long window = s.left < 0 || s.right < 0 ? all : ((long long)s.left + s.right + kKeyBlock) / kQueryTile + 1;
+  if (window > all) window = all;
+  // tiles of a block of each kind, of the whole call
+  const long long sink_tiles = all * G, tiles = window * G;
+  const long long total = heads * (r.sink_blocks * sink_tiles + (r.blocks - r.sink_blocks) * tiles);
+  // A workgroup's share: two thirds of what an even deal to the resident ones would give, at least 8 tiles.
+  long long most = total * 2 / (3 * slots);
+  if (most < 8) most = 8;
+  auto shares = [&](long long t) { const long long x = (t + most - 1) / most; return (int)(x < 1 ? 1 : x < 64 ? x : 64); };
+  r.sink_share = shares(sink_tiles);
+  r.share = shares(tiles);
+  r.workgroups = (long long)heads * ((long long)r.sink_blocks * r.sink_share + (long long)(r.blocks - r.sink_blocks) * r.share);
+  r.parts = (long long)heads * ((r.sink_share > 1 ? (long long)r.sink_blocks * r.sink_share : 0) +
+                                (r.share > 1 ? (long long)(r.blocks - r.sink_blocks) * r.share : 0));
+  return r;
+}
+
 // One call of linattn_window_fwd / linattn_window_bwd.
 struct WindowArgs {
   const void *q, *k, *v, *out, *dout;
   void *o, *dq, *dk, *dv;
   float* lse;               // written by the forward, read by the backward
-  float* delta;             // fp32 [B*H][n], workspace of the backward
+  float *nl, *nd;           // workspace of the backward: fp32 [B*H][n] each, -lse / scale (-inf where nothing is seen) and -delta
+  float* parts;             // and (bf16) fp32 [part][2][key block][d], the parts of key_split
   const int* lengths;       // nullable
   int B, H, HK, n, d;
   Rows qr, kr;              // rows of q, out, dout, dq and of k, v, dk, dv

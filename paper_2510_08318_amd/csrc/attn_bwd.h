@@ -1,0 +1,448 @@
+// Backward of windowed softmax attention on the matrix cores (bf16 operands, fp32 scores, gradients and sums), without atomics: one kernel owns the
+// rows of dq, one those of dk and dv, and each works the probabilities out again from the forward's lse.
+#pragma once
+#include "attn_rows.h"
+#include "mfma16.h"
+
+namespace linattn {
+namespace attn {
+
+constexpr int BT = 64;                       // keys, or queries, of a tile
+
+struct BwdRows {
+  const void *q, *k, *v, *out, *dout;
+  void *dq, *dk, *dv;
+  const float* lse;
+  float *nl, *nd;           // fp32 [B*H][n], written by the query side: -lse / scale (-inf where nothing is seen), -delta
+  float* parts;             // fp32 [part][2][key_block][D]: dk (not yet scaled) and dv of the key blocks that several workgroups share
+  const int* lengths;
+  int B, H, HK, G, n;
+  int blocks;               // row blocks, or key blocks, of a (batch item, key head)
+  int sink_blocks;          // key blocks that hold first tokens
+  int sink_share, share;    // workgroups to such a block, to another
+  Rows qr, kr;
+  Sight sight;
+  float scale, scale2;
+};
+
+__device__ __forceinline__ uint4 pack8(const f32x16& e, int h) {
+  return make_uint4(pack_bf16x2(e[8 * h], e[8 * h + 1]), pack_bf16x2(e[8 * h + 2], e[8 * h + 3]), pack_bf16x2(e[8 * h + 4], e[8 * h + 5]),
+                    pack_bf16x2(e[8 * h + 6], e[8 * h + 7]));
+}
+// ---- dq -----------------------------------------------------------------------------------
+// Queries on the lanes, as in the forward: S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T.
+// EXACT: delta from a first pass over the keys, sum_j p_ij dp_ij, and not from dout . out.  Where a row sees few keys its output is as large as the
+// values, and the rounding of the stored output would be the largest error of dq and dk.
+template <int D, bool EXACT>
+__global__ __launch_bounds__(256, 2) void window_dq_kernel(BwdRows a) {
+  constexpr int NW = 4, KB = BT / 32, KS = D / 16, CB = D / 32, BM = 32 * NW, TILE = BT * D * 2;
+  extern __shared__ __align__(16) char smem[];
+  const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
+  const int id = xcd_stretch(blockIdx.x, gridDim.x), bk = id / a.blocks, block = row_block(a.sight, id % a.blocks, a.blocks);
+  const int b = bk / a.HK, hk = bk % a.HK, G = a.G;
+  const int len = clamp_length(a.lengths, b, a.n), rows = len * G, all = a.n * G;
+  const int row0 = block * BM + w * 32;
+
+  const int r0 = row0 + m, t = r0 / G, h = hk * G + (r0 - t * G);
+  const bool store = r0 < all, live = r0 < rows;
+  const size_t at = (size_t)b * a.qr.sb + (size_t)h * a.qr.sh + (size_t)t * a.qr.sn, li = ((size_t)b * a.H + h) * a.n + t;
+  const int lo = live ? key_lo(a.sight, t) : 0, hi = live ? key_hi(a.sight, t, len) : 0;
+  uint4 q[KS], go[KS];
+  float delta = 0.f, lse = live ? a.lse[li] : -INFINITY;
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    const size_t c = at + 16 * ks + 8 * g;
+    q[ks] = live ? *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + c) : make_uint4(0, 0, 0, 0);
+    go[ks] = live ? *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.dout) + c) : make_uint4(0, 0, 0, 0);
+  }
+  if (!EXACT) {
+    uint4 ov[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+      ov[ks] = live ? *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.out) + at + 16 * ks + 8 * g) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      float x[8], y[8];
+      unpack_bf16x8(ov[ks], x);
+      unpack_bf16x8(go[ks], y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) delta = fmaf(x[e], y[e], delta);
+    }
+    float x, y;
+    pair32(delta, x, y);
+    delta = x + y;
+  }
+  const bool some = lse != -INFINITY;
+  const float nl2 = some ? -lse * kLog2e : -INFINITY;
+
+  const int last_row = ((block + 1) * BM < rows ? (block + 1) * BM : rows) - 1, wlast = (row0 + 32 < rows ? row0 + 32 : rows) - 1;
+  const KeyTiles<BT> tiles(a.sight, block * BM / G, last_row < block * BM ? -1 : last_row / G, len);
+  const WaveSight sight(a.sight, row0 / G, wlast < row0 ? -1 : wlast / G, len, row0 + 32 <= rows);
+  const size_t kv = (size_t)b * a.kr.sb + (size_t)hk * a.kr.sh, pitch = a.kr.sn * 2;
+  const char *kbase = static_cast<const char*>(a.k) + kv * 2, *vbase = static_cast<const char*>(a.v) + kv * 2;
+  const RowTile<D, NW, BT> loader(w, lane);
+  const uint32_t lds = lds_address(smem);
+  auto request = [&](int i) {
+    const int j0 = tiles.start(i);
+    const uint32_t to = lds + (uint32_t)(i & 1) * 2 * TILE;
+    loader.load(kbase, pitch, j0, tiles.end, to, w);
+    loader.load(vbase, pitch, j0, tiles.end, to + TILE, w);
+  };
+  const uint32_t rows_at = row_at<D>(lane), turned_rows = turned_at<D>(lane);
+
+  f32x16 dq[CB];
+#pragma unroll
+  for (int c = 0; c < CB; ++c) dq[c] = fill16(0.f);
+
+  // one pass over the tiles: use(kb, p, dp, kt) of the probabilities and dP of 32 keys
+  auto pass = [&](auto use) {
+    if (tiles.count) request(0);
+    lds_loads_landed();
+    __syncthreads();
+    for (int it = 0; it < tiles.count; ++it) {
+      if (it + 1 < tiles.count) request(it + 1);
+      const int j0 = tiles.start(it);
+      const uint32_t kt = lds + (uint32_t)(it & 1) * 2 * TILE, vt = kt + TILE;
+      if (!sight.nothing(j0, BT)) {
+        const bool plain = sight.everything(j0, BT);
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+          f32x16 s = fill16(0.f), dp = fill16(0.f);
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) {
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(row_chunk<D>(kt + rows_at, ks, 32 * kb)), as_bf16x8(q[ks]), s, 0, 0, 0);
+            dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(row_chunk<D>(vt + rows_at, ks, 32 * kb)), as_bf16x8(go[ks]), dp, 0, 0, 0);
+          }
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale2, nl2));
+          if (!plain) {
+            asm volatile("");        // a branch: as selects, the mask is computed for every tile
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int j = j0 + 32 * kb + 8 * (r / 4) + 4 * g + r % 4;
+              const bool on = j < hi && (j >= lo || j < a.sight.sinks);
+              s[r] = on ? s[r] : 0.f;
+              dp[r] = on ? dp[r] : 0.f;
+            }
+          }
+          use(kb, s, dp, kt);
+        }
+      }
+      lds_loads_landed();
+      __syncthreads();
+    }
+  };
+  if (EXACT) {
+    pass([&](int, const f32x16& p, const f32x16& dp, uint32_t) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) delta = fmaf(p[r], dp[r], delta);
+    });
+    float x, y;
+    pair32(delta, x, y);
+    delta = x + y;
+  }
+  if (store && g == 0) {
+    a.nl[li] = some ? -lse / a.scale : -INFINITY;
+    a.nd[li] = -delta;
+  }
+  pass([&](int kb, const f32x16& p, f32x16& dp, uint32_t kt) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dp[r] = p[r] * (dp[r] - delta);
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+      const uint4 ds = pack8(dp, st);
+#pragma unroll
+      for (int c = 0; c < CB; ++c) {
+        dq[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(turned<D>(kt + turned_rows, c, 16 * (2 * kb + st)), as_bf16x8(ds), dq[c], 0, 0, 0);
+      }
+    }
+  });
+
+  // Masked keys have dS = 0, which an infinity or NaN in k would make NaN: rows that come out not finite are done again key by key.
+  if (!sight.whole && !live) {
+#pragma unroll
+    for (int c = 0; c < CB; ++c) dq[c] = fill16(0.f);
+  }
+  float test = 0.f;
+#pragma unroll
+  for (int c = 0; c < CB; ++c)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) test = fmaf(0.f, dq[c][r], test);
+  uint32_t again = (uint32_t)__ballot(test != 0.f) | (uint32_t)(__ballot(test != 0.f) >> 32);
+  if (store && !(again >> m & 1)) {
+    uint16_t* to = static_cast<uint16_t*>(a.dq) + at + 4 * g;
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        *reinterpret_cast<uint2*>(to + 32 * c + 2 * r) = make_uint2(pack_bf16x2(dq[c][r] * a.scale, dq[c][r + 1] * a.scale),
+                                                                    pack_bf16x2(dq[c][r + 2] * a.scale, dq[c][r + 3] * a.scale));
+  }
+  for (; again; again &= again - 1) {
+    const int x = __ffs(again) - 1, rr = row0 + x, tt = rr / G, hh = hk * G + (rr - tt * G);
+    const size_t from = (size_t)b * a.qr.sb + (size_t)hh * a.qr.sh + (size_t)tt * a.qr.sn;
+    PlainScratch<D>& ps = reinterpret_cast<PlainScratch<D>*>(smem)[w];
+    ps.put(ps.a, static_cast<const uint16_t*>(a.q) + from, lane);
+    ps.put(ps.b, static_cast<const uint16_t*>(a.dout) + from, lane);
+    const TokenKeys<uint16_t> keys{reinterpret_cast<const uint16_t*>(kbase), reinterpret_cast<const uint16_t*>(vbase), a.kr.sn};
+    float acc[D / 64];
+    plain_dq_row<D>(keys, ps.a, ps.b, ps.p, tt, len, a.sight, a.scale2, __shfl(some ? -lse / a.scale : -INFINITY, x), __shfl(delta, x), lane, acc);
+    for (int c = 0; c < D / 64; ++c) store1(static_cast<uint16_t*>(a.dq) + from + lane + 64 * c, a.scale * acc[c]);
+  }
+}
+
+// ---- dk, dv -------------------------------------------------------------------------------
+
+// A workgroup's key block and its share of it.
+struct KeyShare {
+  int bk, block, part, parts, slot;      // slot: of its partial sums, -1 where it is the only one
+};
+__device__ __forceinline__ KeyShare key_share(const BwdRows& a, int id, int count) {
+  // the blocks of the first tokens come first, as their workgroups may have the most to do, and in turn to the XCDs
+  KeyShare r;
+  const int heads = a.B * a.HK, sink_wgs = heads * a.sink_blocks * a.sink_share, ns = a.sink_blocks > 0 ? a.sink_blocks : 1;
+  const int rest = a.blocks - a.sink_blocks > 0 ? a.blocks - a.sink_blocks : 1;
+  if (id < sink_wgs) {
+    const int x = id / a.sink_share;
+    r.part = id % a.sink_share; r.parts = a.sink_share; r.block = x % ns; r.bk = x / ns;
+    r.slot = a.sink_share > 1 ? id : -1;
+  } else {
+    const int y = xcd_stretch(id - sink_wgs, count - sink_wgs), x = y / a.share;
+    r.part = y % a.share; r.parts = a.share; r.block = a.sink_blocks + x % rest; r.bk = x / rest;
+    r.slot = a.share > 1 ? (a.sink_share > 1 ? sink_wgs : 0) + y : -1;
+  }
+  return r;
+}
+
+// Keys on the lanes: S = Q K^T, dP = dO V^T with queries on the accumulator rows, started from -lse / scale and -delta, so that p = exp2(scale2 S)
+// and dS = p dP; dV^T += dO^T P, dK^T += Q^T dS with P and dS as they lie.
+// Width 128: eight wavefronts, k in LDS.  With k and v in registers beside the 128 of the sums, a lane needs more than the 256 that two wavefronts to a SIMD
+// leave it.
+template <int D>
+__global__ __launch_bounds__(2 * key_block(D), 2) void window_dkv_kernel(BwdRows a) {
+  constexpr int BK = key_block(D), NW = BK / 32, KS = D / 16, CB = D / 32, TILE = BT * D * 2, BUF = 2 * TILE + 2 * BT * 4;
+  constexpr bool KLDS = D == 128;
+  extern __shared__ __align__(16) char smem[];
+  const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
+  const KeyShare ks_ = key_share(a, blockIdx.x, gridDim.x);
+  const int b = ks_.bk / a.HK, hk = ks_.bk % a.HK, G = a.G;
+  const int len = clamp_length(a.lengths, b, a.n);
+  const int jb0 = ks_.block * BK, jb1 = (jb0 + BK < len ? jb0 + BK : len) - 1;      // the block's keys
+  const int j = jb0 + 32 * w + m;
+  const bool live = j < len;
+  const int lo = live ? query_lo(a.sight, j) : 0, hi = live ? query_hi(a.sight, j, len) : 0;
+  const size_t at = (size_t)b * a.kr.sb + (size_t)hk * a.kr.sh + (size_t)j * a.kr.sn;
+  uint4 k[KLDS ? 1 : KS], v[KS];
+  const uint32_t kat = lds_address(smem) + 2 * BUF + w * 32 * D * 2;      // k: the wavefront's own rows, no barrier
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    const size_t c = at + 16 * ks + 8 * g;
+    uint4& kr = k[KLDS ? 0 : ks];
+    kr = live ? *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.k) + c) : make_uint4(0, 0, 0, 0);
+    v[ks] = live ? *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.v) + c) : make_uint4(0, 0, 0, 0);
+    if (KLDS) *reinterpret_cast<uint4*>(smem + 2 * BUF + (32 * w + m) * (D * 2) + (((2 * ks + g) ^ swz<D>(m)) * 16)) = kr;
+  }
+  f32x16 dk[CB], dv[CB];
+#pragma unroll
+  for (int c = 0; c < CB; ++c) { dk[c] = fill16(0.f); dv[c] = fill16(0.f); }
+
+  // the query tiles of the block, head after head of the group, and this workgroup's share of them
+  const int q0 = jb1 >= jb0 ? query_lo(a.sight, jb0) / BT : 0;
+  const int qe = jb1 < jb0 ? 0 : jb0 < a.sight.sinks ? len : query_hi(a.sight, jb1, len);
+  const int T = (qe + BT - 1) / BT > q0 ? (qe + BT - 1) / BT - q0 : 0;
+  const int per = (T * G + ks_.parts - 1) / ks_.parts, e0 = ks_.part * per, e1 = e0 + per < T * G ? e0 + per : T * G;
+  // what the wavefront's keys are seen by
+  const int jw0 = jb0 + 32 * w, jw1 = (jw0 + 32 < len ? jw0 + 32 : len) - 1;
+  const bool any = jw1 >= jw0, whole = jw0 + 32 <= len;
+  const int wlo0 = query_lo(a.sight, jw0), wlo1 = query_lo(a.sight, jw1 < 0 ? 0 : jw1);
+  const int whi1 = jw0 < a.sight.sinks ? len : query_hi(a.sight, jw1 < 0 ? 0 : jw1, len);
+  const int whi0 = jw1 < a.sight.sinks ? len : query_hi(a.sight, jw0 < a.sight.sinks ? a.sight.sinks : jw0, len);
+
+  const size_t pitch = a.qr.sn * 2;
+  const RowTile<D, NW, BT> loader(w, lane);
+  const uint32_t lds = lds_address(smem);
+  auto request = [&](int e) {
+    const int hd = e / T, i0 = (q0 + e - hd * T) * BT, h = hk * G + hd;
+    const size_t base = ((size_t)b * a.qr.sb + (size_t)h * a.qr.sh) * 2, li = ((size_t)b * a.H + h) * a.n;
+    const uint32_t to = lds + (uint32_t)(e & 1) * BUF;
+    loader.load(static_cast<const char*>(a.q) + base, pitch, i0, len, to, w);
+    loader.load(static_cast<const char*>(a.dout) + base, pitch, i0, len, to + TILE, w);
+    if (w < 2) {
+      const int i = i0 + lane < len ? i0 + lane : len - 1;
+      const float* from = (w == 0 ? a.nl : a.nd) + li + i;
+      asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" ::"s"(to + 2 * TILE + w * BT * 4), "v"(from) : "memory");
+    }
+  };
+
+  if (e0 < e1) request(e0);
+  lds_loads_landed();
+  __syncthreads();
+  for (int e = e0; e < e1; ++e) {
+    if (e + 1 < e1) request(e + 1);
+    const int i0 = (q0 + e % T) * BT;
+    const uint32_t qt = lds + (uint32_t)(e & 1) * BUF, gt = qt + TILE;
+    const float* nl = reinterpret_cast<const float*>(smem + (e & 1) * BUF + 2 * TILE);
+    if (any && i0 < whi1 && i0 + BT > wlo0) {
+      const bool plain = whole && i0 >= wlo1 && i0 + BT <= whi0;
+#pragma unroll
+      for (int qb = 0; qb < BT / 32; ++qb) {
+        f32x16 s, dp;
+        const int lz = (int)opaque_lane(lane);        // (addresses are worked out here, and k operands read again, not held)
+        const uint32_t ra = row_at<D>(lz), ta = turned_at<D>(lz);
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const float4 x = *reinterpret_cast<const float4*>(nl + 32 * qb + 2 * r + 4 * g), y = *reinterpret_cast<const float4*>(nl + BT + 32 * qb + 2 * r + 4 * g);
+          s[r] = x.x; s[r + 1] = x.y; s[r + 2] = x.z; s[r + 3] = x.w;
+          dp[r] = y.x; dp[r + 1] = y.y; dp[r + 2] = y.z; dp[r + 3] = y.w;
+        }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(row_chunk<D>(qt + ra, ks, 32 * qb)), as_bf16x8(KLDS ? row_chunk<D>(kat + ra, ks, 0) : k[ks]), s, 0, 0, 0);
+          dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(row_chunk<D>(gt + ra, ks, 32 * qb)), as_bf16x8(v[ks]), dp, 0, 0, 0);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r] * a.scale2);
+        if (!plain) {
+          asm volatile("");
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int i = i0 + 32 * qb + 8 * (r / 4) + 4 * g + r % 4;
+            const bool on = i >= lo && i < hi;
+            s[r] = on ? s[r] : 0.f;
+            dp[r] = on ? dp[r] : 0.f;
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dp[r] *= s[r];
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+          const uint4 p = pack8(s, st), ds = pack8(dp, st);
+#pragma unroll
+          for (int c = 0; c < CB; ++c) {
+            dv[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(turned<D>(gt + ta, c, 16 * (2 * qb + st)), as_bf16x8(p), dv[c], 0, 0, 0);
+            dk[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(turned<D>(qt + ta, c, 16 * (2 * qb + st)), as_bf16x8(ds), dk[c], 0, 0, 0);
+          }
+        }
+      }
+    }
+    lds_loads_landed();
+    __syncthreads();
+  }
+
+  // as for dq: masked queries have P = dS = 0
+  if (!whole && !live) {
+#pragma unroll
+    for (int c = 0; c < CB; ++c) { dk[c] = fill16(0.f); dv[c] = fill16(0.f); }
+  }
+  float test = 0.f;
+#pragma unroll
+  for (int c = 0; c < CB; ++c)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) test = fmaf(0.f, dk[c][r], fmaf(0.f, dv[c][r], test));
+  uint32_t again = (uint32_t)__ballot(test != 0.f) | (uint32_t)(__ballot(test != 0.f) >> 32);
+  float* const part = a.parts + (ks_.slot < 0 ? 0 : (size_t)ks_.slot * 2 * BK * D);
+  if (!(again >> m & 1)) {
+    if (ks_.slot >= 0) {
+      float* to = part + (size_t)(32 * w + m) * D + 4 * g;
+#pragma unroll
+      for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          *reinterpret_cast<float4*>(to + 32 * c + 2 * r) = make_float4(dk[c][r], dk[c][r + 1], dk[c][r + 2], dk[c][r + 3]);
+          *reinterpret_cast<float4*>(to + BK * D + 32 * c + 2 * r) = make_float4(dv[c][r], dv[c][r + 1], dv[c][r + 2], dv[c][r + 3]);
+        }
+    } else if (j < a.n) {
+      uint16_t *tk = static_cast<uint16_t*>(a.dk) + at + 4 * g, *tv = static_cast<uint16_t*>(a.dv) + at + 4 * g;
+#pragma unroll
+      for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          *reinterpret_cast<uint2*>(tk + 32 * c + 2 * r) = make_uint2(pack_bf16x2(dk[c][r] * a.scale, dk[c][r + 1] * a.scale),
+                                                                      pack_bf16x2(dk[c][r + 2] * a.scale, dk[c][r + 3] * a.scale));
+          *reinterpret_cast<uint2*>(tv + 32 * c + 2 * r) = make_uint2(pack_bf16x2(dv[c][r], dv[c][r + 1]), pack_bf16x2(dv[c][r + 2], dv[c][r + 3]));
+        }
+    }
+  }
+  for (; again; again &= again - 1) {
+    const int x = 32 * w + __ffs(again) - 1, jj = jb0 + x;
+    const size_t from = (size_t)b * a.kr.sb + (size_t)hk * a.kr.sh + (size_t)jj * a.kr.sn;
+    PlainScratch<D>& ps = reinterpret_cast<PlainScratch<D>*>(smem)[w];
+    ps.put(ps.a, static_cast<const uint16_t*>(a.k) + from, lane);
+    ps.put(ps.b, static_cast<const uint16_t*>(a.v) + from, lane);
+    const int jlo = query_lo(a.sight, jj), jhi = query_hi(a.sight, jj, len);
+    float sk[D / 64] = {}, sv[D / 64] = {};
+    for (int e = e0; e < e1; ++e) {
+      const int hd = e / T, i0 = (q0 + e - hd * T) * BT, h = hk * G + hd;
+      const size_t base = (size_t)b * a.qr.sb + (size_t)h * a.qr.sh, li = ((size_t)b * a.H + h) * a.n;
+      const TokenKeys<uint16_t> rows{static_cast<const uint16_t*>(a.q) + base, static_cast<const uint16_t*>(a.dout) + base, a.qr.sn};
+      plain_dkv_row<D>(rows, ps.a, ps.b, ps.p, ps.s, i0 > jlo ? i0 : jlo, i0 + BT < jhi ? i0 + BT : jhi, a.scale2, a.nl + li, a.nd + li, lane, sk, sv);
+    }
+    for (int c = 0; c < D / 64; ++c) {
+      if (ks_.slot >= 0) {
+        part[(size_t)x * D + lane + 64 * c] = sk[c];
+        part[(size_t)(BK + x) * D + lane + 64 * c] = sv[c];
+      } else {
+        store1(static_cast<uint16_t*>(a.dk) + from + lane + 64 * c, a.scale * sk[c]);
+        store1(static_cast<uint16_t*>(a.dv) + from + lane + 64 * c, sv[c]);
+      }
+    }
+  }
+}
+
+// Sums of the parts of the shared key blocks, in their order.  A thread has four channels of a row of dk or dv.
+template <int D>
+__global__ __launch_bounds__(256) void window_dkv_sum_kernel(BwdRows a, int shared_sinks, int shared_rest) {
+  constexpr int BK = key_block(D);
+  const int heads = a.B * a.HK, items = 2 * BK * D / 4;
+  int x = blockIdx.x / (items / 256);                       // the shared block
+  const int i = blockIdx.x % (items / 256) * 256 + threadIdx.x;
+  int slot, parts, bk, block;
+  if (x < heads * shared_sinks) {
+    parts = a.sink_share; slot = x * parts; block = x % shared_sinks; bk = x / shared_sinks;
+  } else {
+    x -= heads * shared_sinks;
+    parts = a.share; slot = heads * shared_sinks * a.sink_share + x * parts; block = a.sink_blocks + x % shared_rest; bk = x / shared_rest;
+  }
+  const float* from = a.parts + (size_t)slot * 2 * BK * D + 4 * i;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int p = 0; p < parts; ++p) {
+    const float4 y = *reinterpret_cast<const float4*>(from + (size_t)p * 2 * BK * D);
+    s.x += y.x; s.y += y.y; s.z += y.z; s.w += y.w;
+  }
+  const int of = i / (BK * D / 4), row = i % (BK * D / 4) / (D / 4), c = i % (D / 4) * 4, j = block * BK + row;
+  if (j >= a.n) return;
+  const float f = of == 0 ? a.scale : 1.f;
+  uint16_t* to = static_cast<uint16_t*>(of == 0 ? a.dk : a.dv) + (size_t)(bk / a.HK) * a.kr.sb + (size_t)(bk % a.HK) * a.kr.sh + (size_t)j * a.kr.sn + c;
+  *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(s.x * f, s.y * f), pack_bf16x2(s.z * f, s.w * f));
+}
+
+template <int D>
+hipError_t launch_bwd_rows(BwdRows a, hipStream_t s) {
+  constexpr size_t q_smem = 4 * BT * D * 2, k_smem = 2 * (2 * BT * D * 2 + 2 * BT * 4) + (D == 128 ? key_block(D) * D * 2 : 0);
+  a.blocks = (int)(((long long)a.n * a.G + 127) / 128);
+  const int reach = a.sight.left < 0 || a.sight.right < 0 ? a.n : a.sight.left + a.sight.right + 1;
+  const bool exact = (long long)reach + a.sight.sinks <= kFewKeys;
+  const unsigned grid = (unsigned)(a.B * a.HK * a.blocks);
+  if (exact) {
+    constexpr auto kernel = &window_dq_kernel<D, true>;
+    if (hipError_t e = set_smem_once<kernel>(q_smem); e != hipSuccess) return e;
+    kernel<<<grid, 256, q_smem, s>>>(a);
+  } else {
+    constexpr auto kernel = &window_dq_kernel<D, false>;
+    if (hipError_t e = set_smem_once<kernel>(q_smem); e != hipSuccess) return e;
+    kernel<<<grid, 256, q_smem, s>>>(a);
+  }
+  const KeySplit split = key_split(a.B * a.HK, a.G, a.n, D, a.sight);
+  a.blocks = split.blocks; a.sink_blocks = split.sink_blocks; a.sink_share = split.sink_share; a.share = split.share;
+  constexpr auto kernel = &window_dkv_kernel<D>;
+  if (hipError_t e = set_smem_once<kernel>(k_smem); e != hipSuccess) return e;
+  kernel<<<(unsigned)split.workgroups, 2 * key_block(D), k_smem, s>>>(a);
+  if (split.parts) {
+    const int ss = split.sink_share > 1 ? split.sink_blocks : 0, sr = split.share > 1 ? split.blocks - split.sink_blocks : 0;
+    window_dkv_sum_kernel<D><<<(unsigned)(a.B * a.HK * (ss + sr) * (2 * key_block(D) * D / 4 / 256)), 256, 0, s>>>(a, ss, sr);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace attn
+}  // namespace linattn

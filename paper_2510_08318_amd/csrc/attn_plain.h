@@ -79,5 +79,70 @@ __device__ void plain_row(const Keys& keys, const float* sq, float* sp, int p, i
     }
 }
 
+// Sum over the keys of ds_j k_j of the query at position p, in sq, with upstream gradient in sg.  nl: -lse / scale, delta: dout . o.
+template <int D, typename Keys>
+__device__ void plain_dq_row(const Keys& keys, const float* sq, const float* sg, float* sp, int p, int len, const Sight& sight, float scale2, float nl,
+                             float delta, int lane, float (&acc)[D / 64]) {
+  for (int x = 0; x < D / 64; ++x) acc[x] = 0.f;
+  if (nl == -INFINITY) return;
+  const int lo = key_lo(sight, p), hi = key_hi(sight, p, len), first = sight.sinks < lo ? sight.sinks : lo;
+  for (int part = 0; part < 2; ++part)
+    for (int j0 = part ? lo : 0, end = part ? hi : first; j0 < end; j0 += 64) {
+      const int j = j0 + lane;
+      float ds = 0.f;
+      if (j < end) {
+        const float s = dot_row<D>(sq, [&](int c, float* f) { keys.k8(j, c, f); });
+        const float dp = dot_row<D>(sg, [&](int c, float* f) { keys.v8(j, c, f); });
+        ds = __builtin_amdgcn_exp2f((s + nl) * scale2) * (dp - delta);
+      }
+      __builtin_amdgcn_wave_barrier();
+      sp[lane] = ds;
+      __builtin_amdgcn_wave_barrier();
+      const int cnt = end - j0 < 64 ? end - j0 : 64;
+      for (int t = 0; t < cnt; ++t)
+        for (int x = 0; x < D / 64; ++x) acc[x] = fmaf(sp[t], keys.k1(j0 + t, lane + 64 * x), acc[x]);
+    }
+}
+
+// The part of dk (before the scale) and dv of a key, in sk and sv, that the queries i0 .. i1-1 of one head give; rows: their q (as k) and dout (as v).
+template <int D, typename Rows_>
+__device__ void plain_dkv_row(const Rows_& rows, const float* sk, const float* sv, float* sp, float* ss, int i0, int i1, float scale2,
+                              const float* nl, const float* nd, int lane, float (&dk)[D / 64], float (&dv)[D / 64]) {
+  for (; i0 < i1; i0 += 64) {
+    const int i = i0 + lane;
+    float p = 0.f, ds = 0.f;
+    const float l = i < i1 ? nl[i] : -INFINITY;
+    const bool on = l != -INFINITY;
+    if (on) {
+      const float s = dot_row<D>(sk, [&](int c, float* f) { rows.k8(i, c, f); });
+      const float dp = dot_row<D>(sv, [&](int c, float* f) { rows.v8(i, c, f); });
+      p = __builtin_amdgcn_exp2f((s + l) * scale2);
+      ds = p * (dp + nd[i]);
+    }
+    const unsigned long long mask = __ballot(on);
+    __builtin_amdgcn_wave_barrier();
+    sp[lane] = p;
+    ss[lane] = ds;
+    __builtin_amdgcn_wave_barrier();
+    for (int t = 0; t < 64; ++t)
+      if (mask >> t & 1)
+        for (int x = 0; x < D / 64; ++x) {
+          dk[x] = fmaf(ss[t], rows.k1(i0 + t, lane + 64 * x), dk[x]);
+          dv[x] = fmaf(sp[t], rows.v1(i0 + t, lane + 64 * x), dv[x]);
+        }
+  }
+}
+
+// A wavefront's LDS for these.
+template <int D>
+struct PlainScratch {
+  float a[D], b[D], p[64], s[64];
+  template <typename T>
+  __device__ __forceinline__ void put(float* to, const T* row, int lane) {
+    for (int x = lane; x < D; x += 64) to[x] = f32::ldf(row, x);
+    __builtin_amdgcn_wave_barrier();
+  }
+};
+
 }  // namespace attn
 }  // namespace linattn
