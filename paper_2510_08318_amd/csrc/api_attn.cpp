@@ -34,7 +34,7 @@ int check_heads(int B, int H, int HK, int n, int d, int layout) {
   if (B <= 0 || H <= 0 || HK <= 0 || n <= 0 || H % HK) return LINATTN_E_SHAPE;
   if (d != 64 && d != 128) return LINATTN_E_SHAPE;
   if (layout != LINATTN_LAYOUT_BHND && layout != LINATTN_LAYOUT_BNHD) return LINATTN_E_SHAPE;
-  if ((long long)B * H > 65535 || (long long)n * (H / HK) > kMostTokens) return LINATTN_E_SHAPE;
+  if ((long long)B * H > 65535 || (long long)n * (H / HK) > kMostTokens || (long long)B * H * n > 1LL << 37) return LINATTN_E_SHAPE;
   return LINATTN_OK;
 }
 
@@ -101,7 +101,10 @@ int check_cache(const linattn_cache_desc* c, int n, Pool* p, CacheSizes* z) {
   return any_overlap(outs, none) ? LINATTN_E_ALIAS : LINATTN_OK;
 }
 
-size_t attn_work_bytes(const linattn_cache_desc*, int, int) { return 0; }
+size_t attn_work_bytes(const linattn_cache_desc* c, int H, int n) {
+  const int splits = cache_splits(c->B, H, c->H, n, c->d, c->type == LINATTN_CACHE_E4M3, (long long)c->page * c->width);
+  return splits > 1 ? ((size_t)splits * c->B * H * n * (c->d + 2) * sizeof(float) + 255) & ~(size_t)255 : 0;
+}
 
 }  // namespace
 }  // namespace attn

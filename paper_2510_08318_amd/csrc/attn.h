@@ -120,6 +120,27 @@ struct CacheArgs {
   hipStream_t stream;
 };
 
+// Whether a chunk's rows of a key head (its group's heads side by side) go to the kernel that deals keys, not rows, to a workgroup's wavefronts.
+inline bool few_rows(int H, int HK, int n) { return (long long)n * (H / HK) <= 64; }
+// The keys that a row of a chunk sees at most, together with the rest of the chunk's.
+inline long long reach_of(const CacheArgs& a) {
+  const long long all = (long long)a.pool.page * a.pool.width;
+  if (a.sight.left < 0) return all;
+  const long long r = (long long)a.sight.left + a.n + (a.sight.right < 0 ? a.n : a.sight.right) + a.sight.sinks + 64;
+  return r < all ? r : all;
+}
+// Parts that the keys are dealt to, for chunks whose keys number `reach` at most: as many workgroups as fill the chip, with enough tiles each.
+constexpr int kMostSplits = 64;
+inline int cache_splits(int B, int H, int HK, int n, int d, bool e4m3, long long reach) {
+  const bool few = few_rows(H, HK, n);
+  const long long blocks = (long long)B * HK * (few ? 1 : ((long long)n * (H / HK) + 127) / 128);
+  const int tile = few ? (e4m3 || d == 64 ? 64 : 32) * 4 : 64 * 8;      // keys that a part has at least
+  long long s = (few ? 2 * kCUs : 2 * kCUs) / blocks;
+  const long long most = (reach + tile - 1) / tile;
+  s = s < most ? s : most;
+  return s < 1 ? 1 : s < kMostSplits ? (int)s : kMostSplits;
+}
+
 hipError_t launch_window_fwd(const WindowArgs& a, int dtype);
 hipError_t launch_window_bwd(const WindowArgs& a, int dtype);
 hipError_t launch_cache_write(const Pool& p, bool e4m3, const void* k, const void* v, int n, const Rows& r, hipStream_t s);

@@ -25,10 +25,6 @@ struct BwdRows {
   float scale, scale2;
 };
 
-__device__ __forceinline__ uint4 pack8(const f32x16& e, int h) {
-  return make_uint4(pack_bf16x2(e[8 * h], e[8 * h + 1]), pack_bf16x2(e[8 * h + 2], e[8 * h + 3]), pack_bf16x2(e[8 * h + 4], e[8 * h + 5]),
-                    pack_bf16x2(e[8 * h + 6], e[8 * h + 7]));
-}
 // ---- dq -----------------------------------------------------------------------------------
 // Queries on the lanes, as in the forward: S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T.
 // EXACT: delta from a first pass over the keys, sum_j p_ij dp_ij, and not from dout . out.  Where a row sees few keys its output is as large as the
@@ -77,7 +73,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(BwdRows a) {
 
   const int last_row = ((block + 1) * BM < rows ? (block + 1) * BM : rows) - 1, wlast = (row0 + 32 < rows ? row0 + 32 : rows) - 1;
   const KeyTiles<BT> tiles(a.sight, block * BM / G, last_row < block * BM ? -1 : last_row / G, len);
-  const WaveSight sight(a.sight, row0 / G, wlast < row0 ? -1 : wlast / G, len, row0 + 32 <= rows);
+  const WaveSight sight(a.sight, row0 / G, wlast < row0 ? -1 : wlast / G, len);
   const size_t kv = (size_t)b * a.kr.sb + (size_t)hk * a.kr.sh, pitch = a.kr.sn * 2;
   const char *kbase = static_cast<const char*>(a.k) + kv * 2, *vbase = static_cast<const char*>(a.v) + kv * 2;
   const RowTile<D, NW, BT> loader(w, lane);
@@ -159,7 +155,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(BwdRows a) {
   });
 
   // Masked keys have dS = 0, which an infinity or NaN in k would make NaN: rows that come out not finite are done again key by key.
-  if (!sight.whole && !live) {
+  if (!live) {
 #pragma unroll
     for (int c = 0; c < CB; ++c) dq[c] = fill16(0.f);
   }
@@ -253,7 +249,7 @@ __global__ __launch_bounds__(2 * key_block(D), 2) void window_dkv_kernel(BwdRows
   const int per = (T * G + ks_.parts - 1) / ks_.parts, e0 = ks_.part * per, e1 = e0 + per < T * G ? e0 + per : T * G;
   // what the wavefront's keys are seen by
   const int jw0 = jb0 + 32 * w, jw1 = (jw0 + 32 < len ? jw0 + 32 : len) - 1;
-  const bool any = jw1 >= jw0, whole = jw0 + 32 <= len;
+  const bool any = jw1 >= jw0;
   const int wlo0 = query_lo(a.sight, jw0), wlo1 = query_lo(a.sight, jw1 < 0 ? 0 : jw1);
   const int whi1 = jw0 < a.sight.sinks ? len : query_hi(a.sight, jw1 < 0 ? 0 : jw1, len);
   const int whi0 = jw1 < a.sight.sinks ? len : query_hi(a.sight, jw0 < a.sight.sinks ? a.sight.sinks : jw0, len);
@@ -283,7 +279,7 @@ __global__ __launch_bounds__(2 * key_block(D), 2) void window_dkv_kernel(BwdRows
     const uint32_t qt = lds + (uint32_t)(e & 1) * BUF, gt = qt + TILE;
     const float* nl = reinterpret_cast<const float*>(smem + (e & 1) * BUF + 2 * TILE);
     if (any && i0 < whi1 && i0 + BT > wlo0) {
-      const bool plain = whole && i0 >= wlo1 && i0 + BT <= whi0;
+      const bool plain = i0 >= wlo1 && i0 + BT <= whi0;
 #pragma unroll
       for (int qb = 0; qb < BT / 32; ++qb) {
         f32x16 s, dp;
@@ -330,7 +326,7 @@ __global__ __launch_bounds__(2 * key_block(D), 2) void window_dkv_kernel(BwdRows
   }
 
   // as for dq: masked queries have P = dS = 0
-  if (!whole && !live) {
+  if (!live) {
 #pragma unroll
     for (int c = 0; c < CB; ++c) { dk[c] = fill16(0.f); dv[c] = fill16(0.f); }
   }

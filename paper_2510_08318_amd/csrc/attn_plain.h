@@ -51,17 +51,17 @@ __device__ __forceinline__ float dot_row(const float* x, L8 l8) {
   return s;
 }
 
-// o of a row, not yet divided by the sum l; m: the largest score (base 2).  sq: the query's D values, sp: 64 floats, both in LDS and the wavefront's own.
+// o of a row, not yet divided by the sum l; m: the largest score (base 2).  The keys are those of [a0, a1) and [b0, b1) that position p sees.  sq: the
+// query's D values, sp: 64 floats, both in LDS and the wavefront's own.
 template <int D, typename Keys>
-__device__ void plain_row(const Keys& keys, const float* sq, float* sp, int p, int len, const Sight& sight, float scale2, int lane,
-                          float& m, float& l, float (&acc)[D / 64]) {
+__device__ void plain_row(const Keys& keys, const float* sq, float* sp, int p, int len, const Sight& sight, int a0, int a1, int b0, int b1,
+                          float scale2, int lane, float& m, float& l, float (&acc)[D / 64]) {
   m = -INFINITY; l = 0.f;
   for (int i = 0; i < D / 64; ++i) acc[i] = 0.f;
-  const int lo = key_lo(sight, p), hi = key_hi(sight, p, len), first = sight.sinks < lo ? sight.sinks : lo;
   for (int part = 0; part < 2; ++part)
-    for (int j0 = part ? lo : 0, end = part ? hi : (first < hi ? first : hi); j0 < end; j0 += 64) {
+    for (int j0 = part ? b0 : a0, end = part ? b1 : a1; j0 < end; j0 += 64) {
       const int j = j0 + lane;
-      const bool on = j < end && keys.there(j);
+      const bool on = j < end && sees(sight, p, j, len) && keys.there(j);
       const float s = on ? scale2 * dot_row<D>(sq, [&](int c, float* f) { keys.k8(j, c, f); }) : -INFINITY;
       const float mn = fmaxf(m, wave_max(s));
       const float pr = on && s != -INFINITY ? __builtin_amdgcn_exp2f(s - mn) : 0.f;

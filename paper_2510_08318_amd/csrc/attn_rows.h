@@ -8,16 +8,23 @@ namespace attn {
 
 // Rows of a block: the query heads of a key head's group side by side, row = token * G + head, so that a group's keys are read once.
 struct RowsArgs {
-  const void *q, *k, *v;
+  const void* q;
   void* o;
-  float* lse;
-  const int* lengths;
+  float* lse;               // nullable
+  float* parts;             // with several splits: see parts_of
   int B, H, HK, G, n;
   int blocks;               // row blocks of a (batch item, key head)
-  Rows qr, kr;
+  int splits;               // parts that the keys of a block are dealt to
+  Rows qr;
   Sight sight;
   float scale2;             // scale * log2(e)
 };
+// Results over a part of the keys: o not divided by its sum, fp32 [splits][B*H*n][D], and then [splits][B*H*n] pairs of the largest score (base 2) and
+// the sum.
+__device__ __forceinline__ void put_part(const RowsArgs& a, int D, int split, size_t row, float m, float l) {
+  const size_t rows = (size_t)a.B * a.H * a.n;
+  reinterpret_cast<float2*>(a.parts + (size_t)a.splits * rows * D)[(size_t)split * rows + row] = make_float2(m, l);
+}
 
 __device__ __forceinline__ f32x16 fill16(float x) {
   f32x16 r;
@@ -53,25 +60,92 @@ struct KeyTiles {
     count = nsink + (last > wtile ? last - wtile : 0);
   }
   __device__ __forceinline__ int start(int i) const { return (i < nsink ? i : wtile + i - nsink) * KT; }
+  // where tile i starts among the keys of the first tokens, among those of the window
+  __device__ __forceinline__ int sink_key(int i) const { return (i < nsink ? i : nsink) * KT; }
+  __device__ __forceinline__ int window_key(int i) const { return (wtile + (i > nsink ? i - nsink : 0)) * KT; }
 };
-// What a wavefront's rows at positions p0 .. p1 see of a tile from key j0 on: nothing, or everything.
+// What a wavefront's rows at positions p0 .. p1 see of a tile from key j0 on: nothing, or everything.  (Lanes without a token are not looked at: what they
+// come to is dropped.)
 struct WaveSight {
   int lo0, lo1, hi0, hi1, sinks;
-  bool rows, whole;         // whether it has any; whether all of its rows are tokens
-  __device__ __forceinline__ WaveSight(const Sight& s, int p0, int p1, int len, bool all)
-      : lo0(key_lo(s, p0)), lo1(key_lo(s, p1)), hi0(key_hi(s, p0, len)), hi1(key_hi(s, p1, len)), sinks(s.sinks), rows(p1 >= p0), whole(all) {}
+  bool rows;                // whether it has any
+  __device__ __forceinline__ WaveSight(const Sight& s, int p0, int p1, int len)
+      : lo0(key_lo(s, p0)), lo1(key_lo(s, p1)), hi0(key_hi(s, p0, len)), hi1(key_hi(s, p1, len)), sinks(s.sinks), rows(p1 >= p0) {}
   __device__ __forceinline__ bool nothing(int j0, int count) const { return !rows || j0 >= hi1 || (j0 + count <= lo0 && j0 >= sinks); }
-  __device__ __forceinline__ bool everything(int j0, int count) const { return whole && j0 + count <= hi0 && (j0 >= lo1 || j0 + count <= sinks); }
+  __device__ __forceinline__ bool everything(int j0, int count) const { return j0 + count <= hi0 && (j0 >= lo1 || j0 + count <= sinks); }
 };
 
-template <int D, int QB, int NW, int KT, int OCC>
-__global__ __launch_bounds__(64 * NW, OCC) void attn_rows_kernel(RowsArgs a) {
+__device__ __forceinline__ uint4 pack8(const f32x16& e, int h) {
+  return make_uint4(pack_bf16x2(e[8 * h], e[8 * h + 1]), pack_bf16x2(e[8 * h + 2], e[8 * h + 3]), pack_bf16x2(e[8 * h + 4], e[8 * h + 5]),
+                    pack_bf16x2(e[8 * h + 6], e[8 * h + 7]));
+}
+
+// Scores of a query's keys (half of them in each lane of a pair) -> weights 2^(scale2 s - mx), with the running maximum mx, the sum l of the lane's weights, and o
+// brought to it.  The maximum moves only where it has grown by more than 8: the weights are then at most 2^8, and the result the same after
+// the division.
+template <int KB, int CB>
+__device__ __forceinline__ void softmax_step(f32x16 (&s)[KB], float scale2, float& mx, float& l, f32x16 (&o)[CB]) {
+  float top = s[0][0];
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[kb][r]);
+  float x, y;
+  pair32(top, x, y);
+  top = fmaxf(x, y) * scale2;
+  if (__any(top > mx + 8.f)) {
+    const float next = fmaxf(mx, top), alpha = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx - next);
+    mx = next;
+    l *= alpha;
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[c][r] *= alpha;
+  }
+  const float c0 = mx == -INFINITY ? 0.f : -mx;
+  float sum = 0.f;
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[kb][r] = __builtin_amdgcn_exp2f(fmaf(s[kb][r], scale2, c0));
+      sum += s[kb][r];
+    }
+  l += sum;
+}
+
+// Row r of a block once more, key by key, over the keys of tiles it0 .. it1 - 1.
+template <int D, typename Keys, typename Tiles>
+__device__ void plain_again(const RowsArgs& a, const Keys& keys, const Tiles& tiles, int it0, int it1, int r, int b, int hk, int split, int pos0, int len,
+                            PlainScratch<D>& ps, int lane) {
+  const int t = r / a.G, h = hk * a.G + (r - t * a.G);
+  const size_t at = (size_t)b * a.qr.sb + (size_t)h * a.qr.sh + (size_t)t * a.qr.sn, li = ((size_t)b * a.H + h) * a.n + t;
+  ps.put(ps.a, static_cast<const uint16_t*>(a.q) + at, lane);
+  float m, l, acc[D / 64];
+  plain_row<D>(keys, ps.a, ps.p, pos0 + t, len, a.sight, tiles.sink_key(it0), tiles.sink_key(it1), tiles.window_key(it0), tiles.window_key(it1), a.scale2,
+               lane, m, l, acc);
+  if (a.splits > 1) {
+    for (int c = 0; c < D / 64; ++c) a.parts[((size_t)split * a.B * a.H * a.n + li) * D + lane + 64 * c] = acc[c];
+    if (lane == 0) put_part(a, D, split, li, m, l);
+    return;
+  }
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  for (int c = 0; c < D / 64; ++c) store1(static_cast<uint16_t*>(a.o) + at + lane + 64 * c, acc[c] * inv);
+  if (a.lse && lane == 0) a.lse[li] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+template <int D, int KT, typename Source>
+__global__ __launch_bounds__(64 * kRowWaves, 2) void attn_rows_kernel(RowsArgs a, typename Source::Args from) {
+  constexpr int QB = 1, NW = kRowWaves;
   constexpr int KB = KT / 32, KS = D / 16, CB = D / 32, BM = 32 * QB * NW, TILE = KT * D * 2;
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
-  const int id = xcd_stretch(blockIdx.x, gridDim.x), bk = id / a.blocks, block = row_block(a.sight, id % a.blocks, a.blocks);
+  const int id = xcd_stretch(blockIdx.x, gridDim.x), split = id % a.splits, bx = id / a.splits;
+  const int bk = bx / a.blocks, block = row_block(a.sight, bx % a.blocks, a.blocks);
   const int b = bk / a.HK, hk = bk % a.HK, G = a.G;
-  const int len = clamp_length(a.lengths, b, a.n), rows = len * G, all = a.n * G;
+  Source src(from, b, hk, a.n, w, lane);
+  // token t has position pos0 + t; tokens t0 .. count - 1 have rows
+  const int len = src.len, pos0 = len - src.count, t0 = pos0 < 0 ? -pos0 : 0, rows = src.count * G, all = a.n * G;
   const int row0 = block * BM + w * 32 * QB;
 
   // this lane's queries
@@ -84,9 +158,9 @@ __global__ __launch_bounds__(64 * NW, OCC) void attn_rows_kernel(RowsArgs a) {
     const int r = row0 + 32 * i + m, t = r / G, h = hk * G + (r - t * G);
     store[i] = r < all;
     at[i] = (size_t)b * a.qr.sb + (size_t)h * a.qr.sh + (size_t)t * a.qr.sn;
-    const bool live = r < rows;
-    lo[i] = live ? key_lo(a.sight, t) : 0;
-    hi[i] = live ? key_hi(a.sight, t, len) : 0;
+    const bool live = r < rows && t >= t0;
+    lo[i] = live ? key_lo(a.sight, pos0 + t) : 0;
+    hi[i] = live ? key_hi(a.sight, pos0 + t, len) : 0;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
       q[i][ks] = live ? *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + at[i] + 16 * ks + 8 * g) : make_uint4(0, 0, 0, 0);
@@ -103,30 +177,34 @@ __global__ __launch_bounds__(64 * NW, OCC) void attn_rows_kernel(RowsArgs a) {
       for (int r = 0; r < 16; ++r) o[i][c][r] = 0.f;
   }
 
-  const int last_row = ((block + 1) * BM < rows ? (block + 1) * BM : rows) - 1, wlast = (row0 + 32 * QB < rows ? row0 + 32 * QB : rows) - 1;
-  const KeyTiles<KT> tiles(a.sight, block * BM / G, last_row < block * BM ? -1 : last_row / G, len);
-  const WaveSight sight(a.sight, row0 / G, wlast < row0 ? -1 : wlast / G, len, row0 + 32 * QB <= rows);
-  const size_t kv = (size_t)b * a.kr.sb + (size_t)hk * a.kr.sh, pitch = a.kr.sn * 2;
-  const char *kbase = static_cast<const char*>(a.k) + kv * 2, *vbase = static_cast<const char*>(a.v) + kv * 2;
-  const RowTile<D, NW, KT> loader(w, lane);
+  auto from_row = [&](int r) { return pos0 + (r / G > t0 ? r / G : t0); };      // the first position from row r on
+  auto to_row = [&](int r) { r = (r < rows ? r : rows) - 1; return r >= 0 && r / G >= t0 ? pos0 + r / G : -1; };      // the last before row r
+  const int bp0 = from_row(block * BM), bp1 = to_row((block + 1) * BM), wp0 = from_row(row0), wp1 = to_row(row0 + 32 * QB);
+  const KeyTiles<KT> tiles(a.sight, bp0, bp1 < bp0 ? -1 : bp1, len);
+  const WaveSight sight(a.sight, wp0, wp1 < wp0 ? -1 : wp1, len);
+  const int it0 = (int)((long long)tiles.count * split / a.splits), it1 = (int)((long long)tiles.count * (split + 1) / a.splits);
   const uint32_t lds = lds_address(smem);
-  auto request = [&](int i) {
-    const int j0 = tiles.start(i);
-    const uint32_t to = lds + (uint32_t)(i & 1) * 2 * TILE;
-    loader.load(kbase, pitch, j0, tiles.end, to, w);
-    loader.load(vbase, pitch, j0, tiles.end, to + TILE, w);
-  };
+  auto look = [&](int i) { src.look(tiles.start(i), tiles.end); };
+  auto request = [&](int i) { src.request(tiles.start(i), tiles.end, lds + (uint32_t)(i & 1) * 2 * TILE); };
   const uint32_t rows_at = row_at<D>(lane), turned_rows = turned_at<D>(lane);
 
-  if (tiles.count) request(0);
-  lds_loads_landed();
+  if (it0 < it1) {
+    look(it0);
+    request(it0);
+    if (it0 + 1 < it1) look(it0 + 1);
+    src.finish(lds + (uint32_t)(it0 & 1) * 2 * TILE);
+  }
   __syncthreads();
-  for (int it = 0; it < tiles.count; ++it) {
-    if (it + 1 < tiles.count) request(it + 1);
+  for (int it = it0; it < it1; ++it) {
+    const unsigned long long there = src.mask();
+    if (it + 1 < it1) {
+      request(it + 1);
+      if (it + 2 < it1) look(it + 2);
+    }
     const int j0 = tiles.start(it);
     const uint32_t kt = lds + (uint32_t)(it & 1) * 2 * TILE, vt = kt + TILE;
     if (!sight.nothing(j0, KT)) {
-      const bool plain = sight.everything(j0, KT);
+      const bool plain = sight.everything(j0, KT) && there == ~0ull;
       f32x16 s[QB][KB];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
@@ -152,47 +230,15 @@ __global__ __launch_bounds__(64 * NW, OCC) void attn_rows_kernel(RowsArgs a) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
               const int j = j0 + 32 * kb + 8 * (r / 4) + 4 * g + r % 4;
-              s[i][kb][r] = j < hi[i] && (j >= lo[i] || j < a.sight.sinks) ? s[i][kb][r] : -INFINITY;
+              bool on = j < hi[i] && (j >= lo[i] || j < a.sight.sinks);
+              if (Source::kPaged) on = on && (there >> (j - j0) & 1);
+              s[i][kb][r] = on ? s[i][kb][r] : -INFINITY;
             }
         }
-        float top = s[i][0][0];
+        softmax_step<KB, CB>(s[i], a.scale2, mx[i], l[i], o[i]);
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) top = fmaxf(top, s[i][kb][r]);
-        float x, y;
-        pair32(top, x, y);
-        top = fmaxf(x, y) * a.scale2;
-        // The running maximum moves only where it has grown by more than 8: the probabilities are then at most 2^8, and the sums the same
-        // after the division.
-        if (__any(top > mx[i] + 8.f)) {
-          const float next = fmaxf(mx[i], top), alpha = mx[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx[i] - next);
-          mx[i] = next;
-          l[i] *= alpha;
-#pragma unroll
-          for (int c = 0; c < CB; ++c)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[i][c][r] *= alpha;
-        }
-        const float c0 = mx[i] == -INFINITY ? 0.f : -mx[i];
-        float sum = 0.f;
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const float e = __builtin_amdgcn_exp2f(fmaf(s[i][kb][r], a.scale2, c0));
-            s[i][kb][r] = e;
-            sum += e;
-          }
-        l[i] += sum;
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-          for (int h2 = 0; h2 < 2; ++h2) {
-            const f32x16& e = s[i][kb];
-            p[i][2 * kb + h2] = make_uint4(pack_bf16x2(e[8 * h2], e[8 * h2 + 1]), pack_bf16x2(e[8 * h2 + 2], e[8 * h2 + 3]),
-                                           pack_bf16x2(e[8 * h2 + 4], e[8 * h2 + 5]), pack_bf16x2(e[8 * h2 + 6], e[8 * h2 + 7]));
-          }
+          for (int h2 = 0; h2 < 2; ++h2) p[i][2 * kb + h2] = pack8(s[i][kb], h2);
       }
 #pragma unroll
       for (int st = 0; st < 2 * KB; ++st)
@@ -203,7 +249,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void attn_rows_kernel(RowsArgs a) {
           for (int i = 0; i < QB; ++i) o[i][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop, as_bf16x8(p[i][st]), o[i][c], 0, 0, 0);
         }
     }
-    lds_loads_landed();
+    if (it + 1 < it1) src.finish(lds + (uint32_t)((it + 1) & 1) * 2 * TILE);
     __syncthreads();
   }
 
@@ -211,12 +257,12 @@ __global__ __launch_bounds__(64 * NW, OCC) void attn_rows_kernel(RowsArgs a) {
   for (int i = 0; i < QB; ++i) {
     float x, y;
     pair32(l[i], x, y);
-    const float sum = x + y, inv = sum == 0.f ? 0.f : 1.0f / sum;
+    const float sum = hi[i] == 0 ? 0.f : x + y, inv = sum == 0.f ? 0.f : 1.0f / sum;
     const int r = row0 + 32 * i + m, t = r / G;
     const size_t li = ((size_t)b * a.H + hk * G + (r - t * G)) * a.n + t;
     // A key that is masked has weight 0, and 0 times an infinity or NaN in its value would be NaN: rows that come out not finite are done again
     // key by key.
-    if (!sight.whole && hi[i] == 0) {
+    if (hi[i] == 0) {                          // not a token
 #pragma unroll
       for (int c = 0; c < CB; ++c) o[i][c] = fill16(0.f);
     }
@@ -227,39 +273,68 @@ __global__ __launch_bounds__(64 * NW, OCC) void attn_rows_kernel(RowsArgs a) {
       for (int e = 0; e < 16; ++e) test = fmaf(0.f, o[i][c][e], test);
     uint32_t again = (uint32_t)__ballot(test != 0.f) | (uint32_t)(__ballot(test != 0.f) >> 32);
     if (store[i] && !(again >> m & 1)) {
-      uint16_t* out = static_cast<uint16_t*>(a.o) + at[i] + 4 * g;
+      if (a.splits > 1) {
+        float* part = a.parts + ((size_t)split * a.B * a.H * a.n + li) * D + 4 * g;
 #pragma unroll
-      for (int c = 0; c < CB; ++c)
+        for (int c = 0; c < CB; ++c)
 #pragma unroll
-        for (int e = 0; e < 16; e += 4)
-          *reinterpret_cast<uint2*>(out + 32 * c + 2 * e) = make_uint2(pack_bf16x2(o[i][c][e] * inv, o[i][c][e + 1] * inv),
-                                                                       pack_bf16x2(o[i][c][e + 2] * inv, o[i][c][e + 3] * inv));
-      if (a.lse && g == 0) a.lse[li] = sum == 0.f ? -INFINITY : (mx[i] + __builtin_amdgcn_logf(sum)) * kLn2;
+          for (int e = 0; e < 16; e += 4)
+            *reinterpret_cast<float4*>(part + 32 * c + 2 * e) = make_float4(o[i][c][e], o[i][c][e + 1], o[i][c][e + 2], o[i][c][e + 3]);
+        if (g == 0) put_part(a, D, split, li, mx[i], sum);
+      } else {
+        uint16_t* out = static_cast<uint16_t*>(a.o) + at[i] + 4 * g;
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+          for (int e = 0; e < 16; e += 4)
+            *reinterpret_cast<uint2*>(out + 32 * c + 2 * e) = make_uint2(pack_bf16x2(o[i][c][e] * inv, o[i][c][e + 1] * inv),
+                                                                         pack_bf16x2(o[i][c][e + 2] * inv, o[i][c][e + 3] * inv));
+        if (a.lse && g == 0) a.lse[li] = sum == 0.f ? -INFINITY : (mx[i] + __builtin_amdgcn_logf(sum)) * kLn2;
+      }
     }
-    for (; again; again &= again - 1) {
-      const int rr = row0 + 32 * i + __ffs(again) - 1, tt = rr / G, hh = hk * G + (rr - tt * G);
-      const size_t from = (size_t)b * a.qr.sb + (size_t)hh * a.qr.sh + (size_t)tt * a.qr.sn;
-      PlainScratch<D>& ps = reinterpret_cast<PlainScratch<D>*>(smem)[w];
-      ps.put(ps.a, static_cast<const uint16_t*>(a.q) + from, lane);
-      const TokenKeys<uint16_t> keys{reinterpret_cast<const uint16_t*>(kbase), reinterpret_cast<const uint16_t*>(vbase), a.kr.sn};
-      float pm, pl, acc[D / 64];
-      plain_row<D>(keys, ps.a, ps.p, tt, len, a.sight, a.scale2, lane, pm, pl, acc);
-      const float pinv = pl == 0.f ? 0.f : 1.0f / pl;
-      for (int c = 0; c < D / 64; ++c) store1(static_cast<uint16_t*>(a.o) + from + lane + 64 * c, acc[c] * pinv);
-      if (a.lse && lane == 0) a.lse[((size_t)b * a.H + hh) * a.n + tt] = pl == 0.f ? -INFINITY : (pm + __builtin_amdgcn_logf(pl)) * kLn2;
-    }
+    for (; again; again &= again - 1)
+      plain_again<D>(a, src.keys(), tiles, it0, it1, row0 + 32 * i + __ffs(again) - 1, b, hk, split, pos0, len, reinterpret_cast<PlainScratch<D>*>(smem)[w], lane);
   }
 }
 
-template <int D, int QB, int NW, int KT, int OCC>
-hipError_t launch_rows(RowsArgs a, hipStream_t s) {
-  constexpr int BM = 32 * QB * NW;
+// The sum over the splits.  A wavefront to a row.
+template <int D>
+__global__ __launch_bounds__(256) void attn_join_kernel(RowsArgs a) {
+  const int lane = threadIdx.x % 64, t = blockIdx.x * 4 + threadIdx.x / 64, bh = blockIdx.y;
+  if (t >= a.n) return;
+  const size_t rows = (size_t)a.B * a.H * a.n, row = (size_t)bh * a.n + t;
+  const float2* ml = reinterpret_cast<const float2*>(a.parts + (size_t)a.splits * rows * D);
+  // a lane to a split, at most 64 of them
+  const float2 own = lane < a.splits ? ml[(size_t)lane * rows + row] : make_float2(-INFINITY, 0.f);
+  const float top = wave_max(own.x);
+  const float weight = own.x == -INFINITY ? (own.y == 0.f ? 0.f : own.y) : __builtin_amdgcn_exp2f(own.x - top);      // (a sum without a maximum is NaN)
+  const float sum = wave_sum(weight * own.y), inv = sum == 0.f ? 0.f : 1.0f / sum;
+  float acc[D / 64] = {};
+  for (int s = 0; s < a.splits; ++s) {
+    const float f = __shfl(weight, s);
+    if (f != 0.f)
+      for (int c = 0; c < D / 64; ++c) acc[c] = fmaf(f, a.parts[((size_t)s * rows + row) * D + lane + 64 * c], acc[c]);
+  }
+  uint16_t* out = static_cast<uint16_t*>(a.o) + (size_t)(bh / a.H) * a.qr.sb + (size_t)(bh % a.H) * a.qr.sh + (size_t)t * a.qr.sn;
+  for (int c = 0; c < D / 64; ++c) store1(out + lane + 64 * c, acc[c] * inv);
+  if (a.lse && lane == 0) a.lse[row] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+template <int D>
+hipError_t launch_join(const RowsArgs& a, hipStream_t s) {
+  if (a.splits > 1) attn_join_kernel<D><<<dim3((a.n + 3) / 4, a.B * a.H), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+template <int D, int KT, typename Source>
+hipError_t launch_rows(RowsArgs a, const typename Source::Args& from, hipStream_t s) {
+  constexpr int BM = 32 * kRowWaves;
   constexpr size_t smem = 4 * KT * D * 2;
   a.blocks = (int)(((long long)a.n * a.G + BM - 1) / BM);
-  constexpr auto kernel = &attn_rows_kernel<D, QB, NW, KT, OCC>;
+  constexpr auto kernel = &attn_rows_kernel<D, KT, Source>;
   if (hipError_t e = set_smem_once<kernel>(smem); e != hipSuccess) return e;
-  kernel<<<(unsigned)(a.B * a.HK * a.blocks), 64 * NW, smem, s>>>(a);
-  return hipGetLastError();
+  kernel<<<(unsigned)(a.B * a.HK * a.blocks * a.splits), 64 * kRowWaves, smem, s>>>(a, from);
+  return launch_join<D>(a, s);
 }
 
 }  // namespace attn

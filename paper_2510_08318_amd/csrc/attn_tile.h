@@ -1,7 +1,6 @@
 // Tiles of keys and values in LDS for the bf16 attention kernels: rows of D bf16, 16-byte chunks XOR-swizzled by row (swz), and how they are filled.
 #pragma once
-#include "attn.h"
-#include "mfma_common.h"
+#include "attn_pool.h"
 
 namespace linattn {
 namespace attn {
@@ -62,6 +61,96 @@ __device__ __forceinline__ bf16x8 turned(uint32_t at, int c, int row0) {
   const uint32_t x = at ^ (uint32_t)(64 * c), off = (uint32_t)(row0 * D * 2);
   return __builtin_bit_cast(bf16x8, read_tr(x + off, (x ^ 32u) + off + 8 * D * 2));
 }
+
+constexpr int kRowWaves = 4;                 // wavefronts that fill a tile together
+
+// Where a workgroup's keys come from: request(j0, end, lds) asks for the tile of KT keys from j0 on, k at lds and v behind it, one call ahead of its use;
+// look(j0, end) goes before it, one more ahead; finish(), after the tile before is done with, makes it ready up to the barrier.  There is memory behind
+// every key that is asked for; mask(): the keys of the requested tile that the cache has, all ones if all.
+struct TokenArgs {
+  const void *k, *v;
+  const int* lengths;
+  Rows kr;
+};
+template <int D, int KT>
+struct TokenSource {
+  using Args = TokenArgs;
+  static constexpr bool kPaged = false;
+  const char *k, *v;
+  size_t sn;
+  int w, len, count, b, hk;
+  RowTile<D, kRowWaves, KT> rows;
+  __device__ __forceinline__ TokenSource(const Args& a, int b_, int hk_, int n, int w_, int lane) : sn(a.kr.sn), w(w_), b(b_), hk(hk_), rows(w_, lane) {
+    len = clamp_length(a.lengths, b, n);
+    count = len;
+    const size_t at = ((size_t)b * a.kr.sb + (size_t)hk * a.kr.sh) * 2;
+    k = static_cast<const char*>(a.k) + at;
+    v = static_cast<const char*>(a.v) + at;
+  }
+  __device__ __forceinline__ void look(int, int) {}
+  __device__ __forceinline__ void request(int j0, int end, uint32_t lds) {
+    rows.load(k, sn * 2, j0, end, lds, w);
+    rows.load(v, sn * 2, j0, end, lds + KT * D * 2, w);
+  }
+  __device__ __forceinline__ void finish(uint32_t) { lds_loads_landed(); }
+  __device__ __forceinline__ unsigned long long mask() const { return ~0ull; }
+  __device__ __forceinline__ TokenKeys<uint16_t> keys() const { return {reinterpret_cast<const uint16_t*>(k), reinterpret_cast<const uint16_t*>(v), sn}; }
+};
+
+// From the pool of a paged cache.  bf16 rows go straight to LDS; codes come through registers, where they become bf16.
+template <int D, int KT, bool E4M3>
+struct PoolSource {
+  using Args = Pool;
+  static constexpr bool kPaged = true;
+  static constexpr int NW = kRowWaves, LPR = D / (E4M3 ? 16 : 8), N = KT * LPR / (64 * NW);      // lanes to a row, instructions a wavefront
+  static_assert(N >= 1, "whole instructions");
+  const Pool& p;
+  int w, lane, len, count, b, hk;
+  PoolRows next;
+  unsigned long long there;
+  uint4 ck[E4M3 ? N : 1], cv[E4M3 ? N : 1];
+  uint32_t ek, ev;
+  __device__ __forceinline__ PoolSource(const Args& a, int b_, int hk_, int n, int w_, int lane_) : p(a), w(w_), lane(lane_), b(b_), hk(hk_) {
+    len = pool_length(p, b);
+    count = clamp_length(p.counts, b, n);
+  }
+  __device__ __forceinline__ int row(int i) const { return (w * N + i) * (64 / LPR) + lane / LPR; }
+  __device__ __forceinline__ void look(int j0, int end) { next.find(p, b, hk, j0, end, lane); }
+  __device__ __forceinline__ void request(int, int, uint32_t lds) {
+    there = next.there;
+    if constexpr (E4M3) { ek = p.k_exp[next.row]; ev = p.v_exp[next.row]; }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int r = row(i);
+      const long long at = next.of(r) * D;
+      if constexpr (E4M3) {
+        ck[i] = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(p.k) + at + 16 * (lane % LPR));
+        cv[i] = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(p.v) + at + 16 * (lane % LPR));
+      } else {
+        const size_t from = (size_t)at * 2 + (size_t)(((lane % LPR) ^ swz<D>(r)) * 16);
+        load_to_lds(static_cast<const char*>(p.k) + from, lds + (uint32_t)((w * N + i) * 1024));
+        load_to_lds(static_cast<const char*>(p.v) + from, lds + (uint32_t)(KT * D * 2 + (w * N + i) * 1024));
+      }
+    }
+  }
+  __device__ __forceinline__ void finish(uint32_t lds) {
+    if constexpr (E4M3) {
+      typedef __attribute__((address_space(3))) u32x4* P;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int r = row(i), c = 2 * (lane % LPR);
+        const float sk = row_scale((uint8_t)__shfl((int)ek, r)), sv = row_scale((uint8_t)__shfl((int)ev, r));
+        const uint32_t at = lds + (uint32_t)(r * (D * 2)), c0 = (uint32_t)((c ^ swz<D>(r)) * 16), c1 = c0 ^ 16u;
+        *(P)(at + c0) = __builtin_bit_cast(u32x4, decode8(make_uint2(ck[i].x, ck[i].y), sk));
+        *(P)(at + c1) = __builtin_bit_cast(u32x4, decode8(make_uint2(ck[i].z, ck[i].w), sk));
+        *(P)(at + KT * D * 2 + c0) = __builtin_bit_cast(u32x4, decode8(make_uint2(cv[i].x, cv[i].y), sv));
+        *(P)(at + KT * D * 2 + c1) = __builtin_bit_cast(u32x4, decode8(make_uint2(cv[i].z, cv[i].w), sv));
+      }
+    } else lds_loads_landed();
+  }
+  __device__ __forceinline__ unsigned long long mask() const { return KT == 64 ? there : there | ~0ull << KT; }
+  __device__ __forceinline__ PoolKeys<E4M3> keys() const { return {&p, b, hk, D}; }
+};
 
 }  // namespace attn
 }  // namespace linattn

@@ -1,16 +1,9 @@
 // The paged cache: linattn_cache_write, linattn_cache_read, linattn_cache_attn.
-// A quantised row is e4m3 codes and one exponent: x ~ code 2^e, e the least integer with max|x| 2^-e <= 448 and at least kLeastExp.  With a power of
-// two for a scale the codes' rounding is the only one: code 2^e has 4 significant bits and (e >= kLeastExp) the exponent of a normal bf16, so
-// that what is read back, as bf16 or by the attention, is the same value without another rounding.
 #include "../../include/linattn.h"
-#include "attn_plain.h"
+#include "attn_keys.h"
 
 namespace linattn {
 namespace attn {
-
-constexpr int kExpBias = 127;
-constexpr int kMostExp = 120;         // of rows with entries from 448 2^119 on
-constexpr int kLeastExp = -117;      // 2^-9, the smallest code, times 2^-117 is 2^-126, the smallest normal bf16
 
 // e of a row whose largest finite magnitude is amax: 448 = 1.75 2^8.
 __device__ __forceinline__ int row_exponent(float amax) {
@@ -18,41 +11,6 @@ __device__ __forceinline__ int row_exponent(float amax) {
   const int e = (int)(u >> 23) - 127 - 8 + ((u & 0x7fffff) > 0x600000);
   return e < kLeastExp ? kLeastExp : e;
 }
-__device__ __forceinline__ float pow2(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }      // -126 <= e <= 127
-
-// Four codes -> values times s.
-__device__ __forceinline__ void decode4(uint32_t codes, float s, float* f) {
-  const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
-  f[0] = lo[0] * s; f[1] = lo[1] * s; f[2] = hi[0] * s; f[3] = hi[1] * s;
-}
-
-// Rows of one head of the pool, for the sequence b.
-template <bool E4M3>
-struct PoolKeys {
-  const Pool* pool;
-  int b, h, d;
-  __device__ __forceinline__ bool there(int j) const { return pool_row(*pool, b, h, j) >= 0; }
-  __device__ __forceinline__ void row8(const void* base, const uint8_t* exps, int j, int c, float* f) const {
-    const long long r = pool_row(*pool, b, h, j);
-    if constexpr (E4M3) {
-      const uint2 x = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(base) + r * d + c);
-      const float s = pow2((int)exps[r] - kExpBias);
-      decode4(x.x, s, f); decode4(x.y, s, f + 4);
-    } else load8(static_cast<const uint16_t*>(base) + r * d + c, f);
-  }
-  __device__ __forceinline__ float row1(const void* base, const uint8_t* exps, int j, int c) const {
-    const long long r = pool_row(*pool, b, h, j);
-    if constexpr (E4M3) {
-      float f[4];
-      decode4(static_cast<const uint8_t*>(base)[r * d + c], pow2((int)exps[r] - kExpBias), f);
-      return f[0];
-    } else return f32::ldf(static_cast<const uint16_t*>(base), (size_t)(r * d + c));
-  }
-  __device__ __forceinline__ void k8(int j, int c, float* f) const { row8(pool->k, pool->k_exp, j, c, f); }
-  __device__ __forceinline__ void v8(int j, int c, float* f) const { row8(pool->v, pool->v_exp, j, c, f); }
-  __device__ __forceinline__ float k1(int j, int c) const { return row1(pool->k, pool->k_exp, j, c); }
-  __device__ __forceinline__ float v1(int j, int c) const { return row1(pool->v, pool->v_exp, j, c); }
-};
 
 // ---- write --------------------------------------------------------------------------------
 
@@ -161,36 +119,16 @@ hipError_t launch_cache_read(const Pool& p, bool e4m3, void* k, void* v, int n, 
 
 // ---- attention ----------------------------------------------------------------------------
 
-template <int D, bool E4M3>
-__global__ __launch_bounds__(256) void cache_attn_plain_kernel(CacheArgs a) {
-  __shared__ float sq[4][D], sp[4][64];
-  const int lane = threadIdx.x % 64, w = threadIdx.x / 64, bh = blockIdx.y, b = bh / a.H, h = bh % a.H;
-  const int t = blockIdx.x * 4 + w;
-  if (t >= a.n) return;
-  const int len = pool_length(a.pool, b), count = clamp_length(a.pool.counts, b, a.n), pos = len - count + t;
-  const size_t at = head_base(a.qr, bh, a.H) + (size_t)t * a.qr.sn;
-  float m = -INFINITY, l = 0.f, acc[D / 64] = {};
-  if (t < count && pos >= 0) {
-    for (int x = lane; x < D; x += 64) sq[w][x] = f32::ldf(static_cast<const uint16_t*>(a.q), at + x);
-    __builtin_amdgcn_wave_barrier();
-    const PoolKeys<E4M3> keys{&a.pool, b, h / (a.H / a.pool.HK), D};
-    plain_row<D>(keys, sq[w], sp[w], pos, len, a.sight, a.scale * kLog2e, lane, m, l, acc);
-  }
-  const float inv = l == 0.f ? 0.f : 1.0f / l;
-  for (int x = 0; x < D / 64; ++x) store1(static_cast<uint16_t*>(a.o) + at + lane + 64 * x, acc[x] * inv);
-  if (a.lse && lane == 0) a.lse[(size_t)bh * a.n + t] = l == 0.f ? -INFINITY : (m + __log2f(l)) * kLn2;
-}
-
 hipError_t launch_cache_attn(const CacheArgs& a, bool e4m3) {
-  const dim3 grid((a.n + 3) / 4, a.pool.B * a.H);
-  if (a.pool.d == 64) {
-    if (e4m3) cache_attn_plain_kernel<64, true><<<grid, 256, 0, a.stream>>>(a);
-    else cache_attn_plain_kernel<64, false><<<grid, 256, 0, a.stream>>>(a);
-  } else {
-    if (e4m3) cache_attn_plain_kernel<128, true><<<grid, 256, 0, a.stream>>>(a);
-    else cache_attn_plain_kernel<128, false><<<grid, 256, 0, a.stream>>>(a);
+  const Pool& p = a.pool;
+  RowsArgs r{a.q, a.o, a.lse, a.work, p.B, a.H, p.HK, a.H / p.HK, a.n, 0, 1, a.qr, a.sight, a.scale * kLog2e};
+  r.splits = cache_splits(p.B, a.H, p.HK, a.n, p.d, e4m3, reach_of(a));
+  if (few_rows(a.H, p.HK, a.n)) {
+    if (p.d == 64) return e4m3 ? launch_keys<64, true>(r, p, a.stream) : launch_keys<64, false>(r, p, a.stream);
+    return e4m3 ? launch_keys<128, true>(r, p, a.stream) : launch_keys<128, false>(r, p, a.stream);
   }
-  return hipGetLastError();
+  if (p.d == 64) return e4m3 ? launch_rows<64, 64, PoolSource<64, 64, true>>(r, p, a.stream) : launch_rows<64, 64, PoolSource<64, 64, false>>(r, p, a.stream);
+  return e4m3 ? launch_rows<128, 64, PoolSource<128, 64, true>>(r, p, a.stream) : launch_rows<128, 64, PoolSource<128, 64, false>>(r, p, a.stream);
 }
 
 }  // namespace attn

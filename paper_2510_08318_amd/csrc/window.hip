@@ -18,7 +18,8 @@ __global__ __launch_bounds__(256) void window_fwd_plain_kernel(WindowArgs a) {
   if (i < len) {
     ws[w].put(ws[w].a, static_cast<const T*>(a.q) + at, lane);
     const TokenKeys<T> keys{static_cast<const T*>(a.k) + kv, static_cast<const T*>(a.v) + kv, a.kr.sn};
-    plain_row<D>(keys, ws[w].a, ws[w].p, i, len, a.sight, a.scale * kLog2e, lane, m, l, acc);
+    const int lo = key_lo(a.sight, i), hi = key_hi(a.sight, i, len);
+    plain_row<D>(keys, ws[w].a, ws[w].p, i, len, a.sight, 0, a.sight.sinks < lo ? a.sight.sinks : lo, lo, hi, a.scale * kLog2e, lane, m, l, acc);
   }
   const float inv = l == 0.f ? 0.f : 1.0f / l;
   for (int x = 0; x < D / 64; ++x) store1(static_cast<T*>(a.o) + at + lane + 64 * x, acc[x] * inv);
@@ -93,8 +94,9 @@ static hipError_t bwd_as(const WindowArgs& a) {
 
 hipError_t launch_window_fwd(const WindowArgs& a, int dtype) {
   if (dtype == LINATTN_BF16) {
-    const RowsArgs r{a.q, a.k, a.v, a.o, a.lse, a.lengths, a.B, a.H, a.HK, a.H / a.HK, a.n, 0, a.qr, a.kr, a.sight, a.scale * kLog2e};
-    return a.d == 64 ? launch_rows<64, 1, 4, 64, 2>(r, a.stream) : launch_rows<128, 1, 4, 64, 2>(r, a.stream);
+    const TokenArgs keys{a.k, a.v, a.lengths, a.kr};
+    const RowsArgs r{a.q, a.o, a.lse, nullptr, a.B, a.H, a.HK, a.H / a.HK, a.n, 0, 1, a.qr, a.sight, a.scale * kLog2e};
+    return a.d == 64 ? launch_rows<64, 64, TokenSource<64, 64>>(r, keys, a.stream) : launch_rows<128, 64, TokenSource<128, 64>>(r, keys, a.stream);
   }
   if (dtype == LINATTN_F32) return a.d == 64 ? fwd_as<64, float>(a) : fwd_as<128, float>(a);
   return a.d == 64 ? fwd_as<64, uint16_t>(a) : fwd_as<128, uint16_t>(a);

@@ -137,6 +137,19 @@ def test_bad_cache_calls():
     assert f(x, y, y + 4) == L.E_ALIAS
 
 
+def test_cache_workspace():
+    """A single token of many keys is split, and the split's parts need room."""
+    work = P + 10 * BIG
+    c = _cache(width=100, pages=300)
+    need = L.linattn_cache_workspace_bytes(c, 4, 1)
+    assert need > 0 and need % 256 == 0
+    f = lambda w, size: L.linattn_cache_attn(c, L.Sight(-1, 0, 0, 0.0), P + 8 * BIG, P + 9 * BIG, None, 4, 1, w, size, check=False)
+    assert f(None, need) == L.E_WORKSPACE
+    assert f(work, need - 1) == L.E_WORKSPACE
+    assert f(work + 128, need) == L.E_ALIGN
+    assert f(P + 8 * BIG, need) == L.E_ALIAS
+
+
 def test_header_names_and_layouts_match_the_binding(tmp_path):
     header = open(os.path.join(ROOT, "include", "linattn.h")).read()
     consts = dict((m.group(1), int(m.group(2))) for m in re.finditer(r"#define\s+LINATTN_(\w+)\s+(-?\d+)", header))
