@@ -68,7 +68,7 @@ struct WindowArgs {
   const void *q, *k, *v, *out, *dout;
   void *o, *dq, *dk, *dv;
   float* lse;               // written by the forward, read by the backward
-  float *nl, *nd;           // workspace of the backward: fp32 [B*H][n] each, -lse / scale (-inf where nothing is seen) and -delta
+  float *nl, *nd;           // workspace of the backward: fp32 [B*H][n] each, -lse / scale (fp32 tensors: -lse; -inf where nothing is seen) and -delta
   float* parts;             // and (bf16) fp32 [part][2][key block][d], the parts of key_split
   const int* lengths;       // nullable
   int B, H, HK, n, d;

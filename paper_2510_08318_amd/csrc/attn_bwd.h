@@ -182,7 +182,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(BwdRows a) {
     ps.put(ps.b, static_cast<const uint16_t*>(a.dout) + from, lane);
     const TokenKeys<uint16_t> keys{reinterpret_cast<const uint16_t*>(kbase), reinterpret_cast<const uint16_t*>(vbase), a.kr.sn};
     float acc[D / 64];
-    plain_dq_row<D>(keys, ps.a, ps.b, ps.p, tt, len, a.sight, a.scale2, __shfl(some ? -lse / a.scale : -INFINITY, x), __shfl(delta, x), lane, acc);
+    plain_dq_row<D>(keys, ps.a, ps.b, ps.p, tt, len, a.sight, a.scale2, __shfl(some ? -lse / a.scale : -INFINITY, x), a.scale2, __shfl(delta, x), lane, acc);
     for (int c = 0; c < D / 64; ++c) store1(static_cast<uint16_t*>(a.dq) + from + lane + 64 * c, a.scale * acc[c]);
   }
 }
@@ -371,7 +371,7 @@ __global__ __launch_bounds__(2 * key_block(D), 2) void window_dkv_kernel(BwdRows
       const int hd = e / T, i0 = (q0 + e - hd * T) * BT, h = hk * G + hd;
       const size_t base = (size_t)b * a.qr.sb + (size_t)h * a.qr.sh, li = ((size_t)b * a.H + h) * a.n;
       const TokenKeys<uint16_t> rows{static_cast<const uint16_t*>(a.q) + base, static_cast<const uint16_t*>(a.dout) + base, a.qr.sn};
-      plain_dkv_row<D>(rows, ps.a, ps.b, ps.p, ps.s, i0 > jlo ? i0 : jlo, i0 + BT < jhi ? i0 + BT : jhi, a.scale2, a.nl + li, a.nd + li, lane, sk, sv);
+      plain_dkv_row<D>(rows, ps.a, ps.b, ps.p, ps.s, i0 > jlo ? i0 : jlo, i0 + BT < jhi ? i0 + BT : jhi, a.scale2, a.scale2, a.nl + li, a.nd + li, lane, sk, sv);
     }
     for (int c = 0; c < D / 64; ++c) {
       if (ks_.slot >= 0) {

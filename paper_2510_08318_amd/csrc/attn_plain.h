@@ -79,10 +79,10 @@ __device__ void plain_row(const Keys& keys, const float* sq, float* sp, int p, i
     }
 }
 
-// Sum over the keys of ds_j k_j of the query at position p, in sq, with upstream gradient in sg.  nl: -lse / scale, delta: dout . o.
+// Sum over the keys of ds_j k_j of the query at position p, in sq, with upstream gradient in sg.  p = 2^(scale2 s + nl nl2), delta: dout . o.
 template <int D, typename Keys>
 __device__ void plain_dq_row(const Keys& keys, const float* sq, const float* sg, float* sp, int p, int len, const Sight& sight, float scale2, float nl,
-                             float delta, int lane, float (&acc)[D / 64]) {
+                             float nl2, float delta, int lane, float (&acc)[D / 64]) {
   for (int x = 0; x < D / 64; ++x) acc[x] = 0.f;
   if (nl == -INFINITY) return;
   const int lo = key_lo(sight, p), hi = key_hi(sight, p, len), first = sight.sinks < lo ? sight.sinks : lo;
@@ -93,7 +93,7 @@ __device__ void plain_dq_row(const Keys& keys, const float* sq, const float* sg,
       if (j < end) {
         const float s = dot_row<D>(sq, [&](int c, float* f) { keys.k8(j, c, f); });
         const float dp = dot_row<D>(sg, [&](int c, float* f) { keys.v8(j, c, f); });
-        ds = __builtin_amdgcn_exp2f((s + nl) * scale2) * (dp - delta);
+        ds = __builtin_amdgcn_exp2f(fmaf(s, scale2, nl * nl2)) * (dp - delta);
       }
       __builtin_amdgcn_wave_barrier();
       sp[lane] = ds;
@@ -106,7 +106,7 @@ __device__ void plain_dq_row(const Keys& keys, const float* sq, const float* sg,
 
 // The part of dk (before the scale) and dv of a key, in sk and sv, that the queries i0 .. i1-1 of one head give; rows: their q (as k) and dout (as v).
 template <int D, typename Rows_>
-__device__ void plain_dkv_row(const Rows_& rows, const float* sk, const float* sv, float* sp, float* ss, int i0, int i1, float scale2,
+__device__ void plain_dkv_row(const Rows_& rows, const float* sk, const float* sv, float* sp, float* ss, int i0, int i1, float scale2, float nl2,
                               const float* nl, const float* nd, int lane, float (&dk)[D / 64], float (&dv)[D / 64]) {
   for (; i0 < i1; i0 += 64) {
     const int i = i0 + lane;
@@ -116,7 +116,7 @@ __device__ void plain_dkv_row(const Rows_& rows, const float* sk, const float* s
     if (on) {
       const float s = dot_row<D>(sk, [&](int c, float* f) { rows.k8(i, c, f); });
       const float dp = dot_row<D>(sv, [&](int c, float* f) { rows.v8(i, c, f); });
-      p = __builtin_amdgcn_exp2f((s + l) * scale2);
+      p = __builtin_amdgcn_exp2f(fmaf(s, scale2, l * nl2));
       ds = p * (dp + nd[i]);
     }
     const unsigned long long mask = __ballot(on);

@@ -1,6 +1,7 @@
 // Softmax attention with a sliding window and first tokens: linattn_window_fwd, linattn_window_bwd.
 #include "../../include/linattn.h"
 #include "attn_bwd.h"
+#include "attn_f32.h"
 
 namespace linattn {
 namespace attn {
@@ -44,7 +45,7 @@ __global__ __launch_bounds__(256) void window_dq_plain_kernel(WindowArgs a) {
     for (int x = lane; x < D; x += 64) delta = fmaf(f32::ldf(static_cast<const T*>(a.out), at + x), ws[w].b[x], delta);
     delta = wave_sum(delta);
     const TokenKeys<T> keys{static_cast<const T*>(a.k) + kv, static_cast<const T*>(a.v) + kv, a.kr.sn};
-    plain_dq_row<D>(keys, ws[w].a, ws[w].b, ws[w].p, i, len, a.sight, a.scale * kLog2e, nl, delta, lane, acc);
+    plain_dq_row<D>(keys, ws[w].a, ws[w].b, ws[w].p, i, len, a.sight, a.scale * kLog2e, nl, a.scale * kLog2e, delta, lane, acc);
   }
   if (lane == 0) {
     a.nl[(size_t)bh * a.n + i] = nl;
@@ -69,7 +70,7 @@ __global__ __launch_bounds__(256) void window_dkv_plain_kernel(WindowArgs a) {
       const int bh = b * a.H + hk * G + g;
       const size_t base = head_base(a.qr, bh, a.H);
       const TokenKeys<T> rows{static_cast<const T*>(a.q) + base, static_cast<const T*>(a.dout) + base, a.qr.sn};
-      plain_dkv_row<D>(rows, ws[w].a, ws[w].b, ws[w].p, ws[w].s, query_lo(a.sight, j), query_hi(a.sight, j, len), a.scale * kLog2e,
+      plain_dkv_row<D>(rows, ws[w].a, ws[w].b, ws[w].p, ws[w].s, query_lo(a.sight, j), query_hi(a.sight, j, len), a.scale * kLog2e, a.scale * kLog2e,
                        a.nl + (size_t)bh * a.n, a.nd + (size_t)bh * a.n, lane, dk, dv);
     }
   }
@@ -98,7 +99,7 @@ hipError_t launch_window_fwd(const WindowArgs& a, int dtype) {
     const RowsArgs r{a.q, a.o, a.lse, nullptr, a.B, a.H, a.HK, a.H / a.HK, a.n, 0, 1, a.qr, a.sight, a.scale * kLog2e};
     return a.d == 64 ? launch_rows<64, 64, TokenSource<64, 64>>(r, keys, a.stream) : launch_rows<128, 64, TokenSource<128, 64>>(r, keys, a.stream);
   }
-  if (dtype == LINATTN_F32) return a.d == 64 ? fwd_as<64, float>(a) : fwd_as<128, float>(a);
+  if (dtype == LINATTN_F32) return a.d == 64 ? launch_fwd_f32<64>(a) : launch_fwd_f32<128>(a);
   return a.d == 64 ? fwd_as<64, uint16_t>(a) : fwd_as<128, uint16_t>(a);
 }
 hipError_t launch_window_bwd(const WindowArgs& a, int dtype) {
@@ -110,7 +111,7 @@ hipError_t launch_window_bwd(const WindowArgs& a, int dtype) {
     r.qr = a.qr; r.kr = a.kr; r.sight = a.sight; r.scale = a.scale; r.scale2 = a.scale * kLog2e;
     return a.d == 64 ? launch_bwd_rows<64>(r, a.stream) : launch_bwd_rows<128>(r, a.stream);
   }
-  if (dtype == LINATTN_F32) return a.d == 64 ? bwd_as<64, float>(a) : bwd_as<128, float>(a);
+  if (dtype == LINATTN_F32) return a.d == 64 ? launch_bwd_f32<64>(a) : launch_bwd_f32<128>(a);
   return a.d == 64 ? bwd_as<64, uint16_t>(a) : bwd_as<128, uint16_t>(a);
 }
 
