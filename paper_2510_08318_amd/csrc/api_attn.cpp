@@ -58,7 +58,7 @@ int check_window(const linattn_window_desc* w, WindowArgs* a, WindowSizes* z) {
   z->lse = (size_t)w->B * w->H * w->n * sizeof(float);
   z->parts = (2 * z->lse + 255) & ~(size_t)255;
   z->work = z->parts;
-  if (w->dtype == LINATTN_BF16) z->work += (size_t)key_split(w->B * w->HK, w->H / w->HK, w->n, w->d, a->sight).parts * 2 * key_block(w->d) * w->d * sizeof(float);
+  if (w->dtype != LINATTN_F32) z->work += (size_t)key_split(w->B * w->HK, w->H / w->HK, w->n, w->d, a->sight).parts * 2 * key_block(w->d) * w->d * sizeof(float);
   return LINATTN_OK;
 }
 

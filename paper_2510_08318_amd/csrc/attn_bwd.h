@@ -28,8 +28,8 @@ struct BwdRows {
 // ---- dq -----------------------------------------------------------------------------------
 // Queries on the lanes, as in the forward: S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T.
 // EXACT: delta from a first pass over the keys, sum_j p_ij dp_ij, and not from dout . out.  Where a row sees few keys its output is as large as the
-// values, and the rounding of the stored output would be the largest error of dq and dk.
-template <int D, bool EXACT>
+// values, and the rounding of the stored output would be the largest error of dq and dk.  With fp32 arithmetic (PIECES 3) always.
+template <int D, bool EXACT, int PIECES>
 __global__ __launch_bounds__(256, 2) void window_dq_kernel(BwdRows a) {
   constexpr int NW = 4, KB = BT / 32, KS = D / 16, CB = D / 32, BM = 32 * NW, TILE = BT * D * 2;
   extern __shared__ __align__(16) char smem[];
@@ -146,11 +146,10 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(BwdRows a) {
     for (int r = 0; r < 16; ++r) dp[r] = p[r] * (dp[r] - delta);
 #pragma unroll
     for (int st = 0; st < 2; ++st) {
-      const uint4 ds = pack8(dp, st);
+      uint4 ds[PIECES];
+      weights_operand<PIECES>(dp, st, ds);
 #pragma unroll
-      for (int c = 0; c < CB; ++c) {
-        dq[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(turned<D>(kt + turned_rows, c, 16 * (2 * kb + st)), as_bf16x8(ds), dq[c], 0, 0, 0);
-      }
+      for (int c = 0; c < CB; ++c) dq[c] = mfma_weights<PIECES>(turned<D>(kt + turned_rows, c, 16 * (2 * kb + st)), ds, dq[c]);
     }
   });
 
@@ -214,7 +213,7 @@ __device__ __forceinline__ KeyShare key_share(const BwdRows& a, int id, int coun
 // and dS = p dP; dV^T += dO^T P, dK^T += Q^T dS with P and dS as they lie.
 // Width 128: eight wavefronts, k in LDS.  With k and v in registers beside the 128 of the sums, a lane needs more than the 256 that two wavefronts to a SIMD
 // leave it.
-template <int D>
+template <int D, int PIECES>
 __global__ __launch_bounds__(2 * key_block(D), 2) void window_dkv_kernel(BwdRows a) {
   constexpr int BK = key_block(D), NW = BK / 32, KS = D / 16, CB = D / 32, TILE = BT * D * 2, BUF = 2 * TILE + 2 * BT * 4;
   constexpr bool KLDS = D == 128;
@@ -312,11 +311,22 @@ __global__ __launch_bounds__(2 * key_block(D), 2) void window_dkv_kernel(BwdRows
         for (int r = 0; r < 16; ++r) dp[r] *= s[r];
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
-          const uint4 p = pack8(s, st), ds = pack8(dp, st);
+          uint4 x[PIECES];
+          if constexpr (PIECES == 1) {
+            const uint4 p[1] = {pack8(s, st)};
+            x[0] = pack8(dp, st);
 #pragma unroll
-          for (int c = 0; c < CB; ++c) {
-            dv[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(turned<D>(gt + ta, c, 16 * (2 * qb + st)), as_bf16x8(p), dv[c], 0, 0, 0);
-            dk[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(turned<D>(qt + ta, c, 16 * (2 * qb + st)), as_bf16x8(ds), dk[c], 0, 0, 0);
+            for (int c = 0; c < CB; ++c) {
+              dv[c] = mfma_weights<1>(turned<D>(gt + ta, c, 16 * (2 * qb + st)), p, dv[c]);
+              dk[c] = mfma_weights<1>(turned<D>(qt + ta, c, 16 * (2 * qb + st)), x, dk[c]);
+            }
+          } else {
+            weights_operand<PIECES>(s, st, x);
+#pragma unroll
+            for (int c = 0; c < CB; ++c) dv[c] = mfma_weights<PIECES>(turned<D>(gt + ta, c, 16 * (2 * qb + st)), x, dv[c]);
+            weights_operand<PIECES>(dp, st, x);
+#pragma unroll
+            for (int c = 0; c < CB; ++c) dk[c] = mfma_weights<PIECES>(turned<D>(qt + ta, c, 16 * (2 * qb + st)), x, dk[c]);
           }
         }
       }
@@ -412,25 +422,25 @@ __global__ __launch_bounds__(256) void window_dkv_sum_kernel(BwdRows a, int shar
   *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(s.x * f, s.y * f), pack_bf16x2(s.z * f, s.w * f));
 }
 
-template <int D>
+template <int D, int PIECES>
 hipError_t launch_bwd_rows(BwdRows a, hipStream_t s) {
   constexpr size_t q_smem = 4 * BT * D * 2, k_smem = 2 * (2 * BT * D * 2 + 2 * BT * 4) + (D == 128 ? key_block(D) * D * 2 : 0);
   a.blocks = (int)(((long long)a.n * a.G + 127) / 128);
   const int reach = a.sight.left < 0 || a.sight.right < 0 ? a.n : a.sight.left + a.sight.right + 1;
-  const bool exact = (long long)reach + a.sight.sinks <= kFewKeys;
+  const bool exact = PIECES > 1 || (long long)reach + a.sight.sinks <= kFewKeys;
   const unsigned grid = (unsigned)(a.B * a.HK * a.blocks);
   if (exact) {
-    constexpr auto kernel = &window_dq_kernel<D, true>;
+    constexpr auto kernel = &window_dq_kernel<D, true, PIECES>;
     if (hipError_t e = set_smem_once<kernel>(q_smem); e != hipSuccess) return e;
     kernel<<<grid, 256, q_smem, s>>>(a);
-  } else {
-    constexpr auto kernel = &window_dq_kernel<D, false>;
+  } else if constexpr (PIECES == 1) {
+    constexpr auto kernel = &window_dq_kernel<D, false, 1>;
     if (hipError_t e = set_smem_once<kernel>(q_smem); e != hipSuccess) return e;
     kernel<<<grid, 256, q_smem, s>>>(a);
   }
   const KeySplit split = key_split(a.B * a.HK, a.G, a.n, D, a.sight);
   a.blocks = split.blocks; a.sink_blocks = split.sink_blocks; a.sink_share = split.sink_share; a.share = split.share;
-  constexpr auto kernel = &window_dkv_kernel<D>;
+  constexpr auto kernel = &window_dkv_kernel<D, PIECES>;
   if (hipError_t e = set_smem_once<kernel>(k_smem); e != hipSuccess) return e;
   kernel<<<(unsigned)split.workgroups, 2 * key_block(D), k_smem, s>>>(a);
   if (split.parts) {

@@ -80,6 +80,26 @@ __device__ __forceinline__ uint4 pack8(const f32x16& e, int h) {
                     pack_bf16x2(e[8 * h + 6], e[8 * h + 7]));
 }
 
+// The operand of weights e[8h .. 8h+7]: PIECES of 1 rounds them to bf16, 3 hands them on whole, as the exact sum of three bf16 numbers (LINATTN_BF16_F32MATH: the other
+// operand of their product is bf16, so three products give it in fp32).
+template <int PIECES>
+__device__ __forceinline__ void weights_operand(const f32x16& e, int h, uint4 (&p)[PIECES]) {
+  if constexpr (PIECES == 1) p[0] = pack8(e, h);
+  else {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = e[8 * h + i];
+    f32::split8(f, p);
+  }
+}
+// acc += a p, the smallest piece first
+template <int PIECES>
+__device__ __forceinline__ f32x16 mfma_weights(bf16x8 a, const uint4 (&p)[PIECES], f32x16 acc) {
+#pragma unroll
+  for (int i = PIECES - 1; i >= 0; --i) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, as_bf16x8(p[i]), acc, 0, 0, 0);
+  return acc;
+}
+
 // Scores of a query's keys (half of them in each lane of a pair) -> weights 2^(scale2 s - mx), with the running maximum mx, the sum l of the lane's weights, and o
 // brought to it.  The maximum moves only where it has grown by more than 8: the weights are then at most 2^8, and the result the same after
 // the division.
@@ -134,7 +154,7 @@ __device__ void plain_again(const RowsArgs& a, const Keys& keys, const Tiles& ti
   if (a.lse && lane == 0) a.lse[li] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-template <int D, int KT, typename Source>
+template <int D, int KT, typename Source, int PIECES>
 __global__ __launch_bounds__(64 * kRowWaves, 2) void attn_rows_kernel(RowsArgs a, typename Source::Args from) {
   constexpr int QB = 1, NW = kRowWaves;
   constexpr int KB = KT / 32, KS = D / 16, CB = D / 32, BM = 32 * QB * NW, TILE = KT * D * 2;
@@ -220,7 +240,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attn_rows_kernel(RowsArgs a
 #pragma unroll
           for (int i = 0; i < QB; ++i) s[i][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop, as_bf16x8(q[i][ks]), s[i][kb], 0, 0, 0);
         }
-      uint4 p[QB][2 * KB];
+      uint4 p[QB][PIECES == 1 ? 2 * KB : 1];
 #pragma unroll
       for (int i = 0; i < QB; ++i) {
         if (!plain) {
@@ -241,13 +261,20 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attn_rows_kernel(RowsArgs a
           for (int h2 = 0; h2 < 2; ++h2) p[i][2 * kb + h2] = pack8(s[i][kb], h2);
       }
 #pragma unroll
-      for (int st = 0; st < 2 * KB; ++st)
+      for (int st = 0; st < 2 * KB; ++st) {
+        uint4 x[QB][PIECES];
+#pragma unroll
+        for (int i = 0; i < QB; ++i) {
+          if constexpr (PIECES == 1) x[i][0] = p[i][st];
+          else weights_operand<PIECES>(s[i][st / 2], st % 2, x[i]);
+        }
 #pragma unroll
         for (int c = 0; c < CB; ++c) {
           const bf16x8 vop = turned<D>(vt + turned_rows, c, 16 * st);
 #pragma unroll
-          for (int i = 0; i < QB; ++i) o[i][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop, as_bf16x8(p[i][st]), o[i][c], 0, 0, 0);
+          for (int i = 0; i < QB; ++i) o[i][c] = mfma_weights<PIECES>(vop, x[i], o[i][c]);
         }
+      }
     }
     if (it + 1 < it1) src.finish(lds + (uint32_t)((it + 1) & 1) * 2 * TILE);
     __syncthreads();
@@ -326,12 +353,12 @@ hipError_t launch_join(const RowsArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int D, int KT, typename Source>
+template <int D, int KT, typename Source, int PIECES = 1>
 hipError_t launch_rows(RowsArgs a, const typename Source::Args& from, hipStream_t s) {
   constexpr int BM = 32 * kRowWaves;
   constexpr size_t smem = 4 * KT * D * 2;
   a.blocks = (int)(((long long)a.n * a.G + BM - 1) / BM);
-  constexpr auto kernel = &attn_rows_kernel<D, KT, Source>;
+  constexpr auto kernel = &attn_rows_kernel<D, KT, Source, PIECES>;
   if (hipError_t e = set_smem_once<kernel>(smem); e != hipSuccess) return e;
   kernel<<<(unsigned)(a.B * a.HK * a.blocks * a.splits), 64 * kRowWaves, smem, s>>>(a, from);
   return launch_join<D>(a, s);

@@ -179,26 +179,27 @@ def _need(ok: bool, what: str):
 
 
 def _on_device_of(fn):
-    """Runs `fn` with the device of its first tensor argument current (the library launches on the current device)."""
+    """Runs `fn` with the device of its first argument current (the library launches on the current device)."""
     @functools.wraps(fn)
-    def call(*args, **kw):
-        t = args[0] if isinstance(args[0], torch.Tensor) else args[0].k
-        _need(t.is_cuda, "tensors must be on the GPU")
-        if t.device.index == torch.cuda.current_device():
-            return fn(*args, **kw)
-        with torch.cuda.device(t.device):
-            return fn(*args, **kw)
+    def call(first, *args, **kw):
+        index = first.get_device() if isinstance(first, torch.Tensor) else first.index
+        if index == torch.cuda.current_device():
+            return fn(first, *args, **kw)
+        _need(index >= 0, "tensors must be on the GPU")
+        with torch.cuda.device(index):
+            return fn(first, *args, **kw)
     return call
 
 
-def _check_tokens(name, t, shape, dtype, device):
-    _need(t.device == device and t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous(),
-          f"{name}: expected a contiguous {dtype} tensor {tuple(shape)} on {device}")
+def _check_tokens(name, t, shape, dtype, index):
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)} on GPU {index}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
 
 
-def _check_ints(name, t, shape, device):
+def _check_ints(name, t, shape, index):
     if t is not None:
-        _check_tokens(name, t, shape, torch.int32, device)
+        _check_tokens(name, t, shape, torch.int32, index)
 
 
 def _token_dims(t, layout):
@@ -217,10 +218,11 @@ def _window_desc(q, k, v, left, right, sinks, scale, layout, lengths, f32_math):
     B, H, n, d = _token_dims(q, layout)
     HK = _token_dims(k, layout)[1]
     _need(q.dtype in (torch.bfloat16, torch.float32), "bf16 or fp32 tensors")
-    _check_tokens("q", q, q.shape, q.dtype, q.device)
-    for name, t in (("k", k), ("v", v)):
-        _check_tokens(name, t, _token_shape(B, HK, n, d, layout), q.dtype, q.device)
-    _check_ints("lengths", lengths, (B,), q.device)
+    index, shape = q.get_device(), _token_shape(B, HK, n, d, layout)
+    _check_tokens("q", q, q.shape, q.dtype, index)
+    _check_tokens("k", k, shape, q.dtype, index)
+    _check_tokens("v", v, shape, q.dtype, index)
+    _check_ints("lengths", lengths, (B,), index)
     dtype = (B_.BF16_F32MATH if f32_math else B_.BF16) if q.dtype == torch.bfloat16 else B_.F32
     return B_.WindowDesc(dtype, B, H, HK, n, d, B_.LAYOUT_BNHD if layout == "bnhd" else B_.LAYOUT_BHND,
                          B_.Sight(left, right, sinks, scale), B_._ptr(lengths), None, 0)
@@ -235,8 +237,8 @@ def window_attention(q, k, v, *, left=-1, right=-1, sinks=0, scale=0.0, layout="
     desc = _window_desc(q, k, v, left, right, sinks, scale, layout, lengths, f32_math)
     out = torch.empty_like(q) if out is None else out
     lse = torch.empty((desc.B, desc.H, desc.n), dtype=torch.float32, device=q.device) if lse is None else lse
-    _check_tokens("out", out, q.shape, q.dtype, q.device)
-    _check_tokens("lse", lse, (desc.B, desc.H, desc.n), torch.float32, q.device)
+    _check_tokens("out", out, q.shape, q.dtype, q.get_device())
+    _check_tokens("lse", lse, (desc.B, desc.H, desc.n), torch.float32, q.get_device())
     B_.linattn_window_fwd(desc, q, k, v, out, lse, _current_stream())
     return out, lse
 
@@ -248,8 +250,8 @@ def window_attention_backward(q, k, v, out, lse, dout, *, left=-1, right=-1, sin
     desc = _window_desc(q, k, v, left, right, sinks, scale, layout, lengths, f32_math)
     dq, dk, dv = [torch.empty_like(t) if g is None else g for g, t in ((dq, q), (dk, k), (dv, v))]
     for name, t, like in (("out", out, q), ("dout", dout, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, v)):
-        _check_tokens(name, t, like.shape, q.dtype, q.device)
-    _check_tokens("lse", lse, (desc.B, desc.H, desc.n), torch.float32, q.device)
+        _check_tokens(name, t, like.shape, q.dtype, q.get_device())
+    _check_tokens("lse", lse, (desc.B, desc.H, desc.n), torch.float32, q.get_device())
     size = B_.linattn_window_workspace_bytes(desc)
     work = torch.empty(size, dtype=torch.uint8, device=q.device)
     desc.workspace, desc.workspace_bytes = B_._ptr(work), size
@@ -268,15 +270,17 @@ class PagedCache:
         self.k, self.v, self.table, self.lengths, self.k_exp, self.v_exp = k, v, table, lengths, k_exp, v_exp
         self.pages, self.H, self.page, self.d = k.shape
         self.B, self.width = table.shape
+        self.index = k.get_device()
+        _need(self.index >= 0, "tensors must be on the GPU")
         quantised = k.dtype == torch.float8_e4m3fn
         for name, t in (("k", k), ("v", v)):
-            _check_tokens(name, t, k.shape, k.dtype, k.device)
-        _check_ints("table", table, table.shape, k.device)
-        _check_ints("lengths", lengths, (self.B,), k.device)
+            _check_tokens(name, t, k.shape, k.dtype, self.index)
+        _check_ints("table", table, table.shape, self.index)
+        _check_ints("lengths", lengths, (self.B,), self.index)
         _need((k_exp is not None and v_exp is not None) == quantised, "k_exp and v_exp go with float8 rows")
         for name, t in (("k_exp", k_exp), ("v_exp", v_exp)):
             if t is not None:
-                _check_tokens(name, t, k.shape[:3], torch.uint8, k.device)
+                _check_tokens(name, t, k.shape[:3], torch.uint8, self.index)
         self._desc = B_.CacheDesc(B_.CACHE_E4M3 if quantised else B_.CACHE_BF16, self.B, self.H, self.d, self.page, self.pages, self.width,
                                   0, *[B_._ptr(t) for t in (k, v, k_exp, v_exp, table, lengths)], None)
 
@@ -288,7 +292,7 @@ class PagedCache:
         return cls(*rows, torch.full((B, width), -1, dtype=torch.int32, device=device), torch.zeros(B, dtype=torch.int32, device=device), *exps)
 
     def _describe(self, layout, counts):
-        _check_ints("counts", counts, (self.B,), self.k.device)
+        _check_ints("counts", counts, (self.B,), self.index)
         desc = B_.CacheDesc.from_buffer_copy(self._desc)
         desc.layout, desc.counts = B_.LAYOUT_BNHD if layout == "bnhd" else B_.LAYOUT_BHND, B_._ptr(counts)
         return desc
@@ -298,8 +302,9 @@ class PagedCache:
         """Put a chunk's rows into the cache.  k, v: bf16 [B, n, H, d] or [B, H, n, d]; counts: int32 [B], the new tokens of each sequence
         (None: n), at its positions lengths - counts, ..."""
         n = _token_dims(k, layout)[2]
-        for name, t in (("k", k), ("v", v)):
-            _check_tokens(name, t, _token_shape(self.B, self.H, n, self.d, layout), torch.bfloat16, self.k.device)
+        shape = _token_shape(self.B, self.H, n, self.d, layout)
+        _check_tokens("k", k, shape, torch.bfloat16, self.index)
+        _check_tokens("v", v, shape, torch.bfloat16, self.index)
         B_.linattn_cache_write(self._describe(layout, counts), k, v, n, _current_stream())
 
     @_on_device_of
@@ -309,7 +314,7 @@ class PagedCache:
         shape = _token_shape(self.B, self.H, n, self.d, layout)
         k, v = [torch.empty(shape, dtype=torch.bfloat16, device=self.k.device) if t is None else t for t in (k, v)]
         for name, t in (("k", k), ("v", v)):
-            _check_tokens(name, t, shape, torch.bfloat16, self.k.device)
+            _check_tokens(name, t, shape, torch.bfloat16, self.index)
         B_.linattn_cache_read(self._describe(layout, None), k, v, n, _current_stream())
         return k, v
 
@@ -319,11 +324,11 @@ class PagedCache:
         multiple of the cache's heads; left, right, sinks, scale as in window_attention, by position in the sequence.
         Returns (out, lse); lse is fp32 [B, H, n]."""
         B, H, n, d = _token_dims(q, layout)
-        _check_tokens("q", q, _token_shape(self.B, H, n, self.d, layout), torch.bfloat16, self.k.device)
+        _check_tokens("q", q, _token_shape(self.B, H, n, self.d, layout), torch.bfloat16, self.index)
         out = torch.empty_like(q) if out is None else out
         lse = torch.empty((B, H, n), dtype=torch.float32, device=q.device) if lse is None else lse
-        _check_tokens("out", out, q.shape, q.dtype, q.device)
-        _check_tokens("lse", lse, (B, H, n), torch.float32, q.device)
+        _check_tokens("out", out, q.shape, q.dtype, self.index)
+        _check_tokens("lse", lse, (B, H, n), torch.float32, self.index)
         desc = self._describe(layout, counts)
         size = B_.linattn_cache_workspace_bytes(desc, H, n)
         work = torch.empty(size, dtype=torch.uint8, device=q.device) if size else None
