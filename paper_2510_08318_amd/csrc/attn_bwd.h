@@ -29,8 +29,10 @@ struct BwdRows {
 // Queries on the lanes, as in the forward: S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T.
 // EXACT: delta from a first pass over the keys, sum_j p_ij dp_ij, and not from dout . out.  Where a row sees few keys its output is as large as the
 // values, and the rounding of the stored output would be the largest error of dq and dk.  With fp32 arithmetic (PIECES 3) always.
+constexpr float kHeavyWeight = 0.125f;      // (see window_dq_kernel)
+
 template <int D, bool EXACT, int PIECES>
-__global__ __launch_bounds__(256, 2) void window_dq_kernel(BwdRows a) {
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void window_dq_kernel(BwdRows a) {
   constexpr int NW = 4, KB = BT / 32, KS = D / 16, CB = D / 32, BM = 32 * NW, TILE = BT * D * 2;
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
@@ -39,12 +41,27 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(BwdRows a) {
   const int len = clamp_length(a.lengths, b, a.n), rows = len * G, all = a.n * G;
   const int row0 = block * BM + w * 32;
 
-  const int r0 = row0 + m, t = r0 / G, h = hk * G + (r0 - t * G);
-  const bool store = r0 < all, live = r0 < rows;
-  const size_t at = (size_t)b * a.qr.sb + (size_t)h * a.qr.sh + (size_t)t * a.qr.sn, li = ((size_t)b * a.H + h) * a.n + t;
-  const int lo = live ? key_lo(a.sight, t) : 0, hi = live ? key_hi(a.sight, t, len) : 0;
+  // where a lane's row lies (worked out again after the loop, where there are registers for it)
+  struct Place {
+    int t;
+    bool store, live;
+    size_t at, li;
+  };
+  auto place = [&](int lane_) {
+    Place p;
+    const int r = row0 + lane_ % 32;
+    p.t = r / G;
+    const int h = hk * G + (r - p.t * G);
+    p.store = r < all; p.live = r < rows;
+    p.at = (size_t)b * a.qr.sb + (size_t)h * a.qr.sh + (size_t)p.t * a.qr.sn;
+    p.li = ((size_t)b * a.H + h) * a.n + p.t;
+    return p;
+  };
+  const Place first = place(lane);
+  const bool live = first.live;
+  const size_t at = first.at;
   uint4 q[KS], go[KS];
-  float delta = 0.f, lse = live ? a.lse[li] : -INFINITY;
+  float delta = 0.f;
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
     const size_t c = at + 16 * ks + 8 * g;
@@ -68,8 +85,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(BwdRows a) {
     pair32(delta, x, y);
     delta = x + y;
   }
-  const bool some = lse != -INFINITY;
-  const float nl2 = some ? -lse * kLog2e : -INFINITY;
+  const float lse = live ? a.lse[first.li] : -INFINITY, nl2 = lse == -INFINITY ? lse : -lse * kLog2e;
 
   const int last_row = ((block + 1) * BM < rows ? (block + 1) * BM : rows) - 1, wlast = (row0 + 32 < rows ? row0 + 32 : rows) - 1;
   const KeyTiles<BT> tiles(a.sight, block * BM / G, last_row < block * BM ? -1 : last_row / G, len);
@@ -84,7 +100,6 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(BwdRows a) {
     loader.load(kbase, pitch, j0, tiles.end, to, w);
     loader.load(vbase, pitch, j0, tiles.end, to + TILE, w);
   };
-  const uint32_t rows_at = row_at<D>(lane), turned_rows = turned_at<D>(lane);
 
   f32x16 dq[CB];
 #pragma unroll
@@ -104,6 +119,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(BwdRows a) {
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
           f32x16 s = fill16(0.f), dp = fill16(0.f);
+          const uint32_t rows_at = row_at<D>((int)opaque_lane(lane));
 #pragma unroll
           for (int ks = 0; ks < KS; ++ks) {
             s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(row_chunk<D>(kt + rows_at, ks, 32 * kb)), as_bf16x8(q[ks]), s, 0, 0, 0);
@@ -112,7 +128,8 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(BwdRows a) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale2, nl2));
           if (!plain) {
-            asm volatile("");        // a branch: as selects, the mask is computed for every tile
+            const Place mine = place((int)opaque_lane(lane));      // (opaque: a branch; as selects, the mask is computed for every tile)
+            const int lo = mine.live ? key_lo(a.sight, mine.t) : 0, hi = mine.live ? key_hi(a.sight, mine.t, len) : 0;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
               const int j = j0 + 32 * kb + 8 * (r / 4) + 4 * g + r % 4;
@@ -121,7 +138,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(BwdRows a) {
               dp[r] = on ? dp[r] : 0.f;
             }
           }
-          use(kb, s, dp, kt);
+          use(kb, s, dp, kt, j0);
         }
       }
       lds_loads_landed();
@@ -129,7 +146,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(BwdRows a) {
     }
   };
   if (EXACT) {
-    pass([&](int, const f32x16& p, const f32x16& dp, uint32_t) {
+    pass([&](int, const f32x16& p, const f32x16& dp, uint32_t, int) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) delta = fmaf(p[r], dp[r], delta);
     });
@@ -137,13 +154,28 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(BwdRows a) {
     pair32(delta, x, y);
     delta = x + y;
   }
-  if (store && g == 0) {
-    a.nl[li] = some ? -lse / a.scale : -INFINITY;
-    a.nd[li] = -delta;
-  }
-  pass([&](int kb, const f32x16& p, f32x16& dp, uint32_t kt) {
+  // delta from the stored output is off by what its rounding took, which is the sum of the row's dS; the key side gets it corrected.  dq is off by that times the
+  // mean key of the row, which is small beside a key unless a few have most of the weight: the heaviest one's part of it is taken out at the end (12
+  // heads x 4133 x 64, causal, normalised q and k of scale 0.5 to 1.5: error of dq 2.6e-3, with it 2.4e-3, where rounding dS and dq alone is 2.35e-3).
+  float off = 0.f, heavy = kHeavyWeight;
+  int at_key = -1;
+  pass([&](int kb, const f32x16& p, f32x16& dp, uint32_t kt, int j0) {
+    const uint32_t turned_rows = turned_at<D>((int)opaque_lane(lane));
+    if (!EXACT) {
+      float top = p[0];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) dp[r] = p[r] * (dp[r] - delta);
+      for (int r = 1; r < 16; ++r) top = fmaxf(top, p[r]);
+      if (__any(top > heavy)) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (p[r] > heavy) { heavy = p[r]; at_key = j0 + 32 * kb + 8 * (r / 4) + 4 * g + r % 4; }
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      dp[r] = p[r] * (dp[r] - delta);
+      if (!EXACT) off += dp[r];
+    }
 #pragma unroll
     for (int st = 0; st < 2; ++st) {
       uint4 ds[PIECES];
@@ -152,9 +184,40 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(BwdRows a) {
       for (int c = 0; c < CB; ++c) dq[c] = mfma_weights<PIECES>(turned<D>(kt + turned_rows, c, 16 * (2 * kb + st)), ds, dq[c]);
     }
   });
+  if (!EXACT) {
+    float x, y;
+    pair32(off, x, y);
+    off = x + y;
+    delta += off;
+    if (__any(at_key >= 0)) {
+      float h0, h1, k0, k1;
+      pair32(heavy, h0, h1);
+      pair32(__builtin_bit_cast(float, at_key), k0, k1);
+      heavy = fmaxf(h0, h1);
+      at_key = __builtin_bit_cast(int, h1 > h0 ? k1 : k0);
+      if (at_key >= 0) {
+        const uint16_t* kr = reinterpret_cast<const uint16_t*>(kbase + (size_t)at_key * pitch) + 4 * g;
+        const float f = -off * heavy;
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+          for (int r = 0; r < 16; r += 4) {
+            const uint2 y4 = *reinterpret_cast<const uint2*>(kr + 32 * c + 2 * r);
+            dq[c][r] = fmaf(f, f32::lo_f32(y4.x), dq[c][r]); dq[c][r + 1] = fmaf(f, f32::hi_f32(y4.x), dq[c][r + 1]);
+            dq[c][r + 2] = fmaf(f, f32::lo_f32(y4.y), dq[c][r + 2]); dq[c][r + 3] = fmaf(f, f32::hi_f32(y4.y), dq[c][r + 3]);
+          }
+      }
+    }
+  }
+  const Place here = place((int)opaque_lane(lane));
+  const float nl = nl2 == -INFINITY ? nl2 : nl2 / a.scale2;
+  if (here.store && g == 0) {
+    a.nl[here.li] = nl;
+    a.nd[here.li] = -delta;
+  }
 
   // Masked keys have dS = 0, which an infinity or NaN in k would make NaN: rows that come out not finite are done again key by key.
-  if (!live) {
+  if (!here.live) {
 #pragma unroll
     for (int c = 0; c < CB; ++c) dq[c] = fill16(0.f);
   }
@@ -164,8 +227,8 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(BwdRows a) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) test = fmaf(0.f, dq[c][r], test);
   uint32_t again = (uint32_t)__ballot(test != 0.f) | (uint32_t)(__ballot(test != 0.f) >> 32);
-  if (store && !(again >> m & 1)) {
-    uint16_t* to = static_cast<uint16_t*>(a.dq) + at + 4 * g;
+  if (here.store && !(again >> m & 1)) {
+    uint16_t* to = static_cast<uint16_t*>(a.dq) + here.at + 4 * g;
 #pragma unroll
     for (int c = 0; c < CB; ++c)
 #pragma unroll
@@ -181,7 +244,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(BwdRows a) {
     ps.put(ps.b, static_cast<const uint16_t*>(a.dout) + from, lane);
     const TokenKeys<uint16_t> keys{reinterpret_cast<const uint16_t*>(kbase), reinterpret_cast<const uint16_t*>(vbase), a.kr.sn};
     float acc[D / 64];
-    plain_dq_row<D>(keys, ps.a, ps.b, ps.p, tt, len, a.sight, a.scale2, __shfl(some ? -lse / a.scale : -INFINITY, x), a.scale2, __shfl(delta, x), lane, acc);
+    plain_dq_row<D>(keys, ps.a, ps.b, ps.p, tt, len, a.sight, a.scale2, __shfl(nl, x), a.scale2, __shfl(delta, x), lane, acc);
     for (int c = 0; c < D / 64; ++c) store1(static_cast<uint16_t*>(a.dq) + from + lane + 64 * c, a.scale * acc[c]);
   }
 }
