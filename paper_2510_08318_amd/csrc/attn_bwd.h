@@ -36,7 +36,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void window_dq_kernel(BwdRows
   constexpr int NW = 4, KB = BT / 32, KS = D / 16, CB = D / 32, BM = 32 * NW, TILE = BT * D * 2;
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
-  const int id = xcd_stretch(blockIdx.x, gridDim.x), bk = id / a.blocks, block = row_block(a.sight, id % a.blocks, a.blocks);
+  const PairPlace where = pair_place(blockIdx.x, a.B * a.HK, a.blocks);
+  const int bk = where.pair, block = row_block(a.sight, where.at, a.blocks);
   const int b = bk / a.HK, hk = bk % a.HK, G = a.G;
   const int len = clamp_length(a.lengths, b, a.n), rows = len * G, all = a.n * G;
   const int row0 = block * BM + w * 32;
@@ -255,7 +256,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void window_dq_kernel(BwdRows
 struct KeyShare {
   int bk, block, part, parts, slot;      // slot: of its partial sums, -1 where it is the only one
 };
-__device__ __forceinline__ KeyShare key_share(const BwdRows& a, int id, int count) {
+__device__ __forceinline__ KeyShare key_share(const BwdRows& a, int id) {
   // the blocks of the first tokens come first, as their workgroups may have the most to do, and in turn to the XCDs
   KeyShare r;
   const int heads = a.B * a.HK, sink_wgs = heads * a.sink_blocks * a.sink_share, ns = a.sink_blocks > 0 ? a.sink_blocks : 1;
@@ -265,9 +266,9 @@ __device__ __forceinline__ KeyShare key_share(const BwdRows& a, int id, int coun
     r.part = id % a.sink_share; r.parts = a.sink_share; r.block = x % ns; r.bk = x / ns;
     r.slot = a.sink_share > 1 ? id : -1;
   } else {
-    const int y = xcd_stretch(id - sink_wgs, count - sink_wgs), x = y / a.share;
-    r.part = y % a.share; r.parts = a.share; r.block = a.sink_blocks + x % rest; r.bk = x / rest;
-    r.slot = a.share > 1 ? (a.sink_share > 1 ? sink_wgs : 0) + y : -1;
+    const PairPlace place = pair_place(id - sink_wgs, heads, rest * a.share);
+    r.part = place.at % a.share; r.parts = a.share; r.block = a.sink_blocks + place.at / a.share; r.bk = place.pair;
+    r.slot = a.share > 1 ? (a.sink_share > 1 ? sink_wgs : 0) + (place.pair * rest + place.at / a.share) * a.share + r.part : -1;
   }
   return r;
 }
@@ -282,7 +283,7 @@ __global__ __launch_bounds__(2 * key_block(D), 2) void window_dkv_kernel(BwdRows
   constexpr bool KLDS = D == 128;
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
-  const KeyShare ks_ = key_share(a, blockIdx.x, gridDim.x);
+  const KeyShare ks_ = key_share(a, blockIdx.x);
   const int b = ks_.bk / a.HK, hk = ks_.bk % a.HK, G = a.G;
   const int len = clamp_length(a.lengths, b, a.n);
   const int jb0 = ks_.block * BK, jb1 = (jb0 + BK < len ? jb0 + BK : len) - 1;      // the block's keys

@@ -72,7 +72,9 @@ __global__ __launch_bounds__(256, 2) void window_fwd_f32_kernel(WindowArgs a) {
   constexpr int CB = D / 32, NW = kRowWaves;
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
-  const int id = xcd_stretch(blockIdx.x, gridDim.x), blocks = (a.n + 31) / 32, bh = id / blocks, block = row_block(a.sight, id % blocks, blocks);
+  const int blocks = (a.n + 31) / 32;
+  const PairPlace place = pair_place(blockIdx.x, a.B * a.H, blocks);
+  const int bh = place.pair, block = row_block(a.sight, place.at, blocks);
   const int b = bh / a.H, h = bh % a.H, len = clamp_length(a.lengths, b, a.n), t = block * 32 + m;
   const bool live = t < len;
   const float* qbase = static_cast<const float*>(a.q) + head_base(a.qr, bh, a.H);
@@ -173,7 +175,9 @@ __global__ __launch_bounds__(256, 1) void window_dq_f32_kernel(WindowArgs a) {
   constexpr int CB = D / 32, NW = kRowWaves;
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
-  const int id = xcd_stretch(blockIdx.x, gridDim.x), blocks = (a.n + 31) / 32, bh = id / blocks, block = row_block(a.sight, id % blocks, blocks);
+  const int blocks = (a.n + 31) / 32;
+  const PairPlace place = pair_place(blockIdx.x, a.B * a.H, blocks);
+  const int bh = place.pair, block = row_block(a.sight, place.at, blocks);
   const int b = bh / a.H, h = bh % a.H, len = clamp_length(a.lengths, b, a.n), t = block * 32 + m;
   const bool live = t < len;
   const size_t head = head_base(a.qr, bh, a.H), row = head + (size_t)t * a.qr.sn, li = (size_t)bh * a.n + t;

@@ -40,6 +40,18 @@ __device__ __forceinline__ int xcd_stretch(int i, int count) {
   return x < full ? x * per + at : full * per + (x - full) * (per - 1) + at;
 }
 
+// Workgroup id of pairs * per -> its (batch item, key head) pair and its place among the pair's `per` workgroups.  A pair's workgroups, which read the same
+// keys, go to one XCD, neighbouring pairs (of one item, or of sequences of unlike lengths) to different ones; the pairs that are left over are cut into stretches.
+struct PairPlace {
+  int pair, at;
+};
+__device__ __forceinline__ PairPlace pair_place(int id, int pairs, int per) {
+  const int each = pairs / kXCDs * per, x = id % kXCDs, i = id / kXCDs;
+  if (i < each) return {x + kXCDs * (i / per), i % per};
+  const int rest = xcd_stretch(id - kXCDs * each, (pairs % kXCDs) * per);
+  return {pairs / kXCDs * kXCDs + rest / per, rest % per};
+}
+
 // The row block of the i-th workgroup of a head.  Where a row's keys grow along the sequence (a limit on one side only) long and short blocks alternate, so
 // that any stretch of them has the same work.
 __device__ __forceinline__ int row_block(const Sight& s, int i, int blocks) {
@@ -160,8 +172,8 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attn_rows_kernel(RowsArgs a
   constexpr int KB = KT / 32, KS = D / 16, CB = D / 32, BM = 32 * QB * NW, TILE = KT * D * 2;
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
-  const int id = xcd_stretch(blockIdx.x, gridDim.x), split = id % a.splits, bx = id / a.splits;
-  const int bk = bx / a.blocks, block = row_block(a.sight, bx % a.blocks, a.blocks);
+  const PairPlace place = pair_place(blockIdx.x, a.B * a.HK, a.blocks * a.splits);
+  const int bk = place.pair, split = place.at % a.splits, block = row_block(a.sight, place.at / a.splits, a.blocks);
   const int b = bk / a.HK, hk = bk % a.HK, G = a.G;
   Source src(from, b, hk, a.n, w, lane);
   // token t has position pos0 + t; tokens t0 .. count - 1 have rows
