@@ -94,9 +94,10 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void window_dq_kernel(BwdRows
   const size_t kv = (size_t)b * a.kr.sb + (size_t)hk * a.kr.sh, pitch = a.kr.sn * 2;
   const char *kbase = static_cast<const char*>(a.k) + kv * 2, *vbase = static_cast<const char*>(a.v) + kv * 2;
   const RowTile<D, NW, BT> loader(w, lane);
+  const TileOrder<BT> order(tiles, 0, tiles.count);
   const uint32_t lds = lds_address(smem);
   auto request = [&](int i) {
-    const int j0 = tiles.start(i);
+    const int j0 = tiles.start(order(i));
     const uint32_t to = lds + (uint32_t)(i & 1) * 2 * TILE;
     loader.load(kbase, pitch, j0, tiles.end, to, w);
     loader.load(vbase, pitch, j0, tiles.end, to + TILE, w);
@@ -113,7 +114,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void window_dq_kernel(BwdRows
     __syncthreads();
     for (int it = 0; it < tiles.count; ++it) {
       if (it + 1 < tiles.count) request(it + 1);
-      const int j0 = tiles.start(it);
+      const int j0 = tiles.start(order(it));
       const uint32_t kt = lds + (uint32_t)(it & 1) * 2 * TILE, vt = kt + TILE;
       if (!sight.nothing(j0, BT)) {
         const bool plain = sight.everything(j0, BT);
@@ -310,6 +311,12 @@ __global__ __launch_bounds__(2 * key_block(D), 2) void window_dkv_kernel(BwdRows
   const int qe = jb1 < jb0 ? 0 : jb0 < a.sight.sinks ? len : query_hi(a.sight, jb1, len);
   const int T = (qe + BT - 1) / BT > q0 ? (qe + BT - 1) / BT - q0 : 0;
   const int per = (T * G + ks_.parts - 1) / ks_.parts, e0 = ks_.part * per, e1 = e0 + per < T * G ? e0 + per : T * G;
+  // the first query of the e-th tile; a whole block's tiles in an order that neighbouring blocks share (TileOrder)
+  const int turn = ks_.parts == 1 && T > 0 ? q0 % T : 0;
+  auto first_query = [&](int e) {
+    const int x = e % T - turn;
+    return (q0 + (x < 0 ? x + T : x)) * BT;
+  };
   // what the wavefront's keys are seen by
   const int jw0 = jb0 + 32 * w, jw1 = (jw0 + 32 < len ? jw0 + 32 : len) - 1;
   const bool any = jw1 >= jw0;
@@ -321,7 +328,7 @@ __global__ __launch_bounds__(2 * key_block(D), 2) void window_dkv_kernel(BwdRows
   const RowTile<D, NW, BT> loader(w, lane);
   const uint32_t lds = lds_address(smem);
   auto request = [&](int e) {
-    const int hd = e / T, i0 = (q0 + e - hd * T) * BT, h = hk * G + hd;
+    const int hd = e / T, i0 = first_query(e), h = hk * G + hd;
     const size_t base = ((size_t)b * a.qr.sb + (size_t)h * a.qr.sh) * 2, li = ((size_t)b * a.H + h) * a.n;
     const uint32_t to = lds + (uint32_t)(e & 1) * BUF;
     loader.load(static_cast<const char*>(a.q) + base, pitch, i0, len, to, w);
@@ -338,7 +345,7 @@ __global__ __launch_bounds__(2 * key_block(D), 2) void window_dkv_kernel(BwdRows
   __syncthreads();
   for (int e = e0; e < e1; ++e) {
     if (e + 1 < e1) request(e + 1);
-    const int i0 = (q0 + e % T) * BT;
+    const int i0 = first_query(e);
     const uint32_t qt = lds + (uint32_t)(e & 1) * BUF, gt = qt + TILE;
     const float* nl = reinterpret_cast<const float*>(smem + (e & 1) * BUF + 2 * TILE);
     if (any && i0 < whi1 && i0 + BT > wlo0) {
@@ -442,7 +449,7 @@ __global__ __launch_bounds__(2 * key_block(D), 2) void window_dkv_kernel(BwdRows
     const int jlo = query_lo(a.sight, jj), jhi = query_hi(a.sight, jj, len);
     float sk[D / 64] = {}, sv[D / 64] = {};
     for (int e = e0; e < e1; ++e) {
-      const int hd = e / T, i0 = (q0 + e - hd * T) * BT, h = hk * G + hd;
+      const int hd = e / T, i0 = first_query(e), h = hk * G + hd;
       const size_t base = (size_t)b * a.qr.sb + (size_t)h * a.qr.sh, li = ((size_t)b * a.H + h) * a.n;
       const TokenKeys<uint16_t> rows{static_cast<const uint16_t*>(a.q) + base, static_cast<const uint16_t*>(a.dout) + base, a.qr.sn};
       plain_dkv_row<D>(rows, ps.a, ps.b, ps.p, ps.s, i0 > jlo ? i0 : jlo, i0 + BT < jhi ? i0 + BT : jhi, a.scale2, a.scale2, a.nl + li, a.nd + li, lane, sk, sv);

@@ -76,6 +76,24 @@ struct KeyTiles {
   __device__ __forceinline__ int sink_key(int i) const { return (i < nsink ? i : nsink) * KT; }
   __device__ __forceinline__ int window_key(int i) const { return (wtile + (i > nsink ? i - nsink : 0)) * KT; }
 };
+// The order in which a workgroup takes tiles it0 .. it1 - 1: those of the first tokens, then those of the window from the one on whose number is a multiple of
+// how many they are, and the ones before it last.  Neighbouring blocks, whose windows overlap but for a tile or two, then read the same tile at the same time.  Each
+// from its own first tile on, the 64 workgroups of an XCD were spread over more keys than its L2 holds: (figures at attn_rows_kernel)
+template <int KT>
+struct TileOrder {
+  int w0, count, turn;
+  __device__ __forceinline__ TileOrder(const KeyTiles<KT>& t, int it0, int it1) {
+    w0 = it0 > t.nsink ? it0 : t.nsink;
+    count = it1 - w0;
+    turn = count > 0 ? (t.wtile + w0 - t.nsink) % count : 0;
+  }
+  __device__ __forceinline__ int operator()(int i) const {
+    if (i < w0) return i;
+    const int x = i - turn;
+    return x < w0 ? x + count : x;
+  }
+};
+
 // What a wavefront's rows at positions p0 .. p1 see of a tile from key j0 on: nothing, or everything.  (Lanes without a token are not looked at: what they
 // come to is dropped.)
 struct WaveSight {
@@ -215,9 +233,10 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attn_rows_kernel(RowsArgs a
   const KeyTiles<KT> tiles(a.sight, bp0, bp1 < bp0 ? -1 : bp1, len);
   const WaveSight sight(a.sight, wp0, wp1 < wp0 ? -1 : wp1, len);
   const int it0 = (int)((long long)tiles.count * split / a.splits), it1 = (int)((long long)tiles.count * (split + 1) / a.splits);
+  const TileOrder<KT> order(tiles, it0, it1);
   const uint32_t lds = lds_address(smem);
-  auto look = [&](int i) { src.look(tiles.start(i), tiles.end); };
-  auto request = [&](int i) { src.request(tiles.start(i), tiles.end, lds + (uint32_t)(i & 1) * 2 * TILE); };
+  auto look = [&](int i) { src.look(tiles.start(order(i)), tiles.end); };
+  auto request = [&](int i) { src.request(tiles.start(order(i)), tiles.end, lds + (uint32_t)(i & 1) * 2 * TILE); };
   const uint32_t rows_at = row_at<D>(lane), turned_rows = turned_at<D>(lane);
 
   if (it0 < it1) {
@@ -233,7 +252,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attn_rows_kernel(RowsArgs a
       request(it + 1);
       if (it + 2 < it1) look(it + 2);
     }
-    const int j0 = tiles.start(it);
+    const int j0 = tiles.start(order(it));
     const uint32_t kt = lds + (uint32_t)(it & 1) * 2 * TILE, vt = kt + TILE;
     if (!sight.nothing(j0, KT)) {
       const bool plain = sight.everything(j0, KT) && there == ~0ull;
