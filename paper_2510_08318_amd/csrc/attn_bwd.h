@@ -103,6 +103,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void window_dq_kernel(BwdRows
     loader.load(vbase, pitch, j0, tiles.end, to + TILE, w);
   };
 
+  arrived(q);
+  arrived(go);
   f32x16 dq[CB];
 #pragma unroll
   for (int c = 0; c < CB; ++c) dq[c] = fill16(0.f);
@@ -122,11 +124,11 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void window_dq_kernel(BwdRows
         for (int kb = 0; kb < KB; ++kb) {
           f32x16 s = fill16(0.f), dp = fill16(0.f);
           const uint32_t rows_at = row_at<D>((int)opaque_lane(lane));
-#pragma unroll
-          for (int ks = 0; ks < KS; ++ks) {
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(row_chunk<D>(kt + rows_at, ks, 32 * kb)), as_bf16x8(q[ks]), s, 0, 0, 0);
-            dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(row_chunk<D>(vt + rows_at, ks, 32 * kb)), as_bf16x8(go[ks]), dp, 0, 0, 0);
-          }
+          pipelined_operands<2 * KS, 6>([&](int x) { return row_chunk<D>((x % 2 ? vt : kt) + rows_at, x / 2, 32 * kb); },
+                                        [&](int x, uint4 op) {
+                                          if (x % 2) dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(op), as_bf16x8(go[x / 2]), dp, 0, 0, 0);
+                                          else s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(op), as_bf16x8(q[x / 2]), s, 0, 0, 0);
+                                        });
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale2, nl2));
           if (!plain) {
@@ -178,13 +180,13 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void window_dq_kernel(BwdRows
       dp[r] = p[r] * (dp[r] - delta);
       if (!EXACT) off += dp[r];
     }
-#pragma unroll
-    for (int st = 0; st < 2; ++st) {
-      uint4 ds[PIECES];
-      weights_operand<PIECES>(dp, st, ds);
-#pragma unroll
-      for (int c = 0; c < CB; ++c) dq[c] = mfma_weights<PIECES>(turned<D>(kt + turned_rows, c, 16 * (2 * kb + st)), ds, dq[c]);
-    }
+    uint4 ds[PIECES == 1 ? 2 : 1][PIECES];
+    if constexpr (PIECES == 1) { ds[0][0] = pack8(dp, 0); ds[1][0] = pack8(dp, 1); }
+    pipelined_operands<2 * CB, 3>([&](int x) { return __builtin_bit_cast(uint4, turned<D>(kt + turned_rows, x % CB, 16 * (2 * kb + x / CB))); },
+                                  [&](int x, uint4 op) {
+                                    if (PIECES > 1 && x % CB == 0) weights_operand<PIECES>(dp, x / CB, ds[0]);
+                                    dq[x % CB] = mfma_weights<PIECES>(as_bf16x8(op), ds[PIECES == 1 ? x / CB : 0], dq[x % CB]);
+                                  });
   });
   if (!EXACT) {
     float x, y;
@@ -340,6 +342,8 @@ __global__ __launch_bounds__(2 * key_block(D), 2) void window_dkv_kernel(BwdRows
     }
   };
 
+  arrived(k);
+  arrived(v);
   if (e0 < e1) request(e0);
   lds_loads_landed();
   __syncthreads();
@@ -353,6 +357,7 @@ __global__ __launch_bounds__(2 * key_block(D), 2) void window_dkv_kernel(BwdRows
 #pragma unroll
       for (int qb = 0; qb < BT / 32; ++qb) {
         f32x16 s, dp;
+        uint4 held;
         const int lz = (int)opaque_lane(lane);        // (addresses are worked out here, and k operands read again, not held)
         const uint32_t ra = row_at<D>(lz), ta = turned_at<D>(lz);
 #pragma unroll
@@ -361,11 +366,17 @@ __global__ __launch_bounds__(2 * key_block(D), 2) void window_dkv_kernel(BwdRows
           s[r] = x.x; s[r + 1] = x.y; s[r + 2] = x.z; s[r + 3] = x.w;
           dp[r] = y.x; dp[r + 1] = y.y; dp[r + 2] = y.z; dp[r + 3] = y.w;
         }
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(row_chunk<D>(qt + ra, ks, 32 * qb)), as_bf16x8(KLDS ? row_chunk<D>(kat + ra, ks, 0) : k[ks]), s, 0, 0, 0);
-          dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(row_chunk<D>(gt + ra, ks, 32 * qb)), as_bf16x8(v[ks]), dp, 0, 0, 0);
-        }
+        if constexpr (KLDS)      // q, k, dout of a k-step in turn
+          pipelined_operands<2 * KS, 3>([&](int x) { return row_chunk<D>((x % 2 ? kat : qt + 32 * qb * D * 2) + ra, x / 2, 0); },
+                                        [&](int x, uint4 op) {
+                                          if (x % 2) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(held), as_bf16x8(op), s, 0, 0, 0);
+                                          else held = op;
+                                        });
+        else
+          pipelined_operands<KS, 4>([&](int x) { return row_chunk<D>(qt + ra, x, 32 * qb); },
+                                    [&](int x, uint4 op) { s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(op), as_bf16x8(k[x]), s, 0, 0, 0); });
+        pipelined_operands<KS, 4>([&](int x) { return row_chunk<D>(gt + ra, x, 32 * qb); },
+                                  [&](int x, uint4 op) { dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(op), as_bf16x8(v[x]), dp, 0, 0, 0); });
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r] * a.scale2);
         if (!plain) {
@@ -386,11 +397,11 @@ __global__ __launch_bounds__(2 * key_block(D), 2) void window_dkv_kernel(BwdRows
           if constexpr (PIECES == 1) {
             const uint4 p[1] = {pack8(s, st)};
             x[0] = pack8(dp, st);
-#pragma unroll
-            for (int c = 0; c < CB; ++c) {
-              dv[c] = mfma_weights<1>(turned<D>(gt + ta, c, 16 * (2 * qb + st)), p, dv[c]);
-              dk[c] = mfma_weights<1>(turned<D>(qt + ta, c, 16 * (2 * qb + st)), x, dk[c]);
-            }
+            pipelined_operands<2 * CB, 3>([&](int i) { return __builtin_bit_cast(uint4, turned<D>((i % 2 ? qt : gt) + ta, i / 2, 16 * (2 * qb + st))); },
+                                          [&](int i, uint4 op) {
+                                            if (i % 2) dk[i / 2] = mfma_weights<1>(as_bf16x8(op), x, dk[i / 2]);
+                                            else dv[i / 2] = mfma_weights<1>(as_bf16x8(op), p, dv[i / 2]);
+                                          });
           } else {
             weights_operand<PIECES>(s, st, x);
 #pragma unroll

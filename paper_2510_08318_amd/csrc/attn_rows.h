@@ -239,6 +239,8 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attn_rows_kernel(RowsArgs a
   auto request = [&](int i) { src.request(tiles.start(order(i)), tiles.end, lds + (uint32_t)(i & 1) * 2 * TILE); };
   const uint32_t rows_at = row_at<D>(lane), turned_rows = turned_at<D>(lane);
 
+#pragma unroll
+  for (int i = 0; i < QB; ++i) arrived(q[i]);
   if (it0 < it1) {
     look(it0);
     request(it0);
@@ -263,14 +265,10 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attn_rows_kernel(RowsArgs a
         for (int i = 0; i < QB; ++i)
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[i][kb][r] = 0.f;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-          const bf16x8 kop = as_bf16x8(row_chunk<D>(kt + rows_at, ks, 32 * kb));
-#pragma unroll
-          for (int i = 0; i < QB; ++i) s[i][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop, as_bf16x8(q[i][ks]), s[i][kb], 0, 0, 0);
-        }
+      pipelined_operands<KS * KB, 6>([&](int x) { return row_chunk<D>(kt + rows_at, x / KB, 32 * (x % KB)); },
+                                     [&](int x, uint4 kop) {
+                                       s[0][x % KB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kop), as_bf16x8(q[0][x / KB]), s[0][x % KB], 0, 0, 0);
+                                     });
       uint4 p[QB][PIECES == 1 ? 2 * KB : 1];
 #pragma unroll
       for (int i = 0; i < QB; ++i) {

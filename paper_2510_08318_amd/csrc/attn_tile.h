@@ -16,6 +16,14 @@ __device__ __forceinline__ void load_to_lds(const void* at, uint32_t lds) {
 }
 __device__ __forceinline__ void lds_loads_landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
+// Operands that a kernel loads before its loop.  The compiler has to see them arrive there: it would otherwise wait for them at their first use, in every turn of the
+// loop, and with them for the tile that has just been asked for (forward, 12 heads x 32760 x 128: 1528 us, with this and reads ahead of the scores' products (figure)).
+template <int N>
+__device__ __forceinline__ void arrived(uint4 (&x)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i].x), "+v"(x[i].y), "+v"(x[i].z), "+v"(x[i].w));
+}
+
 // Rows j0 .. j0+KT-1 of a token tensor, by NW wavefronts: each instruction brings 1024 bytes, 512 / D rows.  Rows from `end` on are row end - 1 again (what is
 // computed with them is masked).
 template <int D, int NW, int KT>
