@@ -124,7 +124,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void window_dq_kernel(BwdRows
         for (int kb = 0; kb < KB; ++kb) {
           f32x16 s = fill16(0.f), dp = fill16(0.f);
           const uint32_t rows_at = row_at<D>((int)opaque_lane(lane));
-          pipelined_operands<2 * KS, 6>([&](int x) { return row_chunk<D>((x % 2 ? vt : kt) + rows_at, x / 2, 32 * kb); },
+          pipelined_operands<2 * KS, 4>([&](int x) { return row_chunk<D>((x % 2 ? vt : kt) + rows_at, x / 2, 32 * kb); },
                                         [&](int x, uint4 op) {
                                           if (x % 2) dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(op), as_bf16x8(go[x / 2]), dp, 0, 0, 0);
                                           else s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(op), as_bf16x8(q[x / 2]), s, 0, 0, 0);

@@ -89,9 +89,9 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void attn_keys_kernel(RowsArgs a
   PoolRows next;
   unsigned long long there_next = 0;
   uint32_t ek = 0, ev = 0;
-  auto look = [&](int i) { next.find(pool, b, hk, tiles.start(i), tiles.end, lane); };
+  auto look = [&](int i) { next.find<TK>(pool, b, hk, tiles.start(i), tiles.end, lane); };
   auto request = [&](int i, uint32_t to) {
-    there_next = TK == 64 ? next.there : next.there | ~0ull << 32;
+    there_next = next.there;
 #pragma unroll
     for (int x = 0; x < T::N; ++x) {
       const int r = x * (64 / T::LPR) + lane / T::LPR;

@@ -54,15 +54,26 @@ struct PoolKeys {
   __device__ __forceinline__ float v1(int j, int c) const { return row1(pool->v, pool->v_exp, j, c); }
 };
 
-// The pool's rows of a tile's keys, lane by lane (key j0 + lane, the last key again from `end` on): a row, and whether there is one for every key.
+// The pool's rows of a tile's keys, lane by lane (key j0 + lane, the last key again from `end` on): a row, and which keys have one.
+// The table is read through the scalar cache, an entry at a time (a tile has two pages at most where they are no smaller): a vector load's answer could not be
+// waited for without all the loads that were asked for before it, a tile that is on its way among them.
 struct PoolRows {
   long long row;           // of this lane's key, row 0 where there is none
   unsigned long long there;
+  template <int KT>
   __device__ __forceinline__ void find(const Pool& p, int b, int h, int j0, int end, int lane) {
-    const int j = j0 + lane < end ? j0 + lane : end - 1;
-    const long long r = pool_row(p, b, h, j);
-    there = __ballot(r >= 0);
-    row = r < 0 ? 0 : r;
+    const int last = j0 + KT < end ? j0 + KT - 1 : end - 1, j = j0 + lane < last ? j0 + lane : last, mine = page_of(p, j);
+    typedef __attribute__((address_space(4))) const int* Table;
+    const Table table = (Table)(uintptr_t)p.table;
+    const int i1 = __builtin_amdgcn_readfirstlane(page_of(p, last));
+    int entry = -1;
+    for (int i = __builtin_amdgcn_readfirstlane(page_of(p, j0)); i <= i1; ++i) {
+      const int e = table[(size_t)b * p.width + i];
+      entry = mine == i ? e : entry;
+    }
+    const bool ok = (unsigned)entry < (unsigned)p.pages;
+    there = __ballot(ok);
+    row = ok ? ((long long)entry * p.HK + h) * p.page + (j - mine * p.page) : 0;
   }
   __device__ __forceinline__ long long of(int i) const {
     return (long long)((unsigned long long)(uint32_t)__shfl((int)row, i) | (unsigned long long)(uint32_t)__shfl((int)(row >> 32), i) << 32);

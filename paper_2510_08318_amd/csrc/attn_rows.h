@@ -184,10 +184,11 @@ __device__ void plain_again(const RowsArgs& a, const Keys& keys, const Tiles& ti
   if (a.lse && lane == 0) a.lse[li] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
+// Two tiles in LDS and one barrier a tile.  (With a second barrier, between the scores and the product with v, a buffer can be asked for half a tile earlier; but then
+// the exponentials no longer overlap with that product: 12 heads x 32760 x 128, window 2 x 3120, 1562 us in place of 1507, on one machine.)
 template <int D, int KT, typename Source, int PIECES>
 __global__ __launch_bounds__(64 * kRowWaves, 2) void attn_rows_kernel(RowsArgs a, typename Source::Args from) {
-  constexpr int QB = 1, NW = kRowWaves;
-  constexpr int KB = KT / 32, KS = D / 16, CB = D / 32, BM = 32 * QB * NW, TILE = KT * D * 2;
+  constexpr int NW = kRowWaves, KB = KT / 32, KS = D / 16, CB = D / 32, BM = 32 * NW, TILE = KT * D * 2;
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
   const PairPlace place = pair_place(blockIdx.x, a.B * a.HK, a.blocks * a.splits);
@@ -196,161 +197,126 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attn_rows_kernel(RowsArgs a
   Source src(from, b, hk, a.n, w, lane);
   // token t has position pos0 + t; tokens t0 .. count - 1 have rows
   const int len = src.len, pos0 = len - src.count, t0 = pos0 < 0 ? -pos0 : 0, rows = src.count * G, all = a.n * G;
-  const int row0 = block * BM + w * 32 * QB;
+  const int row0 = block * BM + w * 32;
 
-  // this lane's queries
-  uint4 q[QB][KS];
-  int lo[QB], hi[QB];
-  size_t at[QB];
-  bool store[QB];
+  // this lane's query
+  const int r = row0 + m, t = r / G, h = hk * G + (r - t * G);
+  const size_t at = (size_t)b * a.qr.sb + (size_t)h * a.qr.sh + (size_t)t * a.qr.sn;
+  const bool store = r < all, live = r < rows && t >= t0;
+  const int lo = live ? key_lo(a.sight, pos0 + t) : 0, hi = live ? key_hi(a.sight, pos0 + t, len) : 0;
+  uint4 q[KS];
 #pragma unroll
-  for (int i = 0; i < QB; ++i) {
-    const int r = row0 + 32 * i + m, t = r / G, h = hk * G + (r - t * G);
-    store[i] = r < all;
-    at[i] = (size_t)b * a.qr.sb + (size_t)h * a.qr.sh + (size_t)t * a.qr.sn;
-    const bool live = r < rows && t >= t0;
-    lo[i] = live ? key_lo(a.sight, pos0 + t) : 0;
-    hi[i] = live ? key_hi(a.sight, pos0 + t, len) : 0;
+  for (int ks = 0; ks < KS; ++ks)
+    q[ks] = live ? *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + at + 16 * ks + 8 * g) : make_uint4(0, 0, 0, 0);
+  f32x16 o[CB];
+  float mx = -INFINITY, l = 0.f;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-      q[i][ks] = live ? *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + at[i] + 16 * ks + 8 * g) : make_uint4(0, 0, 0, 0);
-  }
+  for (int c = 0; c < CB; ++c) o[c] = fill16(0.f);
 
-  f32x16 o[QB][CB];
-  float mx[QB], l[QB];
-#pragma unroll
-  for (int i = 0; i < QB; ++i) {
-    mx[i] = -INFINITY; l[i] = 0.f;
-#pragma unroll
-    for (int c = 0; c < CB; ++c)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) o[i][c][r] = 0.f;
-  }
-
-  auto from_row = [&](int r) { return pos0 + (r / G > t0 ? r / G : t0); };      // the first position from row r on
-  auto to_row = [&](int r) { r = (r < rows ? r : rows) - 1; return r >= 0 && r / G >= t0 ? pos0 + r / G : -1; };      // the last before row r
-  const int bp0 = from_row(block * BM), bp1 = to_row((block + 1) * BM), wp0 = from_row(row0), wp1 = to_row(row0 + 32 * QB);
+  auto from_row = [&](int x) { return pos0 + (x / G > t0 ? x / G : t0); };      // the first position from row x on
+  auto to_row = [&](int x) { x = (x < rows ? x : rows) - 1; return x >= 0 && x / G >= t0 ? pos0 + x / G : -1; };      // the last before row x
+  const int bp0 = from_row(block * BM), bp1 = to_row((block + 1) * BM), wp0 = from_row(row0), wp1 = to_row(row0 + 32);
   const KeyTiles<KT> tiles(a.sight, bp0, bp1 < bp0 ? -1 : bp1, len);
   const WaveSight sight(a.sight, wp0, wp1 < wp0 ? -1 : wp1, len);
   const int it0 = (int)((long long)tiles.count * split / a.splits), it1 = (int)((long long)tiles.count * (split + 1) / a.splits);
   const TileOrder<KT> order(tiles, it0, it1);
   const uint32_t lds = lds_address(smem);
+  auto ktile = [&](int i) { return lds + (uint32_t)((i - it0) & 1) * 2 * TILE; };
   auto look = [&](int i) { src.look(tiles.start(order(i)), tiles.end); };
-  auto request = [&](int i) { src.request(tiles.start(order(i)), tiles.end, lds + (uint32_t)(i & 1) * 2 * TILE); };
   const uint32_t rows_at = row_at<D>(lane), turned_rows = turned_at<D>(lane);
 
-#pragma unroll
-  for (int i = 0; i < QB; ++i) arrived(q[i]);
+  arrived(q);
+  auto ask = [&](int i) { src.ask_k(ktile(i)); src.ask_v(ktile(i) + TILE); };
+  auto put = [&](int i) { src.put_k(ktile(i)); src.put_v(ktile(i) + TILE); };
+  unsigned long long there = ~0ull;      // the keys that the tile has
   if (it0 < it1) {
     look(it0);
-    request(it0);
+    there = src.there;
+    ask(it0);
+    put(it0);
     if (it0 + 1 < it1) look(it0 + 1);
-    src.finish(lds + (uint32_t)(it0 & 1) * 2 * TILE);
   }
+  src.landed();
   __syncthreads();
   for (int it = it0; it < it1; ++it) {
-    const unsigned long long there = src.mask();
+    const unsigned long long there_next = src.there;
     if (it + 1 < it1) {
-      request(it + 1);
+      ask(it + 1);
       if (it + 2 < it1) look(it + 2);
     }
     const int j0 = tiles.start(order(it));
-    const uint32_t kt = lds + (uint32_t)(it & 1) * 2 * TILE, vt = kt + TILE;
     if (!sight.nothing(j0, KT)) {
-      const bool plain = sight.everything(j0, KT) && there == ~0ull;
-      f32x16 s[QB][KB];
+      const uint32_t kt = ktile(it), vt = kt + TILE;
+      f32x16 s[KB];
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int i = 0; i < QB; ++i)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[i][kb][r] = 0.f;
+      for (int kb = 0; kb < KB; ++kb) s[kb] = fill16(0.f);
       pipelined_operands<KS * KB, 6>([&](int x) { return row_chunk<D>(kt + rows_at, x / KB, 32 * (x % KB)); },
                                      [&](int x, uint4 kop) {
-                                       s[0][x % KB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kop), as_bf16x8(q[0][x / KB]), s[0][x % KB], 0, 0, 0);
+                                       s[x % KB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kop), as_bf16x8(q[x / KB]), s[x % KB], 0, 0, 0);
                                      });
-      uint4 p[QB][PIECES == 1 ? 2 * KB : 1];
-#pragma unroll
-      for (int i = 0; i < QB; ++i) {
-        if (!plain) {
-          asm volatile("");        // a branch: as selects, the mask is computed for every tile
-#pragma unroll
-          for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const int j = j0 + 32 * kb + 8 * (r / 4) + 4 * g + r % 4;
-              bool on = j < hi[i] && (j >= lo[i] || j < a.sight.sinks);
-              if (Source::kPaged) on = on && (there >> (j - j0) & 1);
-              s[i][kb][r] = on ? s[i][kb][r] : -INFINITY;
-            }
-        }
-        softmax_step<KB, CB>(s[i], a.scale2, mx[i], l[i], o[i]);
+      if (!(sight.everything(j0, KT) && there == ~0ull)) {
+        asm volatile("");        // a branch: as selects, the mask is computed for every tile
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
-          for (int h2 = 0; h2 < 2; ++h2) p[i][2 * kb + h2] = pack8(s[i][kb], h2);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int j = j0 + 32 * kb + 8 * (e / 4) + 4 * g + e % 4;
+            bool on = j < hi && (j >= lo || j < a.sight.sinks);
+            if (Source::kPaged) on = on && (there >> (j - j0) & 1);
+            s[kb][e] = on ? s[kb][e] : -INFINITY;
+          }
       }
+      softmax_step<KB, CB>(s, a.scale2, mx, l, o);
 #pragma unroll
       for (int st = 0; st < 2 * KB; ++st) {
-        uint4 x[QB][PIECES];
+        uint4 x[PIECES];
+        weights_operand<PIECES>(s[st / 2], st % 2, x);
 #pragma unroll
-        for (int i = 0; i < QB; ++i) {
-          if constexpr (PIECES == 1) x[i][0] = p[i][st];
-          else weights_operand<PIECES>(s[i][st / 2], st % 2, x[i]);
-        }
-#pragma unroll
-        for (int c = 0; c < CB; ++c) {
-          const bf16x8 vop = turned<D>(vt + turned_rows, c, 16 * st);
-#pragma unroll
-          for (int i = 0; i < QB; ++i) o[i][c] = mfma_weights<PIECES>(vop, x[i], o[i][c]);
-        }
+        for (int c = 0; c < CB; ++c) o[c] = mfma_weights<PIECES>(turned<D>(vt + turned_rows, c, 16 * st), x, o[c]);
       }
     }
-    if (it + 1 < it1) src.finish(lds + (uint32_t)((it + 1) & 1) * 2 * TILE);
+    if (it + 1 < it1) put(it + 1);
+    there = there_next;
+    src.landed();
     __syncthreads();
   }
 
+  // A key that is masked has weight 0, and 0 times an infinity or NaN in its value would be NaN: rows that come out not finite are done again
+  // key by key.
+  float x, y;
+  pair32(l, x, y);
+  const float sum = live ? x + y : 0.f, inv = sum == 0.f ? 0.f : 1.0f / sum;
+  if (!live) {
 #pragma unroll
-  for (int i = 0; i < QB; ++i) {
-    float x, y;
-    pair32(l[i], x, y);
-    const float sum = hi[i] == 0 ? 0.f : x + y, inv = sum == 0.f ? 0.f : 1.0f / sum;
-    const int r = row0 + 32 * i + m, t = r / G;
-    const size_t li = ((size_t)b * a.H + hk * G + (r - t * G)) * a.n + t;
-    // A key that is masked has weight 0, and 0 times an infinity or NaN in its value would be NaN: rows that come out not finite are done again
-    // key by key.
-    if (hi[i] == 0) {                          // not a token
-#pragma unroll
-      for (int c = 0; c < CB; ++c) o[i][c] = fill16(0.f);
-    }
-    float test = 0.f * sum;
-#pragma unroll
-    for (int c = 0; c < CB; ++c)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) test = fmaf(0.f, o[i][c][e], test);
-    uint32_t again = (uint32_t)__ballot(test != 0.f) | (uint32_t)(__ballot(test != 0.f) >> 32);
-    if (store[i] && !(again >> m & 1)) {
-      if (a.splits > 1) {
-        float* part = a.parts + ((size_t)split * a.B * a.H * a.n + li) * D + 4 * g;
-#pragma unroll
-        for (int c = 0; c < CB; ++c)
-#pragma unroll
-          for (int e = 0; e < 16; e += 4)
-            *reinterpret_cast<float4*>(part + 32 * c + 2 * e) = make_float4(o[i][c][e], o[i][c][e + 1], o[i][c][e + 2], o[i][c][e + 3]);
-        if (g == 0) put_part(a, D, split, li, mx[i], sum);
-      } else {
-        uint16_t* out = static_cast<uint16_t*>(a.o) + at[i] + 4 * g;
-#pragma unroll
-        for (int c = 0; c < CB; ++c)
-#pragma unroll
-          for (int e = 0; e < 16; e += 4)
-            *reinterpret_cast<uint2*>(out + 32 * c + 2 * e) = make_uint2(pack_bf16x2(o[i][c][e] * inv, o[i][c][e + 1] * inv),
-                                                                         pack_bf16x2(o[i][c][e + 2] * inv, o[i][c][e + 3] * inv));
-        if (a.lse && g == 0) a.lse[li] = sum == 0.f ? -INFINITY : (mx[i] + __builtin_amdgcn_logf(sum)) * kLn2;
-      }
-    }
-    for (; again; again &= again - 1)
-      plain_again<D>(a, src.keys(), tiles, it0, it1, row0 + 32 * i + __ffs(again) - 1, b, hk, split, pos0, len, reinterpret_cast<PlainScratch<D>*>(smem)[w], lane);
+    for (int c = 0; c < CB; ++c) o[c] = fill16(0.f);
   }
+  const size_t li = ((size_t)b * a.H + h) * a.n + t;
+  float test = 0.f * sum;
+#pragma unroll
+  for (int c = 0; c < CB; ++c)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) test = fmaf(0.f, o[c][e], test);
+  uint32_t again = (uint32_t)__ballot(test != 0.f) | (uint32_t)(__ballot(test != 0.f) >> 32);
+  if (store && !(again >> m & 1)) {
+    if (a.splits > 1) {
+      float* part = a.parts + ((size_t)split * a.B * a.H * a.n + li) * D + 4 * g;
+#pragma unroll
+      for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4*>(part + 32 * c + 2 * e) = make_float4(o[c][e], o[c][e + 1], o[c][e + 2], o[c][e + 3]);
+      if (g == 0) put_part(a, D, split, li, mx, sum);
+    } else {
+      uint16_t* out = static_cast<uint16_t*>(a.o) + at + 4 * g;
+#pragma unroll
+      for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4)
+          *reinterpret_cast<uint2*>(out + 32 * c + 2 * e) = make_uint2(pack_bf16x2(o[c][e] * inv, o[c][e + 1] * inv), pack_bf16x2(o[c][e + 2] * inv, o[c][e + 3] * inv));
+      if (a.lse && g == 0) a.lse[li] = sum == 0.f ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * kLn2;
+    }
+  }
+  for (; again; again &= again - 1)
+    plain_again<D>(a, src.keys(), tiles, it0, it1, row0 + __ffs(again) - 1, b, hk, split, pos0, len, reinterpret_cast<PlainScratch<D>*>(smem)[w], lane);
 }
 
 // The sum over the splits.  A wavefront to a row.

@@ -72,9 +72,9 @@ __device__ __forceinline__ bf16x8 turned(uint32_t at, int c, int row0) {
 
 constexpr int kRowWaves = 4;                 // wavefronts that fill a tile together
 
-// Where a workgroup's keys come from: request(j0, end, lds) asks for the tile of KT keys from j0 on, k at lds and v behind it, one call ahead of its use;
-// look(j0, end) goes before it, one more ahead; finish(), after the tile before is done with, makes it ready up to the barrier.  There is memory behind
-// every key that is asked for; mask(): the keys of the requested tile that the cache has, all ones if all.
+// Where a workgroup's keys come from.  look(j0, end): the tile of KT keys from j0 on (there is memory behind every key below end, of later ones the last is taken again) is
+// what the next ask_k and ask_v are for, which request its k or its v; put_k and put_v, before the next of them, bring what came through registers to LDS; landed() waits
+// for what goes there directly.  there: the keys of the tile that exist.
 struct TokenArgs {
   const void *k, *v;
   const int* lengths;
@@ -95,13 +95,14 @@ struct TokenSource {
     k = static_cast<const char*>(a.k) + at;
     v = static_cast<const char*>(a.v) + at;
   }
-  __device__ __forceinline__ void look(int, int) {}
-  __device__ __forceinline__ void request(int j0, int end, uint32_t lds) {
-    rows.load(k, sn * 2, j0, end, lds, w);
-    rows.load(v, sn * 2, j0, end, lds + KT * D * 2, w);
-  }
-  __device__ __forceinline__ void finish(uint32_t) { lds_loads_landed(); }
-  __device__ __forceinline__ unsigned long long mask() const { return ~0ull; }
+  int j0, end;
+  static constexpr unsigned long long there = ~0ull;
+  __device__ __forceinline__ void look(int j0_, int end_) { j0 = j0_; end = end_; }
+  __device__ __forceinline__ void ask_k(uint32_t lds) { rows.load(k, sn * 2, j0, end, lds, w); }
+  __device__ __forceinline__ void ask_v(uint32_t lds) { rows.load(v, sn * 2, j0, end, lds, w); }
+  __device__ __forceinline__ void put_k(uint32_t) {}
+  __device__ __forceinline__ void put_v(uint32_t) {}
+  __device__ __forceinline__ void landed() { lds_loads_landed(); }
   __device__ __forceinline__ TokenKeys<uint16_t> keys() const { return {reinterpret_cast<const uint16_t*>(k), reinterpret_cast<const uint16_t*>(v), sn}; }
 };
 
@@ -114,7 +115,7 @@ struct PoolSource {
   static_assert(N >= 1, "whole instructions");
   const Pool& p;
   int w, lane, len, count, b, hk;
-  PoolRows next;
+  PoolRows at;
   unsigned long long there;
   uint4 ck[E4M3 ? N : 1], cv[E4M3 ? N : 1];
   uint32_t ek, ev;
@@ -123,40 +124,38 @@ struct PoolSource {
     count = clamp_length(p.counts, b, n);
   }
   __device__ __forceinline__ int row(int i) const { return (w * N + i) * (64 / LPR) + lane / LPR; }
-  __device__ __forceinline__ void look(int j0, int end) { next.find(p, b, hk, j0, end, lane); }
-  __device__ __forceinline__ void request(int, int, uint32_t lds) {
-    there = next.there;
-    if constexpr (E4M3) { ek = p.k_exp[next.row]; ev = p.v_exp[next.row]; }
+  __device__ __forceinline__ void look(int j0, int end) {
+    at.find<KT>(p, b, hk, j0, end, lane);
+    there = at.there;
+  }
+  __device__ __forceinline__ void ask(const void* pool, const uint8_t* exps, uint32_t lds, uint4* codes, uint32_t& e) {
+    if constexpr (E4M3) e = exps[at.row];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int r = row(i);
-      const long long at = next.of(r) * D;
-      if constexpr (E4M3) {
-        ck[i] = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(p.k) + at + 16 * (lane % LPR));
-        cv[i] = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(p.v) + at + 16 * (lane % LPR));
-      } else {
-        const size_t from = (size_t)at * 2 + (size_t)(((lane % LPR) ^ swz<D>(r)) * 16);
-        load_to_lds(static_cast<const char*>(p.k) + from, lds + (uint32_t)((w * N + i) * 1024));
-        load_to_lds(static_cast<const char*>(p.v) + from, lds + (uint32_t)(KT * D * 2 + (w * N + i) * 1024));
-      }
+      const long long from = at.of(r) * D;
+      if constexpr (E4M3) codes[i] = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(pool) + from + 16 * (lane % LPR));
+      else load_to_lds(static_cast<const char*>(pool) + (size_t)from * 2 + (size_t)(((lane % LPR) ^ swz<D>(r)) * 16), lds + (uint32_t)((w * N + i) * 1024));
     }
   }
-  __device__ __forceinline__ void finish(uint32_t lds) {
+  __device__ __forceinline__ void put(uint32_t lds, const uint4* codes, uint32_t e) {
     if constexpr (E4M3) {
       typedef __attribute__((address_space(3))) u32x4* P;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int r = row(i), c = 2 * (lane % LPR);
-        const float sk = row_scale((uint8_t)__shfl((int)ek, r)), sv = row_scale((uint8_t)__shfl((int)ev, r));
-        const uint32_t at = lds + (uint32_t)(r * (D * 2)), c0 = (uint32_t)((c ^ swz<D>(r)) * 16), c1 = c0 ^ 16u;
-        *(P)(at + c0) = __builtin_bit_cast(u32x4, decode8(make_uint2(ck[i].x, ck[i].y), sk));
-        *(P)(at + c1) = __builtin_bit_cast(u32x4, decode8(make_uint2(ck[i].z, ck[i].w), sk));
-        *(P)(at + KT * D * 2 + c0) = __builtin_bit_cast(u32x4, decode8(make_uint2(cv[i].x, cv[i].y), sv));
-        *(P)(at + KT * D * 2 + c1) = __builtin_bit_cast(u32x4, decode8(make_uint2(cv[i].z, cv[i].w), sv));
+        const float s = row_scale((uint8_t)__shfl((int)e, r));
+        const uint32_t to = lds + (uint32_t)(r * (D * 2)), c0 = (uint32_t)((c ^ swz<D>(r)) * 16);
+        *(P)(to + c0) = __builtin_bit_cast(u32x4, decode8(make_uint2(codes[i].x, codes[i].y), s));
+        *(P)(to + (c0 ^ 16u)) = __builtin_bit_cast(u32x4, decode8(make_uint2(codes[i].z, codes[i].w), s));
       }
-    } else lds_loads_landed();
+    }
   }
-  __device__ __forceinline__ unsigned long long mask() const { return KT == 64 ? there : there | ~0ull << KT; }
+  __device__ __forceinline__ void ask_k(uint32_t lds) { ask(p.k, p.k_exp, lds, ck, ek); }
+  __device__ __forceinline__ void ask_v(uint32_t lds) { ask(p.v, p.v_exp, lds, cv, ev); }
+  __device__ __forceinline__ void put_k(uint32_t lds) { put(lds, ck, ek); }
+  __device__ __forceinline__ void put_v(uint32_t lds) { put(lds, cv, ev); }
+  __device__ __forceinline__ void landed() { if constexpr (!E4M3) lds_loads_landed(); }
   __device__ __forceinline__ PoolKeys<E4M3> keys() const { return {&p, b, hk, D}; }
 };
 

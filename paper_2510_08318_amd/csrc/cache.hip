@@ -69,34 +69,61 @@ __global__ __launch_bounds__(256) void cache_write_kernel(Pool p, const uint16_t
 
 // ---- read ---------------------------------------------------------------------------------
 
+// A thread has 16 bytes of a row of k and of v in the tensors, for kReadItems rows: their loads are in flight together.  Bound by memory.
+constexpr int kReadItems = 4;
 template <int D, bool E4M3, bool HEADS_INNER>
 __global__ __launch_bounds__(256) void cache_read_kernel(Pool p, uint16_t* k, uint16_t* v, int n, Rows r) {
-  constexpr int LANES = D / 8;
-  const int part = threadIdx.x % LANES, b = blockIdx.y;
-  const long long item = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
-  if (item >= (long long)n * p.HK) return;
-  const int t = (int)(HEADS_INNER ? item / p.HK : item % n), h = (int)(HEADS_INNER ? item % p.HK : item / n);
-  const size_t at = (size_t)b * r.sb + (size_t)h * r.sh + (size_t)t * r.sn + 8 * part;
-  float fk[8] = {}, fv[8] = {};
-  if (t < pool_length(p, b) && pool_row(p, b, h, t) >= 0) {
-    const PoolKeys<E4M3> keys{&p, b, h, D};
-    keys.k8(t, 8 * part, fk);
-    keys.v8(t, 8 * part, fv);
+  constexpr int LANES = D / 8, ROWS = 256 / LANES;
+  const int part = threadIdx.x % LANES, b = blockIdx.y, len = pool_length(p, b);
+  const long long item0 = (long long)blockIdx.x * (ROWS * kReadItems) + threadIdx.x / LANES, items = (long long)n * p.HK;
+  size_t at[kReadItems];
+  long long row[kReadItems];
+  typename std::conditional<E4M3, u32x2, u32x4>::type ck[kReadItems], cv[kReadItems];
+  uint8_t ek[kReadItems], ev[kReadItems];
+#pragma unroll
+  for (int i = 0; i < kReadItems; ++i) {
+    const long long item = item0 + i * ROWS < items ? item0 + i * ROWS : items - 1;
+    const int t = (int)(HEADS_INNER ? item / p.HK : item % n), h = (int)(HEADS_INNER ? item % p.HK : item / n);
+    at[i] = (size_t)b * r.sb + (size_t)h * r.sh + (size_t)t * r.sn + 8 * part;
+    row[i] = t < len ? pool_row(p, b, h, t) : -1;
   }
-  *reinterpret_cast<uint4*>(k + at) = make_uint4(pack_bf16x2(fk[0], fk[1]), pack_bf16x2(fk[2], fk[3]), pack_bf16x2(fk[4], fk[5]), pack_bf16x2(fk[6], fk[7]));
-  *reinterpret_cast<uint4*>(v + at) = make_uint4(pack_bf16x2(fv[0], fv[1]), pack_bf16x2(fv[2], fv[3]), pack_bf16x2(fv[4], fv[5]), pack_bf16x2(fv[6], fv[7]));
+#pragma unroll
+  for (int i = 0; i < kReadItems; ++i) {
+    using C = decltype(ck[0] + ck[0]);
+    const size_t from = (size_t)(row[i] < 0 ? 0 : row[i]) * LANES + part;
+    ck[i] = __builtin_nontemporal_load(static_cast<const C*>(p.k) + from);
+    cv[i] = __builtin_nontemporal_load(static_cast<const C*>(p.v) + from);
+    if constexpr (E4M3) { ek[i] = p.k_exp[row[i] < 0 ? 0 : row[i]]; ev[i] = p.v_exp[row[i] < 0 ? 0 : row[i]]; }
+  }
+#pragma unroll
+  for (int i = 0; i < kReadItems; ++i) {
+    if (item0 + i * ROWS >= items) break;
+    uint4 x, y;
+    if constexpr (E4M3) {
+      x = decode8(make_uint2(ck[i][0], ck[i][1]), row_scale(ek[i]));
+      y = decode8(make_uint2(cv[i][0], cv[i][1]), row_scale(ev[i]));
+    } else {
+      x = __builtin_bit_cast(uint4, ck[i]);
+      y = __builtin_bit_cast(uint4, cv[i]);
+    }
+    if (row[i] < 0) x = y = make_uint4(0, 0, 0, 0);
+    st_nt(reinterpret_cast<uint4*>(k + at[i]), x);
+    st_nt(reinterpret_cast<uint4*>(v + at[i]), y);
+  }
 }
 
-template <int D, bool E4M3>
-static dim3 copy_grid(const Pool& p, int n) { return dim3((unsigned)(((long long)n * p.HK + 2048 / D - 1) / (2048 / D)), p.B); }
+static dim3 copy_grid(const Pool& p, int n, int items) {      // items: rows of a thread
+  const int rows = 2048 / p.d * items;
+  return dim3((unsigned)(((long long)n * p.HK + rows - 1) / rows), p.B);
+}
 
 hipError_t launch_cache_write(const Pool& p, bool e4m3, const void* k, const void* v, int n, const Rows& r, hipStream_t s) {
   auto go = [&](auto d, auto quantised) {
     constexpr int D = decltype(d)::value;
     constexpr bool E = decltype(quantised)::value;
     const auto *kk = static_cast<const uint16_t*>(k), *vv = static_cast<const uint16_t*>(v);
-    if (r.sh < r.sn) cache_write_kernel<D, E, true><<<copy_grid<D, E>(p, n), 256, 0, s>>>(p, kk, vv, n, r);
-    else cache_write_kernel<D, E, false><<<copy_grid<D, E>(p, n), 256, 0, s>>>(p, kk, vv, n, r);
+    if (r.sh < r.sn) cache_write_kernel<D, E, true><<<copy_grid(p, n, 1), 256, 0, s>>>(p, kk, vv, n, r);
+    else cache_write_kernel<D, E, false><<<copy_grid(p, n, 1), 256, 0, s>>>(p, kk, vv, n, r);
   };
   using std::integral_constant;
   if (p.d == 64) e4m3 ? go(integral_constant<int, 64>{}, std::true_type{}) : go(integral_constant<int, 64>{}, std::false_type{});
@@ -108,8 +135,8 @@ hipError_t launch_cache_read(const Pool& p, bool e4m3, void* k, void* v, int n, 
     constexpr int D = decltype(d)::value;
     constexpr bool E = decltype(quantised)::value;
     auto *kk = static_cast<uint16_t*>(k), *vv = static_cast<uint16_t*>(v);
-    if (r.sh < r.sn) cache_read_kernel<D, E, true><<<copy_grid<D, E>(p, n), 256, 0, s>>>(p, kk, vv, n, r);
-    else cache_read_kernel<D, E, false><<<copy_grid<D, E>(p, n), 256, 0, s>>>(p, kk, vv, n, r);
+    if (r.sh < r.sn) cache_read_kernel<D, E, true><<<copy_grid(p, n, kReadItems), 256, 0, s>>>(p, kk, vv, n, r);
+    else cache_read_kernel<D, E, false><<<copy_grid(p, n, kReadItems), 256, 0, s>>>(p, kk, vv, n, r);
   };
   using std::integral_constant;
   if (p.d == 64) e4m3 ? go(integral_constant<int, 64>{}, std::true_type{}) : go(integral_constant<int, 64>{}, std::false_type{});
