@@ -260,19 +260,20 @@ typedef struct linattn_window_desc {
   linattn_sight sight;
   const int* lengths;     /* optional device [B]: tokens of each item, the others are padding.  Padding is not read; its rows of out, dq, dk, dv are
                              zeros, of lse -inf.  NULL: n each. */
-  void* workspace;        /* linattn_window_bwd only: device scratch, 256-byte aligned, not shared by calls that overlap in time */
+  void* workspace;        /* device scratch, 256-byte aligned, not shared by calls that overlap in time.  The backward needs it; the forward of short
+                             sequences in LINATTN_F32 is faster with it, and takes NULL */
   size_t workspace_bytes;
 } linattn_window_desc;
 
-/* Scratch bytes linattn_window_bwd needs (the forward needs none).  Pure function of the descriptor's numbers; 0 for an invalid one. */
+/* Scratch bytes of a workspace for linattn_window_bwd, or for linattn_window_fwd if that gets one.  Pure function of the descriptor's numbers; 0 for an invalid one. */
 size_t linattn_window_workspace_bytes(const linattn_window_desc* desc);
 
 /* Forward.  lse: optional device fp32 [B, H, n], what the backward needs and what joins results over parts of the keys.
- * Errors: E_NULL, E_DTYPE, E_SHAPE, E_VALUE, E_ALIGN, E_ALIAS, E_HIP. */
+ * Errors: E_NULL, E_DTYPE, E_SHAPE, E_VALUE, E_ALIGN, E_WORKSPACE (one that is too small), E_ALIAS, E_HIP. */
 int linattn_window_fwd(const linattn_window_desc* desc, const void* q, const void* k, const void* v, void* out, float* lse, void* stream);
 
 /* Backward for L with dL/dout = dout, from the forward's out and lse; writes dq, dk, dv (dk and dv summed over the query heads of a group).
- * Errors: as above, and E_WORKSPACE. */
+ * Errors: as above, E_WORKSPACE also without one. */
 int linattn_window_bwd(const linattn_window_desc* desc, const void* q, const void* k, const void* v, const void* out, const float* lse,
                        const void* dout, void* dq, void* dk, void* dv, void* stream);
 

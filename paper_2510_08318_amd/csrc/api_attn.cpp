@@ -58,7 +58,11 @@ int check_window(const linattn_window_desc* w, WindowArgs* a, WindowSizes* z) {
   z->lse = (size_t)w->B * w->H * w->n * sizeof(float);
   z->parts = (2 * z->lse + 255) & ~(size_t)255;
   z->work = z->parts;
-  if (w->dtype != LINATTN_F32) z->work += (size_t)key_split(w->B * w->HK, w->H / w->HK, w->n, w->d, a->sight).parts * 2 * key_block(w->d) * w->d * sizeof(float);
+  if (w->dtype == LINATTN_F32) {
+    const long long blocks = (w->n + 31) / 32;
+    const size_t q = (size_t)f32_shares(blocks * w->B * w->H) * w->B * w->H * (w->d + 2), k = (size_t)f32_shares(blocks * w->B * w->HK) * w->B * w->HK * 2 * w->d;
+    if (f32_shares(blocks * w->B * w->HK) > 1) z->work += (((q > k ? q : k) * w->n * sizeof(float)) + 255) & ~(size_t)255;
+  } else z->work += (size_t)key_split(w->B * w->HK, w->H / w->HK, w->n, w->d, a->sight).parts * 2 * key_block(w->d) * w->d * sizeof(float);
   return LINATTN_OK;
 }
 
@@ -129,6 +133,13 @@ int linattn_window_fwd(const linattn_window_desc* w, const void* q, const void* 
   if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out) || misaligned(lse, 4)) return LINATTN_E_ALIGN;
   const Region outs[2] = {{out, z.q}, {lse, z.lse}}, ins[3] = {{q, z.q}, {k, z.k}, {v, z.k}};
   if (any_overlap(outs, ins)) return LINATTN_E_ALIAS;
+  if (w->workspace) {
+    if (misaligned(w->workspace, 256)) return LINATTN_E_ALIGN;
+    if (w->workspace_bytes < z.work) return LINATTN_E_WORKSPACE;
+    const Region work[1] = {{w->workspace, z.work}}, tensors[5] = {{q, z.q}, {k, z.k}, {v, z.k}, {out, z.q}, {lse, z.lse}};
+    if (any_overlap(work, tensors)) return LINATTN_E_ALIAS;
+    a.parts = z.work > z.parts ? reinterpret_cast<float*>(static_cast<char*>(w->workspace) + z.parts) : nullptr;
+  }
   a.q = q; a.k = k; a.v = v; a.o = out; a.lse = lse;
   a.stream = static_cast<hipStream_t>(stream);
   return launch_window_fwd(a, w->dtype) == hipSuccess ? LINATTN_OK : LINATTN_E_HIP;
@@ -152,7 +163,7 @@ int linattn_window_bwd(const linattn_window_desc* w, const void* q, const void* 
   a.lse = const_cast<float*>(lse);
   a.nl = static_cast<float*>(w->workspace);
   a.nd = a.nl + (size_t)w->B * w->H * w->n;
-  a.parts = reinterpret_cast<float*>(static_cast<char*>(w->workspace) + z.parts);
+  a.parts = z.work > z.parts ? reinterpret_cast<float*>(static_cast<char*>(w->workspace) + z.parts) : nullptr;
   a.stream = static_cast<hipStream_t>(stream);
   return launch_window_bwd(a, w->dtype) == hipSuccess ? LINATTN_OK : LINATTN_E_HIP;
 }

@@ -69,7 +69,9 @@ struct WindowArgs {
   void *o, *dq, *dk, *dv;
   float* lse;               // written by the forward, read by the backward
   float *nl, *nd;           // workspace of the backward: fp32 [B*H][n] each, -lse / scale (fp32 tensors: -lse; -inf where nothing is seen) and -delta
-  float* parts;             // and (bf16) fp32 [part][2][key block][d], the parts of key_split
+  float* parts;             // and the sums' parts: bf16 tensors fp32 [part][2][key block][d] (key_split); fp32 tensors [share][row][d], with pairs of maximum and
+                            // sum behind them (forward), [share][key][2][d]; null: no shares
+  int shares;               // fp32 tensors: workgroups to a block of 32 rows
   const int* lengths;       // nullable
   int B, H, HK, n, d;
   Rows qr, kr;              // rows of q, out, dout, dq and of k, v, dk, dv
@@ -119,6 +121,9 @@ struct CacheArgs {
   float scale;
   hipStream_t stream;
 };
+
+// Workgroups to a block of 32 rows of fp32 tensors: as many as there are compute units for.
+inline int f32_shares(long long blocks) { return blocks * 2 > kCUs ? 1 : blocks * 8 <= kCUs ? 8 : (int)(kCUs / blocks); }
 
 // Whether a chunk's rows of a key head (its group's heads side by side) go to the kernel that deals keys, not rows, to a workgroup's wavefronts.
 inline bool few_rows(int H, int HK, int n) { return (long long)n * (H / HK) <= 64; }

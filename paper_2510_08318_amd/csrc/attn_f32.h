@@ -2,7 +2,9 @@
 // the lanes of each of its four wavefronts, which take the tiles of 32 that the rows see in turn and join their results in LDS at the end: a short sequence then
 // has four times the wavefronts, and nothing waits for a barrier.  An operand is read from global memory where it is used: a 16-byte load feeds four
 // instructions of 64 cycles, so the caches are idle most of the time, and LDS would save nothing.
-// Contraction over the channels: lane group g has channels g D/2 .. (k-step x: channel g D/2 + x).  Contraction over the tile's rows: k-step r has the rows
+// Where the blocks of 32 rows are fewer than the compute units, `shares` workgroups have the tiles of one in turn, and write fp32 parts that a second kernel
+// sums in their order.
+// Contraction over the channels: four k-steps have eight channels, of which lane group g has the four from 4 g on.  Contraction over the tile's rows: k-step r has the rows
 // that register r of a score block holds, 8 (r/4) + 4 g + r%4.  Accumulator rows m of block c are channels CB m + c.
 #pragma once
 #include "attn_rows.h"
@@ -12,10 +14,10 @@ namespace attn {
 
 __device__ __forceinline__ f32x16 mfma_f32(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
 
-// S[i][lane's row] += rows i of the tile . the lane's row x, whose D/2 channels of group g are in registers.  row: of tile row `lane % 32`.
+// S[i][lane's row] += rows i of the tile . the lane's row x, whose channels of group g are in registers.  row: of tile row `lane % 32`.
 template <int D>
 __device__ __forceinline__ void scores_f32(const float* row, int g, const float4 (&x)[D / 8], f32x16& s) {
-  pipelined_operands<D / 8, 6>([&](int i) { return *reinterpret_cast<const uint4*>(row + g * (D / 2) + 4 * i); },
+  pipelined_operands<D / 8, 6>([&](int i) { return *reinterpret_cast<const uint4*>(row + 8 * i + 4 * g); },
                                [&](int i, uint4 v) {
                                  float f[4];
                                  f32::unpack_f32x4(v, f);
@@ -55,7 +57,7 @@ __device__ __forceinline__ void put_acc_f32(float* block, int lane, const f32x16
 template <int D>
 __device__ __forceinline__ void load_half_row(const float* row, int g, bool live, float4 (&x)[D / 8]) {
 #pragma unroll
-  for (int i = 0; i < D / 8; ++i) x[i] = live ? *reinterpret_cast<const float4*>(row + g * (D / 2) + 4 * i) : make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i = 0; i < D / 8; ++i) x[i] = live ? *reinterpret_cast<const float4*>(row + 8 * i + 4 * g) : make_float4(0.f, 0.f, 0.f, 0.f);
 }
 
 // p = exp(scale s - lse) = 2^(scale2 s - lse log2(e)): the forward's weights up to the rounding of lse itself, with the product in two parts.  nl: -lse.
@@ -73,8 +75,8 @@ __global__ __launch_bounds__(256, 2) void window_fwd_f32_kernel(WindowArgs a) {
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
   const int blocks = (a.n + 31) / 32;
-  const PairPlace place = pair_place(blockIdx.x, a.B * a.H, blocks);
-  const int bh = place.pair, block = row_block(a.sight, place.at, blocks);
+  const PairPlace place = pair_place(blockIdx.x, a.B * a.H, blocks * a.shares);
+  const int bh = place.pair, share = place.at % a.shares, block = row_block(a.sight, place.at / a.shares, blocks);
   const int b = bh / a.H, h = bh % a.H, len = clamp_length(a.lengths, b, a.n), t = block * 32 + m;
   const bool live = t < len;
   const float* qbase = static_cast<const float*>(a.q) + head_base(a.qr, bh, a.H);
@@ -91,7 +93,7 @@ __global__ __launch_bounds__(256, 2) void window_fwd_f32_kernel(WindowArgs a) {
   const int p1 = (block * 32 + 32 < len ? block * 32 + 32 : len) - 1;
   const KeyTiles<32> tiles(a.sight, block * 32, p1 < block * 32 ? -1 : p1, len);
   const WaveSight sight(a.sight, block * 32, p1 < block * 32 ? -1 : p1, len);
-  for (int it = w; it < tiles.count; it += NW) {
+  for (int it = share * NW + w; it < tiles.count; it += NW * a.shares) {
     const int j0 = tiles.start(it), last = tiles.end - 1 - j0;
     f32x16 s[1] = {fill16(0.f)};
     scores_f32<D>(kbase + (size_t)(j0 + (m < last ? m : last)) * a.kr.sn, g, q, s[0]);
@@ -130,7 +132,13 @@ __global__ __launch_bounds__(256, 2) void window_fwd_f32_kernel(WindowArgs a) {
           test = fmaf(0.f, z, test);
         }
       }
-      if (__any(test != 0.f)) { again |= 1u << i; continue; }
+      if (a.shares == 1 && __any(test != 0.f)) { again |= 1u << i; continue; }
+    }
+    if (a.shares > 1) {
+      const size_t rows = (size_t)a.B * a.H * a.n, row = (size_t)share * rows + (size_t)bh * a.n + tt;
+      for (int c = 0; c < D / 64; ++c) a.parts[row * D + lane + 64 * c] = acc[c];
+      if (lane == 0) reinterpret_cast<float2*>(a.parts + (size_t)a.shares * rows * D)[row] = make_float2(top, sum);
+      continue;
     }
     const float inv = sum == 0.f ? 0.f : 1.0f / sum;
     float* out = static_cast<float*>(a.o) + head_base(a.qr, bh, a.H) + (size_t)tt * a.qr.sn;
@@ -153,9 +161,9 @@ __global__ __launch_bounds__(256, 2) void window_fwd_f32_kernel(WindowArgs a) {
   }
 }
 
-// The sums of the four wavefronts' [32][D] blocks, row by row: put(row, sums of channels lane, lane + 64); `again` gets those that are not finite.
+// The sums of the four wavefronts' [32][D] blocks, row by row: put(row, sums of channels lane, lane + 64); `again` gets those that are not finite, if they are looked for.
 template <int D, typename Put>
-__device__ __forceinline__ void join_rows_f32(const float* os, int w, int lane, int rows, unsigned& again, Put put) {
+__device__ __forceinline__ void join_rows_f32(const float* os, int w, int lane, int rows, bool look, unsigned& again, Put put) {
   constexpr int NW = kRowWaves;
   for (int i = 0; i < 32 / NW; ++i) {
     const int rr = w * (32 / NW) + i;
@@ -165,7 +173,7 @@ __device__ __forceinline__ void join_rows_f32(const float* os, int w, int lane, 
       for (int v = 0; v < NW; ++v) acc[c] += os[(v * 32 + rr) * D + lane + 64 * c];
       test = fmaf(0.f, acc[c], test);
     }
-    if (__any(test != 0.f)) again |= 1u << i;
+    if (look && __any(test != 0.f)) again |= 1u << i;
     else put(rr, acc);
   }
 }
@@ -176,8 +184,8 @@ __global__ __launch_bounds__(256, 1) void window_dq_f32_kernel(WindowArgs a) {
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
   const int blocks = (a.n + 31) / 32;
-  const PairPlace place = pair_place(blockIdx.x, a.B * a.H, blocks);
-  const int bh = place.pair, block = row_block(a.sight, place.at, blocks);
+  const PairPlace place = pair_place(blockIdx.x, a.B * a.H, blocks * a.shares);
+  const int bh = place.pair, share = place.at % a.shares, block = row_block(a.sight, place.at / a.shares, blocks);
   const int b = bh / a.H, h = bh % a.H, len = clamp_length(a.lengths, b, a.n), t = block * 32 + m;
   const bool live = t < len;
   const size_t head = head_base(a.qr, bh, a.H), row = head + (size_t)t * a.qr.sn, li = (size_t)bh * a.n + t;
@@ -190,14 +198,14 @@ __global__ __launch_bounds__(256, 1) void window_dq_f32_kernel(WindowArgs a) {
   float delta = 0.f;
 #pragma unroll
   for (int i = 0; i < D / 8; ++i) {
-    const float4 y = live ? *reinterpret_cast<const float4*>(static_cast<const float*>(a.out) + row + g * (D / 2) + 4 * i) : make_float4(0.f, 0.f, 0.f, 0.f);
+    const float4 y = live ? *reinterpret_cast<const float4*>(static_cast<const float*>(a.out) + row + 8 * i + 4 * g) : make_float4(0.f, 0.f, 0.f, 0.f);
     delta = fmaf(go[i].x, y.x, fmaf(go[i].y, y.y, fmaf(go[i].z, y.z, fmaf(go[i].w, y.w, delta))));
   }
   float x, y;
   pair32(delta, x, y);
   delta = x + y;
   const float lse = live ? a.lse[li] : -INFINITY, nl = lse == -INFINITY ? lse : -lse;
-  if (t < a.n && w == 0 && g == 0) { a.nl[li] = nl; a.nd[li] = -delta; }
+  if (t < a.n && w == 0 && g == 0 && share == 0) { a.nl[li] = nl; a.nd[li] = -delta; }
   f32x16 dq[CB];
 #pragma unroll
   for (int c = 0; c < CB; ++c) dq[c] = fill16(0.f);
@@ -205,7 +213,7 @@ __global__ __launch_bounds__(256, 1) void window_dq_f32_kernel(WindowArgs a) {
   const int p1 = (block * 32 + 32 < len ? block * 32 + 32 : len) - 1;
   const KeyTiles<32> tiles(a.sight, block * 32, p1 < block * 32 ? -1 : p1, len);
   const WaveSight sight(a.sight, block * 32, p1 < block * 32 ? -1 : p1, len);
-  for (int it = w; it < tiles.count; it += NW) {
+  for (int it = share * NW + w; it < tiles.count; it += NW * a.shares) {
     const int j0 = tiles.start(it), last = tiles.end - 1 - j0, mine = j0 + (m < last ? m : last);
     f32x16 s = fill16(0.f), dp = fill16(-delta);
     scores_f32<D>(kbase + (size_t)mine * a.kr.sn, g, q, s);
@@ -230,8 +238,12 @@ __global__ __launch_bounds__(256, 1) void window_dq_f32_kernel(WindowArgs a) {
   __syncthreads();
   unsigned again = 0;
   float* const to = static_cast<float*>(a.dq) + head + (size_t)block * 32 * a.qr.sn;
-  join_rows_f32<D>(os, w, lane, a.n - block * 32, again, [&](int rr, const float (&acc)[D / 64]) {
-    for (int c = 0; c < D / 64; ++c) to[(size_t)rr * a.qr.sn + lane + 64 * c] = a.scale * acc[c];
+  float* const part = a.parts + ((size_t)share * a.B * a.H * a.n + (size_t)bh * a.n + block * 32) * D;
+  join_rows_f32<D>(os, w, lane, a.n - block * 32, a.shares == 1, again, [&](int rr, const float (&acc)[D / 64]) {
+    for (int c = 0; c < D / 64; ++c) {
+      if (a.shares > 1) part[(size_t)rr * D + lane + 64 * c] = acc[c];
+      else to[(size_t)rr * a.qr.sn + lane + 64 * c] = a.scale * acc[c];
+    }
   });
   __syncthreads();
   for (; again; again &= again - 1) {
@@ -253,7 +265,7 @@ __global__ __launch_bounds__(256, 1) void window_dkv_f32_kernel(WindowArgs a) {
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32, G = a.H / a.HK;
   // blocks in turn to the XCDs: those of the first tokens, at the start of each head, have the most to do
-  const int block = blockIdx.x / (a.B * a.HK), bk = blockIdx.x % (a.B * a.HK), b = bk / a.HK, hk = bk % a.HK;
+  const int x0 = blockIdx.x / (a.B * a.HK), block = x0 / a.shares, share = x0 % a.shares, bk = blockIdx.x % (a.B * a.HK), b = bk / a.HK, hk = bk % a.HK;
   const int len = clamp_length(a.lengths, b, a.n), jb = block * 32, j = jb + m, j1 = (jb + 32 < len ? jb + 32 : len) - 1;
   const bool live = j < len;
   const int lo = live ? query_lo(a.sight, j) : 0, hi = live ? query_hi(a.sight, j, len) : 0;
@@ -272,7 +284,7 @@ __global__ __launch_bounds__(256, 1) void window_dkv_f32_kernel(WindowArgs a) {
     const size_t base = head_base(a.qr, b * a.H + hk * G + hd, a.H);
     return TokenKeys<float>{static_cast<const float*>(a.q) + base, static_cast<const float*>(a.dout) + base, a.qr.sn};
   };
-  for (int e = w; e < T * G; e += NW) {
+  for (int e = share * NW + w; e < T * G; e += NW * a.shares) {
     const int hd = e / T, i0 = (q0 + e - hd * T) * 32, last = len - 1 - i0, mine = i0 + (m < last ? m : last);
     const TokenKeys<float> rows = rows_of_head(hd);
     const size_t li = (size_t)(b * a.H + hk * G + hd) * a.n + i0;
@@ -310,14 +322,21 @@ __global__ __launch_bounds__(256, 1) void window_dkv_f32_kernel(WindowArgs a) {
   float *const tk = static_cast<float*>(a.dk) + head + (size_t)jb * a.kr.sn, *const tv = static_cast<float*>(a.dv) + head + (size_t)jb * a.kr.sn;
   put_acc_f32<D>(os + w * 32 * D, lane, dk);
   __syncthreads();
-  join_rows_f32<D>(os, w, lane, a.n - jb, again, [&](int rr, const float (&acc)[D / 64]) {
-    for (int c = 0; c < D / 64; ++c) tk[(size_t)rr * a.kr.sn + lane + 64 * c] = a.scale * acc[c];
+  float* const part = a.parts + ((size_t)share * a.B * a.HK * a.n + (size_t)bk * a.n + jb) * 2 * D;      // dk, dv of a key side by side
+  join_rows_f32<D>(os, w, lane, a.n - jb, a.shares == 1, again, [&](int rr, const float (&acc)[D / 64]) {
+    for (int c = 0; c < D / 64; ++c) {
+      if (a.shares > 1) part[(size_t)rr * 2 * D + lane + 64 * c] = acc[c];
+      else tk[(size_t)rr * a.kr.sn + lane + 64 * c] = a.scale * acc[c];
+    }
   });
   __syncthreads();
   put_acc_f32<D>(os + w * 32 * D, lane, dv);
   __syncthreads();
-  join_rows_f32<D>(os, w, lane, a.n - jb, again, [&](int rr, const float (&acc)[D / 64]) {
-    for (int c = 0; c < D / 64; ++c) tv[(size_t)rr * a.kr.sn + lane + 64 * c] = acc[c];
+  join_rows_f32<D>(os, w, lane, a.n - jb, a.shares == 1, again, [&](int rr, const float (&acc)[D / 64]) {
+    for (int c = 0; c < D / 64; ++c) {
+      if (a.shares > 1) part[(size_t)rr * 2 * D + D + lane + 64 * c] = acc[c];
+      else tv[(size_t)rr * a.kr.sn + lane + 64 * c] = acc[c];
+    }
   });
   __syncthreads();
   for (; again; again &= again - 1) {
@@ -338,22 +357,114 @@ __global__ __launch_bounds__(256, 1) void window_dkv_f32_kernel(WindowArgs a) {
   }
 }
 
+// The sums over the shares, a wavefront to a row; rows that are not finite once more over what they see alone.
 template <int D>
-hipError_t launch_fwd_f32(const WindowArgs& a) {
-  constexpr auto kernel = &window_fwd_f32_kernel<D>;
-  if (hipError_t e = set_smem_once<kernel>(kF32Smem(D)); e != hipSuccess) return e;
-  kernel<<<(unsigned)((a.n + 31) / 32 * (long long)(a.B * a.H)), 256, kF32Smem(D), a.stream>>>(a);
+__global__ __launch_bounds__(256) void window_fwd_sum_f32_kernel(WindowArgs a) {
+  __shared__ PlainScratch<D> ws[4];
+  const int lane = threadIdx.x % 64, t = blockIdx.x * 4 + threadIdx.x / 64, bh = blockIdx.y, b = bh / a.H, h = bh % a.H;
+  if (t >= a.n) return;
+  const size_t rows = (size_t)a.B * a.H * a.n, row = (size_t)bh * a.n + t, at = head_base(a.qr, bh, a.H) + (size_t)t * a.qr.sn;
+  const float2* ml = reinterpret_cast<const float2*>(a.parts + (size_t)a.shares * rows * D);
+  const float2 own = lane < a.shares ? ml[(size_t)lane * rows + row] : make_float2(-INFINITY, 0.f);
+  float m = wave_max(own.x);
+  const float weight = own.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(own.x - m);
+  float l = wave_sum(weight * own.y), acc[D / 64] = {}, test = 0.f * (own.y + l);
+  for (int s = 0; s < a.shares; ++s) {
+    const float f = __shfl(weight, s);
+    for (int c = 0; c < D / 64; ++c) {
+      const float x = a.parts[((size_t)s * rows + row) * D + lane + 64 * c];
+      acc[c] = fmaf(f, x, acc[c]);
+      test = fmaf(0.f, x, test);
+    }
+  }
+  const int len = clamp_length(a.lengths, b, a.n);
+  if (t < len && __any(test != 0.f)) {
+    PlainScratch<D>& ps = ws[threadIdx.x / 64];
+    ps.put(ps.a, static_cast<const float*>(a.q) + at, lane);
+    const size_t kv = head_base(a.kr, b * a.HK + h / (a.H / a.HK), a.HK);
+    const TokenKeys<float> keys{static_cast<const float*>(a.k) + kv, static_cast<const float*>(a.v) + kv, a.kr.sn};
+    const int lo = key_lo(a.sight, t), hi = key_hi(a.sight, t, len);
+    plain_row<D>(keys, ps.a, ps.p, t, len, a.sight, 0, a.sight.sinks < lo ? a.sight.sinks : lo, lo, hi, a.scale * kLog2e, lane, m, l, acc);
+  }
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  for (int c = 0; c < D / 64; ++c) static_cast<float*>(a.o)[at + lane + 64 * c] = acc[c] * inv;
+  if (a.lse && lane == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+template <int D>
+__global__ __launch_bounds__(256) void window_dq_sum_f32_kernel(WindowArgs a) {
+  __shared__ PlainScratch<D> ws[4];
+  const int lane = threadIdx.x % 64, t = blockIdx.x * 4 + threadIdx.x / 64, bh = blockIdx.y, b = bh / a.H, h = bh % a.H;
+  if (t >= a.n) return;
+  const size_t rows = (size_t)a.B * a.H * a.n, row = (size_t)bh * a.n + t, at = head_base(a.qr, bh, a.H) + (size_t)t * a.qr.sn;
+  float acc[D / 64] = {}, test = 0.f;
+  for (int c = 0; c < D / 64; ++c) {
+    for (int s = 0; s < a.shares; ++s) acc[c] += a.parts[((size_t)s * rows + row) * D + lane + 64 * c];
+    test = fmaf(0.f, acc[c], test);
+  }
+  const int len = clamp_length(a.lengths, b, a.n);
+  if (t < len && __any(test != 0.f)) {
+    PlainScratch<D>& ps = ws[threadIdx.x / 64];
+    ps.put(ps.a, static_cast<const float*>(a.q) + at, lane);
+    ps.put(ps.b, static_cast<const float*>(a.dout) + at, lane);
+    const size_t kv = head_base(a.kr, b * a.HK + h / (a.H / a.HK), a.HK);
+    const TokenKeys<float> keys{static_cast<const float*>(a.k) + kv, static_cast<const float*>(a.v) + kv, a.kr.sn};
+    plain_dq_row<D>(keys, ps.a, ps.b, ps.p, t, len, a.sight, a.scale * kLog2e, a.nl[row], kLog2e, -a.nd[row], lane, acc);
+  }
+  for (int c = 0; c < D / 64; ++c) static_cast<float*>(a.dq)[at + lane + 64 * c] = a.scale * acc[c];
+}
+template <int D>
+__global__ __launch_bounds__(256) void window_dkv_sum_f32_kernel(WindowArgs a) {
+  __shared__ PlainScratch<D> ws[4];
+  const int lane = threadIdx.x % 64, j = blockIdx.x * 4 + threadIdx.x / 64, bk = blockIdx.y, b = bk / a.HK, hk = bk % a.HK, G = a.H / a.HK;
+  if (j >= a.n) return;
+  const size_t rows = (size_t)a.B * a.HK * a.n, row = (size_t)bk * a.n + j, at = head_base(a.kr, bk, a.HK) + (size_t)j * a.kr.sn;
+  float dk[D / 64] = {}, dv[D / 64] = {}, test = 0.f;
+  for (int c = 0; c < D / 64; ++c) {
+    for (int s = 0; s < a.shares; ++s) {
+      const float* from = a.parts + ((size_t)s * rows + row) * 2 * D + lane + 64 * c;
+      dk[c] += from[0];
+      dv[c] += from[D];
+    }
+    test = fmaf(0.f, dk[c], fmaf(0.f, dv[c], test));
+  }
+  const int len = clamp_length(a.lengths, b, a.n);
+  if (j < len && __any(test != 0.f)) {
+    PlainScratch<D>& ps = ws[threadIdx.x / 64];
+    ps.put(ps.a, static_cast<const float*>(a.k) + at, lane);
+    ps.put(ps.b, static_cast<const float*>(a.v) + at, lane);
+    for (int c = 0; c < D / 64; ++c) dk[c] = dv[c] = 0.f;
+    for (int hd = 0; hd < G; ++hd) {
+      const int bh = b * a.H + hk * G + hd;
+      const size_t base = head_base(a.qr, bh, a.H), li = (size_t)bh * a.n;
+      const TokenKeys<float> from{static_cast<const float*>(a.q) + base, static_cast<const float*>(a.dout) + base, a.qr.sn};
+      plain_dkv_row<D>(from, ps.a, ps.b, ps.p, ps.s, query_lo(a.sight, j), query_hi(a.sight, j, len), a.scale * kLog2e, kLog2e, a.nl + li, a.nd + li, lane, dk, dv);
+    }
+  }
+  for (int c = 0; c < D / 64; ++c) {
+    static_cast<float*>(a.dk)[at + lane + 64 * c] = a.scale * dk[c];
+    static_cast<float*>(a.dv)[at + lane + 64 * c] = dv[c];
+  }
+}
+
+template <int D, typename Main, typename Sum>
+hipError_t launch_f32(Main, Sum, WindowArgs a, int heads) {
+  constexpr auto main = Main::value;
+  constexpr auto sum = Sum::value;
+  const long long blocks = (a.n + 31) / 32 * (long long)(a.B * heads);
+  a.shares = a.parts ? f32_shares(blocks) : 1;
+  if (hipError_t e = set_smem_once<main>(kF32Smem(D)); e != hipSuccess) return e;
+  main<<<(unsigned)(blocks * a.shares), 256, kF32Smem(D), a.stream>>>(a);
+  if (a.shares > 1) sum<<<dim3((a.n + 3) / 4, a.B * heads), 256, 0, a.stream>>>(a);
   return hipGetLastError();
 }
 template <int D>
+hipError_t launch_fwd_f32(const WindowArgs& a) {
+  return launch_f32<D>(KernelTag<&window_fwd_f32_kernel<D>>{}, KernelTag<&window_fwd_sum_f32_kernel<D>>{}, a, a.H);
+}
+template <int D>
 hipError_t launch_bwd_f32(const WindowArgs& a) {
-  constexpr auto dq = &window_dq_f32_kernel<D>;
-  if (hipError_t e = set_smem_once<dq>(kF32Smem(D)); e != hipSuccess) return e;
-  dq<<<(unsigned)((a.n + 31) / 32 * (long long)(a.B * a.H)), 256, kF32Smem(D), a.stream>>>(a);
-  constexpr auto dkv = &window_dkv_f32_kernel<D>;
-  if (hipError_t e = set_smem_once<dkv>(kF32Smem(D)); e != hipSuccess) return e;
-  dkv<<<(unsigned)((a.n + 31) / 32 * (long long)(a.B * a.HK)), 256, kF32Smem(D), a.stream>>>(a);
-  return hipGetLastError();
+  if (hipError_t e = launch_f32<D>(KernelTag<&window_dq_f32_kernel<D>>{}, KernelTag<&window_dq_sum_f32_kernel<D>>{}, a, a.H); e != hipSuccess) return e;
+  return launch_f32<D>(KernelTag<&window_dkv_f32_kernel<D>>{}, KernelTag<&window_dkv_sum_f32_kernel<D>>{}, a, a.HK);
 }
 
 }  // namespace attn

@@ -228,6 +228,13 @@ def _window_desc(q, k, v, left, right, sinks, scale, layout, lengths, f32_math):
                          B_.Sight(left, right, sinks, scale), B_._ptr(lengths), None, 0)
 
 
+def _workspace(desc, q):
+    size = B_.linattn_window_workspace_bytes(desc)
+    work = torch.empty(size, dtype=torch.uint8, device=q.device)
+    desc.workspace, desc.workspace_bytes = B_._ptr(work), size
+    return work
+
+
 @_on_device_of
 def window_attention(q, k, v, *, left=-1, right=-1, sinks=0, scale=0.0, layout="bhnd", lengths=None, f32_math=False, out=None, lse=None):
     """Softmax attention in which token i sees tokens i - left .. i + right and the first `sinks` tokens (up to i + right); a negative
@@ -239,6 +246,9 @@ def window_attention(q, k, v, *, left=-1, right=-1, sinks=0, scale=0.0, layout="
     lse = torch.empty((desc.B, desc.H, desc.n), dtype=torch.float32, device=q.device) if lse is None else lse
     _check_tokens("out", out, q.shape, q.dtype, q.get_device())
     _check_tokens("lse", lse, (desc.B, desc.H, desc.n), torch.float32, q.get_device())
+    work = None
+    if desc.dtype == B_.F32:
+        work = _workspace(desc, q)
     B_.linattn_window_fwd(desc, q, k, v, out, lse, _current_stream())
     return out, lse
 
@@ -252,9 +262,7 @@ def window_attention_backward(q, k, v, out, lse, dout, *, left=-1, right=-1, sin
     for name, t, like in (("out", out, q), ("dout", dout, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, v)):
         _check_tokens(name, t, like.shape, q.dtype, q.get_device())
     _check_tokens("lse", lse, (desc.B, desc.H, desc.n), torch.float32, q.get_device())
-    size = B_.linattn_window_workspace_bytes(desc)
-    work = torch.empty(size, dtype=torch.uint8, device=q.device)
-    desc.workspace, desc.workspace_bytes = B_._ptr(work), size
+    work = _workspace(desc, q)      # (a name holds it until the call has been queued)
     B_.linattn_window_bwd(desc, q, k, v, out, lse, dout, dq, dk, dv, _current_stream())
     return dq, dk, dv
 
