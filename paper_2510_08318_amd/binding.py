@@ -199,7 +199,7 @@ def _ref(desc):
 
 
 def _done(st: int, where: str, check: bool) -> int:
-    if st != OK and check:
+    if st and check:
         raise LinattnError(st, where)
     return st
 

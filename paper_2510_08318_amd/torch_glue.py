@@ -178,14 +178,19 @@ def _need(ok: bool, what: str):
         raise ValueError(what)
 
 
+@functools.lru_cache(maxsize=None)
+def _one_device() -> bool:
+    return torch.cuda.device_count() == 1
+
+
 def _on_device_of(fn):
     """Runs `fn` with the device of its first argument current (the library launches on the current device)."""
     @functools.wraps(fn)
     def call(first, *args, **kw):
         index = first.get_device() if isinstance(first, torch.Tensor) else first.index
-        if index == torch.cuda.current_device():
-            return fn(first, *args, **kw)
         _need(index >= 0, "tensors must be on the GPU")
+        if _one_device() or index == torch.cuda.current_device():
+            return fn(first, *args, **kw)
         with torch.cuda.device(index):
             return fn(first, *args, **kw)
     return call
@@ -230,9 +235,16 @@ def _window_desc(q, k, v, left, right, sinks, scale, layout, lengths, f32_math):
 
 def _workspace(desc, q):
     size = B_.linattn_window_workspace_bytes(desc)
-    work = torch.empty(size, dtype=torch.uint8, device=q.device)
+    work = q.new_empty(size, dtype=torch.uint8)
     desc.workspace, desc.workspace_bytes = B_._ptr(work), size
     return work
+
+
+def _lse(q, lse, shape):
+    if lse is None:
+        return q.new_empty(shape, dtype=torch.float32)
+    _check_tokens("lse", lse, shape, torch.float32, q.get_device())
+    return lse
 
 
 @_on_device_of
@@ -242,14 +254,14 @@ def window_attention(q, k, v, *, left=-1, right=-1, sinks=0, scale=0.0, layout="
     lengths: int32 [B], the tokens of each item; the rest is padding.  scale: 0 for 1/sqrt(d).  f32_math: fp32 arithmetic on bf16 tensors.
     Returns (out, lse); lse is fp32 [B, H, n]."""
     desc = _window_desc(q, k, v, left, right, sinks, scale, layout, lengths, f32_math)
-    out = torch.empty_like(q) if out is None else out
-    lse = torch.empty((desc.B, desc.H, desc.n), dtype=torch.float32, device=q.device) if lse is None else lse
-    _check_tokens("out", out, q.shape, q.dtype, q.get_device())
-    _check_tokens("lse", lse, (desc.B, desc.H, desc.n), torch.float32, q.get_device())
-    work = None
-    if desc.dtype == B_.F32:
-        work = _workspace(desc, q)
-    B_.linattn_window_fwd(desc, q, k, v, out, lse, _current_stream())
+    index = q.get_device()
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _check_tokens("out", out, q.shape, q.dtype, index)
+    lse = _lse(q, lse, (desc.B, desc.H, desc.n))
+    work = _workspace(desc, q) if desc.dtype == B_.F32 else None      # (a name holds it until the call has been queued)
+    B_.linattn_window_fwd(desc, q, k, v, out, lse, _raw_stream(index))
     return out, lse
 
 
@@ -258,12 +270,13 @@ def window_attention_backward(q, k, v, out, lse, dout, *, left=-1, right=-1, sin
                               f32_math=False, dq=None, dk=None, dv=None):
     """Gradients of window_attention (same keyword arguments) for the upstream gradient dout, from its out and lse."""
     desc = _window_desc(q, k, v, left, right, sinks, scale, layout, lengths, f32_math)
+    index = q.get_device()
     dq, dk, dv = [torch.empty_like(t) if g is None else g for g, t in ((dq, q), (dk, k), (dv, v))]
     for name, t, like in (("out", out, q), ("dout", dout, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, v)):
-        _check_tokens(name, t, like.shape, q.dtype, q.get_device())
-    _check_tokens("lse", lse, (desc.B, desc.H, desc.n), torch.float32, q.get_device())
+        _check_tokens(name, t, like.shape, q.dtype, index)
+    _check_tokens("lse", lse, (desc.B, desc.H, desc.n), torch.float32, index)
     work = _workspace(desc, q)      # (a name holds it until the call has been queued)
-    B_.linattn_window_bwd(desc, q, k, v, out, lse, dout, dq, dk, dv, _current_stream())
+    B_.linattn_window_bwd(desc, q, k, v, out, lse, dout, dq, dk, dv, _raw_stream(index))
     return dq, dk, dv
 
 
@@ -313,7 +326,7 @@ class PagedCache:
         shape = _token_shape(self.B, self.H, n, self.d, layout)
         _check_tokens("k", k, shape, torch.bfloat16, self.index)
         _check_tokens("v", v, shape, torch.bfloat16, self.index)
-        B_.linattn_cache_write(self._describe(layout, counts), k, v, n, _current_stream())
+        B_.linattn_cache_write(self._describe(layout, counts), k, v, n, _raw_stream(self.index))
 
     @_on_device_of
     def read(self, n, *, layout="bnhd", k=None, v=None):
@@ -323,7 +336,7 @@ class PagedCache:
         k, v = [torch.empty(shape, dtype=torch.bfloat16, device=self.k.device) if t is None else t for t in (k, v)]
         for name, t in (("k", k), ("v", v)):
             _check_tokens(name, t, shape, torch.bfloat16, self.index)
-        B_.linattn_cache_read(self._describe(layout, None), k, v, n, _current_stream())
+        B_.linattn_cache_read(self._describe(layout, None), k, v, n, _raw_stream(self.index))
         return k, v
 
     @_on_device_of
@@ -333,12 +346,13 @@ class PagedCache:
         Returns (out, lse); lse is fp32 [B, H, n]."""
         B, H, n, d = _token_dims(q, layout)
         _check_tokens("q", q, _token_shape(self.B, H, n, self.d, layout), torch.bfloat16, self.index)
-        out = torch.empty_like(q) if out is None else out
-        lse = torch.empty((B, H, n), dtype=torch.float32, device=q.device) if lse is None else lse
-        _check_tokens("out", out, q.shape, q.dtype, self.index)
-        _check_tokens("lse", lse, (B, H, n), torch.float32, self.index)
+        if out is None:
+            out = torch.empty_like(q)
+        else:
+            _check_tokens("out", out, q.shape, q.dtype, self.index)
+        lse = _lse(q, lse, (B, H, n))
         desc = self._describe(layout, counts)
         size = B_.linattn_cache_workspace_bytes(desc, H, n)
-        work = torch.empty(size, dtype=torch.uint8, device=q.device) if size else None
-        B_.linattn_cache_attn(desc, B_.Sight(left, right, sinks, scale), q, out, lse, H, n, work, size, _current_stream())
+        work = q.new_empty(size, dtype=torch.uint8) if size else None
+        B_.linattn_cache_attn(desc, B_.Sight(left, right, sinks, scale), q, out, lse, H, n, work, size, _raw_stream(self.index))
         return out, lse
