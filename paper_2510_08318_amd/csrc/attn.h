@@ -125,6 +125,14 @@ struct CacheArgs {
 // Workgroups to a block of 32 rows of fp32 tensors: as many as there are compute units for.
 inline int f32_shares(long long blocks) { return blocks * 2 > kCUs ? 1 : blocks * 8 <= kCUs ? 8 : (int)(kCUs / blocks); }
 
+// Whether a forward call goes to the kernel that deals keys, not rows, to a workgroup's wavefronts: where its blocks of 32 rows are no more than the compute units
+// and see some keys.  Us, blocks of 128 rows / of 32, window to both sides: 4 heads x 1000 x 64, 128 13.8 / 9.1; 2 heads x 4000 x 128, causal 76 / 48; but 16 heads x
+// 1000 x 64 (512 blocks), 256 16.6 / 20.6, 4 x 60 x 64 5.4 / 6.2.
+inline bool few_blocks(long long pairs, long long rows, int n, const Sight& s) {
+  const long long reach = s.left < 0 || s.right < 0 ? n : (long long)s.left + s.right + s.sinks;
+  return pairs * ((rows + 31) / 32) <= kCUs && (reach < n ? reach : n) >= 128;
+}
+
 // Whether a chunk's rows of a key head (its group's heads side by side) go to the kernel that deals keys, not rows, to a workgroup's wavefronts.
 inline bool few_rows(int H, int HK, int n) { return (long long)n * (H / HK) <= 64; }
 // The keys that a row of a chunk sees at most, together with the rest of the chunk's.

@@ -1,5 +1,5 @@
-// Attention of few rows (a token or some, with the heads of their group) over a paged cache, which is bound by reading the cache once: the keys are dealt to
-// workgroups and there to wavefronts.  A wavefront has tiles of its own in LDS and no barrier in its loop; the next tile is on its way while one is worked
+// Attention with the keys, not the rows, dealt to a workgroup's wavefronts: of few rows (a token or some, with the heads of their group) over a paged cache, which is
+// bound by reading the cache once, and of short sequences, of which blocks of 128 rows would leave most of the chip empty.  A wavefront has tiles of its own in LDS and no barrier in its loop; the next tile is on its way while one is worked
 // on, 32 KB a wavefront and 64 KB in flight for a compute unit.  Codes stay codes in LDS (half the bytes) and become bf16 where the operand is made.
 #pragma once
 #include "attn_rows.h"
@@ -49,20 +49,67 @@ struct KeyTile {
   }
 };
 
-template <int D, int QB, bool E4M3>
-__global__ __launch_bounds__(64 * kRowWaves, 1) void attn_keys_kernel(RowsArgs a, Pool pool) {
+// Where the keys come from: look(j0, end) finds the rows of a tile (of keys from `end` on the last one's again), k_row and v_row are where row r of it lies.
+template <int D, bool E4M3>
+struct KeysOfPool {
+  using Args = Pool;
+  static constexpr bool kE4M3 = E4M3;
+  const Pool& p;
+  int b, hk, lane, len, count;
+  PoolRows rows;
+  unsigned long long there;
+  __device__ __forceinline__ KeysOfPool(const Args& a, int b_, int hk_, int n, int lane_) : p(a), b(b_), hk(hk_), lane(lane_) {
+    len = pool_length(p, b);
+    count = clamp_length(p.counts, b, n);
+  }
+  template <int TK>
+  __device__ __forceinline__ void look(int j0, int end) {
+    rows.find<TK>(p, b, hk, j0, end, lane);
+    there = rows.there;
+  }
+  __device__ __forceinline__ size_t offset(int r) const { return (size_t)rows.of(r) * (D * (E4M3 ? 1 : 2)); }
+  __device__ __forceinline__ const char* k_row(size_t at) const { return static_cast<const char*>(p.k) + at; }
+  __device__ __forceinline__ const char* v_row(size_t at) const { return static_cast<const char*>(p.v) + at; }
+  __device__ __forceinline__ PoolKeys<E4M3> keys() const { return {&p, b, hk, D}; }
+};
+template <int D>
+struct KeysOfTokens {
+  using Args = TokenArgs;
+  static constexpr bool kE4M3 = false;
+  const char *k, *v;
+  size_t sn;
+  int len, count, j0, last;
+  static constexpr unsigned long long there = ~0ull;
+  __device__ __forceinline__ KeysOfTokens(const Args& a, int b, int hk, int n, int) : sn(a.kr.sn) {
+    count = len = clamp_length(a.lengths, b, n);
+    const size_t at = ((size_t)b * a.kr.sb + (size_t)hk * a.kr.sh) * 2;
+    k = static_cast<const char*>(a.k) + at;
+    v = static_cast<const char*>(a.v) + at;
+  }
+  template <int TK>
+  __device__ __forceinline__ void look(int j, int end) { j0 = j; last = end - 1; }
+  __device__ __forceinline__ size_t offset(int r) const { return (size_t)(j0 + r < last ? j0 + r : last) * sn * 2; }
+  __device__ __forceinline__ const char* k_row(size_t at) const { return k + at; }
+  __device__ __forceinline__ const char* v_row(size_t at) const { return v + at; }
+  __device__ __forceinline__ TokenKeys<uint16_t> keys() const { return {reinterpret_cast<const uint16_t*>(k), reinterpret_cast<const uint16_t*>(v), sn}; }
+};
+
+template <int D, int QB, typename From>
+__global__ __launch_bounds__(64 * kRowWaves, 1) void attn_keys_kernel(RowsArgs a, typename From::Args from_args) {
+  constexpr bool E4M3 = From::kE4M3;
   using T = KeyTile<D, E4M3>;
   constexpr int KS = D / 16, CB = D / 32, TK = T::TK, KB = T::KB, NW = kRowWaves, WAVE = 4 * T::BYTES + 256;
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
-  const int split = blockIdx.x, b = blockIdx.y / a.HK, hk = blockIdx.y % a.HK, G = a.G;
-  const int len = pool_length(pool, b), count = clamp_length(pool.counts, b, a.n), pos0 = len - count, t0 = pos0 < 0 ? -pos0 : 0, rows = count * G, all = a.n * G;
+  const int split = blockIdx.x % a.splits, row0 = blockIdx.x / a.splits * (32 * QB), b = blockIdx.y / a.HK, hk = blockIdx.y % a.HK, G = a.G;
+  From src(from_args, b, hk, a.n, lane);
+  const int len = src.len, count = src.count, pos0 = len - count, t0 = pos0 < 0 ? -pos0 : 0, rows = count * G, all = a.n * G;
 
   uint4 q[QB][KS];
   int lo[QB], hi[QB];
 #pragma unroll
   for (int i = 0; i < QB; ++i) {
-    const int r = 32 * i + m, t = r / G, h = hk * G + (r - t * G);
+    const int r = row0 + 32 * i + m, t = r / G, h = hk * G + (r - t * G);
     const bool live = r < rows && t >= t0;
     lo[i] = live ? key_lo(a.sight, pos0 + t) : 0;
     hi[i] = live ? key_hi(a.sight, pos0 + t, len) : 0;
@@ -79,27 +126,27 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void attn_keys_kernel(RowsArgs a
     for (int c = 0; c < CB; ++c) o[i][c] = fill16(0.f);
   }
 
-  const int p0 = pos0 + t0, p1 = count > t0 ? len - 1 : -1;
+  const int first = row0 / G > t0 ? row0 / G : t0, end_row = (row0 + 32 * QB < rows ? row0 + 32 * QB : rows) - 1;
+  const int p0 = pos0 + first, p1 = end_row >= 0 && end_row / G >= first ? pos0 + end_row / G : -1;
   const KeyTiles<TK> tiles(a.sight, p0, p1, len);
   const WaveSight sight(a.sight, p0, p1, len);
   const int it0 = (int)((long long)tiles.count * split / a.splits), it1 = (int)((long long)tiles.count * (split + 1) / a.splits);
   const uint32_t lds = lds_address(smem) + (uint32_t)(w * WAVE);
   float* const vs = reinterpret_cast<float*>(smem + w * WAVE + 4 * T::BYTES);      // the scales of the tile's v rows
   const T tile(lane);
-  PoolRows next;
   unsigned long long there_next = 0;
   uint32_t ek = 0, ev = 0;
-  auto look = [&](int i) { next.find<TK>(pool, b, hk, tiles.start(i), tiles.end, lane); };
+  auto look = [&](int i) { src.template look<TK>(tiles.start(i), tiles.end); };
   auto request = [&](int i, uint32_t to) {
-    there_next = next.there;
+    there_next = src.there;
 #pragma unroll
     for (int x = 0; x < T::N; ++x) {
       const int r = x * (64 / T::LPR) + lane / T::LPR;
-      const size_t from = (size_t)next.of(r) * T::RB + (size_t)(((lane % T::LPR) ^ T::swizzle(r)) * 16);
-      load_to_lds(static_cast<const char*>(pool.k) + from, to + x * 1024);
-      load_to_lds(static_cast<const char*>(pool.v) + from, to + T::BYTES + x * 1024);
+      const size_t from = src.offset(r) + (size_t)(((lane % T::LPR) ^ T::swizzle(r)) * 16);
+      load_to_lds(src.k_row(from), to + x * 1024);
+      load_to_lds(src.v_row(from), to + T::BYTES + x * 1024);
     }
-    if constexpr (E4M3) { ek = pool.k_exp[next.row]; ev = pool.v_exp[next.row]; }
+    if constexpr (E4M3) { ek = src.p.k_exp[src.rows.row]; ev = src.p.v_exp[src.rows.row]; }
   };
   int it = it0 + w;
   if (it < it1) {
@@ -172,10 +219,11 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void attn_keys_kernel(RowsArgs a
       }
   }
 
-  // The wavefronts' parts, joined in LDS: [wavefront][row][D] and the pairs of maximum and sum behind them.
+  // The wavefronts' parts, joined in LDS: [wavefront][row][OS] and the pairs of maximum and sum behind them.  Eight threads have a row.
   __syncthreads();
+  constexpr int OS = D + 4;                              // floats from row to row, so that rows begin in different banks
   float* const os = reinterpret_cast<float*>(smem);
-  float2* const ml = reinterpret_cast<float2*>(os + NW * 32 * D);
+  float2* const ml = reinterpret_cast<float2*>(os + NW * 32 * OS);
 #pragma unroll
   for (int i = 0; i < QB; ++i) {
     float x, y;
@@ -184,64 +232,77 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void attn_keys_kernel(RowsArgs a
     for (int c = 0; c < CB; ++c)
 #pragma unroll
       for (int e = 0; e < 16; e += 4)
-        *reinterpret_cast<float4*>(os + (w * 32 + m) * D + 32 * c + 2 * e + 4 * g) =
+        *reinterpret_cast<float4*>(os + (w * 32 + m) * OS + 32 * c + 2 * e + 4 * g) =
             make_float4(o[i][c][e], o[i][c][e + 1], o[i][c][e + 2], o[i][c][e + 3]);
     if (g == 0) ml[w * 32 + m] = make_float2(mx[i], x + y);
     __syncthreads();
-    unsigned again = 0;                                  // rows of this wavefront's share that are not finite
-    for (int x32 = 0; x32 < 32 / NW; ++x32) {
-      const int rr = w * (32 / NW) + x32, r = 32 * i + rr, t = r / G, h = hk * G + (r - t * G);
-      if (r >= all) break;
-      float top = -INFINITY, sum = 0.f, acc[D / 64] = {};
-      const bool live = r < rows && t >= t0;
-      if (live) {
-        for (int v = 0; v < NW; ++v) top = fmaxf(top, ml[v * 32 + rr].x);
-        float test = 0.f;
-        for (int v = 0; v < NW; ++v) {
-          const float2 e = ml[v * 32 + rr];
-          const float f = e.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(e.x - top);
-          sum = fmaf(f, e.y, sum);
-          test = fmaf(0.f, e.y, test);
-          for (int c = 0; c < D / 64; ++c) {
-            const float z = os[(v * 32 + rr) * D + lane + 64 * c];
-            acc[c] = fmaf(f, z, acc[c]);
-            test = fmaf(0.f, z, test);
-          }
-        }
-        if (__any(test != 0.f)) { again |= 1u << x32; continue; }
+    const int rr = w * 8 + lane / 8, part = lane % 8, r = row0 + 32 * i + rr, t = r / G, h = hk * G + (r - t * G);
+    const bool live = r < rows && t >= t0;
+    float top = -INFINITY, sum = 0.f, test = 0.f, f[NW];
+    float4 acc[D / 32];
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) acc[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int v = 0; v < NW; ++v) top = fmaxf(top, ml[v * 32 + rr].x);
+#pragma unroll
+    for (int v = 0; v < NW; ++v) {
+      const float2 e = ml[v * 32 + rr];
+      f[v] = e.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(e.x - top);
+      sum = fmaf(f[v], e.y, sum);
+      test = fmaf(0.f, e.y, test);
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) {
+        const float4 z = *reinterpret_cast<const float4*>(os + (v * 32 + rr) * OS + 32 * c + 4 * part);
+        acc[c].x = fmaf(f[v], z.x, acc[c].x); acc[c].y = fmaf(f[v], z.y, acc[c].y);
+        acc[c].z = fmaf(f[v], z.z, acc[c].z); acc[c].w = fmaf(f[v], z.w, acc[c].w);
+        test = fmaf(0.f, z.x, fmaf(0.f, z.y, fmaf(0.f, z.z, fmaf(0.f, z.w, test))));
       }
-      const size_t at = (size_t)b * a.qr.sb + (size_t)h * a.qr.sh + (size_t)t * a.qr.sn, li = ((size_t)b * a.H + h) * a.n + t;
+    }
+    if (!live) {
+      top = -INFINITY; sum = 0.f; test = 0.f;
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) acc[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    const unsigned long long off = __ballot(test != 0.f);
+    if (r < all && !(off >> (lane & 56) & 255)) {
+      const size_t at = (size_t)b * a.qr.sb + (size_t)h * a.qr.sh + (size_t)t * a.qr.sn + 4 * part, li = ((size_t)b * a.H + h) * a.n + t;
       if (a.splits > 1) {
-        for (int c = 0; c < D / 64; ++c) a.parts[((size_t)split * a.B * a.H * a.n + li) * D + lane + 64 * c] = acc[c];
-        if (lane == 0) put_part(a, D, split, li, top, sum);
+        float* to = a.parts + ((size_t)split * a.B * a.H * a.n + li) * D + 4 * part;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) *reinterpret_cast<float4*>(to + 32 * c) = acc[c];
+        if (part == 0) put_part(a, D, split, li, top, sum);
       } else {
         const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-        for (int c = 0; c < D / 64; ++c) store1(static_cast<uint16_t*>(a.o) + at + lane + 64 * c, acc[c] * inv);
-        if (a.lse && lane == 0) a.lse[li] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c)
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.o) + at + 32 * c) =
+              make_uint2(pack_bf16x2(acc[c].x * inv, acc[c].y * inv), pack_bf16x2(acc[c].z * inv, acc[c].w * inv));
+        if (a.lse && part == 0) a.lse[li] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
       }
     }
     __syncthreads();
-    if (again) {
-      const PoolKeys<E4M3> keys{&pool, b, hk, D};
-      for (; again; again &= again - 1)
-        plain_again<D>(a, keys, tiles, it0, it1, 32 * i + w * (32 / NW) + __ffs(again) - 1, b, hk, split, pos0, len, reinterpret_cast<PlainScratch<D>*>(smem)[w], lane);
-    }
-    __syncthreads();
+    for (int x8 = 0; x8 < 8; ++x8)
+      if (off >> (8 * x8) & 255)
+        plain_again<D>(a, src.keys(), tiles, it0, it1, row0 + 32 * i + w * 8 + x8, b, hk, split, pos0, len, reinterpret_cast<PlainScratch<D>*>(smem)[w], lane);
+    if (QB > 1) __syncthreads();
   }
 }
 
-template <int D, bool E4M3>
-hipError_t launch_keys(const RowsArgs& a, const Pool& p, hipStream_t s) {
-  using T = KeyTile<D, E4M3>;
-  constexpr size_t tiles = kRowWaves * (4 * T::BYTES + 256), join = kRowWaves * 32 * (D * 4 + 8), smem = tiles > join ? tiles : join;
-  auto go = [&](auto kernel) -> hipError_t {
+template <int D, typename From>
+hipError_t launch_keys(RowsArgs a, const typename From::Args& from, hipStream_t s) {
+  using T = KeyTile<D, From::kE4M3>;
+  constexpr size_t tiles = kRowWaves * (4 * T::BYTES + 256), join = kRowWaves * 32 * ((D + 4) * 4 + 8), smem = tiles > join ? tiles : join;
+  auto go = [&](auto kernel, int rows) -> hipError_t {
     constexpr auto k = decltype(kernel)::value;
     if (hipError_t e = set_smem_once<k>(smem); e != hipSuccess) return e;
-    k<<<dim3(a.splits, a.B * a.HK), 64 * kRowWaves, smem, s>>>(a, p);
+    a.blocks = (a.n * a.G + rows - 1) / rows;
+    k<<<dim3(a.splits * a.blocks, a.B * a.HK), 64 * kRowWaves, smem, s>>>(a, from);
     return launch_join<D>(a, s);
   };
-  if (a.n * a.G <= 32) return go(KernelTag<&attn_keys_kernel<D, 1, E4M3>>{});
-  return go(KernelTag<&attn_keys_kernel<D, 2, E4M3>>{});
+  // blocks of 64 rows where there are more than 32 and a cache is to be read once
+  if constexpr (!std::is_same_v<typename From::Args, TokenArgs>)
+    if (a.n * a.G > 32) return go(KernelTag<&attn_keys_kernel<D, 2, From>>{}, 64);
+  return go(KernelTag<&attn_keys_kernel<D, 1, From>>{}, 32);
 }
 
 }  // namespace attn

@@ -332,10 +332,18 @@ __global__ __launch_bounds__(256) void attn_join_kernel(RowsArgs a) {
   const float weight = own.x == -INFINITY ? (own.y == 0.f ? 0.f : own.y) : __builtin_amdgcn_exp2f(own.x - top);      // (a sum without a maximum is NaN)
   const float sum = wave_sum(weight * own.y), inv = sum == 0.f ? 0.f : 1.0f / sum;
   float acc[D / 64] = {};
-  for (int s = 0; s < a.splits; ++s) {
-    const float f = __shfl(weight, s);
-    if (f != 0.f)
-      for (int c = 0; c < D / 64; ++c) acc[c] = fmaf(f, a.parts[((size_t)s * rows + row) * D + lane + 64 * c], acc[c]);
+  for (int s0 = 0; s0 < a.splits; s0 += 8) {      // eight parts in flight
+    float x[8][D / 64];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c) x[i][c] = s0 + i < a.splits ? a.parts[((size_t)(s0 + i) * rows + row) * D + lane + 64 * c] : 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float f = __shfl(weight, s0 + i);
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c) acc[c] = f == 0.f ? acc[c] : fmaf(f, x[i][c], acc[c]);
+    }
   }
   uint16_t* out = static_cast<uint16_t*>(a.o) + (size_t)(bh / a.H) * a.qr.sb + (size_t)(bh % a.H) * a.qr.sh + (size_t)t * a.qr.sn;
   for (int c = 0; c < D / 64; ++c) store1(out + lane + 64 * c, acc[c] * inv);

@@ -151,8 +151,8 @@ hipError_t launch_cache_attn(const CacheArgs& a, bool e4m3) {
   RowsArgs r{a.q, a.o, a.lse, a.work, p.B, a.H, p.HK, a.H / p.HK, a.n, 0, 1, a.qr, a.sight, a.scale * kLog2e};
   r.splits = cache_splits(p.B, a.H, p.HK, a.n, p.d, e4m3, reach_of(a));
   if (few_rows(a.H, p.HK, a.n)) {
-    if (p.d == 64) return e4m3 ? launch_keys<64, true>(r, p, a.stream) : launch_keys<64, false>(r, p, a.stream);
-    return e4m3 ? launch_keys<128, true>(r, p, a.stream) : launch_keys<128, false>(r, p, a.stream);
+    if (p.d == 64) return e4m3 ? launch_keys<64, KeysOfPool<64, true>>(r, p, a.stream) : launch_keys<64, KeysOfPool<64, false>>(r, p, a.stream);
+    return e4m3 ? launch_keys<128, KeysOfPool<128, true>>(r, p, a.stream) : launch_keys<128, KeysOfPool<128, false>>(r, p, a.stream);
   }
   if (p.d == 64) return e4m3 ? launch_rows<64, 64, PoolSource<64, 64, true>>(r, p, a.stream) : launch_rows<64, 64, PoolSource<64, 64, false>>(r, p, a.stream);
   return e4m3 ? launch_rows<128, 64, PoolSource<128, 64, true>>(r, p, a.stream) : launch_rows<128, 64, PoolSource<128, 64, false>>(r, p, a.stream);

@@ -1,6 +1,7 @@
 // Softmax attention with a sliding window and first tokens: linattn_window_fwd, linattn_window_bwd.
 #include "../../include/linattn.h"
 #include "attn_bwd.h"
+#include "attn_keys.h"
 #include "attn_f32.h"
 
 namespace linattn {
@@ -10,6 +11,7 @@ template <int D, int PIECES>
 static hipError_t fwd_as(const WindowArgs& a) {
   const TokenArgs keys{a.k, a.v, a.lengths, a.kr};
   const RowsArgs r{a.q, a.o, a.lse, nullptr, a.B, a.H, a.HK, a.H / a.HK, a.n, 0, 1, a.qr, a.sight, a.scale * kLog2e};
+  if (PIECES == 1 && few_blocks((long long)a.B * a.HK, (long long)a.n * r.G, a.n, a.sight)) return launch_keys<D, KeysOfTokens<D>>(r, keys, a.stream);
   return launch_rows<D, 64, TokenSource<D, 64>, PIECES>(r, keys, a.stream);
 }
 template <int D, int PIECES>

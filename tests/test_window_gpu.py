@@ -114,6 +114,18 @@ def test_shared_key_heads(H, HK):
     _check("bf16", 1, H, HK, 280, 64, 60, 0, 5, "bnhd")
 
 
+@pytest.mark.parametrize("left,right,sinks", SIGHTS)
+@pytest.mark.parametrize("n", [31, 64, 130, 200])
+def test_bf16_many_heads(n, left, right, sinks):
+    """As many blocks as have the forward take rows, not keys, to a wavefront; items of unlike lengths."""
+    _check("bf16", 10, 16, 8, n, 64, left, right, sinks, "bnhd", lengths=[n, 1, n // 2, n, n, n - 1, 0, n, n, 7 % n])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_bf16_many_heads_longer(d):
+    _check("bf16", 3, 12, 12, 1000, d, 300, 0, 70)
+
+
 @pytest.mark.parametrize("n,left,right,sinks", [(700, 150, 150, 40), (900, -1, 0, 0), (1100, 300, 0, 130)])
 @pytest.mark.parametrize("d", [64, 128])
 def test_longer_sequences(n, left, right, sinks, d):
