@@ -267,12 +267,20 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attn_rows_kernel(RowsArgs a
           }
       }
       softmax_step<KB, CB>(s, a.scale2, mx, l, o);
+      if constexpr (Source::kPaged) {      // (short of registers the compiler would read an operand, wait, multiply, and so on)
+        uint4 x[2 * KB][1];
 #pragma unroll
-      for (int st = 0; st < 2 * KB; ++st) {
-        uint4 x[PIECES];
-        weights_operand<PIECES>(s[st / 2], st % 2, x);
+        for (int st = 0; st < 2 * KB; ++st) weights_operand<1>(s[st / 2], st % 2, x[st]);
+        pipelined_operands<2 * KB * CB, 3>([&](int i) { return __builtin_bit_cast(uint4, turned<D>(vt + turned_rows, i % CB, 16 * (i / CB))); },
+                                           [&](int i, uint4 op) { o[i % CB] = mfma_weights<1>(as_bf16x8(op), x[i / CB], o[i % CB]); });
+      } else {
 #pragma unroll
-        for (int c = 0; c < CB; ++c) o[c] = mfma_weights<PIECES>(turned<D>(vt + turned_rows, c, 16 * st), x, o[c]);
+        for (int st = 0; st < 2 * KB; ++st) {
+          uint4 x[PIECES];
+          weights_operand<PIECES>(s[st / 2], st % 2, x);
+#pragma unroll
+          for (int c = 0; c < CB; ++c) o[c] = mfma_weights<PIECES>(turned<D>(vt + turned_rows, c, 16 * st), x, o[c]);
+        }
       }
     }
     if (it + 1 < it1) put(it + 1);
