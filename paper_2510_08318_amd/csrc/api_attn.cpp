@@ -34,7 +34,7 @@ int check_heads(int B, int H, int HK, int n, int d, int layout) {
   if (B <= 0 || H <= 0 || HK <= 0 || n <= 0 || H % HK) return LINATTN_E_SHAPE;
   if (d != 64 && d != 128) return LINATTN_E_SHAPE;
   if (layout != LINATTN_LAYOUT_BHND && layout != LINATTN_LAYOUT_BNHD) return LINATTN_E_SHAPE;
-  if ((long long)B * H > 65535 || (long long)n * (H / HK) > kMostTokens || (long long)B * H * n > 1LL << 37) return LINATTN_E_SHAPE;
+  if ((long long)B * H > 65535 || (long long)n * (H / HK) > kMostTokens || (long long)B * H * n > 1LL << 35) return LINATTN_E_SHAPE;
   return LINATTN_OK;
 }
 

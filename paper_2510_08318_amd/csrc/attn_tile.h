@@ -17,7 +17,8 @@ __device__ __forceinline__ void load_to_lds(const void* at, uint32_t lds) {
 __device__ __forceinline__ void lds_loads_landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // Operands that a kernel loads before its loop.  The compiler has to see them arrive there: it would otherwise wait for them at their first use, in every turn of the
-// loop, and with them for the tile that has just been asked for (forward, 12 heads x 32760 x 128: 1528 us, with this and reads ahead of the scores' products (figure)).
+// loop, and with them for the tile that has just been asked for (forward, 12 heads x 32760 x 128, window 2 x 3120: 1528 us, so, and with the operands of the scores read
+// ahead, 1507).
 template <int N>
 __device__ __forceinline__ void arrived(uint4 (&x)[N]) {
 #pragma unroll

@@ -34,7 +34,7 @@ __device__ __forceinline__ uint32_t encode4(const float* f, float s, float most)
   return u;
 }
 
-// A row of d bf16 to d / 8 lanes.
+// A row of d bf16 to d / 8 lanes.  A chunk of 4680 x 12 x 128 takes 12 us quantised (43 MB), a token of each of 64 sequences 3.2 us, a launch.
 template <int D, bool E4M3>
 __device__ __forceinline__ void write_row(const uint16_t* src, void* pool, uint8_t* exps, long long row, int part) {
   const uint4 x = *reinterpret_cast<const uint4*>(src + 8 * part);
@@ -69,7 +69,8 @@ __global__ __launch_bounds__(256) void cache_write_kernel(Pool p, const uint16_t
 
 // ---- read ---------------------------------------------------------------------------------
 
-// A thread has 16 bytes of a row of k and of v in the tensors, for kReadItems rows: their loads are in flight together.  Bound by memory.
+// A thread has 16 bytes of a row of k and of v in the tensors, for kReadItems rows: their loads are in flight together.  Bound by memory: 4 x 32760 x
+// 12 x 128 e4m3 (a third of it behind the sequences' ends), 148 MB read and 786 written in 195 us = 4.8 TB/s; with a row a thread 257.
 constexpr int kReadItems = 4;
 template <int D, bool E4M3, bool HEADS_INNER>
 __global__ __launch_bounds__(256) void cache_read_kernel(Pool p, uint16_t* k, uint16_t* v, int n, Rows r) {

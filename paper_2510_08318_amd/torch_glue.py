@@ -184,15 +184,16 @@ def _one_device() -> bool:
 
 
 def _on_device_of(fn):
-    """Runs `fn` with the device of its first argument current (the library launches on the current device)."""
+    """Runs `fn` with the device of its first argument (a cache, or the tensor q) current: the library launches on the current device."""
     @functools.wraps(fn)
-    def call(first, *args, **kw):
-        index = first.get_device() if isinstance(first, torch.Tensor) else first.index
-        _need(index >= 0, "tensors must be on the GPU")
+    def call(*args, **kw):
+        first = args[0] if args else kw.get("q")
+        index = first.index if isinstance(first, PagedCache) else first.get_device() if isinstance(first, torch.Tensor) else -1
+        _need(index >= 0, "q: a tensor on the GPU")
         if _one_device() or index == torch.cuda.current_device():
-            return fn(first, *args, **kw)
+            return fn(*args, **kw)
         with torch.cuda.device(index):
-            return fn(first, *args, **kw)
+            return fn(*args, **kw)
     return call
 
 

@@ -57,6 +57,35 @@ def test_bad_window_tensors():
     assert e.value.status == L.E_NULL
 
 
+def test_a_forward_workspace_is_optional_but_checked():
+    size = L.linattn_window_workspace_bytes(_window())
+    t = [P + i * BIG for i in range(5)]
+    f = lambda w: L.linattn_window_fwd(w, *t, check=False)
+    assert f(_window(workspace=P + 20 * BIG, workspace_bytes=size - 1)) == L.E_WORKSPACE
+    assert f(_window(workspace=P + 20 * BIG + 64, workspace_bytes=size)) == L.E_ALIGN
+    assert f(_window(workspace=P, workspace_bytes=size)) == L.E_ALIAS
+    # short fp32 sequences: room for parts of the sums; long ones need none
+    extra = lambda n: L.linattn_window_workspace_bytes(_window(dtype=L.F32, n=n)) - 2 * 2 * 4 * n * 4
+    assert extra(128) > 128 * 4 and extra(128 * 64) == 0
+
+
+def test_sizes_without_memory_behind_them_are_refused():
+    assert L.linattn_window_workspace_bytes(_window(B=1, H=64, HK=64, n=1 << 30)) == 0
+    assert L.linattn_window_workspace_bytes(_window(B=1, H=8, HK=2, n=1 << 29)) == 0            # n times the heads of a group
+
+
+def test_tensors_off_the_gpu_are_refused_by_the_glue():
+    import torch
+    from paper_2510_08318_amd import torch_glue as G
+    x = torch.zeros((1, 2, 4, 64), dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        G.window_attention(x, x, x)
+    with pytest.raises(ValueError):
+        G.window_attention_backward(x, x, x, x, x, x)
+    with pytest.raises(ValueError):
+        G.PagedCache.empty(4, 16, 2, 64, 1, 4, device="cpu")
+
+
 def test_bad_window_backward_calls():
     size = L.linattn_window_workspace_bytes(_window())
     assert size > 0 and size % 256 == 0

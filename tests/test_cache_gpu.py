@@ -193,6 +193,61 @@ def test_counts_beyond_the_chunk_and_the_sequence():
     _attend([30, 5, 12], [50, 8, 0], 8, 2, 2, 64, 8, False, -1, 0, 0, "bnhd")
 
 
+@pytest.mark.parametrize("n", [8, 100])
+def test_chunks_longer_than_their_sequences(n):
+    """Without counts every sequence has n new tokens; those before its start are padding."""
+    _attend([3, 120, 8], None, n, 4, 2, 64, 16, True, 20, 0, 2, "bhnd")
+
+
+def test_pools_past_32_bits():
+    """Pages behind 4 GB of a pool, written, read back and attended to."""
+    import torch
+    from paper_2510_08318_amd import torch_glue as G
+    H, d, page = 8, 128, 128
+    pages = 45_000                                                        # 5.9 GB of codes, 46 million exponents
+    for quantised in (True, False):
+        c = G.PagedCache.empty(pages if quantised else pages // 2, page, H, d, 1, 3, quantised=quantised)
+        small = G.PagedCache.empty(3, page, H, d, 1, 3, quantised=quantised)
+        c.table.copy_(torch.tensor([[c.pages - 1, c.pages - 7, c.pages - 2]], dtype=torch.int32))
+        small.table.copy_(torch.tensor([[2, 0, 1]], dtype=torch.int32))
+        gen = torch.Generator(device="cuda").manual_seed(4)
+        k, v, q = [torch.randn((1, 300, H, d), device="cuda", generator=gen).to(torch.bfloat16) for _ in range(3)]
+        res = []
+        for cache in (c, small):
+            cache.lengths.fill_(300)
+            cache.write(k, v)
+            res.append([*cache.read(300), *cache.attend(q, left=100), *cache.attend(q[:, -1:].contiguous())])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(*res))
+        del c
+
+
+def test_the_glue_refuses_what_the_library_cannot_see():
+    import torch
+    from paper_2510_08318_amd import binding as L, torch_glue as G
+    c, _ = _filled([20, 20], 2, 64, 16, True, "bnhd", 3)
+    q = torch.zeros((2, 3, 4, 64), dtype=torch.bfloat16, device="cuda")
+    k = torch.zeros((2, 3, 2, 64), dtype=torch.bfloat16, device="cuda")
+    for bad in (q.float(), q[:1], q[..., :32].contiguous(), q.transpose(1, 2), q[:, :, :3].contiguous()):
+        with pytest.raises((ValueError, L.LinattnError)):
+            c.attend(bad)
+    for bad in (k.float(), k[:1], k[:, :, :1].contiguous(), q):
+        with pytest.raises(ValueError):
+            c.write(bad, k)
+        with pytest.raises(ValueError):
+            c.write(k, bad)
+    for counts in (torch.zeros(2, dtype=torch.int64, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32)):
+        with pytest.raises(ValueError):
+            c.write(k, k, counts=counts)
+    with pytest.raises(L.LinattnError):
+        c.read(0)
+    with pytest.raises(ValueError):
+        c.read(5, layout="hbnd")
+    for change in (dict(table=c.table.long()), dict(lengths=c.lengths[:1]), dict(k_exp=None), dict(v=c.v[:2]), dict(k=c.k.float())):
+        with pytest.raises(ValueError):
+            G.PagedCache(**{**dict(k=c.k, v=c.v, table=c.table, lengths=c.lengths, k_exp=c.k_exp, v_exp=c.v_exp), **change})
+
+
 @pytest.mark.parametrize("n", [1, 40])
 @pytest.mark.parametrize("e4m3", [False, True])
 def test_table_entries_that_name_no_page(n, e4m3):

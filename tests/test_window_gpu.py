@@ -272,3 +272,80 @@ def test_the_softmax_branch_of_a_mixed_layer():
         total = G.to_host_f64(linear[i]) + G.to_host_f64(soft[i])
         scale = np.sqrt(np.mean(want[i] ** 2)) + np.sqrt(np.mean(sm ** 2))
         assert np.abs(total - want[i] - sm).max() <= 1e-2 * max(np.abs(want[i]).max() + np.abs(sm).max(), scale)
+
+
+@pytest.mark.parametrize("mode", MODES)
+def test_without_lse_and_without_workspace(mode):
+    """The ABI's optional arguments: the forward without lse, and (fp32) without the workspace that its shared blocks need."""
+    import torch
+    from paper_2510_08318_amd import binding as L, torch_glue as G
+    q, k, v, _ = _make(mode, 2, 2, 2, 100, 64, "bhnd", 3)
+    kw = dict(left=30, right=0, sinks=2, f32_math=mode == "f32math")
+    want, _ = G.window_attention(q, k, v, **kw)
+    dtype = {"bf16": L.BF16, "f32math": L.BF16_F32MATH, "f32": L.F32}[mode]
+    desc = L.WindowDesc(dtype, 2, 2, 2, 100, 64, 0, L.Sight(30, 0, 2, 0.0), None, None, 0)
+    out = torch.empty_like(q)
+    L.linattn_window_fwd(desc, q, k, v, out, None, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert (out.float() - want.float()).abs().max() <= 2 * U[mode] * want.float().abs().max()
+
+
+def test_the_glue_refuses_what_the_library_cannot_see():
+    import torch
+    from paper_2510_08318_amd import binding as L, torch_glue as G
+    q, k, v, do = _make("bf16", 1, 2, 2, 40, 64, "bhnd", 3)
+    out, lse = G.window_attention(q, k, v)
+    bad = [dict(q=q.transpose(1, 2)), dict(q=q.half()), dict(k=k.float()), dict(v=v[:, :, :20]), dict(k=k[:, :1]), dict(v=v.cpu()), dict(q=q[0])]
+    for change in bad:
+        with pytest.raises((ValueError, L.LinattnError)):
+            G.window_attention(**{**dict(q=q, k=k, v=v), **change})
+    for kw in (dict(layout="nbhd"), dict(lengths=torch.tensor([40], device="cuda")), dict(lengths=torch.tensor([40, 40], dtype=torch.int32, device="cuda")),
+               dict(out=q.float()), dict(lse=lse[:, :1]), dict(sinks=-1), dict(scale=-1.0)):
+        with pytest.raises((ValueError, L.LinattnError)):
+            G.window_attention(q, k, v, **kw)
+    for args in ((q, k, v, out.float(), lse, do), (q, k, v, out, lse[:, :1], do), (q, k, v, out, lse.double(), do), (q, k, v, out, lse, do[:, :, :3])):
+        with pytest.raises(ValueError):
+            G.window_attention_backward(*args)
+
+
+def test_offsets_past_32_bits():
+    """600000 tokens of 32 heads, 4.9 GB a tensor: the last tokens' results are those of the last tokens alone."""
+    import torch
+    from paper_2510_08318_amd import torch_glue as G
+    n, H, d, tail = 600_000, 32, 128, 400
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    ts = []
+    for _ in range(4):
+        t = torch.empty((1, n, H, d), dtype=torch.bfloat16, device="cuda")
+        t.normal_(generator=gen)
+        ts.append(t)
+    q, k, v, do = ts
+    kw = dict(left=60, right=0, layout="bnhd")
+    out, lse = G.window_attention(q, k, v, **kw)
+    grads = G.window_attention_backward(q, k, v, out, lse, do, **kw)
+    s = [t[:, -tail:].contiguous() for t in ts]
+    out2, lse2 = G.window_attention(*s[:3], **kw)
+    grads2 = G.window_attention_backward(*s[:3], out2, lse2, s[3], **kw)
+    torch.cuda.synchronize()
+    assert (lse[:, :, -300:] - lse2[:, :, -300:]).abs().max() <= 1e-4
+    for a, b in zip((out, *grads), (out2, *grads2)):
+        x, y = a[:, -300:].float(), b[:, -300:].float()
+        # two roundings of operands and one of the result on each side, of numbers as large as the largest
+        assert (x - y).abs().max() <= 6 * 2.0 ** -8 * y.abs().max()
+
+
+def test_inputs_made_on_another_stream():
+    """The calls run on the current stream, after what it waited for."""
+    import torch
+    from paper_2510_08318_amd import torch_glue as G
+    q, k, v, _ = _make("bf16", 1, 4, 4, 500, 64, "bhnd", 8)
+    want, _ = G.window_attention(q, k, v, left=100)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        with torch.cuda.stream(side):
+            side.wait_stream(torch.cuda.default_stream())
+            k2 = (k.float() * 2 - k.float()).to(k.dtype)
+            got, _ = G.window_attention(q, k2, v, left=100)
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(want, got)
