@@ -70,7 +70,7 @@ __global__ __launch_bounds__(256) void cache_write_kernel(Pool p, const uint16_t
 // ---- read ---------------------------------------------------------------------------------
 
 // A thread has 16 bytes of a row of k and of v in the tensors, for kReadItems rows: their loads are in flight together.  Bound by memory: 4 x 32760 x
-// 12 x 128 e4m3 (a third of it behind the sequences' ends), 148 MB read and 786 written in 195 us = 4.8 TB/s; with a row a thread 257.
+// 12 x 128 e4m3 (a third of it behind the sequences' ends), 287 MB read and 805 written in 195 us = 5.6 TB/s; with a row a thread 257.
 constexpr int kReadItems = 4;
 template <int D, bool E4M3, bool HEADS_INNER>
 __global__ __launch_bounds__(256) void cache_read_kernel(Pool p, uint16_t* k, uint16_t* v, int n, Rows r) {
