@@ -251,7 +251,7 @@ int linattn_bwd(const void* q, const void* k, const void* v, const void* dout,
  * the usual time).  A row's sum of |v| times 2^8 has to stay below fp32's largest value; magnitudes below 2^-100 may count as zero. */
 typedef struct linattn_sight {
   int left, right, sinks;
-  float scale;            /* 0: 1 / sqrt(d) */
+  float scale;            /* 2^-100 to 2^100; 0: 1 / sqrt(d) */
 } linattn_sight;
 
 /* q, out, dout, dq: H heads; k, v, dk, dv: HK heads; all of n tokens, in `layout`.  Token i of a batch item has position i. */

@@ -22,7 +22,8 @@ Rows rows_of(int H, int n, int d, int layout) {
 }
 
 int check_sight(const linattn_sight& s, int d, Sight* sight, float* scale) {
-  if (s.sinks < 0 || !(s.scale >= 0.f) || std::isinf(s.scale)) return LINATTN_E_VALUE;
+  // (the backward starts its scores from -lse / scale)
+  if (s.sinks < 0 || !(s.scale == 0.f || (s.scale >= 0x1p-100f && s.scale <= 0x1p100f))) return LINATTN_E_VALUE;
   sight->left = s.left < 0 || s.left >= kMostTokens ? -1 : s.left;
   sight->right = s.right < 0 || s.right >= kMostTokens ? -1 : s.right;
   sight->sinks = s.sinks < kMostTokens ? s.sinks : kMostTokens;

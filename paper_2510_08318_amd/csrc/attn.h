@@ -148,7 +148,7 @@ inline int cache_splits(int B, int H, int HK, int n, int d, bool e4m3, long long
   const bool few = few_rows(H, HK, n);
   const long long blocks = (long long)B * HK * (few ? 1 : ((long long)n * (H / HK) + 127) / 128);
   const int tile = few ? (e4m3 || d == 64 ? 64 : 32) * 4 : 64 * 8;      // keys that a part has at least
-  long long s = (few ? 2 * kCUs : 2 * kCUs) / blocks;
+  long long s = 2 * kCUs / blocks;
   const long long most = (reach + tile - 1) / tile;
   s = s < most ? s : most;
   return s < 1 ? 1 : s < kMostSplits ? (int)s : kMostSplits;

@@ -34,6 +34,16 @@ def test_bad_window_descriptors(change, status):
     assert L.linattn_window_workspace_bytes(w) == 0
 
 
+@pytest.mark.parametrize("scale,good", [(0.0, True), (-0.0, True), (2.0 ** -100, True), (2.0 ** 100, True), (2.0 ** -101, False), (1e-40, False), (2.0 ** 101, False), (3e38, False)])
+def test_range_of_the_scale(scale, good):
+    w, c = _window(scale=scale), _cache()
+    t = [P + i * BIG for i in range(9)]
+    assert (L.linattn_window_workspace_bytes(w) > 0) == good
+    assert L.linattn_window_bwd(w, *t, check=False) == (L.E_WORKSPACE if good else L.E_VALUE)
+    q = [P + (20 + i) * BIG for i in range(2)]
+    assert L.linattn_cache_attn(c, L.Sight(-1, 0, 0, scale), None if good else q[0], q[1], None, 4, 1, None, 0, check=False) == (L.E_NULL if good else L.E_VALUE)
+
+
 def test_bad_window_tensors():
     w = _window()
     q, k, v, o, lse = [P + i * BIG for i in range(5)]
