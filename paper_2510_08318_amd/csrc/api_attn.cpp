@@ -107,7 +107,7 @@ int check_cache(const linattn_cache_desc* c, int n, Pool* p, CacheSizes* z) {
 }
 
 size_t attn_work_bytes(const linattn_cache_desc* c, int H, int n) {
-  const int splits = cache_splits(c->B, H, c->H, n, c->d, c->type == LINATTN_CACHE_E4M3, (long long)c->page * c->width);
+  const int splits = cache_splits(c->B, H, c->H, n, c->d, c->type == LINATTN_CACHE_E4M3, (long long)c->page * c->width).splits;
   return splits > 1 ? ((size_t)splits * c->B * H * n * (c->d + 2) * sizeof(float) + 255) & ~(size_t)255 : 0;
 }
 

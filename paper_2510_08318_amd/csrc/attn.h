@@ -142,16 +142,28 @@ inline long long reach_of(const CacheArgs& a) {
   const long long r = (long long)a.sight.left + a.n + (a.sight.right < 0 ? a.n : a.sight.right) + a.sight.sinks + 64;
   return r < all ? r : all;
 }
-// Parts that the keys are dealt to, for chunks whose keys number `reach` at most: as many workgroups as fill the chip, with enough tiles each.
-constexpr int kMostSplits = 64;
-inline int cache_splits(int B, int H, int HK, int n, int d, bool e4m3, long long reach) {
+// Parts that the keys of a row are dealt to, for chunks whose keys number `reach` at most: as many workgroups as fill the chip, with enough tiles each.  Blocks of rows that
+// nearly fill it, or two or three times, are cut as well where parts stay long: the last round is then full, and sums over some 8192 keys (`keys`; each sequence gets
+// parts by its own length, see splits_of) are worth writing and reading.  12 heads x 4680 rows over 32760 x 128, e4m3, 444 blocks in 512 places, us: 1300, in four parts 1200
+// (a sequence of 16384 in a table of 32768 592 / 603, of 8000, one part, 293 / 302: the empty workgroups and the join); 8 heads x 4680 over 32760 x 64 709 / 506; 512 rows over
+// 32760, 20000, 9000 and 3000, 32/8 heads x 128, 852 / 727.  Shorter parts do not pay: 512 rows over a window of 4096, 152, in four parts 187.
+constexpr int kMostSplits = 64, kLongPart = 8192;
+struct KeyParts {
+  int splits, keys;
+};
+inline KeyParts cache_splits(int B, int H, int HK, int n, int d, bool e4m3, long long reach) {
   const bool few = few_rows(H, HK, n);
   const long long blocks = (long long)B * HK * (few ? 1 : ((long long)n * (H / HK) + 127) / 128);
-  const int tile = few ? (e4m3 || d == 64 ? 64 : 32) * 4 : 64 * 8;      // keys that a part has at least
-  long long s = 2 * kCUs / blocks;
-  const long long most = (reach + tile - 1) / tile;
+  const int tile = few ? (e4m3 || d == 64 ? 64 : 32) * 4 : 64 * 8;
+  long long s = 2 * kCUs / blocks, most = (reach + tile - 1) / tile;
+  int keys = 0;
+  if (!few && s <= 1 && reach >= 2 * kLongPart) {
+    s = 8 * kCUs / blocks;
+    keys = kLongPart;
+    most = (reach + keys / 2) / keys;
+  }
   s = s < most ? s : most;
-  return s < 1 ? 1 : s < kMostSplits ? (int)s : kMostSplits;
+  return {s < 1 ? 1 : s < kMostSplits ? (int)s : kMostSplits, keys};
 }
 
 hipError_t launch_window_fwd(const WindowArgs& a, int dtype);

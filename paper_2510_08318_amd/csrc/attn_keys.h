@@ -284,7 +284,8 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void attn_keys_kernel(RowsArgs a
     __syncthreads();
     for (int x8 = 0; x8 < 8; ++x8)
       if (off >> (8 * x8) & 255)
-        plain_again<D>(a, src.keys(), tiles, it0, it1, row0 + 32 * i + w * 8 + x8, b, hk, split, pos0, len, reinterpret_cast<PlainScratch<D>*>(smem)[w], lane);
+        plain_again<D>(a, src.keys(), tiles, it0, it1, row0 + 32 * i + w * 8 + x8, b, hk, split, a.splits, pos0, len, reinterpret_cast<PlainScratch<D>*>(smem)[w],
+                       lane);
     if (QB > 1) __syncthreads();
   }
 }

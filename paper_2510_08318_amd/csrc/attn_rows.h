@@ -18,7 +18,16 @@ struct RowsArgs {
   Rows qr;
   Sight sight;
   float scale2;             // scale * log2(e)
+  // of a pool's keys `splits` is the most that a sequence gets, and each has about part_keys of its keys at least (0: all get `splits`)
+  int part_keys, reach;
+  const int* lengths;
 };
+// Splits of a sequence of len tokens, in the kernel and in the join.
+__device__ __forceinline__ int splits_of(const RowsArgs& a, int len) {
+  if (a.part_keys == 0) return a.splits;
+  const int s = ((len < a.reach ? len : a.reach) + a.part_keys / 2) / a.part_keys;
+  return s < 1 ? 1 : s < a.splits ? s : a.splits;
+}
 // Results over a part of the keys: o not divided by its sum, fp32 [splits][B*H*n][D], and then [splits][B*H*n] pairs of the largest score (base 2) and
 // the sum.
 __device__ __forceinline__ void put_part(const RowsArgs& a, int D, int split, size_t row, float m, float l) {
@@ -167,15 +176,15 @@ __device__ __forceinline__ void softmax_step(f32x16 (&s)[KB], float scale2, floa
 
 // Row r of a block once more, key by key, over the keys of tiles it0 .. it1 - 1.
 template <int D, typename Keys, typename Tiles>
-__device__ void plain_again(const RowsArgs& a, const Keys& keys, const Tiles& tiles, int it0, int it1, int r, int b, int hk, int split, int pos0, int len,
-                            PlainScratch<D>& ps, int lane) {
+__device__ void plain_again(const RowsArgs& a, const Keys& keys, const Tiles& tiles, int it0, int it1, int r, int b, int hk, int split, int splits, int pos0,
+                            int len, PlainScratch<D>& ps, int lane) {
   const int t = r / a.G, h = hk * a.G + (r - t * a.G);
   const size_t at = (size_t)b * a.qr.sb + (size_t)h * a.qr.sh + (size_t)t * a.qr.sn, li = ((size_t)b * a.H + h) * a.n + t;
   ps.put(ps.a, static_cast<const uint16_t*>(a.q) + at, lane);
   float m, l, acc[D / 64];
   plain_row<D>(keys, ps.a, ps.p, pos0 + t, len, a.sight, tiles.sink_key(it0), tiles.sink_key(it1), tiles.window_key(it0), tiles.window_key(it1), a.scale2,
                lane, m, l, acc);
-  if (a.splits > 1) {
+  if (splits > 1) {
     for (int c = 0; c < D / 64; ++c) a.parts[((size_t)split * a.B * a.H * a.n + li) * D + lane + 64 * c] = acc[c];
     if (lane == 0) put_part(a, D, split, li, m, l);
     return;
@@ -199,11 +208,15 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attn_rows_kernel(RowsArgs a
   constexpr int NW = kRowWaves, KB = KT / 32, KS = D / 16, CB = D / 32, BM = 32 * NW, TILE = KT * D * 2;
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
-  const PairPlace place = pair_place(blockIdx.x, a.B * a.HK, a.blocks * a.splits);
-  const int bk = place.pair, split = place.at % a.splits, block = row_block(a.sight, place.at / a.splits, a.blocks);
+  // (first parts first: where a sequence has only one, the workgroups that leave at once come behind those that have work)
+  const int pairs = a.B * a.HK, split = (int)blockIdx.x / (pairs * a.blocks);
+  const PairPlace place = pair_place((int)blockIdx.x - split * pairs * a.blocks, pairs, a.blocks);
+  const int bk = place.pair, block = row_block(a.sight, place.at, a.blocks);
   const int b = bk / a.HK, hk = bk % a.HK, G = a.G;
   Source src(from, b, hk, a.n, w, lane);
   // token t has position pos0 + t; tokens t0 .. count - 1 have rows
+  const int splits = Source::kPaged ? splits_of(a, src.len) : 1;
+  if (split >= splits) return;
   const int len = src.len, pos0 = len - src.count, t0 = pos0 < 0 ? -pos0 : 0, rows = src.count * G, all = a.n * G;
   const int row0 = block * BM + w * 32;
 
@@ -226,7 +239,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attn_rows_kernel(RowsArgs a
   const int bp0 = from_row(block * BM), bp1 = to_row((block + 1) * BM), wp0 = from_row(row0), wp1 = to_row(row0 + 32);
   const KeyTiles<KT> tiles(a.sight, bp0, bp1 < bp0 ? -1 : bp1, len);
   const WaveSight sight(a.sight, wp0, wp1 < wp0 ? -1 : wp1, len);
-  const int it0 = (int)((long long)tiles.count * split / a.splits), it1 = (int)((long long)tiles.count * (split + 1) / a.splits);
+  const int it0 = (int)((long long)tiles.count * split / splits), it1 = (int)((long long)tiles.count * (split + 1) / splits);
   const TileOrder<KT> order(tiles, it0, it1);
   const uint32_t lds = lds_address(smem);
   auto ktile = [&](int i) { return lds + (uint32_t)((i - it0) & 1) * 2 * TILE; };
@@ -314,7 +327,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attn_rows_kernel(RowsArgs a
     for (int e = 0; e < 16; ++e) test = fmaf(0.f, o[c][e], test);
   uint32_t again = (uint32_t)__ballot(test != 0.f) | (uint32_t)(__ballot(test != 0.f) >> 32);
   if (store && !(again >> m & 1)) {
-    if (a.splits > 1) {
+    if (splits > 1) {
       float* part = a.parts + ((size_t)split * a.B * a.H * a.n + li) * D + 4 * g;
 #pragma unroll
       for (int c = 0; c < CB; ++c)
@@ -332,28 +345,30 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attn_rows_kernel(RowsArgs a
     }
   }
   for (; again; again &= again - 1)
-    plain_again<D>(a, src.keys(), tiles, it0, it1, row0 + __ffs(again) - 1, b, hk, split, pos0, len, reinterpret_cast<PlainScratch<D>*>(smem)[w], lane);
+    plain_again<D>(a, src.keys(), tiles, it0, it1, row0 + __ffs(again) - 1, b, hk, split, splits, pos0, len, reinterpret_cast<PlainScratch<D>*>(smem)[w],
+                   lane);
 }
 
 // The sum over the splits.  A wavefront to a row.
 template <int D>
 __global__ __launch_bounds__(256) void attn_join_kernel(RowsArgs a) {
   const int lane = threadIdx.x % 64, t = blockIdx.x * 4 + threadIdx.x / 64, bh = blockIdx.y;
-  if (t >= a.n) return;
+  const int splits = splits_of(a, a.part_keys ? clamp_length(a.lengths, bh / a.H, a.reach) : 0);
+  if (t >= a.n || (splits == 1 && a.part_keys)) return;      // (one part: the kernel has stored the result)
   const size_t rows = (size_t)a.B * a.H * a.n, row = (size_t)bh * a.n + t;
   const float2* ml = reinterpret_cast<const float2*>(a.parts + (size_t)a.splits * rows * D);
   // a lane to a split, at most 64 of them
-  const float2 own = lane < a.splits ? ml[(size_t)lane * rows + row] : make_float2(-INFINITY, 0.f);
+  const float2 own = lane < splits ? ml[(size_t)lane * rows + row] : make_float2(-INFINITY, 0.f);
   const float top = wave_max(own.x);
   const float weight = own.x == -INFINITY ? (own.y == 0.f ? 0.f : own.y) : __builtin_amdgcn_exp2f(own.x - top);      // (a sum without a maximum is NaN)
   const float sum = wave_sum(weight * own.y), inv = sum == 0.f ? 0.f : 1.0f / sum;
   float acc[D / 64] = {};
-  for (int s0 = 0; s0 < a.splits; s0 += 8) {      // eight parts in flight
+  for (int s0 = 0; s0 < splits; s0 += 8) {      // eight parts in flight
     float x[8][D / 64];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
-      for (int c = 0; c < D / 64; ++c) x[i][c] = s0 + i < a.splits ? a.parts[((size_t)(s0 + i) * rows + row) * D + lane + 64 * c] : 0.f;
+      for (int c = 0; c < D / 64; ++c) x[i][c] = s0 + i < splits ? a.parts[((size_t)(s0 + i) * rows + row) * D + lane + 64 * c] : 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float f = __shfl(weight, s0 + i);

@@ -150,10 +150,14 @@ hipError_t launch_cache_read(const Pool& p, bool e4m3, void* k, void* v, int n, 
 hipError_t launch_cache_attn(const CacheArgs& a, bool e4m3) {
   const Pool& p = a.pool;
   RowsArgs r{a.q, a.o, a.lse, a.work, p.B, a.H, p.HK, a.H / p.HK, a.n, 0, 1, a.qr, a.sight, a.scale * kLog2e};
-  r.splits = cache_splits(p.B, a.H, p.HK, a.n, p.d, e4m3, reach_of(a));
+  const KeyParts parts = cache_splits(p.B, a.H, p.HK, a.n, p.d, e4m3, reach_of(a));
+  r.splits = parts.splits;
   if (few_rows(a.H, p.HK, a.n)) {
     if (p.d == 64) return e4m3 ? launch_keys<64, KeysOfPool<64, true>>(r, p, a.stream) : launch_keys<64, KeysOfPool<64, false>>(r, p, a.stream);
     return e4m3 ? launch_keys<128, KeysOfPool<128, true>>(r, p, a.stream) : launch_keys<128, KeysOfPool<128, false>>(r, p, a.stream);
+  }
+  if (parts.splits > 1) {
+    r.part_keys = parts.keys; r.reach = (int)reach_of(a); r.lengths = p.lengths;
   }
   if (p.d == 64) return e4m3 ? launch_rows<64, 64, PoolSource<64, 64, true>>(r, p, a.stream) : launch_rows<64, 64, PoolSource<64, 64, false>>(r, p, a.stream);
   return e4m3 ? launch_rows<128, 64, PoolSource<128, 64, true>>(r, p, a.stream) : launch_rows<128, 64, PoolSource<128, 64, false>>(r, p, a.stream);

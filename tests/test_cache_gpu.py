@@ -347,3 +347,50 @@ def test_captured_steps_replay():
         torch.cuda.synchronize()
         assert torch.equal(caches[0].lengths, caches[1].lengths)
         assert torch.equal(out, want) and torch.equal(lse, wl), i
+
+
+@pytest.mark.parametrize("e4m3,d,left,sinks", [(False, 64, -1, 0), (True, 128, -1, 0), (False, 128, 20400, 2)])
+def test_long_parts_of_unlike_sequences(e4m3, d, left, sinks):
+    """Blocks of rows that fill the chip, over sequences whose keys go in three parts, in two, in one, and an empty one; with a window also a key that is NaN, which a
+    hundred of the rows do not see."""
+    import torch
+    from paper_2510_08318_amd import torch_glue as G
+    lengths, n, H, page, width = [24000, 12288, 3000, 0], 1000, 12, 64, 384
+    torch.manual_seed(11)
+    c = G.PagedCache.empty(4 * width, page, H, d, 4, width, quantised=e4m3)
+    c.table.copy_(torch.randperm(4 * width, device="cuda").view(4, width).int())
+    c.lengths.copy_(torch.tensor(lengths, dtype=torch.int32))
+    counts = c.lengths.clone()
+    kv = [torch.randn((4, 24000, H, d), device="cuda").to(torch.bfloat16) for _ in range(2)]
+    if left >= 0:
+        kv[0][0, 3500, 11] = kv[1][0, 3500, 11] = float("nan")
+    c.write(*kv, counts=counts)
+    held = c.read(24000)
+    q = torch.randn((4, n, H, d), device="cuda").to(torch.bfloat16)
+    desc = c._describe("bnhd", None)
+    assert G.B_.linattn_cache_workspace_bytes(desc, H, n) == 3 * 4 * H * n * (d + 2) * 4
+    out, lse = c.attend(q, left=left, sinks=sinks)
+    again, _ = c.attend(q, left=left, sinks=sinks)
+    torch.cuda.synchronize()
+    assert torch.equal(out.view(torch.int16), again.view(torch.int16))
+    rows = np.arange(0, n, 9)
+    for b, length in enumerate(lengths):
+        if length == 0:
+            assert (out[b] == 0).all() and torch.isneginf(lse[b]).all()
+            continue
+        pos = length - n + rows
+        ok = S.seen(pos, range(length), length, left, 0, sinks)
+        for h in (0, 11):
+            x = q[b, rows, h].double().cpu().numpy()
+            k, v = [t[b, :length, h].double().cpu().numpy() for t in held]
+            got, gl = out[b, rows, h].double().cpu().numpy(), lse[b, h, rows].double().cpu().numpy()
+            sound = np.ones(len(rows), bool)
+            if left >= 0 and b == 0 and h == 11:
+                sound = ~ok[:, 3500]
+                assert 5 < sound.sum() < 20 and np.isnan(got[~sound]).all() and np.isfinite(got[sound]).all()
+            args = (x[sound], k, v, ok[sound], d ** -0.5)
+            o, l, _ = S.forward(*args)
+            bo, bl = S.forward_bounds(*args, 2.0 ** -8)
+            over = np.abs(got[sound] - o) - bo - 2.0 ** -8 * np.abs(o)
+            assert (over <= 0).all(), (b, h, over.max())
+            assert (np.abs(gl[sound] - l) <= bl).all(), (b, h)
