@@ -340,7 +340,7 @@ __global__ __launch_bounds__(2 * key_block(D), 2) void window_dkv_kernel(BwdRows
     if (w < 2) {
       const int i = i0 + lane < len ? i0 + lane : len - 1;
       const float* from = (w == 0 ? a.nl : a.nd) + li + i;
-      asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" ::"s"(to + 2 * TILE + w * BT * 4), "v"(from) : "memory");
+      load_word_to_lds(from, to + 2 * TILE + w * BT * 4);
     }
   };
 

@@ -5,15 +5,21 @@
 namespace linattn {
 namespace attn {
 
-// 16 bytes a lane from global memory straight to LDS, at `lds` + 16 lane (lds uniform).  As assembly, because the compiler, which cannot tell the
-// buffer that is being filled from the one that is being read, waits for the builtin's loads before every LDS read.  The caller waits:
+// 16 (or 4) bytes a lane from global memory straight to LDS, at `lds` + 16 (4) lane (lds uniform).  As assembly, because the compiler, which cannot tell the
+// buffer that is being filled from the one that is being read, waits for the builtin's loads before every LDS read.  What it would do for the builtin is therefore done
+// here: m0, which holds the LDS address, has to be written one wait state before the load that uses it (the hardware does not hold the load back).  The caller waits:
 // lds_loads_landed() before the barrier that hands the tile over.
+#define LINATTN_LDS_LOAD(LOAD) "s_mov_b32 m0, %0\n\ts_nop 0\n\t" LOAD
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+  asm volatile(LINATTN_LDS_LOAD("global_load_lds_dwordx4 %1, %2") ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0");
 }
 __device__ __forceinline__ void load_to_lds(const void* at, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(at) : "memory");
+  asm volatile(LINATTN_LDS_LOAD("global_load_lds_dwordx4 %1, off") ::"s"(lds), "v"(at) : "memory", "m0");
 }
+__device__ __forceinline__ void load_word_to_lds(const void* at, uint32_t lds) {
+  asm volatile(LINATTN_LDS_LOAD("global_load_lds_dword %1, off") ::"s"(lds), "v"(at) : "memory", "m0");
+}
+#undef LINATTN_LDS_LOAD
 __device__ __forceinline__ void lds_loads_landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // Operands that a kernel loads before its loop.  The compiler has to see them arrive there: it would otherwise wait for them at their first use, in every turn of the
