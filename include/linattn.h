@@ -307,7 +307,8 @@ typedef struct linattn_cache_desc {
   const int* counts;      /* optional device [B]: new tokens of each sequence.  NULL: n */
 } linattn_cache_desc;
 
-/* Put the k and v rows of a chunk into the cache; nothing else in the pool changes.  No two tokens of a call may have the same place.
+/* Put the k and v rows of a chunk into the cache; nothing else in the pool changes.  No two tokens of a call may have the same place.  A token
+ * whose position is page * width or more, or whose table entry names no page, is dropped.
  * Errors: E_NULL, E_DTYPE, E_SHAPE, E_ALIGN, E_ALIAS, E_HIP. */
 int linattn_cache_write(const linattn_cache_desc* desc, const void* k, const void* v, int n, void* stream);
 

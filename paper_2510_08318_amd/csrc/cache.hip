@@ -58,8 +58,11 @@ __global__ __launch_bounds__(256) void cache_write_kernel(Pool p, const uint16_t
   const int part = threadIdx.x % LANES, b = blockIdx.y;
   const long long item = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
   const int t = (int)(HEADS_INNER ? item / p.HK : item % n), h = (int)(HEADS_INNER ? item % p.HK : item / n);
-  const int count = clamp_length(p.counts, b, n), j = pool_length(p, b) - count + t;
-  if (item >= (long long)n * p.HK || t >= count || j < 0) return;
+  const int count = clamp_length(p.counts, b, n), length = p.lengths[b];
+  if (item >= (long long)n * p.HK || t >= count) return;
+  // (places go by lengths as it is: a token past the table has none, and must not take an earlier one's)
+  const int j = (length < 0 ? 0 : length) - count + t;
+  if (j < 0) return;
   const long long row = pool_row(p, b, h, j);
   if (row < 0) return;
   const size_t at = (size_t)b * r.sb + (size_t)h * r.sh + (size_t)t * r.sn;

@@ -394,3 +394,25 @@ def test_long_parts_of_unlike_sequences(e4m3, d, left, sinks):
             over = np.abs(got[sound] - o) - bo - 2.0 ** -8 * np.abs(o)
             assert (over <= 0).all(), (b, h, over.max())
             assert (np.abs(gl[sound] - l) <= bl).all(), (b, h)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("layout", ["bhnd", "bnhd"])
+def test_writes_past_the_table_are_dropped(e4m3, layout):
+    """Chunks of five whose tokens lie past the table's 64 places in part or all: places go by lengths as they are, and no earlier row changes."""
+    import torch
+    page, H, d, n = 16, 2, 64, 5
+    c, _ = _filled([64] * 5, H, d, page, e4m3, layout, 3)
+    gen = torch.Generator().manual_seed(8)
+    x = [torch.randn((5, n, H, d), generator=gen).to(torch.bfloat16) for _ in range(2)]
+    lengths, counts = [65, 67, 69, 1000, 2 ** 31 - 1], [1, 5, 5, 5, 3]
+    before = [t.clone() for t in c.read(64)]
+    c.lengths.copy_(torch.tensor(lengths, dtype=torch.int32))
+    c.write(*[(t.transpose(1, 2) if layout == "bhnd" else t).contiguous().cuda() for t in x], counts=torch.tensor(counts, dtype=torch.int32, device="cuda"),
+            layout=layout)
+    after = c.read(64)
+    torch.cuda.synchronize()
+    for name in range(2):
+        want = before[name].double().cpu().numpy()
+        want[1, 62:] = _held(x[name][1, :2], e4m3)             # positions 62 .. 66 of the second sequence: two have a place
+        assert np.array_equal(after[name].double().cpu().numpy(), want)
