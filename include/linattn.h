@@ -241,7 +241,8 @@ int linattn_bwd(const void* q, const void* k, const void* v, const void* dout,
  * (a window of left tokens before and right tokens after it, and the first `sinks` tokens as far as they are not
  * beyond the window's right end; right = 0 is causal, a negative number is no limit).  A row that sees nothing has out = 0 and lse = -inf.
  * The conventions at the top of this file hold.  Numbers in device memory (lengths, counts, tables) cannot be checked on the host: the
- * kernels bring lengths and counts into range and take a table entry that names no page of the pool for keys that are not there.
+ * kernels take negative lengths and counts for 0, lengths of token tensors and counts beyond n for n, and keys that the table has no page of the pool
+ * for as not there.
  *
  * Numeric domain: scores, their softmax, and all sums are fp32.  LINATTN_BF16: the probabilities, and in the backward their gradients, enter the
  * matrix cores as bf16 (the stored type of the values they multiply, so that neither has a range of its own); with the store of the
@@ -292,7 +293,8 @@ int linattn_window_bwd(const linattn_window_desc* desc, const void* q, const voi
  * page's head lie together: the pools are [pages, H, page, d], the exponents [pages, H, page].
  * A chunk of n tokens per sequence (k, v of a write; q, out of an attention) is bf16 [B, H, n, d] or [B, n, H, d]; its token t has position
  * lengths[b] - counts[b] + t, and tokens from counts[b] on, or with a negative position, are padding: not read, not written
- * to the cache, their rows of out are zeros and of lse -inf.  lengths counts the chunk, before the write as after.
+ * to the cache, their rows of out are zeros and of lse -inf.  lengths counts the chunk, before the write as after.  A sequence may have outgrown
+ * its table: its tokens keep their positions (lengths up to 2^30), those from page * width on have no keys.
  */
 typedef struct linattn_cache_desc {
   int type;               /* LINATTN_CACHE_BF16 or LINATTN_CACHE_E4M3 */

@@ -8,8 +8,6 @@ namespace linattn {
 namespace attn {
 namespace {
 
-constexpr int kMostTokens = 1 << 30;
-
 bool misaligned(const void* p, uintptr_t to = 16) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);

@@ -8,14 +8,15 @@ namespace attn {
 
 // Which keys the query at position p sees of a sequence of `len` tokens: j < len, j <= p + right (right >= 0), and j >= p - left
 // (left >= 0) or j < sinks.  As ranges: the first tokens [0, first) and the window [lo, hi), first <= lo.
-// left, right: -1 (no limit) or below 2^30; positions below 2^30, so that the sums fit 32 bits.
+// left, right: -1 (no limit) or below kMostTokens, positions and lengths up to it, so that sums and differences fit 32 bits.
+constexpr int kMostTokens = 1 << 30;
 struct Sight {
   int left, right, sinks;
 };
 __host__ __device__ inline int key_lo(const Sight& s, int p) { return s.left < 0 || p < s.left ? 0 : p - s.left; }
-__host__ __device__ inline int key_hi(const Sight& s, int p, int len) { return s.right < 0 || p + s.right >= len ? len : p + s.right + 1; }
+__host__ __device__ inline int key_hi(const Sight& s, int p, int len) { return s.right < 0 || p >= len - s.right ? len : p + s.right + 1; }
 __host__ __device__ inline bool sees(const Sight& s, int p, int j, int len) {
-  return j < len && (s.right < 0 || j <= p + s.right) && (s.left < 0 || j >= p - s.left || j < s.sinks);
+  return j < len && (s.right < 0 || j - s.right <= p) && (s.left < 0 || j >= p - s.left || j < s.sinks);
 }
 // The queries that see key j: [query_lo, query_hi).
 __host__ __device__ inline int query_lo(const Sight& s, int j) { return s.right < 0 || j < s.right ? 0 : j - s.right; }
@@ -106,7 +107,9 @@ __device__ __forceinline__ long long pool_row(const Pool& p, int b, int h, int j
   if ((unsigned)at >= (unsigned)p.pages) return -1;
   return ((long long)at * p.HK + h) * p.page + (j - i * p.page);
 }
+// Tokens of sequence b that the table has places for, and, which positions go by, all that it counts.
 __device__ __forceinline__ int pool_length(const Pool& p, int b) { return clamp_length(p.lengths, b, p.width * p.page); }
+__device__ __forceinline__ int pool_tokens(const Pool& p, int b) { return clamp_length(p.lengths, b, kMostTokens); }
 
 // One call of linattn_cache_attn.
 struct CacheArgs {

@@ -56,11 +56,12 @@ struct KeysOfPool {
   using Args = Pool;
   static constexpr bool kE4M3 = E4M3;
   const Pool& p;
-  int b, hk, lane, len, count;
+  int b, hk, lane, len, tokens, count;
   PoolRows rows;
   unsigned long long there;
   __device__ __forceinline__ KeysOfPool(const Args& a, int b_, int hk_, int n, int lane_) : p(a), b(b_), hk(hk_), lane(lane_) {
     len = pool_length(p, b);
+    tokens = pool_tokens(p, b);
     count = clamp_length(p.counts, b, n);
   }
   template <int TK>
@@ -79,10 +80,10 @@ struct KeysOfTokens {
   static constexpr bool kE4M3 = false;
   const char *k, *v;
   size_t sn;
-  int len, count, j0, last;
+  int len, tokens, count, j0, last;
   static constexpr unsigned long long there = ~0ull;
   __device__ __forceinline__ KeysOfTokens(const Args& a, int b, int hk, int n, int) : sn(a.kr.sn) {
-    count = len = clamp_length(a.lengths, b, n);
+    count = tokens = len = clamp_length(a.lengths, b, n);
     const size_t at = ((size_t)b * a.kr.sb + (size_t)hk * a.kr.sh) * 2;
     k = static_cast<const char*>(a.k) + at;
     v = static_cast<const char*>(a.v) + at;
@@ -104,7 +105,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void attn_keys_kernel(RowsArgs a
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
   const int split = blockIdx.x % a.splits, row0 = blockIdx.x / a.splits * (32 * QB), b = blockIdx.y / a.HK, hk = blockIdx.y % a.HK, G = a.G;
   From src(from_args, b, hk, a.n, lane);
-  const int len = src.len, count = src.count, pos0 = len - count, t0 = pos0 < 0 ? -pos0 : 0, rows = count * G, all = a.n * G;
+  const int len = src.len, count = src.count, pos0 = src.tokens - count, t0 = pos0 < 0 ? -pos0 : 0, rows = count * G, all = a.n * G;
 
   uint4 q[QB][KS];
   int lo[QB], hi[QB];

@@ -217,7 +217,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attn_rows_kernel(RowsArgs a
   // token t has position pos0 + t; tokens t0 .. count - 1 have rows
   const int splits = Source::kPaged ? splits_of(a, src.len) : 1;
   if (split >= splits) return;
-  const int len = src.len, pos0 = len - src.count, t0 = pos0 < 0 ? -pos0 : 0, rows = src.count * G, all = a.n * G;
+  const int len = src.len, pos0 = src.tokens - src.count, t0 = pos0 < 0 ? -pos0 : 0, rows = src.count * G, all = a.n * G;
   const int row0 = block * BM + w * 32;
 
   // this lane's query

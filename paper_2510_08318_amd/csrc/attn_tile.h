@@ -81,7 +81,8 @@ constexpr int kRowWaves = 4;                 // wavefronts that fill a tile toge
 
 // Where a workgroup's keys come from.  look(j0, end): the tile of KT keys from j0 on (there is memory behind every key below end, of later ones the last is taken again) is
 // what the next ask_k and ask_v are for, which request its k or its v; put_k and put_v, before the next of them, bring what came through registers to LDS; landed() waits
-// for what goes there directly.  there: the keys of the tile that exist.
+// for what goes there directly.  there: the keys of the tile that exist.  len: the sequence's keys; tokens: its tokens, of which the last `count` are the chunk's (more
+// than len where a sequence has outgrown its table).
 struct TokenArgs {
   const void *k, *v;
   const int* lengths;
@@ -93,11 +94,11 @@ struct TokenSource {
   static constexpr bool kPaged = false;
   const char *k, *v;
   size_t sn;
-  int w, len, count, b, hk;
+  int w, len, tokens, count, b, hk;
   RowTile<D, kRowWaves, KT> rows;
   __device__ __forceinline__ TokenSource(const Args& a, int b_, int hk_, int n, int w_, int lane) : sn(a.kr.sn), w(w_), b(b_), hk(hk_), rows(w_, lane) {
     len = clamp_length(a.lengths, b, n);
-    count = len;
+    tokens = count = len;
     const size_t at = ((size_t)b * a.kr.sb + (size_t)hk * a.kr.sh) * 2;
     k = static_cast<const char*>(a.k) + at;
     v = static_cast<const char*>(a.v) + at;
@@ -121,13 +122,14 @@ struct PoolSource {
   static constexpr int NW = kRowWaves, LPR = D / (E4M3 ? 16 : 8), N = KT * LPR / (64 * NW);      // lanes to a row, instructions a wavefront
   static_assert(N >= 1, "whole instructions");
   const Pool& p;
-  int w, lane, len, count, b, hk;
+  int w, lane, len, tokens, count, b, hk;
   PoolRows at;
   unsigned long long there;
   uint4 ck[E4M3 ? N : 1], cv[E4M3 ? N : 1];
   uint32_t ek, ev;
   __device__ __forceinline__ PoolSource(const Args& a, int b_, int hk_, int n, int w_, int lane_) : p(a), w(w_), lane(lane_), b(b_), hk(hk_) {
     len = pool_length(p, b);
+    tokens = pool_tokens(p, b);
     count = clamp_length(p.counts, b, n);
   }
   __device__ __forceinline__ int row(int i) const { return (w * N + i) * (64 / LPR) + lane / LPR; }

@@ -416,3 +416,32 @@ def test_writes_past_the_table_are_dropped(e4m3, layout):
         want = before[name].double().cpu().numpy()
         want[1, 62:] = _held(x[name][1, :2], e4m3)             # positions 62 .. 66 of the second sequence: two have a place
         assert np.array_equal(after[name].double().cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("n", [1, 12, 100])
+@pytest.mark.parametrize("left,right,sinks", [(-1, 0, 0), (20, 0, 3), (20, 40, 0), (7, -1, 0)])
+def test_attention_past_the_table_goes_by_position(e4m3, n, left, right, sinks):
+    """Queries at positions past the 64 places of the table, some, most or all of a chunk: they see those of the 64 keys that their window still reaches."""
+    import torch
+    H, d, cap = 2, 64, 64
+    lengths = [70, 64 + 20 + 5, 64 + n, 500, 2 ** 30]
+    c, kv = _filled([cap] * 5, H, d, 16, e4m3, "bnhd", 3)
+    c.lengths.copy_(torch.tensor(lengths, dtype=torch.int32))
+    q = torch.randn((5, n, H, d), generator=torch.Generator().manual_seed(9)).to(torch.bfloat16)
+    out, lse = c.attend(q.cuda(), left=left, right=right, sinks=sinks)
+    torch.cuda.synchronize()
+    out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    for b in range(5):
+        pos = lengths[b] - n + np.arange(n)
+        ok = S.seen(pos, range(cap), cap, left, right, sinks)
+        ok[pos < 0] = False
+        for h in range(H):
+            x = np.where((pos >= 0)[:, None], q[b, :, h].double().numpy(), 0.0)
+            args = (x, _held(kv[0][b], e4m3)[:, h], _held(kv[1][b], e4m3)[:, h], ok, d ** -0.5)
+            o, l, _ = S.forward(*args)
+            bo, bl = S.forward_bounds(*args, 2.0 ** -8)
+            assert (np.abs(out[b, :, h] - o) <= bo + 2.0 ** -8 * np.abs(o)).all(), (b, h)
+            assert np.array_equal(np.isneginf(lse[b, h]), np.isneginf(l)), (b, h)
+            some = np.isfinite(l)
+            assert (np.abs(lse[b, h][some] - l[some]) <= bl[some]).all(), (b, h)
