@@ -281,30 +281,45 @@ def window_attention_backward(q, k, v, out, lse, dout, *, left=-1, right=-1, sin
     return dq, dk, dv
 
 
+def _cache_tensor(name):
+    """Attribute of a PagedCache for one of its tensors."""
+    return property(lambda self: self._tensors[name], lambda self, t: self._take({**self._tensors, name: t}))
+
+
 class PagedCache:
     """Keys and values of B sequences in pages of a pool (see linattn_cache_desc).  k, v: [pages, H, page, d], bfloat16 or float8_e4m3fn; k_exp,
     v_exp (float8 only): uint8 [pages, H, page]; table: int32 [B, width]; lengths: int32 [B].  The caller owns the tensors and writes table
-    and lengths: a chunk's tokens are counted in lengths before it is written or attended to."""
+    and lengths: a chunk's tokens are counted in lengths before it is written or attended to.  A tensor may be replaced by assigning to its attribute; the new one
+    is checked beside the others as here.  (A captured graph goes on using those of its capture.)"""
 
     def __init__(self, k, v, table, lengths, k_exp=None, v_exp=None):
+        self._take(dict(k=k, v=v, table=table, lengths=lengths, k_exp=k_exp, v_exp=v_exp))
+
+    def _take(self, tensors):
+        """Check the tensors and make them the cache's: their addresses go into the description that calls hand over."""
+        k, v, table, lengths, k_exp, v_exp = [tensors[name] for name in ("k", "v", "table", "lengths", "k_exp", "v_exp")]
+        for name in ("k", "v", "table", "lengths"):
+            _need(isinstance(tensors[name], torch.Tensor), f"{name}: a tensor")
         _need(k.dim() == 4 and k.dtype in (torch.bfloat16, torch.float8_e4m3fn), "k: a bf16 or float8_e4m3fn tensor [pages, H, page, d]")
         _need(table.dim() == 2, "table: [B, width]")
-        self.k, self.v, self.table, self.lengths, self.k_exp, self.v_exp = k, v, table, lengths, k_exp, v_exp
-        self.pages, self.H, self.page, self.d = k.shape
-        self.B, self.width = table.shape
-        self.index = k.get_device()
-        _need(self.index >= 0, "tensors must be on the GPU")
+        index = k.get_device()
+        _need(index >= 0, "tensors must be on the GPU")
         quantised = k.dtype == torch.float8_e4m3fn
         for name, t in (("k", k), ("v", v)):
-            _check_tokens(name, t, k.shape, k.dtype, self.index)
-        _check_ints("table", table, table.shape, self.index)
-        _check_ints("lengths", lengths, (self.B,), self.index)
+            _check_tokens(name, t, k.shape, k.dtype, index)
+        _check_ints("table", table, table.shape, index)
+        _check_ints("lengths", lengths, table.shape[:1], index)
         _need((k_exp is not None and v_exp is not None) == quantised, "k_exp and v_exp go with float8 rows")
         for name, t in (("k_exp", k_exp), ("v_exp", v_exp)):
             if t is not None:
-                _check_tokens(name, t, k.shape[:3], torch.uint8, self.index)
+                _check_tokens(name, t, k.shape[:3], torch.uint8, index)
+        self._tensors, self.index = tensors, index
+        self.pages, self.H, self.page, self.d = k.shape
+        self.B, self.width = table.shape
         self._desc = B_.CacheDesc(B_.CACHE_E4M3 if quantised else B_.CACHE_BF16, self.B, self.H, self.d, self.page, self.pages, self.width,
                                   0, *[B_._ptr(t) for t in (k, v, k_exp, v_exp, table, lengths)], None)
+
+    k, v, table, lengths, k_exp, v_exp = [_cache_tensor(name) for name in ("k", "v", "table", "lengths", "k_exp", "v_exp")]
 
     @classmethod
     def empty(cls, pages, page, H, d, B, width, *, quantised=False, device="cuda"):

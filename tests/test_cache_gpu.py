@@ -445,3 +445,51 @@ def test_attention_past_the_table_goes_by_position(e4m3, n, left, right, sinks):
             assert np.array_equal(np.isneginf(lse[b, h]), np.isneginf(l)), (b, h)
             some = np.isfinite(l)
             assert (np.abs(lse[b, h][some] - l[some]) <= bl[some]).all(), (b, h)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_assigned_tensors_are_the_ones_that_calls_use(e4m3):
+    """lengths, tables and pools that are replaced, not written in place; the old tensors stay alive here, so that nothing reads freed memory."""
+    import torch
+    c, _ = _filled([40, 64], 2, 64, 16, e4m3, "bnhd", 3)
+    q = torch.randn((2, 3, 2, 64), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).cuda()
+    old = [c.lengths, c.table, c.k, c.v, c.k_exp, c.v_exp]
+
+    def results():
+        res = [*c.read(64), *c.attend(q)]
+        torch.cuda.synchronize()
+        return res
+
+    def same(a, b):
+        return all(torch.equal(x, y) for x, y in zip(a, b))
+    first = results()
+    c.lengths = c.lengths - 5
+    got = results()
+    old[0].sub_(5)
+    c.lengths = old[0]
+    assert same(got, results()) and not same(got, first)
+    c.table = c.table.flip(0).contiguous()                     # sequences change places; the table of the second is full
+    c.lengths = c.lengths.flip(0).contiguous()
+    swapped = results()
+    assert torch.equal(swapped[0][0], got[0][1]) and torch.equal(swapped[1][1], got[1][0])
+    zeros = torch.zeros_like(c.v.view(torch.uint8)).view(c.v.dtype)
+    c.v = zeros
+    assert (results()[1] == 0).all() and torch.equal(results()[0], swapped[0])
+    c.v = old[3]
+    wide = torch.cat((c.table, torch.full_like(c.table, -1)), 1)
+    c.table = wide
+    assert c.width == 8 and same(swapped, results())
+
+
+def test_assigned_tensors_are_checked():
+    import torch
+    c, _ = _filled([40, 64], 2, 64, 16, True, "bnhd", 3)
+    bad = dict(lengths=[c.lengths.long(), c.lengths[:1], c.lengths.cpu(), None], table=[c.table.long(), c.table[:1], c.table[0], c.table.t(), None],
+               k=[c.k[:2], c.k.view(torch.uint8), None], v=[c.v[:, :, :8], c.v.to(torch.bfloat16)], k_exp=[None, c.k_exp.int()], v_exp=[c.v_exp[:1]])
+    for name, values in bad.items():
+        for value in values:
+            kept = getattr(c, name)
+            with pytest.raises((ValueError, AttributeError, TypeError)):
+                setattr(c, name, value)
+            assert getattr(c, name) is kept
+    assert torch.isfinite(c.read(40)[0]).all()
