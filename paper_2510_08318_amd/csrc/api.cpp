@@ -226,7 +226,7 @@ const char* linattn_strerror(int status) {
     case LINATTN_E_HIP: return "a HIP launch failed";
     case LINATTN_E_STATE: return "linattn_bwd needs the descriptor's state buffer, or the state buffer is too small for this batch size";
     case LINATTN_E_ALIAS: return "an output aliases an input";
-    case LINATTN_E_VALUE: return "a number is outside its range (sinks >= 0; scale finite and >= 0)";
+    case LINATTN_E_VALUE: return "a number is outside its range (sinks >= 0; scale 0 or 2^-100 to 2^100)";
     default: return "unknown status";
   }
 }

@@ -226,3 +226,12 @@ int main() {
     subprocess.run(["g++", "-std=c++17", "-O1", "-D__HIP_PLATFORM_AMD__", "-I", os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include"),
                     "-I", os.path.join(ROOT, "paper_2510_08318_amd", "csrc"), str(src), "-o", str(exe)], check=True)
     subprocess.run([str(exe)], check=True)
+
+
+def test_the_refusal_of_a_number_names_the_range_in_force():
+    """Of scales next to its ends, those that are refused lie outside what the message names."""
+    text = L.lib().linattn_strerror(L.E_VALUE).decode()
+    lo, hi = [2.0 ** int(x) for x in re.search(r"scale 0 or 2\^(-?\d+) to 2\^(-?\d+)", text).groups()]
+    assert "sinks >= 0" in text
+    for scale in (0.0, lo, hi, lo * 0.999, hi * 1.001, -lo, 1e-40, 3e38):
+        assert (L.linattn_window_workspace_bytes(_window(scale=scale)) > 0) == (scale == 0.0 or lo <= scale <= hi), scale
