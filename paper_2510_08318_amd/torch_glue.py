@@ -253,7 +253,8 @@ def window_attention(q, k, v, *, left=-1, right=-1, sinks=0, scale=0.0, layout="
     """Softmax attention in which token i sees tokens i - left .. i + right and the first `sinks` tokens (up to i + right); a negative
     limit is none, right=0 is causal.  q [B, H, n, d] ("bhnd") or [B, n, H, d] ("bnhd"); k, v with H or a divisor of H heads.
     lengths: int32 [B], the tokens of each item; the rest is padding.  scale: 0 for 1/sqrt(d).  f32_math: fp32 arithmetic on bf16 tensors.
-    Returns (out, lse); lse is fp32 [B, H, n]."""
+    Returns (out, lse); lse is fp32 [B, H, n].  Nothing is recorded for autograd, also where inputs require a gradient: window_attention_backward
+    gives it, and a torch.autograd.Function around the two has it recorded."""
     desc = _window_desc(q, k, v, left, right, sinks, scale, layout, lengths, f32_math)
     index = q.get_device()
     if out is None:
@@ -269,7 +270,8 @@ def window_attention(q, k, v, *, left=-1, right=-1, sinks=0, scale=0.0, layout="
 @_on_device_of
 def window_attention_backward(q, k, v, out, lse, dout, *, left=-1, right=-1, sinks=0, scale=0.0, layout="bhnd", lengths=None,
                               f32_math=False, dq=None, dk=None, dv=None):
-    """Gradients of window_attention (same keyword arguments) for the upstream gradient dout, from its out and lse."""
+    """Gradients (dq, dk, dv) of window_attention (same keyword arguments) for the upstream gradient dout, from its out and lse.  Nothing is recorded for
+    autograd."""
     desc = _window_desc(q, k, v, left, right, sinks, scale, layout, lengths, f32_math)
     index = q.get_device()
     dq, dk, dv = [torch.empty_like(t) if g is None else g for g, t in ((dq, q), (dk, k), (dv, v))]
@@ -337,7 +339,7 @@ class PagedCache:
     @_on_device_of
     def write(self, k, v, *, counts=None, layout="bnhd"):
         """Put a chunk's rows into the cache.  k, v: bf16 [B, n, H, d] or [B, H, n, d]; counts: int32 [B], the new tokens of each sequence
-        (None: n), at its positions lengths - counts, ..."""
+        (None: n), at its positions lengths - counts, ...; tokens past the table are dropped.  Nothing is recorded for autograd."""
         n = _token_dims(k, layout)[2]
         shape = _token_shape(self.B, self.H, n, self.d, layout)
         _check_tokens("k", k, shape, torch.bfloat16, self.index)
@@ -359,7 +361,7 @@ class PagedCache:
     def attend(self, q, *, counts=None, left=-1, right=0, sinks=0, scale=0.0, layout="bnhd", out=None, lse=None):
         """Attention of a chunk over the cache, which holds the chunk's own keys already (write).  q: bf16 [B, n, H, d] or [B, H, n, d] with a
         multiple of the cache's heads; left, right, sinks, scale as in window_attention, by position in the sequence.
-        Returns (out, lse); lse is fp32 [B, H, n]."""
+        Returns (out, lse); lse is fp32 [B, H, n].  Nothing is recorded for autograd, and there is no backward pass."""
         B, H, n, d = _token_dims(q, layout)
         _check_tokens("q", q, _token_shape(self.B, H, n, self.d, layout), torch.bfloat16, self.index)
         if out is None:

@@ -235,3 +235,10 @@ def test_the_refusal_of_a_number_names_the_range_in_force():
     assert "sinks >= 0" in text
     for scale in (0.0, lo, hi, lo * 0.999, hi * 1.001, -lo, 1e-40, 3e38):
         assert (L.linattn_window_workspace_bytes(_window(scale=scale)) > 0) == (scale == 0.0 or lo <= scale <= hi), scale
+
+
+def test_the_glue_says_that_autograd_records_nothing():
+    """Their results carry no gradient even where the inputs ask for one; a caller has to learn that from the documentation."""
+    from paper_2510_08318_amd import torch_glue as G
+    for f in (G.window_attention, G.window_attention_backward, G.PagedCache.write, G.PagedCache.attend):
+        assert "autograd" in f.__doc__, f.__name__

@@ -349,3 +349,30 @@ def test_inputs_made_on_another_stream():
             got, _ = G.window_attention(q, k2, v, left=100)
         torch.cuda.current_stream().wait_stream(side)
         assert torch.equal(want, got)
+
+
+def test_inputs_that_require_a_gradient():
+    """Nothing is recorded for autograd: the same results, without a gradient; a Function around the two calls has autograd give what the backward call does."""
+    import torch
+    from paper_2510_08318_amd import torch_glue as G
+    q, k, v, do = _make("bf16", 1, 2, 2, 100, 64, "bhnd", 3)
+    kw = dict(left=30, right=0)
+    out, lse = G.window_attention(q, k, v, **kw)
+    grads = G.window_attention_backward(q, k, v, out, lse, do, **kw)
+
+    class Recorded(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k, v):
+            out, lse = G.window_attention(q, k, v, **kw)
+            ctx.save_for_backward(q, k, v, out, lse)
+            return out
+
+        @staticmethod
+        def backward(ctx, dout):
+            return G.window_attention_backward(*ctx.saved_tensors, dout.contiguous(), **kw)
+    leaves = [t.clone().requires_grad_() for t in (q, k, v)]
+    got, _ = G.window_attention(*leaves, **kw)
+    assert torch.equal(got, out) and not got.requires_grad
+    Recorded.apply(*leaves).backward(do)
+    torch.cuda.synchronize()
+    assert all(torch.equal(t.grad, g) for t, g in zip(leaves, grads))
