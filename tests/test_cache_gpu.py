@@ -493,3 +493,33 @@ def test_assigned_tensors_are_checked():
                 setattr(c, name, value)
             assert getattr(c, name) is kept
     assert torch.isfinite(c.read(40)[0]).all()
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("layout", ["bhnd", "bnhd"])
+@pytest.mark.parametrize("n,left,right,sinks", [(100, 30, 0, 5), (70, 64, 20, 70), (150, -1, -1, 0), (90, 0, 0, 0)])
+def test_chunks_of_width_64(e4m3, layout, n, left, right, sinks):
+    _attend([200, 150, 301], [n, n - 9, 1], n, 4, 2, 64, 24, e4m3, left, right, sinks, layout)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [1, 20, 90])
+def test_sharp_scores_over_the_cache(e4m3, d, n):
+    """Scores up to a few hundred: most weights vanish, the running maximum moves a lot, and parts of a row differ in it by more than fp32's exponents hold."""
+    import torch
+    lengths, H, HK = [700, 300], 4, 2
+    c, kv = _filled(lengths, HK, d, 32, e4m3, "bnhd", 3)
+    q = (8 * torch.randn((2, n, H, d), generator=torch.Generator().manual_seed(4))).to(torch.bfloat16)
+    out, lse = c.attend(q.cuda(), left=600, sinks=2, scale=0.5)
+    torch.cuda.synchronize()
+    out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    for b, length in enumerate(lengths):
+        ok = S.seen(length - n + np.arange(n), range(length), length, 600, 0, 2)
+        for h in range(H):
+            k, v = [_held(rows[b], e4m3)[:, h // (H // HK)] for rows in kv]
+            args = (q[b, :, h].double().numpy(), k, v, ok, 0.5)
+            o, l, _ = S.forward(*args)
+            bo, bl = S.forward_bounds(*args, 2.0 ** -8)
+            assert (np.abs(out[b, :, h] - o) <= bo + 2.0 ** -8 * np.abs(o)).all(), (b, h)
+            assert (np.abs(lse[b, h] - l) <= bl).all(), (b, h)

@@ -376,3 +376,71 @@ def test_inputs_that_require_a_gradient():
     Recorded.apply(*leaves).backward(do)
     torch.cuda.synchronize()
     assert all(torch.equal(t.grad, g) for t, g in zip(leaves, grads))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("H,HK", [(4, 4), (8, 4), (8, 2)])
+def test_f32_blocks_of_their_own(H, HK, d):
+    """So many blocks of 32 rows that each has one workgroup, which stores its results itself; with eight heads on two, of the query side only.  A padded
+    item, whose padding holds NaN."""
+    lengths = [600, 333]
+
+    def edit(q, k, v, do):
+        for t in (q, k, v, do):
+            t[1, :, 333:] = float("nan")
+    _check("f32", 2, H, HK, 600, d, 100, 20, 5, lengths=lengths, edit=edit)
+
+
+def _check_out_of_sight(mode, B, H, HK, n, d, left, right, sinks, bad, value):
+    """Tokens `bad` hold `value` in q, k, v and dout: whatever does not depend on them is what it is without them, whatever does is not finite."""
+    import torch
+    from paper_2510_08318_amd import torch_glue as G
+    q, k, v, do = _make(mode, B, H, HK, n, d, "bhnd", 6)
+    hq, hk, hv, hd = [_host(x, "bhnd") for x in (q, k, v, do)]
+    for t in (q, k, v, do):
+        t[:, :, bad] = value
+    kw = dict(left=left, right=right, sinks=sinks, f32_math=mode == "f32math")
+    out, lse = G.window_attention(q, k, v, **kw)
+    grads = G.window_attention_backward(q, k, v, out, lse, do, **kw)
+    torch.cuda.synchronize()
+    got, lse = [_host(x, "bhnd") for x in (out, *grads)], G.to_host_f64(lse)
+    ok = S.seen(range(n), range(n), n, left, right, sinks)
+    rows = ~ok[:, bad].any(1)                  # rows that see no such token, and keys that only such rows see
+    keys = ~ok[~rows].any(0)
+    assert 40 < rows.sum() < n and 40 < keys.sum() < n
+    u, op = U[mode], OPERAND[mode]
+    for b in range(B):
+        sums = [np.zeros((HK, n, d)) for _ in range(4)]
+        for h in range(H):
+            g = h // (H // HK)
+            args, dout = (hq[b, h], hk[b, g], hv[b, g], ok, d ** -0.5), hd[b, h]
+            o, l, _ = S.forward(*args)
+            bo, bl = S.forward_bounds(*args, op)
+            _inside(f"out {b} {h}", got[0][b, h][rows], o[rows], (bo + u * np.abs(o))[rows])
+            _inside(f"lse {b} {h}", lse[b, h][rows], l[rows], bl[rows])
+            assert not np.isfinite(got[0][b, h][~rows]).all(-1).any()
+            grad, bound = S.backward(*args, dout), S.backward_bounds(*args, dout, op, u)
+            _inside(f"dq {b} {h}", got[1][b, h][rows], grad[0][rows], (bound[0] + u * np.abs(grad[0]))[rows])
+            for i, x in enumerate((grad[1], grad[2], bound[1], bound[2])):
+                sums[i][g] += x
+        for g in range(HK):
+            for i, name in enumerate(("dk", "dv")):
+                _inside(f"{name} {b} {g}", got[2 + i][b, g][keys], sums[i][g][keys], (sums[2 + i][g] + u * np.abs(sums[i][g]))[keys])
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("d", [64, 128])
+def test_tokens_out_of_sight_of_long_windows(mode, d, value):
+    """Windows of more than 256 keys, key blocks that several workgroups share, of first tokens and of the window: rows and keys next to tokens that they do not
+    see are done again from the stored output's row sums, and into the parts of a sum."""
+    _check_out_of_sight(mode, 1, 4, 2, 900, d, 300, 0, 0, slice(450, 453), value)
+    _check_out_of_sight(mode, 1, 4, 2, 900, d, 290, 30, 0, slice(560, 570), value)
+    _check_out_of_sight(mode, 1, 4, 2, 900, d, 300, 0, 70, slice(450, 453), value)
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("d", [64, 128])
+def test_f32_tokens_out_of_sight_of_many_blocks(d, value):
+    """As many blocks as have one workgroup each do such rows again themselves."""
+    _check_out_of_sight("f32", 2, 4, 4, 600, d, 90, 10, 0, slice(300, 304), value)
