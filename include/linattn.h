@@ -247,12 +247,13 @@ int linattn_bwd(const void* q, const void* k, const void* v, const void* dout,
  * Numeric domain: scores, their softmax, and all sums are fp32.  LINATTN_BF16: the probabilities, and in the backward their gradients, enter the
  * matrix cores as bf16 (the stored type of the values they multiply, so that neither has a range of its own); with the store of the
  * result that is two roundings of at most 2^-8 relative each (1.7e-3 rms each; the backward takes the row sums dout . out without the rounding of the stored
- * out).  LINATTN_F32 and LINATTN_BF16_F32MATH: fp32 arithmetic.  The results of a row depend on the keys that it sees and on nothing else: an infinity
+ * out).  The attention over a cache is that form; over LINATTN_CACHE_E4M3 the probabilities may take the scale of their row of v before they are rounded.
+ * LINATTN_F32 and LINATTN_BF16_F32MATH: fp32 arithmetic.  The results of a row depend on the keys that it sees and on nothing else: an infinity
  * or NaN in a token that it does not see, or in the padding, does not reach it (a row whose result is not finite is computed once more key by key, at 10 to 30 times
  * the usual time).  A row's sum of |v| times 2^8 has to stay below fp32's largest value; magnitudes below 2^-100 may count as zero. */
 typedef struct linattn_sight {
   int left, right, sinks;
-  float scale;            /* 2^-100 to 2^100; 0: 1 / sqrt(d) */
+  float scale;            /* 2^-100 to 2^100; 0: 1 / sqrt(d), as in Sec. 3 of the paper (Eq. 6 writes 1 / d for its softmax term) */
 } linattn_sight;
 
 /* q, out, dout, dq: H heads; k, v, dk, dv: HK heads; all of n tokens, in `layout`.  Token i of a batch item has position i. */

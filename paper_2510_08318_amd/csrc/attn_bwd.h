@@ -26,11 +26,16 @@ struct BwdRows {
 };
 
 // ---- dq -----------------------------------------------------------------------------------
-// Queries on the lanes, as in the forward: S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T.  12 heads x 32760 x 128, window 2 x 1560 and 1560 first tokens: 1.40 ms, 970
-// TFLOP/s; the matrix cores are busy 48 % of the cycles, a quarter of a wavefront's time goes to waits.
+// Queries on the lanes, as in the forward: S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T.  12 heads x 32760 x 128, window 2 x 1560 and 1560 first tokens: 1.40 to 1.43 ms,
+// 950 to 970 TFLOP/s; the matrix cores are busy 49 % of the cycles, a quarter of a wavefront's time goes to waits.  Width 64, 2 x 12 heads of unlike lengths to 4133, causal,
+// window 1024: 75 us; the matrix cores are busy 15 % of the cycles, with 1.35 wavefronts to a SIMD on average over the kernel.
+// dS is rounded to bf16, as K is stored (PIECES 1): the error of dq that this and the store leave is 2.35e-3.
 // EXACT: delta from a first pass over the keys, sum_j p_ij dp_ij, and not from dout . out.  Where a row sees few keys its output is as large as the
 // values, and the rounding of the stored output would be the largest error of dq and dk.  With fp32 arithmetic (PIECES 3) always.
-constexpr float kHeavyWeight = 0.125f;      // (see window_dq_kernel)
+// A key counts as a row's heaviest only with more weight than this.  Error of dq (2-norm over two heads, 1e-3), without the correction / above 1/2 / 1/8 / 1/32: 12 heads x 4133 x 64
+// causal 2.75 / 2.59 / 2.50 / 2.49, with scores nine times as large 4.56 / 2.84 / 2.64 / 2.64; window 1024 2.51 / 2.47 / 2.43 / 2.42 and 5.50 / 2.76 / 2.64 / 2.64; 600 x 64, all keys,
+// 2.49 / 2.49 / 2.41 / 2.40 and 4.95 / 2.67 / 2.55 / 2.55.  Us of the backward there: 229 / 227 / 229 / 235, 115 / 115 / 116 / 121, 39 / 39 / 41 / 43.
+constexpr float kHeavyWeight = 0.125f;
 
 template <int D, bool EXACT, int PIECES>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void window_dq_kernel(BwdRows a) {
@@ -278,7 +283,8 @@ __device__ __forceinline__ KeyShare key_share(const BwdRows& a, int id) {
 }
 
 // Keys on the lanes: S = Q K^T, dP = dO V^T with queries on the accumulator rows, started from -lse / scale and -delta, so that p = exp2(scale2 S)
-// and dS = p dP; dV^T += dO^T P, dK^T += Q^T dS with P and dS as they lie.  12 heads x 32760 x 128, window 2 x 1560 and 1560 first tokens: 2.0 ms, 900 TFLOP/s; the
+// and dS = p dP; dV^T += dO^T P, dK^T += Q^T dS with P and dS as they lie (rounded to bf16, as Q and dO are stored: PIECES 1).  12 heads x 32760 x 128, window 2 x 1560 and
+// 1560 first tokens: 2.0 ms, 900 TFLOP/s; the
 // matrix cores are busy 45 % of the cycles, a third of a wavefront's time goes to waits (every operand is read from LDS, 40 KB for the four products of 32 x 32).
 // Width 128: eight wavefronts, k in LDS.  With k and v in registers beside the 128 of the sums, a lane needs more than the 256 that two wavefronts to a SIMD
 // leave it.

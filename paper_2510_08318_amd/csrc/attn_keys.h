@@ -1,7 +1,8 @@
 // Attention with the keys, not the rows, dealt to a workgroup's wavefronts: of few rows (a token or some, with the heads of their group) over a paged cache, which is
 // bound by reading the cache once, and of short sequences, of which blocks of 128 rows would leave most of the chip empty.  A wavefront has tiles of its own in LDS and no barrier in its loop; the next tile is on its way while one is worked
 // on, 32 KB a wavefront and 64 KB in flight for a compute unit.  Codes stay codes in LDS (half the bytes) and become bf16 where the operand is made.
-// One token of 32 sequences up to 16384 tokens, 32 / 8 heads of 128, bf16: 291 us = 5.2 TB/s, where a copy reaches 4.85; one of 2000 tokens, e4m3: 10 us, latency.
+// One token of 32 sequences up to 16384 tokens, 32 / 8 heads of 128: bf16 291 us = 5.2 TB/s, e4m3 159 us = 4.8 (a kernel that only reads, non-temporally, reaches 6.5 to
+// 7.2 on different machines, with plain loads 6.1); one of 2000 tokens, e4m3: 10 us, latency.
 #pragma once
 #include "attn_rows.h"
 
@@ -197,7 +198,8 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void attn_keys_kernel(RowsArgs a
       }
       softmax_step<KB, CB>(s[i], a.scale2, mx[i], l[i], o[i]);
       if constexpr (E4M3) {
-        // the codes of v enter as they are: their scales go to the weights
+        // The codes of v enter as they are: their scales go to the weights, before those are rounded to bf16.  The scales are powers of two, so that the
+        // rounding is the same relative one as of the weights alone.
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll

@@ -120,7 +120,8 @@ __device__ __forceinline__ uint4 pack8(const f32x16& e, int h) {
                     pack_bf16x2(e[8 * h + 6], e[8 * h + 7]));
 }
 
-// The operand of weights e[8h .. 8h+7]: PIECES of 1 rounds them to bf16, 3 hands them on whole, as the exact sum of three bf16 numbers (LINATTN_BF16_F32MATH: the other
+// The operand of weights e[8h .. 8h+7]: PIECES of 1 rounds them to bf16, as the values that they multiply are stored (an error of the result like that of its store,
+// 1.66e-3 in 2-norm each; sums of weights are taken before), 3 hands them on whole, as the exact sum of three bf16 numbers (LINATTN_BF16_F32MATH: the other
 // operand of their product is bf16, so three products give it in fp32).
 template <int PIECES>
 __device__ __forceinline__ void weights_operand(const f32x16& e, int h, uint4 (&p)[PIECES]) {
@@ -198,7 +199,7 @@ __device__ void plain_again(const RowsArgs& a, const Keys& keys, const Tiles& ti
 // the lane, and its weights lie as the right operand of O^T += V^T P^T wants them; V^T comes from transposing LDS reads.  A wavefront has 32 rows and a workgroup four
 // of them, so that two workgroups fit a compute unit: with 64 rows a wavefront LDS is read half as much, but one wavefront to a SIMD leaves nothing to hide its reads
 // (2214 us in place of 1607 at 12 heads x 32760 x 128, window 2 x 3120, 1560 first tokens; 32 keys to a tile 1666, eight wavefronts to a workgroup 1619).
-// There, as built: 1.51 to 1.56 ms on different machines, 940 to 980 TFLOP/s of the 1310 that a large matrix product reaches.  The matrix cores are busy 49 % of the
+// There, as built: 1.41 to 1.56 ms on different machines, 940 to 1040 TFLOP/s of the 1310 to 1350 that a large matrix product reaches.  The matrix cores are busy 49 % of the
 // cycles, a third of a wavefront's time goes to waits for LDS and for the tile's barrier, and the power limit takes the clock to 1.9 GHz; without its LDS reads and loads
 // the kernel reaches 1230, without the softmax 1070.
 // Two tiles in LDS and one barrier a tile.  (With a second barrier, between the scores and the product with v, a buffer can be asked for half a tile earlier; but then
