@@ -167,6 +167,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void attn_keys_kernel(RowsArgs a
       request(it + NW, lds + (uint32_t)(buf ^ 1) * 2 * T::BYTES);
       if (it + 2 * NW < it1) look(it + 2 * NW);
     }
+    if (there == 0) continue;
     const int j0 = tiles.start(it);
     const bool plain = sight.everything(j0, TK) && there == ~0ull;
     f32x16 s[QB][KB];

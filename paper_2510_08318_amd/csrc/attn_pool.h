@@ -54,11 +54,13 @@ struct PoolKeys {
   __device__ __forceinline__ float v1(int j, int c) const { return row1(pool->v, pool->v_exp, j, c); }
 };
 
-// The pool's rows of a tile's keys, lane by lane (key j0 + lane, the last key again from `end` on): a row, and which keys have one.
+// The pool's rows of a tile's keys, lane by lane (key j0 + lane, the last key again from `end` on): a row, and which keys have one.  A key without a page takes the row of
+// the tile's first key that has one: its weight is 0, and 0 times an infinity or NaN in some other sequence's row, or in one that was never written, would have
+// the queries' rows done again key by key.  (A tile in which no key has a page is not looked at.)
 // The table is read through the scalar cache, an entry at a time (a tile has two pages at most where they are no smaller): a vector load's answer could not be
 // waited for without all the loads that were asked for before it, a tile that is on its way among them.
 struct PoolRows {
-  long long row;           // of this lane's key, row 0 where there is none
+  long long row;           // of this lane's key
   unsigned long long there;
   template <int KT>
   __device__ __forceinline__ void find(const Pool& p, int b, int h, int j0, int end, int lane) {
@@ -74,6 +76,10 @@ struct PoolRows {
     const bool ok = (unsigned)entry < (unsigned)p.pages;
     there = __ballot(ok);
     row = ok ? ((long long)entry * p.HK + h) * p.page + (j - mine * p.page) : 0;
+    if (there != ~0ull && there != 0) {
+      const long long other = of(__ffsll(there) - 1);
+      row = ok ? row : other;
+    }
   }
   __device__ __forceinline__ long long of(int i) const {
     return (long long)((unsigned long long)(uint32_t)__shfl((int)row, i) | (unsigned long long)(uint32_t)__shfl((int)(row >> 32), i) << 32);

@@ -267,7 +267,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attn_rows_kernel(RowsArgs a
       if (it + 2 < it1) look(it + 2);
     }
     const int j0 = tiles.start(order(it));
-    if (!sight.nothing(j0, KT)) {
+    if (!sight.nothing(j0, KT) && (!Source::kPaged || there != 0)) {
       const uint32_t kt = ktile(it), vt = kt + TILE;
       f32x16 s[KB];
 #pragma unroll

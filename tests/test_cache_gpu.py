@@ -523,3 +523,33 @@ def test_sharp_scores_over_the_cache(e4m3, d, n):
             bo, bl = S.forward_bounds(*args, 2.0 ** -8)
             assert (np.abs(out[b, :, h] - o) <= bo + 2.0 ** -8 * np.abs(o)).all(), (b, h)
             assert (np.abs(lse[b, h] - l) <= bl).all(), (b, h)
+
+
+@pytest.mark.parametrize("n", [1, 40])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_pages_that_no_table_names_do_not_matter(e4m3, d, n):
+    """A window whose earlier pages have been given back, and a table with a tile's worth of holes: bit for bit the same whatever the first page of the pool,
+    which belongs to no sequence, holds."""
+    import torch
+    from paper_2510_08318_amd import torch_glue as G
+    H, page, width, length = 2, 16, 12, 180
+    gen = torch.Generator().manual_seed(5)
+    c = G.PagedCache.empty(2 * width + 1, page, H, d, 2, width, quantised=e4m3)
+    c.table.copy_(1 + torch.randperm(2 * width, generator=gen).view(2, width).int())
+    c.lengths.fill_(length)
+    k, v, q = [torch.randn((2, m, H, d), generator=gen).to(torch.bfloat16).cuda() for m in (length, length, n)]
+    c.write(k, v)
+    c.table[0, : (length - n - 30) // page] = -1               # what no query's window of 30 reaches
+    c.table[1, 4:8] = c.pages                                  # keys 64 .. 127
+    res = []
+    for byte in (0, 0xff):
+        for t in (c.k, c.v, c.k_exp, c.v_exp):
+            if t is not None:
+                t[0].view(torch.uint8).fill_(byte)
+        res.append([*c.attend(q, left=30), *c.attend(q)])
+    torch.cuda.synchronize()
+    for i in (0, 1):                                           # (of the sequence without its first pages only the window)
+        assert torch.isfinite(res[0][i]).all()
+    for a, b in zip(*res):
+        assert torch.equal(a, b)
