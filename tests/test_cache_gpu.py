@@ -432,13 +432,14 @@ def test_attention_past_the_table_goes_by_position(e4m3, n, left, right, sinks):
     out, lse = c.attend(q.cuda(), left=left, right=right, sinks=sinks)
     torch.cuda.synchronize()
     out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    held = [[_held(x, e4m3) for x in rows] for rows in kv]
     for b in range(5):
         pos = lengths[b] - n + np.arange(n)
         ok = S.seen(pos, range(cap), cap, left, right, sinks)
         ok[pos < 0] = False
         for h in range(H):
             x = np.where((pos >= 0)[:, None], q[b, :, h].double().numpy(), 0.0)
-            args = (x, _held(kv[0][b], e4m3)[:, h], _held(kv[1][b], e4m3)[:, h], ok, d ** -0.5)
+            args = (x, held[0][b][:, h], held[1][b][:, h], ok, d ** -0.5)
             o, l, _ = S.forward(*args)
             bo, bl = S.forward_bounds(*args, 2.0 ** -8)
             assert (np.abs(out[b, :, h] - o) <= bo + 2.0 ** -8 * np.abs(o)).all(), (b, h)
@@ -516,9 +517,10 @@ def test_sharp_scores_over_the_cache(e4m3, d, n):
     out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
     for b, length in enumerate(lengths):
         ok = S.seen(length - n + np.arange(n), range(length), length, 600, 0, 2)
+        k, v = [_held(rows[b], e4m3) for rows in kv]
         for h in range(H):
-            k, v = [_held(rows[b], e4m3)[:, h // (H // HK)] for rows in kv]
-            args = (q[b, :, h].double().numpy(), k, v, ok, 0.5)
+            g = h // (H // HK)
+            args = (q[b, :, h].double().numpy(), k[:, g], v[:, g], ok, 0.5)
             o, l, _ = S.forward(*args)
             bo, bl = S.forward_bounds(*args, 2.0 ** -8)
             assert (np.abs(out[b, :, h] - o) <= bo + 2.0 ** -8 * np.abs(o)).all(), (b, h)
