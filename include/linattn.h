@@ -88,7 +88,7 @@ extern "C" {
 #define LINATTN_E_HIP        -7   /* a HIP launch reported an error */
 #define LINATTN_E_STATE      -8   /* linattn_bwd without a state buffer, or a state buffer too small for this B */
 #define LINATTN_E_ALIAS      -9   /* an output aliases an input */
-#define LINATTN_E_VALUE     -10   /* a number is outside its range (linattn_sight) */
+#define LINATTN_E_VALUE     -10   /* a number is outside its range (linattn_sight, linattn_rotary_desc, linattn_decay_desc) */
 
 /* feature-map kinds */
 #define LINATTN_PHI_HEDGEHOG  1   /* Eq. 5 */
@@ -328,6 +328,84 @@ size_t linattn_cache_workspace_bytes(const linattn_cache_desc* desc, int H, int 
  * Errors: as above, E_VALUE, E_WORKSPACE. */
 int linattn_cache_attn(const linattn_cache_desc* desc, const linattn_sight* sight, const void* q, void* out, float* lse, int H, int n,
                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Rotary positions: what q and k carry before either branch sees them.  Each of up to three axes (frame, row, column; or one, a text's) has dims
+ * channels of a row, axis after axis from channel 0 on; channels behind the last axis stay as they are.  Pair m of an axis' dims / 2 is turned by the token's
+ * position along it,
+ *
+ *   y1 = x1 cos t - x2 sin t,   y2 = x1 sin t + x2 cos t,   t = position base^(-2m / dims)
+ *
+ * All heads of a token are turned alike.  The inverse turns by -t; it is also the gradient: of y with respect to x, for an upstream gradient in y's place.
+ * Angles are reduced in fp64, sines, cosines and products are fp32, and the result is rounded once.  The conventions at the top of this file hold. */
+#define LINATTN_PAIRS_ADJACENT 0   /* pair m of an axis from channel c on: channels c + 2m, c + 2m + 1 */
+#define LINATTN_PAIRS_HALVES   1   /* channels c + m, c + m + dims / 2 */
+
+typedef struct linattn_rotary_desc {
+  int dtype;              /* LINATTN_BF16 (LINATTN_BF16_F32MATH is the same here) or LINATTN_F32 */
+  int B, H, HK, n, d;     /* heads of q and of k, any numbers (HK is not looked at without k); d 64 or 128 */
+  int layout;
+  int axes;               /* 1 to 3 */
+  int dims[3];            /* channels of each axis: even, together at most d */
+  int pairs;              /* LINATTN_PAIRS_ADJACENT or LINATTN_PAIRS_HALVES */
+  int inverse;            /* not 0: by -t */
+  double base;            /* 1 to 2^60; 0: 10000 */
+  int grid[3];            /* tokens along each axis, the last fastest: token i has the coordinates of i in the grid (the first is not looked at, and
+                             has no end), plus */
+  int first[3];           /* these */
+  const int* positions;   /* optional device [position_items, n, axes], in place of grid and first */
+  int position_items;     /* 1 (the same for all items) or B */
+  const int* lengths;     /* optional device [B]: tokens of each item.  Padding is not read; its rows of the results are zeros.  NULL: n each. */
+} linattn_rotary_desc;
+
+/* q_out = turned q, k_out = turned k; k and k_out may both be NULL.  In place: q_out == q, k_out == k; no other overlap.
+ * Errors: E_NULL, E_DTYPE, E_SHAPE, E_VALUE, E_ALIGN, E_ALIAS, E_HIP. */
+int linattn_rotary(const linattn_rotary_desc* desc, const void* q, const void* k, void* q_out, void* k_out, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Linear attention with an order: token t sees the tokens up to itself, each with a weight that falls with the distance, by a constant decay for each head,
+ * lambda = exp(log_decay).  What has passed is held in a state of d x d numbers a head, so sequences can be taken piece by piece, or token by token.
+ *
+ *   S_t = lambda S_{t-1} + k_t v_t^T,   o_t = scale q_t S_t,      that is   o_t = scale (lambda^(t+1) q_t S_in + sum_{j <= t} lambda^(t-j) (q_t . k_j) v_j)
+ *
+ * with no feature map and no denominator (a map of q and k, and a norm of o, are the caller's).  H query heads share HK key heads as in
+ * linattn_window_fwd; every query head has its own decay and state.  The decay is a constant of the layer: there is no gradient for it.
+ *
+ * Numeric domain: states and sums are fp32, and so are all weights lambda^r.  LINATTN_BF16: the products (q . k) lambda^r, the rows k_j or v_j times their weight and the
+ * state's entries enter the matrix cores as bf16 where they make a row of out, dq, dk or dv, with fp32 sums (a rounding of at most 2^-8 relative to the factor each); states
+ * that are handed out (state_out, dstate_in) are products and sums in fp32.  LINATTN_F32, LINATTN_BF16_F32MATH: fp32 arithmetic throughout.  Of a sequence's tokens a row
+ * depends on those that it sees alone: an infinity or NaN in a later token (earlier, for dk and dv), or in the padding, does not reach it.  Magnitudes below 2^-100 may
+ * count as zero. */
+typedef struct linattn_decay_desc {
+  int dtype;              /* LINATTN_BF16, LINATTN_F32 or LINATTN_BF16_F32MATH: type of q, k, v, out, dout, dq, dk, dv */
+  int B, H, HK, n, d;     /* H a multiple of HK, d 64 or 128 */
+  int layout;
+  float scale;            /* 2^-100 to 2^100; 0: 1 / sqrt(d) */
+  const float* log_decay; /* device [H], at most 0 (what is above, or NaN, counts as 0; -inf: a token sees itself alone) */
+  const int* lengths;     /* optional device [B]: tokens of each item, the others are padding.  Padding is not read; its rows of out, dq, dk, dv are zeros, and
+                             state_out is the state behind the last token.  NULL: n each */
+  const int* slots;       /* optional device [B]: the state of item b is row slots[b] of state_in and state_out.  Outside 0 .. states-1 it has none: zeros are read,
+                             nothing is written.  No two items of a call may have the same row, if it writes states.  NULL: row b */
+  int states;             /* with slots: rows of the state tensors */
+  void* workspace;        /* device scratch, 256-byte aligned, not shared by calls that overlap in time */
+  size_t workspace_bytes;
+} linattn_decay_desc;
+
+/* Scratch bytes of a workspace for linattn_decay_fwd (backward = 0) or linattn_decay_bwd.  Pure function of the descriptor's numbers; 0 for an invalid one, and
+ * where none is needed (the workspace may then be NULL). */
+size_t linattn_decay_workspace_bytes(const linattn_decay_desc* desc, int backward);
+
+/* Forward.  state_in, state_out: optional device fp32 [B or states, H, d, d], rows the channels of k, columns those of v; NULL: zeros, not wanted.  They may be the same
+ * tensor.  n = 1 is the step of generation token by token.
+ * Errors: E_NULL, E_DTYPE, E_SHAPE, E_VALUE, E_ALIGN, E_WORKSPACE, E_ALIAS, E_HIP. */
+int linattn_decay_fwd(const linattn_decay_desc* desc, const void* q, const void* k, const void* v, const float* state_in, void* out, float* state_out,
+                      void* stream);
+
+/* Backward for L with dL/dout = dout and dL/dstate_out = dstate_out; writes dq, dk, dv (dk and dv summed over the query heads of a group) and dstate_in = dL/dstate_in.
+ * state_in: the forward's.  dstate_out, dstate_in: optional device fp32 [B, H, d, d], by item also where the forward went by slots.
+ * Errors: as above. */
+int linattn_decay_bwd(const linattn_decay_desc* desc, const void* q, const void* k, const void* v, const float* state_in, const void* dout,
+                      const float* dstate_out, void* dq, void* dk, void* dv, float* dstate_in, void* stream);
 
 /* Static description of a status code. */
 const char* linattn_strerror(int status);

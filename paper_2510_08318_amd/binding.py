@@ -20,11 +20,13 @@ BF16, F32, BF16_F32MATH = 1, 2, 3
 LAYOUT_BHND, LAYOUT_BNHD = 0, 1
 FLAG_CENTRED = 1
 CACHE_BF16, CACHE_E4M3 = 1, 2
+PAIRS_ADJACENT, PAIRS_HALVES = 0, 1
 
 EXPORTS = ("linattn_phi_create", "linattn_phi_destroy", "linattn_workspace_bytes", "linattn_workspace_bytes_wgrads",
            "linattn_fwd", "linattn_fwd_noalloc", "linattn_bwd", "linattn_strerror", "linattn_set_stage_events", "linattn_phi_set_blend",
            "linattn_window_workspace_bytes", "linattn_window_fwd", "linattn_window_bwd",
-           "linattn_cache_workspace_bytes", "linattn_cache_write", "linattn_cache_read", "linattn_cache_attn")
+           "linattn_cache_workspace_bytes", "linattn_cache_write", "linattn_cache_read", "linattn_cache_attn",
+           "linattn_rotary", "linattn_decay_workspace_bytes", "linattn_decay_fwd", "linattn_decay_bwd")
 
 
 class PhiDesc(ctypes.Structure):
@@ -59,6 +61,23 @@ class CacheDesc(ctypes.Structure):
         ("width", ctypes.c_int), ("layout", ctypes.c_int), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
         ("k_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p), ("table", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
         ("counts", ctypes.c_void_p),
+    ]
+
+
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int), ("B", ctypes.c_int), ("H", ctypes.c_int), ("HK", ctypes.c_int), ("n", ctypes.c_int), ("d", ctypes.c_int),
+        ("layout", ctypes.c_int), ("axes", ctypes.c_int), ("dims", ctypes.c_int * 3), ("pairs", ctypes.c_int), ("inverse", ctypes.c_int),
+        ("base", ctypes.c_double), ("grid", ctypes.c_int * 3), ("first", ctypes.c_int * 3), ("positions", ctypes.c_void_p),
+        ("position_items", ctypes.c_int), ("lengths", ctypes.c_void_p),
+    ]
+
+
+class DecayDesc(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int), ("B", ctypes.c_int), ("H", ctypes.c_int), ("HK", ctypes.c_int), ("n", ctypes.c_int), ("d", ctypes.c_int),
+        ("layout", ctypes.c_int), ("scale", ctypes.c_float), ("log_decay", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
+        ("slots", ctypes.c_void_p), ("states", ctypes.c_int), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
     ]
 
 
@@ -112,6 +131,15 @@ def lib() -> ctypes.CDLL:
         L.linattn_cache_read.restype = ci
         L.linattn_cache_attn.argtypes = [cd, ctypes.POINTER(Sight), vp, vp, vp, ci, ci, vp, ctypes.c_size_t, vp]
         L.linattn_cache_attn.restype = ci
+        dd = ctypes.POINTER(DecayDesc)
+        L.linattn_rotary.argtypes = [ctypes.POINTER(RotaryDesc)] + [vp] * 5
+        L.linattn_rotary.restype = ci
+        L.linattn_decay_workspace_bytes.argtypes = [dd, ci]
+        L.linattn_decay_workspace_bytes.restype = ctypes.c_size_t
+        L.linattn_decay_fwd.argtypes = [dd] + [vp] * 7
+        L.linattn_decay_fwd.restype = ci
+        L.linattn_decay_bwd.argtypes = [dd] + [vp] * 11
+        L.linattn_decay_bwd.restype = ci
         L.linattn_strerror.argtypes = [ci]
         L.linattn_strerror.restype = ctypes.c_char_p
         _lib = L
@@ -234,6 +262,24 @@ def linattn_cache_attn(desc, sight, q, out, lse, H: int, n: int, workspace=None,
                        check: bool = True) -> int:
     return _done(lib().linattn_cache_attn(_ref(desc), _ref(sight), _ptr(q), _ptr(out), _ptr(lse), H, n, _ptr(workspace),
                                           workspace_bytes, _ptr(stream)), "linattn_cache_attn", check)
+
+
+def linattn_rotary(desc, q, k, q_out, k_out, stream=None, *, check: bool = True) -> int:
+    return _done(lib().linattn_rotary(_ref(desc), _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), _ptr(stream)), "linattn_rotary", check)
+
+
+def linattn_decay_workspace_bytes(desc, backward: bool = False) -> int:
+    return int(lib().linattn_decay_workspace_bytes(_ref(desc), int(backward)))
+
+
+def linattn_decay_fwd(desc, q, k, v, state_in, out, state_out=None, stream=None, *, check: bool = True) -> int:
+    return _done(lib().linattn_decay_fwd(_ref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(state_in), _ptr(out), _ptr(state_out), _ptr(stream)),
+                 "linattn_decay_fwd", check)
+
+
+def linattn_decay_bwd(desc, q, k, v, state_in, dout, dstate_out, dq, dk, dv, dstate_in=None, stream=None, *, check: bool = True) -> int:
+    return _done(lib().linattn_decay_bwd(_ref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(state_in), _ptr(dout), _ptr(dstate_out), _ptr(dq), _ptr(dk),
+                                         _ptr(dv), _ptr(dstate_in), _ptr(stream)), "linattn_decay_bwd", check)
 
 
 def linattn_set_stage_events(events) -> int:

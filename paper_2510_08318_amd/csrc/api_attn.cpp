@@ -1,6 +1,7 @@
 // Host side of linattn_window_* and linattn_cache_*: argument checks (all of them before the first HIP call) and dispatch.
 #include "../../include/linattn.h"
 #include "attn.h"
+#include "checks.h"
 
 #include <cmath>
 
@@ -8,16 +9,9 @@ namespace linattn {
 namespace attn {
 namespace {
 
-bool misaligned(const void* p, uintptr_t to = 16) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
-bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return a && b && x < y + nb && y < x + na;
-}
+using namespace checks;
 
-Rows rows_of(int H, int n, int d, int layout) {
-  if (layout == LINATTN_LAYOUT_BHND) return Rows{(size_t)H * n * d, (size_t)n * d, (size_t)d};
-  return Rows{(size_t)n * H * d, (size_t)d, (size_t)H * d};
-}
+Rows rows_of(int H, int n, int d, int layout) { return token_rows(H, n, d, layout == LINATTN_LAYOUT_BHND); }
 
 int check_sight(const linattn_sight& s, int d, Sight* sight, float* scale) {
   // (the backward starts its scores from -lse / scale)
@@ -65,22 +59,6 @@ int check_window(const linattn_window_desc* w, WindowArgs* a, WindowSizes* z) {
   return LINATTN_OK;
 }
 
-// Whether one of `outs` overlaps another or one of `ins`.
-struct Region {
-  const void* p;
-  size_t bytes;
-};
-template <int NO, int NI>
-bool any_overlap(const Region (&outs)[NO], const Region (&ins)[NI]) {
-  for (int i = 0; i < NO; ++i) {
-    for (const Region& in : ins)
-      if (overlaps(outs[i].p, outs[i].bytes, in.p, in.bytes)) return true;
-    for (int j = i + 1; j < NO; ++j)
-      if (overlaps(outs[i].p, outs[i].bytes, outs[j].p, outs[j].bytes)) return true;
-  }
-  return false;
-}
-
 struct CacheSizes {
   size_t pool, exps;           // bytes of the k (or v) rows, of their exponents
 };
@@ -115,6 +93,7 @@ size_t attn_work_bytes(const linattn_cache_desc* c, int H, int n) {
 
 using namespace linattn;
 using namespace linattn::attn;
+using namespace linattn::checks;
 
 extern "C" {
 

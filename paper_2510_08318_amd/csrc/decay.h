@@ -1,0 +1,75 @@
+// Causal linear attention with a decay for each head (linattn_decay_*): what the host dispatch and the kernels agree on.
+//
+//   S_t = lambda S_{t-1} + k_t v_t^T        o_t = scale q_t S_t
+//   D_t = lambda D_{t+1} + scale q_t dout_t^T, lambda D_n := dS_out
+//   dq_t = scale S_t dout_t     dk_t = D_t v_t     dv_t = D_t^T k_t     dS_in = lambda D_0
+//
+// All four are one pass with other tensors in its roles.  For token rows a, b, c in the pass's order and a state X,
+//
+//   o_i = out_scale a_i (lambda^i X + in_scale sum_{j <= i} lambda^{i-j} b_j^T c_j)
+//
+//   out: (q, k, v), X = lambda S_in;  dq: (dout, v, k), X = lambda S_in^T;  from the last token back, dv: (k, q, dout), X = dS_out, and dk: (v, dout, q),
+//   X = dS_out^T.  A pass that is `turned` reads its state transposed.
+#pragma once
+#include "kernels.h"
+
+namespace linattn {
+namespace decay {
+
+constexpr int kMostTokens = 1 << 30;
+
+// A token tensor in a role: its head of query head h is h / group.
+struct Role {
+  const void* p;
+  Rows r;
+  int group;
+};
+struct Pass {
+  Role a, b, c;
+  void* o;                  // of query heads, as the tensors or (part) fp32 [B, H, n, d]
+  Rows orow;
+  const float* in;          // state, nullable: zeros
+  float* out;               // nullable; not of a turned pass
+  int turned, back;         // back: from the last token to the first
+  float in_scale, out_scale;
+};
+struct Common {
+  const float* log_decay;   // [H]
+  const int* lengths;       // [B], nullable
+  const int* slots;         // [B], nullable: row of an item in the state tensors
+  int states, B, H, n;
+};
+
+// A head's decay as the kernels use it: what is above 0, or NaN, counts as 0, and -inf as a number whose products with distances stay finite.
+__device__ __forceinline__ float log_decay_of(const Common& c, int h) { return fmaxf(fminf(c.log_decay[h], 0.f), -1e30f); }
+__host__ __device__ inline int length_of(const Common& c, int b) {
+  if (!c.lengths) return c.n;
+  const int x = c.lengths[b];
+  return x < 0 ? 0 : x < c.n ? x : c.n;
+}
+// Row of item b, head h in the state tensors; -1 where its slot is none.
+__device__ __forceinline__ long long state_row(const Common& c, int b, int h) {
+  const int s = c.slots ? c.slots[b] : b;
+  return (unsigned)s < (unsigned)c.states ? (long long)s * c.H + h : -1;
+}
+
+// One call of linattn_decay_fwd / linattn_decay_bwd.
+struct Args {
+  const void *q, *k, *v, *dout;
+  void *o, *dq, *dk, *dv;
+  const float *state, *dstate;
+  float *state_out, *dstate_in;
+  Common c;
+  int HK, d, dtype;
+  Rows qr, kr;
+  float scale;
+  float* work;
+  hipStream_t stream;
+};
+
+size_t work_bytes(int dtype, int B, int H, int HK, int n, int d, bool backward);
+hipError_t launch_fwd(const Args& a);
+hipError_t launch_bwd(const Args& a);
+
+}  // namespace decay
+}  // namespace linattn

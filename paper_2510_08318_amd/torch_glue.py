@@ -2,7 +2,8 @@
 
 Nothing of the operator is computed here; `Layer` owns the buffers a converted attention layer
 needs (W~_q, W~_k, state, workspace), registers them as a phi descriptor and forwards to
-linattn_fwd / linattn_bwd.  `window_attention`, `window_attention_backward` and `PagedCache` do the same for the softmax branch.
+linattn_fwd / linattn_bwd.  `window_attention`, `window_attention_backward` and `PagedCache` do the same for the softmax branch, `rotary` for the positions that q and k
+carry, `decay_attention` and `decay_attention_backward` for causal linear attention with a decay.
 """
 from __future__ import annotations
 
@@ -374,3 +375,157 @@ class PagedCache:
         work = q.new_empty(size, dtype=torch.uint8) if size else None
         B_.linattn_cache_attn(desc, B_.Sight(left, right, sinks, scale), q, out, lse, H, n, work, size, _raw_stream(self.index))
         return out, lse
+
+
+# ---- rotary positions, causal linear attention with a decay -----------------------------------------------------------------
+
+
+def _dtype_code(q, f32_math):
+    _need(q.dtype in (torch.bfloat16, torch.float32), "bf16 or fp32 tensors")
+    return B_.F32 if q.dtype == torch.float32 else B_.BF16_F32MATH if f32_math else B_.BF16
+
+
+def _layout_code(layout):
+    return B_.LAYOUT_BNHD if layout == "bnhd" else B_.LAYOUT_BHND
+
+
+def _result(name, out, like, index):
+    if out is None:
+        return torch.empty_like(like)
+    _check_tokens(name, out, like.shape, like.dtype, index)
+    return out
+
+
+def _int3(name, values, axes):
+    values = [int(x) for x in values]
+    _need(len(values) == axes and all(-(1 << 31) <= x < 1 << 31 for x in values), f"{name}: a 32-bit number for each axis")
+    return (B_.ctypes.c_int * 3)(*values)
+
+
+@_on_device_of
+def rotary(q, k=None, *, dims=None, grid=None, first=None, positions=None, base=10000.0, pairs="adjacent", inverse=False, layout="bhnd", lengths=None,
+           q_out=None, k_out=None):
+    """q and k with each token's rows turned by its position along up to three axes (linattn_rotary).  q, k: bf16 or fp32, [B, heads, n, d] ("bhnd") or
+    [B, n, heads, d] ("bnhd").  dims: channels of each axis, one after the other (None: (d,)); channels behind the last stay as they are.  pairs: "adjacent"
+    channels of an axis, or of its "halves".  Positions: token i has the coordinates of i in `grid` (tokens along each axis, the last fastest; not needed
+    with one axis), plus `first`; or int32 `positions` [n, axes] or [B, n, axes].  inverse: turned back, which is also the gradient: rotary(dq, dk, ...,
+    inverse=True).  lengths: int32 [B], the tokens of each item; the rest is padding.  q_out, k_out may be q and k.  Returns (q_out, k_out), or
+    (q_out, None) without k.  Nothing is recorded for autograd."""
+    B, H, n, d = _token_dims(q, layout)
+    index = q.get_device()
+    dtype = _dtype_code(q, False)
+    _check_tokens("q", q, q.shape, q.dtype, index)
+    HK = H
+    if k is None:
+        _need(k_out is None, "k_out goes with k")
+    else:
+        HK = _token_dims(k, layout)[1]
+        _check_tokens("k", k, _token_shape(B, HK, n, d, layout), q.dtype, index)
+    dims = (d,) if dims is None else dims
+    axes = len(dims)
+    _need(1 <= axes <= 3 and pairs in ("adjacent", "halves"), "dims: one to three axes; pairs: 'adjacent' or 'halves'")
+    _need(grid is not None or positions is not None or axes == 1, "grid: the tokens along each axis")
+    items = 0
+    if positions is not None:
+        _need(grid is None or first is None or not any(first), "positions: in place of grid and first")
+        items = 1 if positions.dim() == 2 else B
+        _check_ints("positions", positions, (n, axes) if items == 1 and positions.dim() == 2 else (B, n, axes), index)
+    _check_ints("lengths", lengths, (B,), index)
+    desc = B_.RotaryDesc(dtype, B, H, HK, n, d, _layout_code(layout), axes, _int3("dims", dims, axes),
+                         B_.PAIRS_HALVES if pairs == "halves" else B_.PAIRS_ADJACENT, int(inverse), base,
+                         _int3("grid", grid if grid is not None else (1,) * axes, axes), _int3("first", first if first is not None else (0,) * axes, axes),
+                         B_._ptr(positions), items, B_._ptr(lengths))
+    q_out = _result("q_out", q_out, q, index)
+    k_out = _result("k_out", k_out, k, index) if k is not None else None
+    B_.linattn_rotary(desc, q, k, q_out, k_out, _raw_stream(index))
+    return q_out, k_out
+
+
+def _check_state(name, t, shape, index):
+    if t is not None:
+        _check_tokens(name, t, shape, torch.float32, index)
+
+
+def _decay_desc(q, k, v, log_decay, slots, states, scale, layout, lengths, f32_math):
+    B, H, n, d = _token_dims(q, layout)
+    HK = _token_dims(k, layout)[1]
+    dtype, index, shape = _dtype_code(q, f32_math), q.get_device(), _token_shape(B, HK, n, d, layout)
+    _check_tokens("q", q, q.shape, q.dtype, index)
+    _check_tokens("k", k, shape, q.dtype, index)
+    _check_tokens("v", v, shape, q.dtype, index)
+    _check_tokens("log_decay", log_decay, (H,), torch.float32, index)
+    _check_ints("lengths", lengths, (B,), index)
+    _check_ints("slots", slots, (B,), index)
+    return B_.DecayDesc(dtype, B, H, HK, n, d, _layout_code(layout), scale, B_._ptr(log_decay), B_._ptr(lengths), B_._ptr(slots), states, None, 0)
+
+
+def _decay_workspace(desc, q, backward):
+    size = B_.linattn_decay_workspace_bytes(desc, backward)
+    if size == 0:
+        return None
+    work = q.new_empty(size, dtype=torch.uint8)
+    desc.workspace, desc.workspace_bytes = B_._ptr(work), size
+    return work
+
+
+def _state_shape(desc):
+    return (desc.states if desc.slots else desc.B, desc.H, desc.d, desc.d)
+
+
+@_on_device_of
+def decay_attention(q, k, v, log_decay, *, state=None, slots=None, scale=0.0, layout="bhnd", lengths=None, f32_math=False, out=None, state_out=None):
+    """Causal linear attention with a decay for each head (linattn_decay_fwd):
+
+        S_t = exp(log_decay) S_{t-1} + k_t v_t^T,    out_t = scale q_t S_t
+
+    q [B, H, n, d] ("bhnd") or [B, n, H, d] ("bnhd"); k, v with H or a divisor of H heads; log_decay fp32 [H], at most 0.  state: fp32 [B, H, d, d], what came
+    before (None: nothing).  state_out: where the state behind the last token goes; None for a new tensor, False where it is not wanted; may be `state`
+    itself.  slots: int32 [B], the items' rows of `state` and state_out, which then are [any, H, d, d] and of which one is given at least (state_out=None then stands for
+    `state` itself).  lengths: int32 [B], the tokens of each item; the rest is padding.  scale: 0 for 1/sqrt(d).  f32_math: fp32 arithmetic on bf16 tensors.  n = 1 is the step of
+    generation token by token.  Returns (out, state_out), or (out, None).  Nothing is recorded for autograd, also where inputs require a gradient:
+    decay_attention_backward gives it, and a torch.autograd.Function around the two has it recorded."""
+    index = q.get_device()
+    if slots is not None:
+        pool = state if state is not None else state_out
+        _need(isinstance(pool, torch.Tensor) and pool.dim() == 4, "slots: rows of state, or of state_out, [any, H, d, d]")
+        states = pool.shape[0]
+        state_out = state if state_out is None else state_out
+    else:
+        states = 0
+    desc = _decay_desc(q, k, v, log_decay, slots, states, scale, layout, lengths, f32_math)
+    shape = _state_shape(desc)
+    _check_state("state", state, shape, index)
+    if state_out is None:
+        state_out = q.new_empty(shape, dtype=torch.float32)
+    elif state_out is False:
+        state_out = None
+    else:
+        _check_state("state_out", state_out, shape, index)
+    out = _result("out", out, q, index)
+    work = _decay_workspace(desc, q, False)      # (a name holds it until the call has been queued)
+    B_.linattn_decay_fwd(desc, q, k, v, state, out, state_out, _raw_stream(index))
+    return out, state_out
+
+
+@_on_device_of
+def decay_attention_backward(q, k, v, log_decay, dout, *, state=None, dstate=None, slots=None, scale=0.0, layout="bhnd", lengths=None, f32_math=False,
+                             dq=None, dk=None, dv=None, dstate_in=None):
+    """Gradients (dq, dk, dv, dstate_in) of decay_attention (same keyword arguments) for the upstream gradients dout and dstate (of state_out; fp32 [B, H, d, d],
+    None: zeros).  dstate_in, the gradient of `state`, is by item, [B, H, d, d], also where states go by slots: None for a new tensor where a state was given (else
+    none is made), False where it is not wanted.  log_decay is a constant of the layer and has no gradient.  Nothing is recorded for autograd."""
+    index = q.get_device()
+    _need(slots is None or state is not None, "slots: rows of state")
+    desc = _decay_desc(q, k, v, log_decay, slots, state.shape[0] if slots is not None else 0, scale, layout, lengths, f32_math)
+    _check_state("state", state, _state_shape(desc), index)
+    by_item = (desc.B, desc.H, desc.d, desc.d)
+    _check_state("dstate", dstate, by_item, index)
+    _check_tokens("dout", dout, q.shape, q.dtype, index)
+    if dstate_in is None and state is not None:
+        dstate_in = q.new_empty(by_item, dtype=torch.float32)
+    elif dstate_in is False:
+        dstate_in = None
+    _check_state("dstate_in", dstate_in, by_item, index)
+    dq, dk, dv = [_result(name, g, like, index) for name, g, like in (("dq", dq, q), ("dk", dk, k), ("dv", dv, v))]
+    work = _decay_workspace(desc, q, True)      # (a name holds it until the call has been queued)
+    B_.linattn_decay_bwd(desc, q, k, v, state, dout, dstate, dq, dk, dv, dstate_in, _raw_stream(index))
+    return dq, dk, dv, dstate_in
