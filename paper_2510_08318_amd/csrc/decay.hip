@@ -1,5 +1,6 @@
 // linattn_decay_fwd, linattn_decay_bwd: launches.
 #include "../../include/linattn.h"
+#include "decay_rows.h"
 #include "decay_step.h"
 
 namespace linattn {
@@ -24,7 +25,97 @@ __global__ __launch_bounds__(256) void sum_heads_kernel(const float* parts, T* t
 }
 
 template <typename T, int D>
+hipError_t sum_heads(const float* parts, void* to, const Args& a) {
+  const int rows = 256 / (D / 4);
+  sum_heads_kernel<T, D><<<dim3((unsigned)(((long long)a.HK * a.c.n + rows - 1) / rows), a.c.B), 256, 0, a.stream>>>(parts, static_cast<T*>(to), a.kr, a.HK, a.c.H / a.HK, a.c.n);
+  return hipGetLastError();
+}
+
+// Tokens up to which the recurrence is taken token by token.
+constexpr int kStepTokens = 16;
+
+struct Layout {             // of the workspace, in floats
+  size_t states, parts;     // all states; dk or dv of all query heads
+};
+Layout layout_of(int dtype, int B, int H, int HK, int n, int d, bool backward) {
+  Layout r{0, 0};
+  const bool chunked = dtype == LINATTN_BF16 && n > kStepTokens;
+  if (chunked) r.states = (size_t)plan_of(B, H, n, d, backward ? 3 : 1, backward ? 2 : 1).segs * (backward ? 2 : 1) * B * H * d * d;
+  if (backward && H != HK) r.parts = (size_t)B * H * n * d;
+  return r;
+}
+
+template <int D, typename O>
+hipError_t launch_rows(const RowArgs& r, hipStream_t s) {
+  constexpr size_t smem = rows_lds<D>();
+  constexpr auto kernel = &decay_rows_kernel<D, O>;
+  if (hipError_t e = set_smem_once<kernel>(smem); e != hipSuccess) return e;
+  kernel<<<(unsigned)(r.c.B * r.c.H * r.plan.segs * r.passes), 256, smem, s>>>(r);
+  return hipGetLastError();
+}
+template <int D, int PIECES>
+hipError_t launch_sums(const SumArgs& r, hipStream_t s) {
+  constexpr size_t smem = sum_lds<D>();
+  constexpr auto kernel = &decay_sum_kernel<D, PIECES>;
+  if (hipError_t e = set_smem_once<kernel>(smem); e != hipSuccess) return e;
+  kernel<<<(unsigned)(r.c.B * r.c.H * r.plan.segs * r.passes), 256, smem, s>>>(r);
+  return hipGetLastError();
+}
+template <int D>
+hipError_t launch_states(const SumArgs& sums, const ScanArgs& scan, hipStream_t s) {
+  bool handed_out = false;
+  for (int i = 0; i < scan.passes; ++i) handed_out |= scan.pass[i].out != nullptr;
+  if (hipError_t e = handed_out ? launch_sums<D, 3>(sums, s) : launch_sums<D, kUpdatePieces>(sums, s); e != hipSuccess) return e;
+  decay_scan_kernel<<<dim3(D * D / 1024, scan.c.B * scan.c.H, scan.passes), 256, 0, s>>>(scan);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t chunked_fwd(const Args& a) {
+  const int G = a.c.H / a.HK;
+  const Plan plan = plan_of(a.c.B, a.c.H, a.c.n, D, 1, 1);
+  const Role q{a.q, a.qr, 1}, k{a.k, a.kr, G}, v{a.v, a.kr, G};
+  const bool states = plan.segs > 1 || a.state_out;
+  if (states) {
+    const SumArgs sums{{{k, v, 0}}, 1, a.c, plan, a.work};
+    const ScanArgs scan{{{a.state, a.state_out, 0, 1.f, 0}}, 1, a.c, plan, a.work, D * D};
+    if (hipError_t e = launch_states<D>(sums, scan, a.stream); e != hipSuccess) return e;
+  }
+  const RowArgs rows{{{Pass{q, k, v, a.o, a.qr, a.state, nullptr, 0, 0, 1.f, a.scale}, states ? a.work : nullptr, 0}}, 1, a.c, plan};
+  return launch_rows<D, uint16_t>(rows, a.stream);
+}
+
+template <int D>
+hipError_t chunked_bwd(const Args& a) {
+  const int G = a.c.H / a.HK;
+  const Plan plan = plan_of(a.c.B, a.c.H, a.c.n, D, 3, 2);
+  const Role q{a.q, a.qr, 1}, k{a.k, a.kr, G}, v{a.v, a.kr, G}, dout{a.dout, a.qr, 1};
+  const Layout lay = layout_of(a.dtype, a.c.B, a.c.H, a.HK, a.c.n, D, true);
+  const bool states = plan.segs > 1 || a.dstate_in;
+  const size_t one = lay.states / 2;
+  float *s = states ? a.work : nullptr, *d = states ? a.work + one : nullptr;
+  if (states) {
+    const SumArgs sums{{{k, v, 0}, {q, dout, 1}}, 2, a.c, plan, a.work};
+    const ScanArgs scan{{{a.state, nullptr, 0, 1.f, 0}, {a.dstate, a.dstate_in, 1, a.scale, 1}}, 2, a.c, plan, a.work, D * D};
+    if (hipError_t e = launch_states<D>(sums, scan, a.stream); e != hipSuccess) return e;
+  }
+  const RowPass dq{Pass{dout, v, k, a.dq, a.qr, a.state, nullptr, 1, 0, 1.f, a.scale}, s, 0};
+  RowPass dv{Pass{k, q, dout, a.dv, a.kr, a.dstate, nullptr, 0, 1, a.scale, 1.f}, d, 1}, dk{Pass{v, dout, q, a.dk, a.kr, a.dstate, nullptr, 1, 1, a.scale, 1.f}, d, 1};
+  if (G == 1) return launch_rows<D, uint16_t>(RowArgs{{dq, dv, dk}, 3, a.c, plan}, a.stream);
+  if (hipError_t e = launch_rows<D, uint16_t>(RowArgs{{dq}, 1, a.c, plan}, a.stream); e != hipSuccess) return e;
+  for (RowPass* x : {&dv, &dk}) {
+    void* to = x->p.o;
+    x->p.o = a.work + lay.states;
+    x->p.orow = Rows{(size_t)a.c.H * a.c.n * D, (size_t)a.c.n * D, (size_t)D};
+    if (hipError_t e = launch_rows<D, float>(RowArgs{{*x}, 1, a.c, plan}, a.stream); e != hipSuccess) return e;
+    if (hipError_t e = sum_heads<uint16_t, D>(a.work + lay.states, to, a); e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+template <typename T, int D>
 hipError_t fwd(const Args& a) {
+  if (a.dtype == LINATTN_BF16 && a.c.n > kStepTokens) return chunked_fwd<D>(a);
   const int G = a.c.H / a.HK;
   Pass p{{a.q, a.qr, 1}, {a.k, a.kr, G}, {a.v, a.kr, G}, a.o, a.qr, a.state, a.state_out, 0, 0, 1.f, a.scale};
   return launch_step<T, T, D>(p, a.c, a.stream);
@@ -32,6 +123,7 @@ hipError_t fwd(const Args& a) {
 
 template <typename T, int D>
 hipError_t bwd(const Args& a) {
+  if (a.dtype == LINATTN_BF16 && a.c.n > kStepTokens) return chunked_bwd<D>(a);
   const int G = a.c.H / a.HK;
   const Role q{a.q, a.qr, 1}, k{a.k, a.kr, G}, v{a.v, a.kr, G}, dout{a.dout, a.qr, 1};
   Common of_items = a.c;      // dS_out and dS_in are by item
@@ -44,24 +136,21 @@ hipError_t bwd(const Args& a) {
     e = launch_step<T, T, D>(dv, of_items, a.stream);
     return e != hipSuccess ? e : launch_step<T, T, D>(dk, of_items, a.stream);
   }
-  const Rows parts{(size_t)a.c.H * a.c.n * D, (size_t)a.c.n * D, (size_t)D};
   for (Pass* p : {&dv, &dk}) {
-    T* to = static_cast<T*>(p->o);
+    void* to = p->o;
     p->o = a.work;
-    p->orow = parts;
-    e = launch_step<T, float, D>(*p, of_items, a.stream);
-    if (e != hipSuccess) return e;
-    const int rows = 256 / (D / 4);
-    sum_heads_kernel<T, D><<<dim3((unsigned)(((long long)a.HK * a.c.n + rows - 1) / rows), a.c.B), 256, 0, a.stream>>>(a.work, to, a.kr, a.HK, G, a.c.n);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    p->orow = Rows{(size_t)a.c.H * a.c.n * D, (size_t)a.c.n * D, (size_t)D};
+    if ((e = launch_step<T, float, D>(*p, of_items, a.stream)) != hipSuccess) return e;
+    if ((e = sum_heads<T, D>(a.work, to, a)) != hipSuccess) return e;
   }
   return e;
 }
 
 }  // namespace
 
-size_t work_bytes(int, int B, int H, int HK, int n, int d, bool backward) {
-  return backward && H != HK ? ((size_t)B * H * n * d * sizeof(float) + 255) & ~(size_t)255 : 0;
+size_t work_bytes(int dtype, int B, int H, int HK, int n, int d, bool backward) {
+  const Layout r = layout_of(dtype, B, H, HK, n, d, backward);
+  return ((r.states + r.parts) * sizeof(float) + 255) & ~(size_t)255;
 }
 
 hipError_t launch_fwd(const Args& a) {

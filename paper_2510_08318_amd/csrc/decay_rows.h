@@ -1,0 +1,448 @@
+// The passes of decay.h on the matrix cores, bf16 operands and fp32 sums: chunks of kChunk tokens, inside of which a row's pairs are taken one by one, while what lies
+// before comes through the state.
+#pragma once
+#include "attn_tile.h"
+#include "decay.h"
+#include "f32_split.h"
+
+namespace linattn {
+namespace decay {
+
+using attn::arrived;
+using attn::lds_loads_landed;
+using attn::load_to_lds;
+using attn::row_at;
+using attn::row_chunk;
+using attn::turned;
+
+// The token at place i of a pass's order; places behind the last token are padding.
+__device__ __forceinline__ int token_at(int i, int len, bool back) { return back && i < len ? len - 1 - i : i; }
+
+// Rows i0 .. i0 + 63 of the pass's order into an LDS tile [64][D], chunks of 16 bytes swizzled by row, by four wavefronts; rows from `end` on are row end - 1 again.
+template <int D>
+struct Tile {
+  static constexpr int ROWS = 512 / D, N = kChunk / ROWS / 4, BYTES = kChunk * D * 2;
+  const char* base;
+  size_t pitch;
+  __device__ __forceinline__ void of(const Role& r, int b, int h) {
+    base = static_cast<const char*>(r.p) + ((size_t)b * r.r.sb + (size_t)(h / r.group) * r.r.sh) * 2;
+    pitch = r.r.sn * 2;
+  }
+  __device__ __forceinline__ void load(int i0, int end, int len, bool back, uint32_t lds, int w, int lane) const {
+#pragma unroll
+    for (int x = 0; x < N; ++x) {
+      const int row = (w * N + x) * ROWS + lane / (D / 8), i = i0 + row < end ? i0 + row : end - 1;
+      const char* at = base + (size_t)token_at(i, len, back) * pitch + (((lane % (D / 8)) ^ swz<D>(row)) * 16);
+      load_to_lds(at, lds + (uint32_t)((w * N + x) * 1024));
+    }
+  }
+};
+
+// Accumulators of a 32 x 32 block have rows 8a + 4g + b in the lanes of group g (registers 4a + b).  With bits 2 and 3 of a column's number exchanged where it becomes an
+// operand's row, those are columns 16 (a / 2) + 8 g + 4 (a % 2) + b: eight adjacent ones to eight registers, so that operands of other tensors are whole 16-byte
+// pieces of their rows, and so are a lane's results.  column_of: the column that operand row m stands for.  turned_columns: the transposing read's address (turned_at) with the
+// columns in that order; in each group of 16 lanes, lane s gives the address of columns 4 (s % 4) .. + 3, and receives column s.
+__device__ __forceinline__ int column_of(int m) { return (m & 19) | ((m & 4) << 1) | ((m & 8) >> 1); }
+template <int D>
+__device__ __forceinline__ uint32_t turned_columns(int lane) {
+  return (uint32_t)tr_lane<D, 4>((unsigned)((lane & ~3) | ((lane & 1) << 1) | ((lane & 2) >> 1)));
+}
+
+__device__ __forceinline__ f32x16 zero16() {
+  f32x16 z;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) z[r] = 0.f;
+  return z;
+}
+__device__ __forceinline__ uint4 pack8(const f32x16& e, int h) {
+  return make_uint4(pack_bf16x2(e[8 * h], e[8 * h + 1]), pack_bf16x2(e[8 * h + 2], e[8 * h + 3]), pack_bf16x2(e[8 * h + 4], e[8 * h + 5]),
+                    pack_bf16x2(e[8 * h + 6], e[8 * h + 7]));
+}
+__device__ __forceinline__ f32x16 mfma(uint4 a, uint4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
+}
+
+// Row of a k-step's element e in lane group g, as the transposing reads give them.
+__device__ __forceinline__ constexpr int row_of(int e, int g) { return 8 * (e / 4) + 4 * g + e % 4; }
+
+// Rows times their weights, as the sum of PIECES bf16 numbers.
+template <int PIECES>
+__device__ __forceinline__ void weigh(uint4 x, const float* w, uint4 (&p)[PIECES]) {
+  const uint32_t in[4] = {x.x, x.y, x.z, x.w};
+  uint32_t out[PIECES][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float a = f32::lo_f32(in[i]) * w[2 * i], b = f32::hi_f32(in[i]) * w[2 * i + 1];
+#pragma unroll
+    for (int j = 0; j < PIECES; ++j) {
+      out[j][i] = pack_bf16x2(a, b);
+      a -= f32::lo_f32(out[j][i]); b -= f32::hi_f32(out[j][i]);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < PIECES; ++j) p[j] = make_uint4(out[j][0], out[j][1], out[j][2], out[j][3]);
+}
+
+// ---- a segment's own sum --------------------------------------------------------------------------------------------
+
+struct SumPass {
+  Role b, c;
+  int back;
+};
+struct SumArgs {
+  SumPass pass[2];
+  int passes;
+  Common c;
+  Plan plan;
+  float* sums;              // [pass][B * H][segment][D][D]
+};
+
+// sum_j lambda^(end - 1 - j) b_j^T c_j over a segment's tokens, end: the first behind them.  The rows c_j enter with their weights, whole, as three bf16 pieces (PIECES 3), where a
+// state is handed out; b_j is bf16 as it is, so that the sum is one of exact products in fp32.
+template <int D, int PIECES>
+__global__ __launch_bounds__(256, 2) void decay_sum_kernel(SumArgs a) {
+  constexpr int CB = D / 32, BLOCKS = CB * CB / 4, KS = kChunk / 16, TILE = Tile<D>::BYTES;
+  extern __shared__ __align__(16) char smem[];
+  const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
+  const int pass = blockIdx.x % a.passes, at = blockIdx.x / a.passes, seg = at % a.plan.segs, bh = at / a.plan.segs, b = bh / a.c.H, h = bh % a.c.H;
+  const SumPass& p = a.pass[pass];
+  const int len = length_of(a.c, b), i0 = seg * a.plan.chunks * kChunk, i1 = min(len, i0 + a.plan.chunks * kChunk);
+  if (i0 >= i1) return;
+  const float decay = log_decay_of(a.c, h);
+  Tile<D> rows, columns;
+  rows.of(p.b, b, h);
+  columns.of(p.c, b, h);
+  const uint32_t lds = lds_address(smem), from = turned_columns<D>(lane);
+  const int cb = w % CB, fb0 = w / CB * BLOCKS;
+  f32x16 sum[BLOCKS];
+#pragma unroll
+  for (int i = 0; i < BLOCKS; ++i) sum[i] = zero16();
+  float rel[KS][8];         // of a whole chunk's tokens, relative to its last
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) rel[ks][e] = expf(decay * (float)(kChunk - 1 - 16 * ks - row_of(e, g)));
+
+  auto ask = [&](int i, int buffer) {
+    rows.load(i, i1, len, p.back, lds + buffer * 2 * TILE, w, lane);
+    columns.load(i, i1, len, p.back, lds + buffer * 2 * TILE + TILE, w, lane);
+  };
+  ask(i0, 0);
+  for (int i = i0, buffer = 0; i < i1; i += kChunk, buffer ^= 1) {
+    lds_loads_landed();
+    __syncthreads();
+    if (i + kChunk < i1) ask(i + kChunk, buffer ^ 1);
+    const uint32_t tile = lds + buffer * 2 * TILE;
+    const bool whole = i + kChunk <= i1;
+    const float after = whole ? expf(decay * (float)(i1 - i - kChunk)) : 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      float wt[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) wt[e] = rel[ks][e] * after;
+      uint4 x = __builtin_bit_cast(uint4, turned<D>(from + tile + TILE, cb, 16 * ks));
+      if (!whole) {
+        uint32_t* v = reinterpret_cast<uint32_t*>(&x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int j = i + 16 * ks + row_of(e, g);
+          wt[e] = j < i1 ? expf(decay * (float)(i1 - 1 - j)) : 0.f;
+          if (j >= i1) v[e / 2] &= e % 2 ? 0xffffu : 0xffff0000u;
+        }
+      }
+      uint4 c[PIECES];
+      weigh<PIECES>(x, wt, c);
+#pragma unroll
+      for (int y = 0; y < BLOCKS; ++y) {
+        const uint4 r = __builtin_bit_cast(uint4, turned<D>(from + tile, fb0 + y, 16 * ks));
+#pragma unroll
+        for (int j = PIECES - 1; j >= 0; --j) sum[y] = mfma(r, c[j], sum[y]);
+      }
+    }
+  }
+  float* out = a.sums + (((size_t)pass * a.c.B * a.c.H + bh) * a.plan.segs + seg) * D * D;
+#pragma unroll
+  for (int y = 0; y < BLOCKS; ++y)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) out[(32 * (fb0 + y) + 16 * (r / 8) + 8 * g + r % 8) * D + 32 * cb + column_of(m)] = sum[y][r];
+}
+
+// ---- the states in front of the segments ------------------------------------------------------------------------------
+
+struct ScanPass {
+  const float* in;          // nullable
+  float* out;               // nullable
+  int back;
+  float in_scale;
+  int by_item;              // states by item, not by slot
+};
+struct ScanArgs {
+  ScanPass pass[2];
+  int passes;
+  Common c;
+  Plan plan;
+  float* sums;              // replaced by the states
+  int size;                 // D * D
+};
+
+// lambda^r as a sum of two fp32 numbers: rounded to one, the products along a sequence would be off by a multiple of its error.
+__device__ __forceinline__ void power_of(float decay, int r, float& hi, float& lo) {
+  const double x = exp((double)decay * (double)r);
+  hi = (float)x;
+  lo = (float)(x - (double)hi);
+}
+
+// Four elements of a head's state a thread, segment after segment: X in front of segment s (as decay.h has it: out's and dq's times lambda) takes the place of its
+// sum, X' = lambda^tokens X + lambda sum.
+__global__ __launch_bounds__(256) void decay_scan_kernel(ScanArgs a) {
+  const int pass = blockIdx.z, bh = blockIdx.y, b = bh / a.c.H, h = bh % a.c.H, e = (blockIdx.x * 256 + threadIdx.x) * 4;
+  const ScanPass& p = a.pass[pass];
+  Common com = a.c;
+  if (p.by_item) { com.slots = nullptr; com.states = com.B; }
+  const int len = length_of(com, b), step = a.plan.chunks * kChunk, live = (len + step - 1) / step;
+  const long long row = state_row(com, b, h);
+  const float decay = log_decay_of(com, h), lambda = expf(decay);
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (p.in && row >= 0) x = *reinterpret_cast<const float4*>(p.in + row * a.size + e);
+  if (!p.back && len > 0) { x.x *= lambda; x.y *= lambda; x.z *= lambda; x.w *= lambda; }
+  float4* at = reinterpret_cast<float4*>(a.sums + ((size_t)pass * a.c.B * a.c.H + bh) * a.plan.segs * a.size + e);
+  const size_t next = a.size / 4;
+  float hi, lo;
+  power_of(decay, step, hi, lo);
+  const float first = p.in_scale * lambda;
+  auto move = [&](float& y, float s) { y = fmaf(y, hi, fmaf(y, lo, first * s)); };
+  constexpr int AHEAD = 4;
+  for (int s0 = 0; s0 < live; s0 += AHEAD) {
+    float4 sum[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) sum[i] = s0 + i < live ? at[(s0 + i) * next] : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      if (s0 + i >= live) break;
+      at[(s0 + i) * next] = x;
+      if (s0 + i == live - 1) {
+        // behind the last token: forward S_n = lambda^(tokens - 1) X + sum, back lambda^tokens X + lambda sum
+        const int tokens = len - (live - 1) * step;
+        float h1, l1;
+        power_of(decay, p.back ? tokens : tokens - 1, h1, l1);
+        const float f = p.back ? first : p.in_scale;
+        x.x = fmaf(x.x, h1, fmaf(x.x, l1, f * sum[i].x)); x.y = fmaf(x.y, h1, fmaf(x.y, l1, f * sum[i].y));
+        x.z = fmaf(x.z, h1, fmaf(x.z, l1, f * sum[i].z)); x.w = fmaf(x.w, h1, fmaf(x.w, l1, f * sum[i].w));
+      } else { move(x.x, sum[i].x); move(x.y, sum[i].y); move(x.z, sum[i].z); move(x.w, sum[i].w); }
+    }
+  }
+  if (p.out && row >= 0) *reinterpret_cast<float4*>(p.out + row * a.size + e) = x;
+}
+
+// ---- rows -----------------------------------------------------------------------------------------------------------
+
+struct RowPass {
+  Pass p;
+  const float* states;      // [B * H][segment][D][D], or null: p.in is in front of the one segment
+  int by_item;
+};
+struct RowArgs {
+  RowPass pass[3];
+  int passes;
+  Common c;
+  Plan plan;
+};
+
+constexpr int kUpdatePieces = 2;
+
+// Rows of a segment, chunk by chunk.  A wavefront has 32 columns of the state X in its accumulators, where they are the left operand of a_i X as they lie (rounded to bf16); the
+// chunk's weights P, on the lanes as S^T = B A^T gives them, are made by three of the wavefronts and go round through LDS.
+template <int D, typename O>
+__global__ __launch_bounds__(256, D == 128 ? 1 : 2) void decay_rows_kernel(RowArgs a) {
+  constexpr int CB = D / 32, FB = D / 32, KS = D / 16, JS = kChunk / 16, IW = 4 / CB, IB = 2 / IW, TILE = Tile<D>::BYTES;
+  extern __shared__ __align__(16) char smem[];
+  const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
+  const int pass = blockIdx.x % a.passes, at = blockIdx.x / a.passes, bh = at / a.plan.segs, b = bh / a.c.H, h = bh % a.c.H;
+  const RowPass& rp = a.pass[pass];
+  const Pass& p = rp.p;
+  const int seg = at % a.plan.segs;
+  const int len = length_of(a.c, b), i0 = seg * a.plan.chunks * kChunk, all = min(a.c.n, i0 + a.plan.chunks * kChunk), i1 = min(len, all);
+  O* const out = static_cast<O*>(p.o) + (size_t)b * p.orow.sb + (size_t)h * p.orow.sh;
+
+  // padding: zeros, D values of a row by D / 8 threads
+  for (int i = max(i0, i1) + threadIdx.x / (D / 8); i < all; i += 256 / (D / 8)) {
+    uint4* z = reinterpret_cast<uint4*>(out + (size_t)i * p.orow.sn + threadIdx.x % (D / 8) * 8);
+    z[0] = make_uint4(0, 0, 0, 0);
+    if constexpr (sizeof(O) == 4) z[1] = make_uint4(0, 0, 0, 0);
+  }
+  if (i0 >= i1) return;
+
+  Tile<D> ta, tb, tc;
+  ta.of(p.a, b, h);
+  tb.of(p.b, b, h);
+  tc.of(p.c, b, h);
+  const uint32_t lds = lds_address(smem), weights = lds + 6 * TILE;
+  auto ask = [&](int i, int buffer) {
+    const uint32_t to = lds + buffer * 3 * TILE;
+    ta.load(i, i1, len, p.back, to, w, lane);
+    tb.load(i, i1, len, p.back, to + TILE, w, lane);
+    tc.load(i, i1, len, p.back, to + 2 * TILE, w, lane);
+  };
+  ask(i0, 0);
+
+  const int cb = w % CB, ib0 = w / CB * IB, column = 32 * cb + column_of(m);
+  const float decay = log_decay_of(a.c, h);
+  f32x16 x[FB];
+  {
+    const float* from = rp.states ? rp.states + ((size_t)bh * a.plan.segs + seg) * D * D : nullptr;
+    float factor = 1.f;
+    if (!from && p.in) {
+      Common com = a.c;
+      if (rp.by_item) { com.slots = nullptr; com.states = com.B; }
+      const long long row = state_row(com, b, h);
+      if (row >= 0) from = p.in + row * D * D;
+      if (!p.back) factor = expf(decay);
+    }
+#pragma unroll
+    for (int f = 0; f < FB; ++f)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int row = 32 * f + 16 * (r / 8) + 8 * g + r % 8;
+        x[f][r] = from ? from[p.turned ? column * D + row : row * D + column] * factor : 0.f;
+      }
+  }
+  // weights: of a pair in a 32 x 32 block on the diagonal, in the one left of it; of a token in the state behind the chunk; of the state in a row, and over a chunk
+  float diag[16], left[16], keep[JS][8], mine[IB];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int gap = m - row_of(r % 8, g) - 16 * (r / 8);
+    diag[r] = gap >= 0 ? expf(decay * (float)gap) * p.in_scale : 0.f;
+    left[r] = expf(decay * (float)(32 + gap)) * p.in_scale;
+  }
+#pragma unroll
+  for (int ks = 0; ks < JS; ++ks)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) keep[ks][e] = expf(decay * (float)(kChunk - 16 * ks - row_of(e, g))) * p.in_scale;
+#pragma unroll
+  for (int i = 0; i < IB; ++i) mine[i] = expf(decay * (float)(32 * (ib0 + i) + m));
+  const float over = expf(decay * (float)kChunk);
+
+  const uint32_t rows_at = row_at<D>(lane), columns_at = turned_columns<D>(lane);
+  for (int i = i0, buffer = 0; i < i1; i += kChunk, buffer ^= 1) {
+    lds_loads_landed();
+    __syncthreads();
+    const bool more = i + kChunk < i1;
+    if (more) ask(i + kChunk, buffer ^ 1);
+    const uint32_t la = lds + buffer * 3 * TILE, lb = la + TILE, lc = lb + TILE;
+    typedef __attribute__((address_space(3))) u32x4* P;
+
+    // weights of block w: (0, 0), (1, 0), (1, 1) of rows and tokens
+    if (w < 3) {
+      const int ib = w > 0, jb = w == 2;
+      f32x16 s = zero16();
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) s = mfma(row_chunk<D>(rows_at + lb, ks, 32 * jb), row_chunk<D>(rows_at + la, ks, 32 * ib), s);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float wt = w == 1 ? left[r] : diag[r];
+        s[r] = w == 1 || row_of(r % 8, g) + 16 * (r / 8) <= m ? s[r] * wt : 0.f;
+      }
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh) *(P)(weights + (uint32_t)((2 * w + hh) * 1024 + 16 * lane)) = __builtin_bit_cast(u32x4, pack8(s, hh));
+    }
+
+    // a_i X, and what lies before the chunk fades
+    f32x16 o[IB];
+    auto before = [&] {
+#pragma unroll
+      for (int y = 0; y < IB; ++y) o[y] = zero16();
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const uint4 xs = pack8(x[ks / 2], ks % 2);
+#pragma unroll
+        for (int y = 0; y < IB; ++y) o[y] = mfma(xs, row_chunk<D>(rows_at + la, ks, 32 * (ib0 + y)), o[y]);
+      }
+#pragma unroll
+      for (int y = 0; y < IB; ++y)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[y][r] *= mine[y];
+    };
+    before();
+    uint4 c[JS];
+#pragma unroll
+    for (int ks = 0; ks < JS; ++ks) c[ks] = __builtin_bit_cast(uint4, turned<D>(columns_at + lc, cb, 16 * ks));
+    __syncthreads();
+
+    auto weight_block = [&](int blk, int hh) { return __builtin_bit_cast(uint4, *(P)(weights + (uint32_t)((2 * blk + hh) * 1024 + 16 * lane))); };
+#pragma unroll
+    for (int y = 0; y < IB; ++y) {
+      const int ib = ib0 + y;
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh) o[y] = mfma(c[hh], weight_block(ib, hh), o[y]);
+      if (ib)
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) o[y] = mfma(c[2 + hh], weight_block(2, hh), o[y]);
+    }
+
+    // A weight of 0 does not keep an infinity or NaN of a later token out of a product: rows that are not finite once more, over what they see.
+    float odd = 0.f;
+#pragma unroll
+    for (int y = 0; y < IB; ++y)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) odd = fmaf(o[y][r], 0.f, odd);
+    if (__any(odd != 0.f)) {
+      before();
+      for (int y = 0; y < IB; ++y)
+        for (int j = 0; j <= 32 * (ib0 + y) + m; ++j) {
+          const int jj = j % 16, src = 32 * ((jj / 4) % 2) + m, elem = jj / 8 * 4 + jj % 4;
+          const int blk = ib0 + y == 0 ? 0 : j < 32 ? 1 : 2;
+          const uint32_t pw = weights + (uint32_t)((2 * blk + j % 32 / 16) * 1024 + 16 * src + 2 * elem);
+          const float wt = __builtin_bit_cast(float, (uint32_t)*(__attribute__((address_space(3))) const uint16_t*)pw << 16);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int ch = 32 * cb + 16 * (r / 8) + 8 * g + r % 8;
+            const uint32_t at = lc + (uint32_t)(j * (D * 2) + (((ch / 8) ^ swz<D>(j)) * 16) + ch % 8 * 2);
+            o[y][r] = fmaf(wt, __builtin_bit_cast(float, (uint32_t)*(__attribute__((address_space(3))) const uint16_t*)at << 16), o[y][r]);
+          }
+        }
+    }
+#pragma unroll
+    for (int y = 0; y < IB; ++y) {
+      const int place = i + 32 * (ib0 + y) + m;
+      if (place >= i1) continue;
+      O* to = out + (size_t)token_at(place, len, p.back) * p.orow.sn + 32 * cb + 8 * g;
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh) {
+        f32x16 v;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) v[r] = o[y][8 * hh + r] * p.out_scale;
+        if constexpr (sizeof(O) == 2) *reinterpret_cast<uint4*>(to + 16 * hh) = pack8(v, 0);
+        else {
+          *reinterpret_cast<float4*>(to + 16 * hh) = make_float4(v[0], v[1], v[2], v[3]);
+          *reinterpret_cast<float4*>(to + 16 * hh + 4) = make_float4(v[4], v[5], v[6], v[7]);
+        }
+      }
+    }
+
+    if (more) {
+#pragma unroll
+      for (int f = 0; f < FB; ++f)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[f][r] *= over;
+#pragma unroll
+      for (int ks = 0; ks < JS; ++ks) {
+        uint4 cw[kUpdatePieces];
+        weigh<kUpdatePieces>(c[ks], keep[ks], cw);
+#pragma unroll
+        for (int f = 0; f < FB; ++f) {
+          const uint4 r = __builtin_bit_cast(uint4, turned<D>(columns_at + lb, f, 16 * ks));
+#pragma unroll
+          for (int j = kUpdatePieces - 1; j >= 0; --j) x[f] = mfma(r, cw[j], x[f]);
+        }
+      }
+    }
+  }
+}
+
+template <int D>
+constexpr int rows_lds() { return 6 * Tile<D>::BYTES + 6 * 1024; }
+template <int D>
+constexpr int sum_lds() { return 4 * Tile<D>::BYTES; }
+
+}  // namespace decay
+}  // namespace linattn
