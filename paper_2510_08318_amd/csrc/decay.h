@@ -67,17 +67,17 @@ struct Args {
   hipStream_t stream;
 };
 
-// How a call's tokens are cut: chunks of kChunk, segments of `chunks` of them, each a workgroup's.  Where there are several, a first kernel takes every segment's own sum
-// of b_j^T c_j, a second the states between them from it.
-constexpr int kChunk = 64;
+// How a call's tokens are cut: chunks of a kernel's own size, segments of several of them, each a workgroup's.  Where there are several segments, a first kernel takes every
+// segment's own sum of b_j^T c_j, a second the states between them from it.
+constexpr int kChunk = 64, kChunkF32 = 32;
 struct Plan {
-  int segs, chunks;
+  int segs, tokens;         // tokens of a segment
 };
-// The number of segments by a count of what each choice costs, in chunks of a workgroup of the rows kernel (1.5 us): as many rounds of resident workgroups as the call makes, and
+// The number of segments by a count of what each choice costs, in chunks of a workgroup of the rows kernel: as many rounds of resident workgroups as the call makes, and
 // with several segments the sums, which read two tensors of three, and two launches more.
-inline Plan plan_of(int B, int H, int n, int d, int row_passes, int sum_passes) {
-  const long long chunks = (n + kChunk - 1) / kChunk, heads = (long long)B * H, slots = kCUs * (d == 128 ? 1 : 2);
-  Plan best{1, (int)chunks};
+inline Plan plan_of(int B, int H, int n, int d, int chunk, int row_passes, int sum_passes) {
+  const long long chunks = (n + chunk - 1) / chunk, heads = (long long)B * H, slots = kCUs * (d == 128 ? 1 : 2);
+  Plan best{1, (int)chunks * chunk};
   double least = 0;
   for (long long want = 1; want <= chunks && want <= 256; ++want) {
     const long long per = (chunks + want - 1) / want, segs = (chunks + per - 1) / per;
@@ -85,7 +85,7 @@ inline Plan plan_of(int B, int H, int n, int d, int row_passes, int sum_passes) 
     const long long rounds = (heads * row_passes * segs + slots - 1) / slots, sums = (heads * sum_passes * segs + slots - 1) / slots;
     double cost = (double)rounds * (double)(per + 1);
     if (segs > 1) cost += (double)sums * (0.6 * (double)per + 1) + 5 + 0.1 * (double)segs;
-    if (want == 1 || cost < least) { least = cost; best = Plan{(int)segs, (int)per}; }
+    if (want == 1 || cost < least) { least = cost; best = Plan{(int)segs, (int)per * chunk}; }
   }
   return best;
 }

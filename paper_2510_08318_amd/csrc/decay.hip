@@ -1,6 +1,6 @@
 // linattn_decay_fwd, linattn_decay_bwd: launches.
 #include "../../include/linattn.h"
-#include "decay_rows.h"
+#include "decay_f32.h"
 #include "decay_step.h"
 
 namespace linattn {
@@ -34,61 +34,61 @@ hipError_t sum_heads(const float* parts, void* to, const Args& a) {
 // Tokens up to which the recurrence is taken token by token.
 constexpr int kStepTokens = 16;
 
+constexpr int chunk_of(int dtype) { return dtype == LINATTN_BF16 ? kChunk : kChunkF32; }
 struct Layout {             // of the workspace, in floats
   size_t states, parts;     // all states; dk or dv of all query heads
 };
 Layout layout_of(int dtype, int B, int H, int HK, int n, int d, bool backward) {
   Layout r{0, 0};
-  const bool chunked = dtype == LINATTN_BF16 && n > kStepTokens;
-  if (chunked) r.states = (size_t)plan_of(B, H, n, d, backward ? 3 : 1, backward ? 2 : 1).segs * (backward ? 2 : 1) * B * H * d * d;
+  if (n > kStepTokens) r.states = (size_t)plan_of(B, H, n, d, chunk_of(dtype), backward ? 3 : 1, backward ? 2 : 1).segs * (backward ? 2 : 1) * B * H * d * d;
   if (backward && H != HK) r.parts = (size_t)B * H * n * d;
   return r;
 }
 
-template <int D, typename O>
+template <auto KERNEL, typename A>
+hipError_t launch(const A& args, const Common& c, const Plan& plan, int passes, int threads, size_t smem, hipStream_t s) {
+  if (hipError_t e = set_smem_once<KERNEL>(smem); e != hipSuccess) return e;
+  KERNEL<<<(unsigned)(c.B * c.H * plan.segs * passes), threads, smem, s>>>(args);
+  return hipGetLastError();
+}
+// T: the tensors' type; F32: fp32 arithmetic; O: the results'
+template <typename T, int D, bool F32, typename O>
 hipError_t launch_rows(const RowArgs& r, hipStream_t s) {
-  constexpr size_t smem = rows_lds<D>();
-  constexpr auto kernel = &decay_rows_kernel<D, O>;
-  if (hipError_t e = set_smem_once<kernel>(smem); e != hipSuccess) return e;
-  kernel<<<(unsigned)(r.c.B * r.c.H * r.plan.segs * r.passes), 256, smem, s>>>(r);
-  return hipGetLastError();
+  if constexpr (F32) return launch<&decay_rows_f32_kernel<T, D, O>>(r, r.c, r.plan, r.passes, 2 * D, rows_f32_lds<D>(), s);
+  else return launch<&decay_rows_kernel<D, O>>(r, r.c, r.plan, r.passes, 256, rows_lds<D>(), s);
 }
-template <int D, int PIECES>
-hipError_t launch_sums(const SumArgs& r, hipStream_t s) {
-  constexpr size_t smem = sum_lds<D>();
-  constexpr auto kernel = &decay_sum_kernel<D, PIECES>;
-  if (hipError_t e = set_smem_once<kernel>(smem); e != hipSuccess) return e;
-  kernel<<<(unsigned)(r.c.B * r.c.H * r.plan.segs * r.passes), 256, smem, s>>>(r);
-  return hipGetLastError();
-}
-template <int D>
+template <typename T, int D, bool F32>
 hipError_t launch_states(const SumArgs& sums, const ScanArgs& scan, hipStream_t s) {
   bool handed_out = false;
   for (int i = 0; i < scan.passes; ++i) handed_out |= scan.pass[i].out != nullptr;
-  if (hipError_t e = handed_out ? launch_sums<D, 3>(sums, s) : launch_sums<D, kUpdatePieces>(sums, s); e != hipSuccess) return e;
+  hipError_t e;
+  if constexpr (F32) e = launch<&decay_sum_f32_kernel<T, D>>(sums, sums.c, sums.plan, sums.passes, 2 * D, sum_f32_lds<D>(), s);
+  else if (handed_out) e = launch<&decay_sum_kernel<D, 3>>(sums, sums.c, sums.plan, sums.passes, 256, sum_lds<D>(), s);
+  else e = launch<&decay_sum_kernel<D, kUpdatePieces>>(sums, sums.c, sums.plan, sums.passes, 256, sum_lds<D>(), s);
+  if (e != hipSuccess) return e;
   decay_scan_kernel<<<dim3(D * D / 1024, scan.c.B * scan.c.H, scan.passes), 256, 0, s>>>(scan);
   return hipGetLastError();
 }
 
-template <int D>
+template <typename T, int D, bool F32>
 hipError_t chunked_fwd(const Args& a) {
   const int G = a.c.H / a.HK;
-  const Plan plan = plan_of(a.c.B, a.c.H, a.c.n, D, 1, 1);
+  const Plan plan = plan_of(a.c.B, a.c.H, a.c.n, D, chunk_of(a.dtype), 1, 1);
   const Role q{a.q, a.qr, 1}, k{a.k, a.kr, G}, v{a.v, a.kr, G};
   const bool states = plan.segs > 1 || a.state_out;
   if (states) {
     const SumArgs sums{{{k, v, 0}}, 1, a.c, plan, a.work};
     const ScanArgs scan{{{a.state, a.state_out, 0, 1.f, 0}}, 1, a.c, plan, a.work, D * D};
-    if (hipError_t e = launch_states<D>(sums, scan, a.stream); e != hipSuccess) return e;
+    if (hipError_t e = launch_states<T, D, F32>(sums, scan, a.stream); e != hipSuccess) return e;
   }
   const RowArgs rows{{{Pass{q, k, v, a.o, a.qr, a.state, nullptr, 0, 0, 1.f, a.scale}, states ? a.work : nullptr, 0}}, 1, a.c, plan};
-  return launch_rows<D, uint16_t>(rows, a.stream);
+  return launch_rows<T, D, F32, T>(rows, a.stream);
 }
 
-template <int D>
+template <typename T, int D, bool F32>
 hipError_t chunked_bwd(const Args& a) {
   const int G = a.c.H / a.HK;
-  const Plan plan = plan_of(a.c.B, a.c.H, a.c.n, D, 3, 2);
+  const Plan plan = plan_of(a.c.B, a.c.H, a.c.n, D, chunk_of(a.dtype), 3, 2);
   const Role q{a.q, a.qr, 1}, k{a.k, a.kr, G}, v{a.v, a.kr, G}, dout{a.dout, a.qr, 1};
   const Layout lay = layout_of(a.dtype, a.c.B, a.c.H, a.HK, a.c.n, D, true);
   const bool states = plan.segs > 1 || a.dstate_in;
@@ -97,33 +97,33 @@ hipError_t chunked_bwd(const Args& a) {
   if (states) {
     const SumArgs sums{{{k, v, 0}, {q, dout, 1}}, 2, a.c, plan, a.work};
     const ScanArgs scan{{{a.state, nullptr, 0, 1.f, 0}, {a.dstate, a.dstate_in, 1, a.scale, 1}}, 2, a.c, plan, a.work, D * D};
-    if (hipError_t e = launch_states<D>(sums, scan, a.stream); e != hipSuccess) return e;
+    if (hipError_t e = launch_states<T, D, F32>(sums, scan, a.stream); e != hipSuccess) return e;
   }
   const RowPass dq{Pass{dout, v, k, a.dq, a.qr, a.state, nullptr, 1, 0, 1.f, a.scale}, s, 0};
   RowPass dv{Pass{k, q, dout, a.dv, a.kr, a.dstate, nullptr, 0, 1, a.scale, 1.f}, d, 1}, dk{Pass{v, dout, q, a.dk, a.kr, a.dstate, nullptr, 1, 1, a.scale, 1.f}, d, 1};
-  if (G == 1) return launch_rows<D, uint16_t>(RowArgs{{dq, dv, dk}, 3, a.c, plan}, a.stream);
-  if (hipError_t e = launch_rows<D, uint16_t>(RowArgs{{dq}, 1, a.c, plan}, a.stream); e != hipSuccess) return e;
+  if (G == 1) return launch_rows<T, D, F32, T>(RowArgs{{dq, dv, dk}, 3, a.c, plan}, a.stream);
+  if (hipError_t e = launch_rows<T, D, F32, T>(RowArgs{{dq}, 1, a.c, plan}, a.stream); e != hipSuccess) return e;
   for (RowPass* x : {&dv, &dk}) {
     void* to = x->p.o;
     x->p.o = a.work + lay.states;
     x->p.orow = Rows{(size_t)a.c.H * a.c.n * D, (size_t)a.c.n * D, (size_t)D};
-    if (hipError_t e = launch_rows<D, float>(RowArgs{{*x}, 1, a.c, plan}, a.stream); e != hipSuccess) return e;
-    if (hipError_t e = sum_heads<uint16_t, D>(a.work + lay.states, to, a); e != hipSuccess) return e;
+    if (hipError_t e = launch_rows<T, D, F32, float>(RowArgs{{*x}, 1, a.c, plan}, a.stream); e != hipSuccess) return e;
+    if (hipError_t e = sum_heads<T, D>(a.work + lay.states, to, a); e != hipSuccess) return e;
   }
   return hipSuccess;
 }
 
-template <typename T, int D>
+template <typename T, int D, bool F32>
 hipError_t fwd(const Args& a) {
-  if (a.dtype == LINATTN_BF16 && a.c.n > kStepTokens) return chunked_fwd<D>(a);
+  if (a.c.n > kStepTokens) return chunked_fwd<T, D, F32>(a);
   const int G = a.c.H / a.HK;
   Pass p{{a.q, a.qr, 1}, {a.k, a.kr, G}, {a.v, a.kr, G}, a.o, a.qr, a.state, a.state_out, 0, 0, 1.f, a.scale};
   return launch_step<T, T, D>(p, a.c, a.stream);
 }
 
-template <typename T, int D>
+template <typename T, int D, bool F32>
 hipError_t bwd(const Args& a) {
-  if (a.dtype == LINATTN_BF16 && a.c.n > kStepTokens) return chunked_bwd<D>(a);
+  if (a.c.n > kStepTokens) return chunked_bwd<T, D, F32>(a);
   const int G = a.c.H / a.HK;
   const Role q{a.q, a.qr, 1}, k{a.k, a.kr, G}, v{a.v, a.kr, G}, dout{a.dout, a.qr, 1};
   Common of_items = a.c;      // dS_out and dS_in are by item
@@ -154,12 +154,14 @@ size_t work_bytes(int dtype, int B, int H, int HK, int n, int d, bool backward) 
 }
 
 hipError_t launch_fwd(const Args& a) {
-  if (a.dtype == LINATTN_F32) return a.d == 64 ? fwd<float, 64>(a) : fwd<float, 128>(a);
-  return a.d == 64 ? fwd<uint16_t, 64>(a) : fwd<uint16_t, 128>(a);
+  if (a.dtype == LINATTN_F32) return a.d == 64 ? fwd<float, 64, true>(a) : fwd<float, 128, true>(a);
+  if (a.dtype == LINATTN_BF16_F32MATH) return a.d == 64 ? fwd<uint16_t, 64, true>(a) : fwd<uint16_t, 128, true>(a);
+  return a.d == 64 ? fwd<uint16_t, 64, false>(a) : fwd<uint16_t, 128, false>(a);
 }
 hipError_t launch_bwd(const Args& a) {
-  if (a.dtype == LINATTN_F32) return a.d == 64 ? bwd<float, 64>(a) : bwd<float, 128>(a);
-  return a.d == 64 ? bwd<uint16_t, 64>(a) : bwd<uint16_t, 128>(a);
+  if (a.dtype == LINATTN_F32) return a.d == 64 ? bwd<float, 64, true>(a) : bwd<float, 128, true>(a);
+  if (a.dtype == LINATTN_BF16_F32MATH) return a.d == 64 ? bwd<uint16_t, 64, true>(a) : bwd<uint16_t, 128, true>(a);
+  return a.d == 64 ? bwd<uint16_t, 64, false>(a) : bwd<uint16_t, 128, false>(a);
 }
 
 }  // namespace decay

@@ -1,0 +1,237 @@
+// The passes of decay.h in fp32 arithmetic, on v_mfma_f32_32x32x2_f32: fp32 tensors, and bf16 tensors widened on their way into LDS.  Chunks of kChunkF32 tokens; a wavefront has 32
+// columns of the state.
+//   lane l = (m, g), m = l % 32, g = l / 32.  A: A[m][g], B: B[g][m], D: rows 8 (r / 4) + 4 g + r % 4 of column m
+// so register r of an accumulator is, as it lies, the operand of a step over rows 8 (r / 4) + r % 4 and that + 4.
+#pragma once
+#include "decay_rows.h"
+
+namespace linattn {
+namespace decay {
+
+__device__ __forceinline__ f32x16 mfma_f32(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
+
+// Rows of a token tensor into an fp32 LDS tile [32][D], its 16-byte pieces swizzled by row, through registers: ask requests, put writes.  Rows from `end` on are row end - 1 again.
+template <typename T, int D>
+struct TileF32 {
+  static constexpr int NT = 2 * D, V = 16 / (int)sizeof(T), N = kChunkF32 * D / V / NT, WORDS = kChunkF32 * D;
+  const T* base;
+  size_t pitch;
+  uint4 x[N];
+  __device__ __forceinline__ void of(const Role& r, int b, int h) {
+    base = static_cast<const T*>(r.p) + (size_t)b * r.r.sb + (size_t)(h / r.group) * r.r.sh;
+    pitch = r.r.sn;
+  }
+  __device__ __forceinline__ void ask(int i0, int end, int len, bool back) {
+#pragma unroll
+    for (int y = 0; y < N; ++y) {
+      const int item = y * NT + threadIdx.x, row = item / (D / V), i = i0 + row < end ? i0 + row : end - 1;
+      x[y] = *reinterpret_cast<const uint4*>(base + (size_t)token_at(i, len, back) * pitch + item % (D / V) * V);
+    }
+  }
+  static __device__ __forceinline__ int word(int row, int c) { return row * D + (((c / 4) ^ (row % (D / 4))) * 4) + c % 4; }
+  __device__ __forceinline__ void put(float* tile) const {
+#pragma unroll
+    for (int y = 0; y < N; ++y) {
+      const int item = y * NT + threadIdx.x, row = item / (D / V), c = item % (D / V) * V;
+      float f[V];
+      if constexpr (V == 8) unpack_bf16x8(x[y], f);
+      else f32::unpack_f32x4(x[y], f);
+#pragma unroll
+      for (int e = 0; e < V; e += 4) *reinterpret_cast<float4*>(tile + word(row, c + e)) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+    }
+  }
+};
+
+__device__ __forceinline__ int row_of_reg(int r, int g) { return 8 * (r / 4) + 4 * g + r % 4; }
+
+// A segment's own sum, as decay_sum_kernel.
+template <typename T, int D>
+__global__ __launch_bounds__(2 * D) void decay_sum_f32_kernel(SumArgs a) {
+  using Tile_ = TileF32<T, D>;
+  constexpr int FB = D / 32, WORDS = Tile_::WORDS;
+  extern __shared__ __align__(16) float tiles[];
+  const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
+  const int pass = blockIdx.x % a.passes, at = blockIdx.x / a.passes, seg = at % a.plan.segs, bh = at / a.plan.segs, b = bh / a.c.H, h = bh % a.c.H;
+  const SumPass& p = a.pass[pass];
+  const int len = length_of(a.c, b), i0 = seg * a.plan.tokens, i1 = min(len, i0 + a.plan.tokens);
+  if (i0 >= i1) return;
+  const float decay = log_decay_of(a.c, h);
+  Tile_ rows, columns;
+  rows.of(p.b, b, h);
+  columns.of(p.c, b, h);
+  f32x16 sum[FB];
+#pragma unroll
+  for (int f = 0; f < FB; ++f) sum[f] = zero16();
+  auto ask = [&](int i) { rows.ask(i, i1, len, p.back); columns.ask(i, i1, len, p.back); };
+  auto put = [&](int buffer) { rows.put(tiles + buffer * 2 * WORDS); columns.put(tiles + buffer * 2 * WORDS + WORDS); };
+  ask(i0);
+  put(0);
+  for (int i = i0, buffer = 0; i < i1; i += kChunkF32, buffer ^= 1) {
+    __syncthreads();
+    const bool more = i + kChunkF32 < i1;
+    if (more) ask(i + kChunkF32);
+    const float *tb = tiles + buffer * 2 * WORDS, *tc = tb + WORDS;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int j = row_of_reg(r, g);
+      const float c = i + j < i1 ? tc[Tile_::word(j, 32 * w + m)] * expf(decay * (float)(i1 - 1 - i - j)) : 0.f;
+#pragma unroll
+      for (int f = 0; f < FB; ++f) sum[f] = mfma_f32(tb[Tile_::word(j, 32 * f + m)], c, sum[f]);
+    }
+    if (more) put(buffer ^ 1);
+  }
+  float* out = a.sums + (((size_t)pass * a.c.B * a.c.H + bh) * a.plan.segs + seg) * D * D;
+#pragma unroll
+  for (int f = 0; f < FB; ++f)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) out[(32 * f + row_of_reg(r, g)) * D + 32 * w + m] = sum[f][r];
+}
+
+// Rows of a segment, as decay_rows_kernel: every wavefront takes 32 channels of the scores a_i . b_j of all pairs, and their sum through LDS gives it all of them, where the product with c_j
+// wants them.
+template <typename T, int D, typename O>
+__global__ __launch_bounds__(2 * D, 1) void decay_rows_f32_kernel(RowArgs a) {
+  using Tile_ = TileF32<T, D>;
+  constexpr int NW = D / 32, FB = D / 32, WORDS = Tile_::WORDS;
+  extern __shared__ __align__(16) float tiles[];
+  float4* const parts = reinterpret_cast<float4*>(tiles + 6 * WORDS);      // [wavefront][4][64]: four registers
+  const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
+  const int pass = blockIdx.x % a.passes, at = blockIdx.x / a.passes, seg = at % a.plan.segs, bh = at / a.plan.segs, b = bh / a.c.H, h = bh % a.c.H;
+  const RowPass& rp = a.pass[pass];
+  const Pass& p = rp.p;
+  const int len = length_of(a.c, b), i0 = seg * a.plan.tokens, all = min(a.c.n, i0 + a.plan.tokens), i1 = min(len, all);
+  O* const out = static_cast<O*>(p.o) + (size_t)b * p.orow.sb + (size_t)h * p.orow.sh;
+  zero_rows<D, 2 * D>(out, p.orow.sn, max(i0, i1), all);
+  if (i0 >= i1) return;
+
+  Tile_ ta, tb, tc;
+  ta.of(p.a, b, h);
+  tb.of(p.b, b, h);
+  tc.of(p.c, b, h);
+  auto ask = [&](int i) { ta.ask(i, i1, len, p.back); tb.ask(i, i1, len, p.back); tc.ask(i, i1, len, p.back); };
+  auto put = [&](int buffer) {
+    float* to = tiles + buffer * 3 * WORDS;
+    ta.put(to);
+    tb.put(to + WORDS);
+    tc.put(to + 2 * WORDS);
+  };
+  ask(i0);
+  put(0);
+  const float decay = log_decay_of(a.c, h);
+  f32x16 x[FB];
+  load_state<D>(a, rp, bh, seg, decay, [&](auto get) {
+#pragma unroll
+    for (int f = 0; f < FB; ++f)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[f][r] = get(32 * f + row_of_reg(r, g), 32 * w + m);
+  });
+  float diag[16], keep[16];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int j = row_of_reg(r, g);
+    diag[r] = j <= m ? expf(decay * (float)(m - j)) * p.in_scale : 0.f;
+    keep[r] = expf(decay * (float)(kChunkF32 - j)) * p.in_scale;
+  }
+  const float mine = expf(decay * (float)m);
+  float hi, lo;
+  power_of(decay, kChunkF32, hi, lo);
+
+  for (int i = i0, buffer = 0; i < i1; i += kChunkF32, buffer ^= 1) {
+    __syncthreads();
+    const bool more = i + kChunkF32 < i1;
+    if (more) ask(i + kChunkF32);
+    const float *la = tiles + buffer * 3 * WORDS, *lb = la + WORDS, *lc = lb + WORDS;
+
+    f32x16 s = zero16();
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float4 kb = *reinterpret_cast<const float4*>(lb + Tile_::word(m, 32 * w + 8 * q + 4 * g)), qa = *reinterpret_cast<const float4*>(la + Tile_::word(m, 32 * w + 8 * q + 4 * g));
+      s = mfma_f32(kb.x, qa.x, s); s = mfma_f32(kb.y, qa.y, s); s = mfma_f32(kb.z, qa.z, s); s = mfma_f32(kb.w, qa.w, s);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) parts[(w * 4 + q) * 64 + lane] = make_float4(s[4 * q], s[4 * q + 1], s[4 * q + 2], s[4 * q + 3]);
+
+    f32x16 o;
+    auto before = [&] {
+      o = zero16();
+#pragma unroll
+      for (int f = 0; f < FB; ++f)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float4 qa = *reinterpret_cast<const float4*>(la + Tile_::word(m, 32 * f + 8 * q + 4 * g));
+          o = mfma_f32(x[f][4 * q], qa.x, o); o = mfma_f32(x[f][4 * q + 1], qa.y, o);
+          o = mfma_f32(x[f][4 * q + 2], qa.z, o); o = mfma_f32(x[f][4 * q + 3], qa.w, o);
+        }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[r] *= mine;
+    };
+    before();
+    float c[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) c[r] = lc[Tile_::word(row_of_reg(r, g), 32 * w + m)];
+    __syncthreads();
+    auto score = [&](int q, int from) {
+      float4 t = parts[q * 64 + from];
+#pragma unroll
+      for (int y = 1; y < NW; ++y) {
+        const float4 u = parts[(y * 4 + q) * 64 + from];
+        t.x += u.x; t.y += u.y; t.z += u.z; t.w += u.w;
+      }
+      return t;
+    };
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float4 t = score(q, lane);
+      const float e[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const int r = 4 * q + y;
+        o = mfma_f32(c[r], row_of_reg(r, g) <= m ? e[y] * diag[r] : 0.f, o);
+      }
+    }
+
+    // rows that are not finite once more, over what they see (see decay_rows_kernel)
+    float odd = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) odd = fmaf(o[r], 0.f, odd);
+    if (__any(odd != 0.f)) {
+      before();
+      for (int j = 0; j <= m; ++j) {
+        const float4 t = score(j / 8, 32 * (j / 4 % 2) + m);
+        const float wt = (j % 4 == 0 ? t.x : j % 4 == 1 ? t.y : j % 4 == 2 ? t.z : t.w) * (expf(decay * (float)(m - j)) * p.in_scale);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[r] = fmaf(wt, lc[Tile_::word(j, 32 * w + row_of_reg(r, g))], o[r]);
+      }
+    }
+    if (i + m < i1) {
+      O* to = out + (size_t)token_at(i + m, len, p.back) * p.orow.sn + 32 * w + 4 * g;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float4 v = make_float4(o[4 * q] * p.out_scale, o[4 * q + 1] * p.out_scale, o[4 * q + 2] * p.out_scale, o[4 * q + 3] * p.out_scale);
+        if constexpr (sizeof(O) == 2) *reinterpret_cast<uint2*>(to + 8 * q) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+        else *reinterpret_cast<float4*>(to + 8 * q) = v;
+      }
+    }
+    if (more) {
+#pragma unroll
+      for (int f = 0; f < FB; ++f)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[f][r] = fmaf(x[f][r], hi, x[f][r] * lo);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float cw = c[r] * keep[r];
+#pragma unroll
+        for (int f = 0; f < FB; ++f) x[f] = mfma_f32(lb[Tile_::word(row_of_reg(r, g), 32 * f + m)], cw, x[f]);
+      }
+      put(buffer ^ 1);
+    }
+  }
+}
+
+template <int D>
+constexpr int rows_f32_lds() { return 6 * kChunkF32 * D * 4 + D / 32 * 4096; }
+template <int D>
+constexpr int sum_f32_lds() { return 4 * kChunkF32 * D * 4; }
+
+}  // namespace decay
+}  // namespace linattn

@@ -106,7 +106,7 @@ __global__ __launch_bounds__(256, 2) void decay_sum_kernel(SumArgs a) {
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
   const int pass = blockIdx.x % a.passes, at = blockIdx.x / a.passes, seg = at % a.plan.segs, bh = at / a.plan.segs, b = bh / a.c.H, h = bh % a.c.H;
   const SumPass& p = a.pass[pass];
-  const int len = length_of(a.c, b), i0 = seg * a.plan.chunks * kChunk, i1 = min(len, i0 + a.plan.chunks * kChunk);
+  const int len = length_of(a.c, b), i0 = seg * a.plan.tokens, i1 = min(len, i0 + a.plan.tokens);
   if (i0 >= i1) return;
   const float decay = log_decay_of(a.c, h);
   Tile<D> rows, columns;
@@ -199,7 +199,7 @@ __global__ __launch_bounds__(256) void decay_scan_kernel(ScanArgs a) {
   const ScanPass& p = a.pass[pass];
   Common com = a.c;
   if (p.by_item) { com.slots = nullptr; com.states = com.B; }
-  const int len = length_of(com, b), step = a.plan.chunks * kChunk, live = (len + step - 1) / step;
+  const int len = length_of(com, b), step = a.plan.tokens, live = (len + step - 1) / step;
   const long long row = state_row(com, b, h);
   const float decay = log_decay_of(com, h), lambda = expf(decay);
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -248,6 +248,33 @@ struct RowArgs {
   Plan plan;
 };
 
+// Rows from..to-1 of a head's results: zeros, for padding.
+template <int D, int NT, typename O>
+__device__ __forceinline__ void zero_rows(O* out, size_t pitch, int from, int to) {
+  for (int i = from + threadIdx.x / (D / 8); i < to; i += NT / (D / 8)) {
+    uint4* z = reinterpret_cast<uint4*>(out + (size_t)i * pitch + threadIdx.x % (D / 8) * 8);
+    z[0] = make_uint4(0, 0, 0, 0);
+    if constexpr (sizeof(O) == 4) z[1] = make_uint4(0, 0, 0, 0);
+  }
+}
+
+// The state X in front of a segment: take(get), get(row, column).
+template <int D, typename Take>
+__device__ __forceinline__ void load_state(const RowArgs& a, const RowPass& rp, int bh, int seg, float decay, Take take) {
+  const float* from = rp.states ? rp.states + ((size_t)bh * a.plan.segs + seg) * D * D : nullptr;
+  float factor = 1.f;
+  if (!from && rp.p.in) {
+    Common com = a.c;
+    if (rp.by_item) { com.slots = nullptr; com.states = com.B; }
+    const long long row = state_row(com, bh / com.H, bh % com.H);
+    if (row >= 0) from = rp.p.in + row * D * D;
+    if (!rp.p.back) factor = expf(decay);
+  }
+  if (!from) take([](int, int) { return 0.f; });
+  else if (rp.p.turned) take([&](int row, int column) { return from[column * D + row] * factor; });
+  else take([&](int row, int column) { return from[row * D + column] * factor; });
+}
+
 constexpr int kUpdatePieces = 2;
 
 // Rows of a segment, chunk by chunk.  A wavefront has 32 columns of the state X in its accumulators, where they are the left operand of a_i X as they lie (rounded to bf16); the
@@ -261,15 +288,10 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void decay_rows_kernel(RowAr
   const RowPass& rp = a.pass[pass];
   const Pass& p = rp.p;
   const int seg = at % a.plan.segs;
-  const int len = length_of(a.c, b), i0 = seg * a.plan.chunks * kChunk, all = min(a.c.n, i0 + a.plan.chunks * kChunk), i1 = min(len, all);
+  const int len = length_of(a.c, b), i0 = seg * a.plan.tokens, all = min(a.c.n, i0 + a.plan.tokens), i1 = min(len, all);
   O* const out = static_cast<O*>(p.o) + (size_t)b * p.orow.sb + (size_t)h * p.orow.sh;
 
-  // padding: zeros, D values of a row by D / 8 threads
-  for (int i = max(i0, i1) + threadIdx.x / (D / 8); i < all; i += 256 / (D / 8)) {
-    uint4* z = reinterpret_cast<uint4*>(out + (size_t)i * p.orow.sn + threadIdx.x % (D / 8) * 8);
-    z[0] = make_uint4(0, 0, 0, 0);
-    if constexpr (sizeof(O) == 4) z[1] = make_uint4(0, 0, 0, 0);
-  }
+  zero_rows<D, 256>(out, p.orow.sn, max(i0, i1), all);
   if (i0 >= i1) return;
 
   Tile<D> ta, tb, tc;
@@ -288,24 +310,12 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void decay_rows_kernel(RowAr
   const int cb = w % CB, ib0 = w / CB * IB, column = 32 * cb + column_of(m);
   const float decay = log_decay_of(a.c, h);
   f32x16 x[FB];
-  {
-    const float* from = rp.states ? rp.states + ((size_t)bh * a.plan.segs + seg) * D * D : nullptr;
-    float factor = 1.f;
-    if (!from && p.in) {
-      Common com = a.c;
-      if (rp.by_item) { com.slots = nullptr; com.states = com.B; }
-      const long long row = state_row(com, b, h);
-      if (row >= 0) from = p.in + row * D * D;
-      if (!p.back) factor = expf(decay);
-    }
+  load_state<D>(a, rp, bh, seg, decay, [&](auto get) {
 #pragma unroll
     for (int f = 0; f < FB; ++f)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int row = 32 * f + 16 * (r / 8) + 8 * g + r % 8;
-        x[f][r] = from ? from[p.turned ? column * D + row : row * D + column] * factor : 0.f;
-      }
-  }
+      for (int r = 0; r < 16; ++r) x[f][r] = get(32 * f + 16 * (r / 8) + 8 * g + r % 8, column);
+  });
   // weights: of a pair in a 32 x 32 block on the diagonal, in the one left of it; of a token in the state behind the chunk; of the state in a row, and over a chunk
   float diag[16], left[16], keep[JS][8], mine[IB];
 #pragma unroll
