@@ -20,7 +20,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
 # always to the accumulation registers (measured on the query-side backward kernel when it used all 512
 # registers of a lane and spent a quarter of its vector instructions moving results between the two files:
 # 149 -> 134 us at 12 heads x 32760 x 128; neutral or slightly worse for the other files).
-EXTRA = dict.fromkeys(("bwd_bf16.hip", "bwd_bf16_stream.hip"), ["-mllvm", "-amdgpu-mfma-vgpr-form"])
+EXTRA = dict.fromkeys(("bwd_bf16.hip", "bwd_bf16_stream.hip", "decay.hip"), ["-mllvm", "-amdgpu-mfma-vgpr-form"])
 
 
 def build(verbose: bool = False) -> str:

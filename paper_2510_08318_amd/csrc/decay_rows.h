@@ -12,23 +12,35 @@ using attn::arrived;
 using attn::lds_loads_landed;
 using attn::load_to_lds;
 using attn::row_at;
-using attn::row_chunk;
 using attn::turned;
 
 // The token at place i of a pass's order; places behind the last token are padding.
 __device__ __forceinline__ int token_at(int i, int len, bool back) { return back && i < len ? len - 1 - i : i; }
 
-// Rows i0 .. i0 + 63 of the pass's order into an LDS tile [64][D], chunks of 16 bytes swizzled by row, by four wavefronts; rows from `end` on are row end - 1 again.
+// Rows i0 .. i0 + 63 of the pass's order into an LDS tile [64][D], chunks of 16 bytes swizzled by row, by four wavefronts; rows from `end` on are row end - 1 again.  Where a chunk is
+// whole, a lane's offsets from its first token in memory are the same for every chunk.
 template <int D>
 struct Tile {
   static constexpr int ROWS = 512 / D, N = kChunk / ROWS / 4, BYTES = kChunk * D * 2;
   const char* base;
   size_t pitch;
-  __device__ __forceinline__ void of(const Role& r, int b, int h) {
+  uint32_t offset[N];
+  __device__ __forceinline__ void of(const Role& r, int b, int h, bool back, int w, int lane) {
     base = static_cast<const char*>(r.p) + ((size_t)b * r.r.sb + (size_t)(h / r.group) * r.r.sh) * 2;
     pitch = r.r.sn * 2;
+#pragma unroll
+    for (int x = 0; x < N; ++x) {
+      const int row = (w * N + x) * ROWS + lane / (D / 8);
+      offset[x] = (uint32_t)(back ? kChunk - 1 - row : row) * (uint32_t)pitch + (uint32_t)(((lane % (D / 8)) ^ swz<D>(row)) * 16);
+    }
   }
   __device__ __forceinline__ void load(int i0, int end, int len, bool back, uint32_t lds, int w, int lane) const {
+    if (i0 + kChunk <= end) {
+      const char* from = base + (size_t)(back ? len - i0 - kChunk : i0) * pitch;
+#pragma unroll
+      for (int x = 0; x < N; ++x) load_to_lds(from, offset[x], lds + (uint32_t)((w * N + x) * 1024));
+      return;
+    }
 #pragma unroll
     for (int x = 0; x < N; ++x) {
       const int row = (w * N + x) * ROWS + lane / (D / 8), i = i0 + row < end ? i0 + row : end - 1;
@@ -54,22 +66,31 @@ __device__ __forceinline__ f32x16 zero16() {
   for (int r = 0; r < 16; ++r) z[r] = 0.f;
   return z;
 }
-__device__ __forceinline__ uint4 pack8(const f32x16& e, int h) {
-  return make_uint4(pack_bf16x2(e[8 * h], e[8 * h + 1]), pack_bf16x2(e[8 * h + 2], e[8 * h + 3]), pack_bf16x2(e[8 * h + 4], e[8 * h + 5]),
-                    pack_bf16x2(e[8 * h + 6], e[8 * h + 7]));
+__device__ __forceinline__ bf16x8 pack8(const f32x16& e, int h) {
+  u32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = pack_bf16x2(e[8 * h + 2 * i], e[8 * h + 2 * i + 1]);
+  return __builtin_bit_cast(bf16x8, r);
 }
-__device__ __forceinline__ f32x16 mfma(uint4 a, uint4 b, f32x16 c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
+__device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+
+// An operand at an LDS address.  (As a vector: a struct of four words is taken apart by the compiler and read in two halves or four quarters.)
+__device__ __forceinline__ bf16x8 operand_at(uint32_t at) {
+  typedef __attribute__((address_space(3))) const bf16x8* P;
+  return *(P)at;
 }
+// 16-byte chunks 2 ks + g of row row0 + m: see row_at
+template <int D>
+__device__ __forceinline__ bf16x8 row_operand(uint32_t at, int ks, int row0) { return operand_at((at ^ (uint32_t)(32 * ks)) + (uint32_t)(row0 * D * 2)); }
 
 // Row of a k-step's element e in lane group g, as the transposing reads give them.
 __device__ __forceinline__ constexpr int row_of(int e, int g) { return 8 * (e / 4) + 4 * g + e % 4; }
 
 // Rows times their weights, as the sum of PIECES bf16 numbers.
 template <int PIECES>
-__device__ __forceinline__ void weigh(uint4 x, const float* w, uint4 (&p)[PIECES]) {
-  const uint32_t in[4] = {x.x, x.y, x.z, x.w};
-  uint32_t out[PIECES][4];
+__device__ __forceinline__ void weigh(bf16x8 x, const float* w, bf16x8 (&p)[PIECES]) {
+  const u32x4 in = __builtin_bit_cast(u32x4, x);
+  u32x4 out[PIECES];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     float a = f32::lo_f32(in[i]) * w[2 * i], b = f32::hi_f32(in[i]) * w[2 * i + 1];
@@ -80,7 +101,7 @@ __device__ __forceinline__ void weigh(uint4 x, const float* w, uint4 (&p)[PIECES
     }
   }
 #pragma unroll
-  for (int j = 0; j < PIECES; ++j) p[j] = make_uint4(out[j][0], out[j][1], out[j][2], out[j][3]);
+  for (int j = 0; j < PIECES; ++j) p[j] = __builtin_bit_cast(bf16x8, out[j]);
 }
 
 // ---- a segment's own sum --------------------------------------------------------------------------------------------
@@ -110,8 +131,8 @@ __global__ __launch_bounds__(256, 2) void decay_sum_kernel(SumArgs a) {
   if (i0 >= i1) return;
   const float decay = log_decay_of(a.c, h);
   Tile<D> rows, columns;
-  rows.of(p.b, b, h);
-  columns.of(p.c, b, h);
+  rows.of(p.b, b, h, p.back, w, lane);
+  columns.of(p.c, b, h, p.back, w, lane);
   const uint32_t lds = lds_address(smem), from = turned_columns<D>(lane);
   const int cb = w % CB, fb0 = w / CB * BLOCKS;
   f32x16 sum[BLOCKS];
@@ -140,21 +161,22 @@ __global__ __launch_bounds__(256, 2) void decay_sum_kernel(SumArgs a) {
       float wt[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) wt[e] = rel[ks][e] * after;
-      uint4 x = __builtin_bit_cast(uint4, turned<D>(from + tile + TILE, cb, 16 * ks));
+      bf16x8 x = turned<D>(from + tile + TILE, cb, 16 * ks);
       if (!whole) {
-        uint32_t* v = reinterpret_cast<uint32_t*>(&x);
+        u32x4 v = __builtin_bit_cast(u32x4, x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int j = i + 16 * ks + row_of(e, g);
           wt[e] = j < i1 ? expf(decay * (float)(i1 - 1 - j)) : 0.f;
           if (j >= i1) v[e / 2] &= e % 2 ? 0xffffu : 0xffff0000u;
         }
+        x = __builtin_bit_cast(bf16x8, v);
       }
-      uint4 c[PIECES];
+      bf16x8 c[PIECES];
       weigh<PIECES>(x, wt, c);
 #pragma unroll
       for (int y = 0; y < BLOCKS; ++y) {
-        const uint4 r = __builtin_bit_cast(uint4, turned<D>(from + tile, fb0 + y, 16 * ks));
+        const bf16x8 r = turned<D>(from + tile, fb0 + y, 16 * ks);
 #pragma unroll
         for (int j = PIECES - 1; j >= 0; --j) sum[y] = mfma(r, c[j], sum[y]);
       }
@@ -275,7 +297,7 @@ __device__ __forceinline__ void load_state(const RowArgs& a, const RowPass& rp, 
   else take([&](int row, int column) { return from[row * D + column] * factor; });
 }
 
-constexpr int kUpdatePieces = 2;
+constexpr int kUpdatePieces = 2, kAhead = 6;      // kAhead: operands that are requested ahead of their products
 
 // Rows of a segment, chunk by chunk.  A wavefront has 32 columns of the state X in its accumulators, where they are the left operand of a_i X as they lie (rounded to bf16); the
 // chunk's weights P, on the lanes as S^T = B A^T gives them, are made by three of the wavefronts and go round through LDS.
@@ -295,9 +317,9 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void decay_rows_kernel(RowAr
   if (i0 >= i1) return;
 
   Tile<D> ta, tb, tc;
-  ta.of(p.a, b, h);
-  tb.of(p.b, b, h);
-  tc.of(p.c, b, h);
+  ta.of(p.a, b, h, p.back, w, lane);
+  tb.of(p.b, b, h, p.back, w, lane);
+  tc.of(p.c, b, h, p.back, w, lane);
   const uint32_t lds = lds_address(smem), weights = lds + 6 * TILE;
   auto ask = [&](int i, int buffer) {
     const uint32_t to = lds + buffer * 3 * TILE;
@@ -316,44 +338,51 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void decay_rows_kernel(RowAr
 #pragma unroll
       for (int r = 0; r < 16; ++r) x[f][r] = get(32 * f + 16 * (r / 8) + 8 * g + r % 8, column);
   });
-  // weights: of a pair in a 32 x 32 block on the diagonal, in the one left of it; of a token in the state behind the chunk; of the state in a row, and over a chunk
-  float diag[16], left[16], keep[JS][8], mine[IB];
+  // weights: of a pair in the wavefront's block; of a token in the state behind the chunk; of the state in a row, and over a chunk
+  float pairs[16], keep[JS][8], mine[IB];
+  const float pair_scale = p.in_scale * p.out_scale;      // (one of them is 1)
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
-    const int gap = m - row_of(r % 8, g) - 16 * (r / 8);
-    diag[r] = gap >= 0 ? expf(decay * (float)gap) * p.in_scale : 0.f;
-    left[r] = expf(decay * (float)(32 + gap)) * p.in_scale;
+    const int gap = m - row_of(r % 8, g) - 16 * (r / 8) + (w == 1 ? 32 : 0);
+    pairs[r] = gap >= 0 ? expf(decay * (float)gap) * pair_scale : 0.f;
   }
 #pragma unroll
   for (int ks = 0; ks < JS; ++ks)
 #pragma unroll
     for (int e = 0; e < 8; ++e) keep[ks][e] = expf(decay * (float)(kChunk - 16 * ks - row_of(e, g))) * p.in_scale;
 #pragma unroll
-  for (int i = 0; i < IB; ++i) mine[i] = expf(decay * (float)(32 * (ib0 + i) + m));
+  for (int i = 0; i < IB; ++i) mine[i] = expf(decay * (float)(32 * (ib0 + i) + m)) * p.out_scale;
   const float over = expf(decay * (float)kChunk);
 
   const uint32_t rows_at = row_at<D>(lane), columns_at = turned_columns<D>(lane);
+  uint32_t weights_at = weights + 16 * (uint32_t)lane;
+  asm volatile("" : "+v"(weights_at));      // (its constant part would not fit the offset of an LDS instruction)
   for (int i = i0, buffer = 0; i < i1; i += kChunk, buffer ^= 1) {
     lds_loads_landed();
     __syncthreads();
     const bool more = i + kChunk < i1;
     if (more) ask(i + kChunk, buffer ^ 1);
     const uint32_t la = lds + buffer * 3 * TILE, lb = la + TILE, lc = lb + TILE;
-    typedef __attribute__((address_space(3))) u32x4* P;
 
     // weights of block w: (0, 0), (1, 0), (1, 1) of rows and tokens
     if (w < 3) {
       const int ib = w > 0, jb = w == 2;
       f32x16 s = zero16();
+      bf16x8 op[2 * KS];
+      auto get = [&](int i) { op[i] = row_operand<D>(rows_at + (i % 2 ? la : lb), i / 2, 32 * (i % 2 ? ib : jb)); };
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) s = mfma(row_chunk<D>(rows_at + lb, ks, 32 * jb), row_chunk<D>(rows_at + la, ks, 32 * ib), s);
+      for (int i = 0; i < kAhead; ++i) get(i);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float wt = w == 1 ? left[r] : diag[r];
-        s[r] = w == 1 || row_of(r % 8, g) + 16 * (r / 8) <= m ? s[r] * wt : 0.f;
+      for (int ks = 0; ks < KS; ++ks) {
+        for (int i = 2 * ks + kAhead; i < 2 * ks + kAhead + 2 && i < 2 * KS; ++i) get(i);
+        __builtin_amdgcn_sched_barrier(0);
+        s = mfma(op[2 * ks], op[2 * ks + 1], s);
+        __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
-      for (int hh = 0; hh < 2; ++hh) *(P)(weights + (uint32_t)((2 * w + hh) * 1024 + 16 * lane)) = __builtin_bit_cast(u32x4, pack8(s, hh));
+      for (int r = 0; r < 16; ++r) s[r] = w == 1 || row_of(r % 8, g) + 16 * (r / 8) <= m ? s[r] * pairs[r] : 0.f;
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh) *(__attribute__((address_space(3))) bf16x8*)(weights_at + (uint32_t)((2 * w + hh) * 1024)) = pack8(s, hh);
     }
 
     // a_i X, and what lies before the chunk fades
@@ -361,11 +390,17 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void decay_rows_kernel(RowAr
     auto before = [&] {
 #pragma unroll
       for (int y = 0; y < IB; ++y) o[y] = zero16();
+      bf16x8 op[KS * IB], xs;
+      auto get = [&](int i) { op[i] = row_operand<D>(rows_at + la, i / IB, 32 * (ib0 + i % IB)); };
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const uint4 xs = pack8(x[ks / 2], ks % 2);
+      for (int i = 0; i < kAhead; ++i) get(i);
 #pragma unroll
-        for (int y = 0; y < IB; ++y) o[y] = mfma(xs, row_chunk<D>(rows_at + la, ks, 32 * (ib0 + y)), o[y]);
+      for (int i = 0; i < KS * IB; ++i) {
+        if (i + kAhead < KS * IB) get(i + kAhead);
+        __builtin_amdgcn_sched_barrier(0);
+        if (i % IB == 0) xs = pack8(x[i / IB / 2], i / IB % 2);
+        o[i % IB] = mfma(xs, op[i], o[i % IB]);
+        __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
       for (int y = 0; y < IB; ++y)
@@ -373,12 +408,12 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void decay_rows_kernel(RowAr
         for (int r = 0; r < 16; ++r) o[y][r] *= mine[y];
     };
     before();
-    uint4 c[JS];
+    bf16x8 c[JS];
 #pragma unroll
-    for (int ks = 0; ks < JS; ++ks) c[ks] = __builtin_bit_cast(uint4, turned<D>(columns_at + lc, cb, 16 * ks));
+    for (int ks = 0; ks < JS; ++ks) c[ks] = turned<D>(columns_at + lc, cb, 16 * ks);
     __syncthreads();
 
-    auto weight_block = [&](int blk, int hh) { return __builtin_bit_cast(uint4, *(P)(weights + (uint32_t)((2 * blk + hh) * 1024 + 16 * lane))); };
+    auto weight_block = [&](int blk, int hh) { return operand_at(weights_at + (uint32_t)((2 * blk + hh) * 1024)); };
 #pragma unroll
     for (int y = 0; y < IB; ++y) {
       const int ib = ib0 + y;
@@ -389,12 +424,17 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void decay_rows_kernel(RowAr
         for (int hh = 0; hh < 2; ++hh) o[y] = mfma(c[2 + hh], weight_block(2, hh), o[y]);
     }
 
-    // A weight of 0 does not keep an infinity or NaN of a later token out of a product: rows that are not finite once more, over what they see.
+    // A weight of 0 does not keep an infinity or NaN of a later token out of a product: where there is one, the chunk's pairs once more, over what a row sees.
     float odd = 0.f;
 #pragma unroll
-    for (int y = 0; y < IB; ++y)
+    for (int ks = 0; ks < JS; ++ks) {
+      const u32x4 words = __builtin_bit_cast(u32x4, c[ks]);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) odd = fmaf(o[y][r], 0.f, odd);
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t two = words[e];      // (the bit cast of a vector's element takes the first one's)
+        odd = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), __builtin_bit_cast(bf16x2, 0u), odd, false);
+      }
+    }
     if (__any(odd != 0.f)) {
       before();
       for (int y = 0; y < IB; ++y)
@@ -418,13 +458,10 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void decay_rows_kernel(RowAr
       O* to = out + (size_t)token_at(place, len, p.back) * p.orow.sn + 32 * cb + 8 * g;
 #pragma unroll
       for (int hh = 0; hh < 2; ++hh) {
-        f32x16 v;
-#pragma unroll
-        for (int r = 0; r < 8; ++r) v[r] = o[y][8 * hh + r] * p.out_scale;
-        if constexpr (sizeof(O) == 2) *reinterpret_cast<uint4*>(to + 16 * hh) = pack8(v, 0);
+        if constexpr (sizeof(O) == 2) *reinterpret_cast<bf16x8*>(to + 16 * hh) = pack8(o[y], hh);
         else {
-          *reinterpret_cast<float4*>(to + 16 * hh) = make_float4(v[0], v[1], v[2], v[3]);
-          *reinterpret_cast<float4*>(to + 16 * hh + 4) = make_float4(v[4], v[5], v[6], v[7]);
+          *reinterpret_cast<float4*>(to + 16 * hh) = make_float4(o[y][8 * hh], o[y][8 * hh + 1], o[y][8 * hh + 2], o[y][8 * hh + 3]);
+          *reinterpret_cast<float4*>(to + 16 * hh + 4) = make_float4(o[y][8 * hh + 4], o[y][8 * hh + 5], o[y][8 * hh + 6], o[y][8 * hh + 7]);
         }
       }
     }
@@ -436,11 +473,11 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void decay_rows_kernel(RowAr
         for (int r = 0; r < 16; ++r) x[f][r] *= over;
 #pragma unroll
       for (int ks = 0; ks < JS; ++ks) {
-        uint4 cw[kUpdatePieces];
+        bf16x8 cw[kUpdatePieces];
         weigh<kUpdatePieces>(c[ks], keep[ks], cw);
 #pragma unroll
         for (int f = 0; f < FB; ++f) {
-          const uint4 r = __builtin_bit_cast(uint4, turned<D>(columns_at + lb, f, 16 * ks));
+          const bf16x8 r = turned<D>(columns_at + lb, f, 16 * ks);
 #pragma unroll
           for (int j = kUpdatePieces - 1; j >= 0; --j) x[f] = mfma(r, cw[j], x[f]);
         }
