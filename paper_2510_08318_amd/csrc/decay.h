@@ -76,7 +76,7 @@ struct Plan {
 // The number of segments by a count of what each choice costs, in chunks of a workgroup of the rows kernel: as many rounds of resident workgroups as the call makes, and
 // with several segments the sums, which read two tensors of three, and two launches more.
 inline Plan plan_of(int B, int H, int n, int d, int chunk, int row_passes, int sum_passes) {
-  const long long chunks = (n + chunk - 1) / chunk, heads = (long long)B * H, slots = kCUs * (d == 128 ? 1 : 2);
+  const long long chunks = (n + chunk - 1) / chunk, heads = (long long)B * H, slots = kCUs * (chunk == kChunkF32 && d == 128 ? 1 : 2);
   Plan best{1, (int)chunks * chunk};
   double least = 0;
   for (long long want = 1; want <= chunks && want <= 256; ++want) {

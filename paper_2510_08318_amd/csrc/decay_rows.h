@@ -207,7 +207,7 @@ struct ScanArgs {
   int size;                 // D * D
 };
 
-// lambda^r as a sum of two fp32 numbers: rounded to one, the products along a sequence would be off by a multiple of its error.
+// lambda^r as a sum of two fp32 numbers: rounded to one, products along a sequence would be off by a multiple of its error.
 __device__ __forceinline__ void power_of(float decay, int r, float& hi, float& lo) {
   const double x = exp((double)decay * (double)r);
   hi = (float)x;
@@ -302,7 +302,7 @@ constexpr int kUpdatePieces = 2, kAhead = 6;      // kAhead: operands that are r
 // Rows of a segment, chunk by chunk.  A wavefront has 32 columns of the state X in its accumulators, where they are the left operand of a_i X as they lie (rounded to bf16); the
 // chunk's weights P, on the lanes as S^T = B A^T gives them, are made by three of the wavefronts and go round through LDS.
 template <int D, typename O>
-__global__ __launch_bounds__(256, D == 128 ? 1 : 2) void decay_rows_kernel(RowArgs a) {
+__global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
   constexpr int CB = D / 32, FB = D / 32, KS = D / 16, JS = kChunk / 16, IW = 4 / CB, IB = 2 / IW, TILE = Tile<D>::BYTES;
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
@@ -320,14 +320,15 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void decay_rows_kernel(RowAr
   ta.of(p.a, b, h, p.back, w, lane);
   tb.of(p.b, b, h, p.back, w, lane);
   tc.of(p.c, b, h, p.back, w, lane);
-  const uint32_t lds = lds_address(smem), weights = lds + 6 * TILE;
-  auto ask = [&](int i, int buffer) {
-    const uint32_t to = lds + buffer * 3 * TILE;
-    ta.load(i, i1, len, p.back, to, w, lane);
-    tb.load(i, i1, len, p.back, to + TILE, w, lane);
-    tc.load(i, i1, len, p.back, to + 2 * TILE, w, lane);
+  // in LDS: a chunk's a, its c, two of b; its pairs' weights; the weights that tokens have in the state behind a chunk
+  const uint32_t lds = lds_address(smem), la = lds, lc = lds + TILE, weights = lds + 4 * TILE, kept = weights + 6 * 1024;
+  auto b_tile = [&](int buffer) { return lds + (uint32_t)(2 + buffer) * TILE; };
+  auto ask_ac = [&](int i) {
+    ta.load(i, i1, len, p.back, la, w, lane);
+    tc.load(i, i1, len, p.back, lc, w, lane);
   };
-  ask(i0, 0);
+  tb.load(i0, i1, len, p.back, b_tile(0), w, lane);
+  ask_ac(i0);
 
   const int cb = w % CB, ib0 = w / CB * IB, column = 32 * cb + column_of(m);
   const float decay = log_decay_of(a.c, h);
@@ -339,17 +340,17 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void decay_rows_kernel(RowAr
       for (int r = 0; r < 16; ++r) x[f][r] = get(32 * f + 16 * (r / 8) + 8 * g + r % 8, column);
   });
   // weights: of a pair in the wavefront's block; of a token in the state behind the chunk; of the state in a row, and over a chunk
-  float pairs[16], keep[JS][8], mine[IB];
+  float pairs[16], mine[IB];
   const float pair_scale = p.in_scale * p.out_scale;      // (one of them is 1)
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
     const int gap = m - row_of(r % 8, g) - 16 * (r / 8) + (w == 1 ? 32 : 0);
     pairs[r] = gap >= 0 ? expf(decay * (float)gap) * pair_scale : 0.f;
   }
-#pragma unroll
-  for (int ks = 0; ks < JS; ++ks)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) keep[ks][e] = expf(decay * (float)(kChunk - 16 * ks - row_of(e, g))) * p.in_scale;
+  if (threadIdx.x < kChunk) {      // [k-step][g][8]
+    const int ks = threadIdx.x / 16, gg = threadIdx.x / 8 % 2, e = threadIdx.x % 8;
+    *(__attribute__((address_space(3))) float*)(kept + 4 * threadIdx.x) = expf(decay * (float)(kChunk - 16 * ks - row_of(e, gg))) * p.in_scale;
+  }
 #pragma unroll
   for (int i = 0; i < IB; ++i) mine[i] = expf(decay * (float)(32 * (ib0 + i) + m)) * p.out_scale;
   const float over = expf(decay * (float)kChunk);
@@ -361,8 +362,8 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void decay_rows_kernel(RowAr
     lds_loads_landed();
     __syncthreads();
     const bool more = i + kChunk < i1;
-    if (more) ask(i + kChunk, buffer ^ 1);
-    const uint32_t la = lds + buffer * 3 * TILE, lb = la + TILE, lc = lb + TILE;
+    if (more) tb.load(i + kChunk, i1, len, p.back, b_tile(buffer ^ 1), w, lane);
+    const uint32_t lb = b_tile(buffer);
 
     // weights of block w: (0, 0), (1, 0), (1, 1) of rows and tokens
     if (w < 3) {
@@ -387,7 +388,7 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void decay_rows_kernel(RowAr
 
     // a_i X, and what lies before the chunk fades
     f32x16 o[IB];
-    auto before = [&] {
+    {
 #pragma unroll
       for (int y = 0; y < IB; ++y) o[y] = zero16();
       bf16x8 op[KS * IB], xs;
@@ -406,25 +407,11 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void decay_rows_kernel(RowAr
       for (int y = 0; y < IB; ++y)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[y][r] *= mine[y];
-    };
-    before();
+    }
     bf16x8 c[JS];
 #pragma unroll
     for (int ks = 0; ks < JS; ++ks) c[ks] = turned<D>(columns_at + lc, cb, 16 * ks);
-    __syncthreads();
-
-    auto weight_block = [&](int blk, int hh) { return operand_at(weights_at + (uint32_t)((2 * blk + hh) * 1024)); };
-#pragma unroll
-    for (int y = 0; y < IB; ++y) {
-      const int ib = ib0 + y;
-#pragma unroll
-      for (int hh = 0; hh < 2; ++hh) o[y] = mfma(c[hh], weight_block(ib, hh), o[y]);
-      if (ib)
-#pragma unroll
-        for (int hh = 0; hh < 2; ++hh) o[y] = mfma(c[2 + hh], weight_block(2, hh), o[y]);
-    }
-
-    // A weight of 0 does not keep an infinity or NaN of a later token out of a product: where there is one, the chunk's pairs once more, over what a row sees.
+    // A weight of 0 does not keep an infinity or NaN of a later token out of a product: where there is one, the chunk's pairs one by one, over what a row sees.
     float odd = 0.f;
 #pragma unroll
     for (int ks = 0; ks < JS; ++ks) {
@@ -435,20 +422,31 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void decay_rows_kernel(RowAr
         odd = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), __builtin_bit_cast(bf16x2, 0u), odd, false);
       }
     }
-    if (__any(odd != 0.f)) {
-      before();
+    const bool one_by_one = __any(odd != 0.f);
+    __syncthreads();
+    if (more) ask_ac(i + kChunk);
+
+    if (!one_by_one) {
+      auto weight_block = [&](int blk, int hh) { return operand_at(weights_at + (uint32_t)((2 * blk + hh) * 1024)); };
+#pragma unroll
+      for (int y = 0; y < IB; ++y) {
+        const int ib = ib0 + y;
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) o[y] = mfma(c[hh], weight_block(ib, hh), o[y]);
+        if (ib)
+#pragma unroll
+          for (int hh = 0; hh < 2; ++hh) o[y] = mfma(c[2 + hh], weight_block(2, hh), o[y]);
+      }
+    } else {
       for (int y = 0; y < IB; ++y)
         for (int j = 0; j <= 32 * (ib0 + y) + m; ++j) {
           const int jj = j % 16, src = 32 * ((jj / 4) % 2) + m, elem = jj / 8 * 4 + jj % 4;
           const int blk = ib0 + y == 0 ? 0 : j < 32 ? 1 : 2;
           const uint32_t pw = weights + (uint32_t)((2 * blk + j % 32 / 16) * 1024 + 16 * src + 2 * elem);
           const float wt = __builtin_bit_cast(float, (uint32_t)*(__attribute__((address_space(3))) const uint16_t*)pw << 16);
+          const uint16_t* from = reinterpret_cast<const uint16_t*>(tc.base + (size_t)token_at(min(i + j, i1 - 1), len, p.back) * tc.pitch) + 32 * cb + 8 * g;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int ch = 32 * cb + 16 * (r / 8) + 8 * g + r % 8;
-            const uint32_t at = lc + (uint32_t)(j * (D * 2) + (((ch / 8) ^ swz<D>(j)) * 16) + ch % 8 * 2);
-            o[y][r] = fmaf(wt, __builtin_bit_cast(float, (uint32_t)*(__attribute__((address_space(3))) const uint16_t*)at << 16), o[y][r]);
-          }
+          for (int r = 0; r < 16; ++r) o[y][r] = fmaf(wt, f32::ldf(from, 16 * (r / 8) + r % 8), o[y][r]);
         }
     }
 #pragma unroll
@@ -474,7 +472,10 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void decay_rows_kernel(RowAr
 #pragma unroll
       for (int ks = 0; ks < JS; ++ks) {
         bf16x8 cw[kUpdatePieces];
-        weigh<kUpdatePieces>(c[ks], keep[ks], cw);
+        float keep[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) keep[e] = *(__attribute__((address_space(3))) const float*)(kept + (uint32_t)(64 * ks + 32 * g + 4 * e));
+        weigh<kUpdatePieces>(c[ks], keep, cw);
 #pragma unroll
         for (int f = 0; f < FB; ++f) {
           const bf16x8 r = turned<D>(columns_at + lb, f, 16 * ks);
@@ -487,7 +488,7 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void decay_rows_kernel(RowAr
 }
 
 template <int D>
-constexpr int rows_lds() { return 6 * Tile<D>::BYTES + 6 * 1024; }
+constexpr int rows_lds() { return 4 * Tile<D>::BYTES + 6 * 1024 + kChunk * 4; }
 template <int D>
 constexpr int sum_lds() { return 4 * Tile<D>::BYTES; }
 
