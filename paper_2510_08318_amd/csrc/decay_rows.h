@@ -10,42 +10,57 @@ namespace decay {
 
 using attn::arrived;
 using attn::lds_loads_landed;
-using attn::load_to_lds;
 using attn::row_at;
 using attn::turned;
+
+// attn::load_to_lds; STREAM: of data that will not be in the caches when it is read again.
+#define LINATTN_LDS_LOAD(LOAD) "s_mov_b32 m0, %0\n\ts_nop 0\n\t" LOAD
+template <bool STREAM>
+__device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t lds) {
+  if constexpr (STREAM) asm volatile(LINATTN_LDS_LOAD("global_load_lds_dwordx4 %1, %2 nt") ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0");
+  else attn::load_to_lds(base, offset, lds);
+}
+template <bool STREAM>
+__device__ __forceinline__ void load_to_lds(const void* at, uint32_t lds) {
+  if constexpr (STREAM) asm volatile(LINATTN_LDS_LOAD("global_load_lds_dwordx4 %1, off nt") ::"s"(lds), "v"(at) : "memory", "m0");
+  else attn::load_to_lds(at, lds);
+}
+#undef LINATTN_LDS_LOAD
 
 // The token at place i of a pass's order; places behind the last token are padding.
 __device__ __forceinline__ int token_at(int i, int len, bool back) { return back && i < len ? len - 1 - i : i; }
 
 // Rows i0 .. i0 + 63 of the pass's order into an LDS tile [64][D], chunks of 16 bytes swizzled by row, by four wavefronts; rows from `end` on are row end - 1 again.  Where a chunk is
-// whole, a lane's offsets from its first token in memory are the same for every chunk.
-template <int D>
+// whole, a lane's offset from its first token in memory is the same for every chunk, and its loads differ by a multiple of the pitch (from the base, a scalar) and in the swizzle.
+template <int D, bool STREAM>
 struct Tile {
   static constexpr int ROWS = 512 / D, N = kChunk / ROWS / 4, BYTES = kChunk * D * 2;
   const char* base;
   size_t pitch;
-  uint32_t offset[N];
+  uint32_t offset;
   __device__ __forceinline__ void of(const Role& r, int b, int h, bool back, int w, int lane) {
     base = static_cast<const char*>(r.p) + ((size_t)b * r.r.sb + (size_t)(h / r.group) * r.r.sh) * 2;
     pitch = r.r.sn * 2;
-#pragma unroll
-    for (int x = 0; x < N; ++x) {
-      const int row = (w * N + x) * ROWS + lane / (D / 8);
-      offset[x] = (uint32_t)(back ? kChunk - 1 - row : row) * (uint32_t)pitch + (uint32_t)(((lane % (D / 8)) ^ swz<D>(row)) * 16);
-    }
+    const int row = w * N * ROWS + lane / (D / 8);
+    offset = (uint32_t)(back ? kChunk - 1 - row : row) * (uint32_t)pitch + (uint32_t)(((lane % (D / 8)) ^ swz<D>(row)) * 16);
   }
   __device__ __forceinline__ void load(int i0, int end, int len, bool back, uint32_t lds, int w, int lane) const {
     if (i0 + kChunk <= end) {
-      const char* from = base + (size_t)(back ? len - i0 - kChunk : i0) * pitch;
+      const uint64_t first = reinterpret_cast<uint64_t>(base) + (size_t)(back ? len - i0 - kChunk : i0) * pitch, step = back ? -(uint64_t)(ROWS * pitch) : (uint64_t)(ROWS * pitch);
+      // (The value is the same in all lanes, but the compiler may work it out in vector registers.  A scalar that a vector instruction wrote may be an address five wait states later, which
+      // the compiler does not look after in assembly.)
+      uint64_t at = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(first >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)first);
+      asm volatile("s_nop 4" : "+s"(at));
+      const char* from = reinterpret_cast<const char*>(at);
 #pragma unroll
-      for (int x = 0; x < N; ++x) load_to_lds(from, offset[x], lds + (uint32_t)((w * N + x) * 1024));
+      for (int x = 0; x < N; ++x, from += step) load_to_lds<STREAM>(from, offset ^ (uint32_t)(swz<D>(ROWS * x) * 16), lds + (uint32_t)((w * N + x) * 1024));
       return;
     }
 #pragma unroll
     for (int x = 0; x < N; ++x) {
       const int row = (w * N + x) * ROWS + lane / (D / 8), i = i0 + row < end ? i0 + row : end - 1;
       const char* at = base + (size_t)token_at(i, len, back) * pitch + (((lane % (D / 8)) ^ swz<D>(row)) * 16);
-      load_to_lds(at, lds + (uint32_t)((w * N + x) * 1024));
+      load_to_lds<STREAM>(at, lds + (uint32_t)((w * N + x) * 1024));
     }
   }
 };
@@ -59,6 +74,8 @@ template <int D>
 __device__ __forceinline__ uint32_t turned_columns(int lane) {
   return (uint32_t)tr_lane<D, 4>((unsigned)((lane & ~3) | ((lane & 1) << 1) | ((lane & 2) >> 1)));
 }
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ f32x16 zero16() {
   f32x16 z;
@@ -79,9 +96,11 @@ __device__ __forceinline__ bf16x8 operand_at(uint32_t at) {
   typedef __attribute__((address_space(3))) const bf16x8* P;
   return *(P)at;
 }
-// 16-byte chunks 2 ks + g of row row0 + m: see row_at
-template <int D>
-__device__ __forceinline__ bf16x8 row_operand(uint32_t at, int ks, int row0) { return operand_at((at ^ (uint32_t)(32 * ks)) + (uint32_t)(row0 * D * 2)); }
+// A value that the compiler cannot see through here: of an LDS address and a constant, the sum is then made in the instruction, and not kept (or made again and again) in a register
+// of its own.
+__device__ __forceinline__ void hide(uint32_t& x) { asm volatile("" : "+v"(x)); }
+// An operand by the transposing reads from the addresses of its first 8 and its other 8 rows
+__device__ __forceinline__ bf16x8 turned_at2(uint32_t lo, uint32_t hi) { return __builtin_bit_cast(bf16x8, read_tr(lo, hi)); }
 
 // Row of a k-step's element e in lane group g, as the transposing reads give them.
 __device__ __forceinline__ constexpr int row_of(int e, int g) { return 8 * (e / 4) + 4 * g + e % 4; }
@@ -120,17 +139,17 @@ struct SumArgs {
 
 // sum_j lambda^(end - 1 - j) b_j^T c_j over a segment's tokens, end: the first behind them.  The rows c_j enter with their weights, whole, as three bf16 pieces (PIECES 3), where a
 // state is handed out; b_j is bf16 as it is, so that the sum is one of exact products in fp32.
-template <int D, int PIECES>
+template <int D, int PIECES, bool STREAM>
 __global__ __launch_bounds__(256, 2) void decay_sum_kernel(SumArgs a) {
-  constexpr int CB = D / 32, BLOCKS = CB * CB / 4, KS = kChunk / 16, TILE = Tile<D>::BYTES;
+  constexpr int CB = D / 32, BLOCKS = CB * CB / 4, KS = kChunk / 16, TILE = Tile<D, false>::BYTES;
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
   const int pass = blockIdx.x % a.passes, at = blockIdx.x / a.passes, seg = at % a.plan.segs, bh = at / a.plan.segs, b = bh / a.c.H, h = bh % a.c.H;
   const SumPass& p = a.pass[pass];
-  const int len = length_of(a.c, b), i0 = seg * a.plan.tokens, i1 = min(len, i0 + a.plan.tokens);
+  const int len = __builtin_amdgcn_readfirstlane(length_of(a.c, b)), i0 = seg * a.plan.tokens, i1 = min(len, i0 + a.plan.tokens);
   if (i0 >= i1) return;
   const float decay = log_decay_of(a.c, h);
-  Tile<D> rows, columns;
+  Tile<D, STREAM> rows, columns;
   rows.of(p.b, b, h, p.back, w, lane);
   columns.of(p.c, b, h, p.back, w, lane);
   const uint32_t lds = lds_address(smem), from = turned_columns<D>(lane);
@@ -214,46 +233,42 @@ __device__ __forceinline__ void power_of(float decay, int r, float& hi, float& l
   lo = (float)(x - (double)hi);
 }
 
-// Four elements of a head's state a thread, segment after segment: X in front of segment s (as decay.h has it: out's and dq's times lambda) takes the place of its
+// Two elements of a head's state a thread, segment after segment: X in front of segment s (as decay.h has it: out's and dq's times lambda) takes the place of its
 // sum, X' = lambda^tokens X + lambda sum.
 __global__ __launch_bounds__(256) void decay_scan_kernel(ScanArgs a) {
-  const int pass = blockIdx.z, bh = blockIdx.y, b = bh / a.c.H, h = bh % a.c.H, e = (blockIdx.x * 256 + threadIdx.x) * 4;
+  const int pass = blockIdx.z, bh = blockIdx.y, b = bh / a.c.H, h = bh % a.c.H, e = (blockIdx.x * 256 + threadIdx.x) * 2;
   const ScanPass& p = a.pass[pass];
   Common com = a.c;
   if (p.by_item) { com.slots = nullptr; com.states = com.B; }
   const int len = length_of(com, b), step = a.plan.tokens, live = (len + step - 1) / step;
   const long long row = state_row(com, b, h);
   const float decay = log_decay_of(com, h), lambda = expf(decay);
-  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (p.in && row >= 0) x = *reinterpret_cast<const float4*>(p.in + row * a.size + e);
-  if (!p.back && len > 0) { x.x *= lambda; x.y *= lambda; x.z *= lambda; x.w *= lambda; }
-  float4* at = reinterpret_cast<float4*>(a.sums + ((size_t)pass * a.c.B * a.c.H + bh) * a.plan.segs * a.size + e);
-  const size_t next = a.size / 4;
-  float hi, lo;
-  power_of(decay, step, hi, lo);
+  f32x2 x = {0.f, 0.f};
+  if (p.in && row >= 0) x = *reinterpret_cast<const f32x2*>(p.in + row * a.size + e);
+  if (!p.back && len > 0) x *= lambda;
+  f32x2* at = reinterpret_cast<f32x2*>(a.sums + ((size_t)pass * a.c.B * a.c.H + bh) * a.plan.segs * a.size + e);
+  const size_t next = a.size / 2;
   const float first = p.in_scale * lambda;
-  auto move = [&](float& y, float s) { y = fmaf(y, hi, fmaf(y, lo, first * s)); };
-  constexpr int AHEAD = 4;
+  float hi, lo, last_hi, last_lo;
+  power_of(decay, step, hi, lo);
+  // behind the last token: forward S_n = lambda^(tokens - 1) X + sum, back lambda^tokens X + lambda sum
+  const int tokens = len - (live - 1) * step;
+  power_of(decay, p.back ? tokens : tokens - 1, last_hi, last_lo);
+  constexpr int AHEAD = 8;
   for (int s0 = 0; s0 < live; s0 += AHEAD) {
-    float4 sum[AHEAD];
+    f32x2 sum[AHEAD];
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) sum[i] = s0 + i < live ? at[(s0 + i) * next] : make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < AHEAD; ++i) sum[i] = s0 + i < live ? at[(s0 + i) * next] : f32x2{0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
       if (s0 + i >= live) break;
       at[(s0 + i) * next] = x;
-      if (s0 + i == live - 1) {
-        // behind the last token: forward S_n = lambda^(tokens - 1) X + sum, back lambda^tokens X + lambda sum
-        const int tokens = len - (live - 1) * step;
-        float h1, l1;
-        power_of(decay, p.back ? tokens : tokens - 1, h1, l1);
-        const float f = p.back ? first : p.in_scale;
-        x.x = fmaf(x.x, h1, fmaf(x.x, l1, f * sum[i].x)); x.y = fmaf(x.y, h1, fmaf(x.y, l1, f * sum[i].y));
-        x.z = fmaf(x.z, h1, fmaf(x.z, l1, f * sum[i].z)); x.w = fmaf(x.w, h1, fmaf(x.w, l1, f * sum[i].w));
-      } else { move(x.x, sum[i].x); move(x.y, sum[i].y); move(x.z, sum[i].z); move(x.w, sum[i].w); }
+      const bool last = s0 + i == live - 1;
+      const float f = last && !p.back ? p.in_scale : first, m = last ? last_hi : hi, l = last ? last_lo : lo;
+      for (int y = 0; y < 2; ++y) x[y] = fmaf(x[y], m, fmaf(x[y], l, f * sum[i][y]));
     }
   }
-  if (p.out && row >= 0) *reinterpret_cast<float4*>(p.out + row * a.size + e) = x;
+  if (p.out && row >= 0) *reinterpret_cast<f32x2*>(p.out + row * a.size + e) = x;
 }
 
 // ---- rows -----------------------------------------------------------------------------------------------------------
@@ -303,20 +318,20 @@ constexpr int kUpdatePieces = 2, kAhead = 6;      // kAhead: operands that are r
 // chunk's weights P, on the lanes as S^T = B A^T gives them, are made by three of the wavefronts and go round through LDS.
 template <int D, typename O>
 __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
-  constexpr int CB = D / 32, FB = D / 32, KS = D / 16, JS = kChunk / 16, IW = 4 / CB, IB = 2 / IW, TILE = Tile<D>::BYTES;
+  constexpr int CB = D / 32, FB = D / 32, KS = D / 16, JS = kChunk / 16, IW = 4 / CB, IB = 2 / IW, TILE = Tile<D, false>::BYTES;
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
   const int pass = blockIdx.x % a.passes, at = blockIdx.x / a.passes, bh = at / a.plan.segs, b = bh / a.c.H, h = bh % a.c.H;
   const RowPass& rp = a.pass[pass];
   const Pass& p = rp.p;
   const int seg = at % a.plan.segs;
-  const int len = length_of(a.c, b), i0 = seg * a.plan.tokens, all = min(a.c.n, i0 + a.plan.tokens), i1 = min(len, all);
+  const int len = __builtin_amdgcn_readfirstlane(length_of(a.c, b)), i0 = seg * a.plan.tokens, all = min(a.c.n, i0 + a.plan.tokens), i1 = min(len, all);
   O* const out = static_cast<O*>(p.o) + (size_t)b * p.orow.sb + (size_t)h * p.orow.sh;
 
   zero_rows<D, 256>(out, p.orow.sn, max(i0, i1), all);
   if (i0 >= i1) return;
 
-  Tile<D> ta, tb, tc;
+  Tile<D, false> ta, tb, tc;
   ta.of(p.a, b, h, p.back, w, lane);
   tb.of(p.b, b, h, p.back, w, lane);
   tc.of(p.c, b, h, p.back, w, lane);
@@ -355,22 +370,40 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
   for (int i = 0; i < IB; ++i) mine[i] = expf(decay * (float)(32 * (ib0 + i) + m)) * p.out_scale;
   const float over = expf(decay * (float)kChunk);
 
-  const uint32_t rows_at = row_at<D>(lane), columns_at = turned_columns<D>(lane);
-  uint32_t weights_at = weights + 16 * (uint32_t)lane;
-  asm volatile("" : "+v"(weights_at));      // (its constant part would not fit the offset of an LDS instruction)
-  for (int i = i0, buffer = 0; i < i1; i += kChunk, buffer ^= 1) {
+  // Addresses in the tile of a, and so, with constants that fit an instruction, in the others: 16-byte pieces 2 ks + g of row m; first and second 8 rows of a block's columns, transposed.
+  uint32_t rows_at[KS], columns_at[FB][2], c_at[2], weights_at = weights + 16 * (uint32_t)lane, kept_at = kept + 32 * (uint32_t)g;
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) rows_at[ks] = la + (row_at<D>(lane) ^ (uint32_t)(32 * ks));
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+#pragma unroll
+    for (int f = 0; f < FB; ++f) columns_at[f][x] = la + (turned_columns<D>(lane) ^ (uint32_t)(64 * f + 32 * x));
+    c_at[x] = lc + (turned_columns<D>(lane) ^ (uint32_t)(64 * cb + 32 * x));
+  }
+  const uint32_t pair_rows = (uint32_t)((w > 0) * 32 * D * 2), pair_tokens = (uint32_t)((w == 2) * 32 * D * 2);
+  auto chunk = [&](int i, auto buffer_) {
+    constexpr int buffer = decltype(buffer_)::value;
+    constexpr uint32_t lb = (uint32_t)(2 + buffer) * TILE;      // from la
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) hide(rows_at[ks]);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+#pragma unroll
+      for (int f = 0; f < FB; ++f) hide(columns_at[f][x]);
+      hide(c_at[x]);
+    }
+    hide(weights_at);
+    hide(kept_at);
     lds_loads_landed();
     __syncthreads();
     const bool more = i + kChunk < i1;
     if (more) tb.load(i + kChunk, i1, len, p.back, b_tile(buffer ^ 1), w, lane);
-    const uint32_t lb = b_tile(buffer);
 
     // weights of block w: (0, 0), (1, 0), (1, 1) of rows and tokens
     if (w < 3) {
-      const int ib = w > 0, jb = w == 2;
       f32x16 s = zero16();
       bf16x8 op[2 * KS];
-      auto get = [&](int i) { op[i] = row_operand<D>(rows_at + (i % 2 ? la : lb), i / 2, 32 * (i % 2 ? ib : jb)); };
+      auto get = [&](int i) { op[i] = operand_at((rows_at[i / 2] + (i % 2 ? pair_rows : pair_tokens)) + (i % 2 ? 0 : lb)); };
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) get(i);
 #pragma unroll
@@ -392,7 +425,7 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
 #pragma unroll
       for (int y = 0; y < IB; ++y) o[y] = zero16();
       bf16x8 op[KS * IB], xs;
-      auto get = [&](int i) { op[i] = row_operand<D>(rows_at + la, i / IB, 32 * (ib0 + i % IB)); };
+      auto get = [&](int i) { op[i] = operand_at(rows_at[i / IB] + (uint32_t)((ib0 + i % IB) * 32 * D * 2)); };
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) get(i);
 #pragma unroll
@@ -410,7 +443,7 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
     }
     bf16x8 c[JS];
 #pragma unroll
-    for (int ks = 0; ks < JS; ++ks) c[ks] = turned<D>(columns_at + lc, cb, 16 * ks);
+    for (int ks = 0; ks < JS; ++ks) c[ks] = turned_at2(c_at[0] + (uint32_t)(16 * ks * D * 2), c_at[1] + (uint32_t)((16 * ks + 8) * D * 2));
     // A weight of 0 does not keep an infinity or NaN of a later token out of a product: where there is one, the chunk's pairs one by one, over what a row sees.
     float odd = 0.f;
 #pragma unroll
@@ -438,6 +471,7 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
           for (int hh = 0; hh < 2; ++hh) o[y] = mfma(c[2 + hh], weight_block(2, hh), o[y]);
       }
     } else {
+#pragma unroll
       for (int y = 0; y < IB; ++y)
         for (int j = 0; j <= 32 * (ib0 + y) + m; ++j) {
           const int jj = j % 16, src = 32 * ((jj / 4) % 2) + m, elem = jj / 8 * 4 + jj % 4;
@@ -474,23 +508,31 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
         bf16x8 cw[kUpdatePieces];
         float keep[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) keep[e] = *(__attribute__((address_space(3))) const float*)(kept + (uint32_t)(64 * ks + 32 * g + 4 * e));
+        for (int half = 0; half < 2; ++half) {
+          const f32x4 four = *(__attribute__((address_space(3))) const f32x4*)(kept_at + (uint32_t)(64 * ks + 16 * half));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) keep[4 * half + e] = four[e];
+        }
         weigh<kUpdatePieces>(c[ks], keep, cw);
 #pragma unroll
         for (int f = 0; f < FB; ++f) {
-          const bf16x8 r = turned<D>(columns_at + lb, f, 16 * ks);
+          const bf16x8 r = turned_at2(columns_at[f][0] + lb + (uint32_t)(16 * ks * D * 2), columns_at[f][1] + lb + (uint32_t)((16 * ks + 8) * D * 2));
 #pragma unroll
           for (int j = kUpdatePieces - 1; j >= 0; --j) x[f] = mfma(r, cw[j], x[f]);
         }
       }
     }
+  };
+  for (int i = i0; i < i1; i += 2 * kChunk) {
+    chunk(i, std::integral_constant<int, 0>{});
+    if (i + kChunk < i1) chunk(i + kChunk, std::integral_constant<int, 1>{});
   }
 }
 
 template <int D>
-constexpr int rows_lds() { return 4 * Tile<D>::BYTES + 6 * 1024 + kChunk * 4; }
+constexpr int rows_lds() { return 4 * Tile<D, false>::BYTES + 6 * 1024 + kChunk * 4; }
 template <int D>
-constexpr int sum_lds() { return 4 * Tile<D>::BYTES; }
+constexpr int sum_lds() { return 4 * Tile<D, false>::BYTES; }
 
 }  // namespace decay
 }  // namespace linattn
