@@ -32,7 +32,7 @@ int check_decay(const linattn_decay_desc* w, decay::Args* a, DecaySizes* z) {
   if (!w->log_decay) return LINATTN_E_NULL;
   if (misaligned(w->log_decay, 4) || misaligned(w->lengths, 4) || misaligned(w->slots, 4)) return LINATTN_E_ALIGN;
   *a = decay::Args{};
-  a->c = decay::Common{w->log_decay, w->lengths, w->slots, w->slots ? w->states : w->B, w->B, w->H, w->n};
+  a->c = decay::Common{w->log_decay, w->lengths, w->slots, w->slots ? w->states : w->B, w->B, w->H, w->H / w->HK, w->n};
   a->HK = w->HK; a->d = w->d; a->dtype = w->dtype;
   a->qr = token_rows(w->H, w->n, w->d, w->layout == LINATTN_LAYOUT_BHND);
   a->kr = token_rows(w->HK, w->n, w->d, w->layout == LINATTN_LAYOUT_BHND);

@@ -26,8 +26,9 @@ struct Role {
 };
 struct Pass {
   Role a, b, c;
-  void* o;                  // of query heads, as the tensors or (part) fp32 [B, H, n, d]
+  void* o;                  // rows of query heads, in the tensors' type, or (part) in fp32 [B, H, n, d]
   Rows orow;
+  int part;
   const float* in;          // state, nullable: zeros
   float* out;               // nullable; not of a turned pass
   int turned, back;         // back: from the last token to the first
@@ -37,7 +38,7 @@ struct Common {
   const float* log_decay;   // [H]
   const int* lengths;       // [B], nullable
   const int* slots;         // [B], nullable: row of an item in the state tensors
-  int states, B, H, n;
+  int states, B, H, group, n;      // group: query heads to a key head
 };
 
 // A head's decay as the kernels use it: what is above 0, or NaN, counts as 0, and -inf as a number whose products with distances stay finite.
@@ -46,6 +47,18 @@ __host__ __device__ inline int length_of(const Common& c, int b) {
   if (!c.lengths) return c.n;
   const int x = c.lengths[b];
   return x < 0 ? 0 : x < c.n ? x : c.n;
+}
+// Workgroup id -> its segment of a pass of a query head.  The workgroups that read the same rows at the same time, of the passes and of the query heads of a group, follow each other on one XCD
+// (ids go to the XCDs in turn).  A pass that goes back has its segments in the other order, over the same tokens where the sequence fills them.
+struct Place {
+  int pass, b, h, seg;
+};
+__device__ __forceinline__ Place place_of(const Common& c, int id, int segs, int passes) {
+  const int members = passes * c.group, heads = c.H / c.group, units = c.B * heads * segs, even = units / kXCDs * kXCDs;
+  const bool mapped = id < even * members;
+  const int i = mapped ? id / kXCDs : id - even * members;
+  const int unit = mapped ? i / members * kXCDs + id % kXCDs : even + i / members, member = i % members, bk = unit / segs;
+  return {member % passes, bk / heads, bk % heads * c.group + member / passes, unit % segs};
 }
 // Row of item b, head h in the state tensors; -1 where its slot is none.
 __device__ __forceinline__ long long state_row(const Common& c, int b, int h) {

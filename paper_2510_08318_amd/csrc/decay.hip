@@ -7,28 +7,47 @@ namespace linattn {
 namespace decay {
 namespace {
 
-// fp32 parts of dk (or dv) of the query heads of a group -> their sum, in order, in the tensor's type.  Four channels a thread.
+// fp32 parts of dv and dk (blockIdx.z) of the query heads of a group -> their sums, in order, in the tensors' type.  Four channels a thread.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void sum_heads_kernel(const float* parts, T* to, Rows r, int HK, int G, int n) {
+__global__ __launch_bounds__(256) void sum_heads_kernel(const float* parts, T* dv, T* dk, Rows r, int HK, int G, int n) {
   const long long i = (long long)blockIdx.x * (256 / (D / 4)) + threadIdx.x / (D / 4);
   const int c = threadIdx.x % (D / 4) * 4, b = blockIdx.y;
   if (i >= (long long)HK * n) return;
   const int h = (int)(i / n), t = (int)(i % n);
+  const size_t head = (size_t)n * D;
+  const float* from = parts + ((size_t)(blockIdx.z * gridDim.y + b) * HK + h) * G * head + (size_t)t * D + c;
   float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int g = 0; g < G; ++g) {
-    const float4 x = *reinterpret_cast<const float4*>(parts + (((size_t)b * HK * G + (size_t)h * G + g) * n + t) * D + c);
+  for (int g = 0; g < G; ++g, from += head) {
+    const float4 x = *reinterpret_cast<const float4*>(from);
     sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
   }
-  T* at = to + (size_t)b * r.sb + (size_t)h * r.sh + (size_t)t * r.sn + c;
+  T* at = (blockIdx.z ? dk : dv) + (size_t)b * r.sb + (size_t)h * r.sh + (size_t)t * r.sn + c;
   if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(at) = make_uint2(pack_bf16x2(sum.x, sum.y), pack_bf16x2(sum.z, sum.w));
   else *reinterpret_cast<float4*>(at) = sum;
 }
 
 template <typename T, int D>
-hipError_t sum_heads(const float* parts, void* to, const Args& a) {
+hipError_t sum_heads(const float* parts, const Args& a) {
   const int rows = 256 / (D / 4);
-  sum_heads_kernel<T, D><<<dim3((unsigned)(((long long)a.HK * a.c.n + rows - 1) / rows), a.c.B), 256, 0, a.stream>>>(parts, static_cast<T*>(to), a.kr, a.HK, a.c.H / a.HK, a.c.n);
+  sum_heads_kernel<T, D><<<dim3((unsigned)(((long long)a.HK * a.c.n + rows - 1) / rows), a.c.B, 2), 256, 0, a.stream>>>(parts, static_cast<T*>(a.dv), static_cast<T*>(a.dk), a.kr, a.HK, a.c.H / a.HK,
+                                                                                                                    a.c.n);
   return hipGetLastError();
+}
+
+// The three passes of the backward, and where those of shared key heads put their parts: fp32 [dv, dk][B, H, n, d].
+template <int D>
+void backward_passes(const Args& a, float* parts, Pass& dq, Pass& dv, Pass& dk) {
+  const int G = a.c.group;
+  const Role q{a.q, a.qr, 1}, k{a.k, a.kr, G}, v{a.v, a.kr, G}, dout{a.dout, a.qr, 1};
+  dq = Pass{dout, v, k, a.dq, a.qr, 0, a.state, nullptr, 1, 0, 1.f, a.scale};
+  dv = Pass{k, q, dout, a.dv, a.kr, 0, a.dstate, a.dstate_in, 0, 1, a.scale, 1.f};
+  dk = Pass{v, dout, q, a.dk, a.kr, 0, a.dstate, nullptr, 1, 1, a.scale, 1.f};
+  if (G == 1) return;
+  const size_t all = (size_t)a.c.B * a.c.H * a.c.n * D;
+  dv.o = parts;
+  dk.o = parts + all;
+  dv.part = dk.part = 1;
+  dv.orow = dk.orow = Rows{(size_t)a.c.H * a.c.n * D, (size_t)a.c.n * D, (size_t)D};
 }
 
 // Tokens up to which the recurrence is taken token by token.
@@ -36,12 +55,12 @@ constexpr int kStepTokens = 16;
 
 constexpr int chunk_of(int dtype) { return dtype == LINATTN_BF16 ? kChunk : kChunkF32; }
 struct Layout {             // of the workspace, in floats
-  size_t states, parts;     // all states; dk or dv of all query heads
+  size_t states, parts;     // all states; dv and dk of all query heads
 };
 Layout layout_of(int dtype, int B, int H, int HK, int n, int d, bool backward) {
   Layout r{0, 0};
   if (n > kStepTokens) r.states = (size_t)plan_of(B, H, n, d, chunk_of(dtype), backward ? 3 : 1, backward ? 2 : 1).segs * (backward ? 2 : 1) * B * H * d * d;
-  if (backward && H != HK) r.parts = (size_t)B * H * n * d;
+  if (backward && H != HK) r.parts = 2 * (size_t)B * H * n * d;
   return r;
 }
 
@@ -51,11 +70,11 @@ hipError_t launch(const A& args, const Common& c, const Plan& plan, int passes, 
   KERNEL<<<(unsigned)(c.B * c.H * plan.segs * passes), threads, smem, s>>>(args);
   return hipGetLastError();
 }
-// T: the tensors' type; F32: fp32 arithmetic; O: the results'
-template <typename T, int D, bool F32, typename O>
+// T: the tensors' type; F32: fp32 arithmetic
+template <typename T, int D, bool F32>
 hipError_t launch_rows(const RowArgs& r, hipStream_t s) {
-  if constexpr (F32) return launch<&decay_rows_f32_kernel<T, D, O>>(r, r.c, r.plan, r.passes, 2 * D, rows_f32_lds<D>(), s);
-  else return launch<&decay_rows_kernel<D, O>>(r, r.c, r.plan, r.passes, 256, rows_lds<D>(), s);
+  if constexpr (F32) return launch<&decay_rows_f32_kernel<T, D>>(r, r.c, r.plan, r.passes, 2 * D, rows_f32_lds<D>(), s);
+  else return launch<&decay_rows_kernel<D>>(r, r.c, r.plan, r.passes, 256, rows_lds<D>(), s);
 }
 template <typename T, int D, bool F32>
 hipError_t launch_states(const SumArgs& sums, const ScanArgs& scan, hipStream_t s) {
@@ -79,7 +98,7 @@ hipError_t launch_states(const SumArgs& sums, const ScanArgs& scan, hipStream_t 
 
 template <typename T, int D, bool F32>
 hipError_t chunked_fwd(const Args& a) {
-  const int G = a.c.H / a.HK;
+  const int G = a.c.group;
   const Plan plan = plan_of(a.c.B, a.c.H, a.c.n, D, chunk_of(a.dtype), 1, 1);
   const Role q{a.q, a.qr, 1}, k{a.k, a.kr, G}, v{a.v, a.kr, G};
   const bool states = plan.segs > 1 || a.state_out;
@@ -88,13 +107,13 @@ hipError_t chunked_fwd(const Args& a) {
     const ScanArgs scan{{{a.state, a.state_out, 0, 1.f, 0}}, 1, a.c, plan, a.work, D * D};
     if (hipError_t e = launch_states<T, D, F32>(sums, scan, a.stream); e != hipSuccess) return e;
   }
-  const RowArgs rows{{{Pass{q, k, v, a.o, a.qr, a.state, nullptr, 0, 0, 1.f, a.scale}, states ? a.work : nullptr, 0}}, 1, a.c, plan};
-  return launch_rows<T, D, F32, T>(rows, a.stream);
+  const RowArgs rows{{{Pass{q, k, v, a.o, a.qr, 0, a.state, nullptr, 0, 0, 1.f, a.scale}, states ? a.work : nullptr, 0}}, 1, a.c, plan};
+  return launch_rows<T, D, F32>(rows, a.stream);
 }
 
 template <typename T, int D, bool F32>
 hipError_t chunked_bwd(const Args& a) {
-  const int G = a.c.H / a.HK;
+  const int G = a.c.group;
   const Plan plan = plan_of(a.c.B, a.c.H, a.c.n, D, chunk_of(a.dtype), 3, 2);
   const Role q{a.q, a.qr, 1}, k{a.k, a.kr, G}, v{a.v, a.kr, G}, dout{a.dout, a.qr, 1};
   const Layout lay = layout_of(a.dtype, a.c.B, a.c.H, a.HK, a.c.n, D, true);
@@ -106,51 +125,32 @@ hipError_t chunked_bwd(const Args& a) {
     const ScanArgs scan{{{a.state, nullptr, 0, 1.f, 0}, {a.dstate, a.dstate_in, 1, a.scale, 1}}, 2, a.c, plan, a.work, D * D};
     if (hipError_t e = launch_states<T, D, F32>(sums, scan, a.stream); e != hipSuccess) return e;
   }
-  const RowPass dq{Pass{dout, v, k, a.dq, a.qr, a.state, nullptr, 1, 0, 1.f, a.scale}, s, 0};
-  RowPass dv{Pass{k, q, dout, a.dv, a.kr, a.dstate, nullptr, 0, 1, a.scale, 1.f}, d, 1}, dk{Pass{v, dout, q, a.dk, a.kr, a.dstate, nullptr, 1, 1, a.scale, 1.f}, d, 1};
-  if (G == 1) return launch_rows<T, D, F32, T>(RowArgs{{dq, dv, dk}, 3, a.c, plan}, a.stream);
-  if (hipError_t e = launch_rows<T, D, F32, T>(RowArgs{{dq}, 1, a.c, plan}, a.stream); e != hipSuccess) return e;
-  for (RowPass* x : {&dv, &dk}) {
-    void* to = x->p.o;
-    x->p.o = a.work + lay.states;
-    x->p.orow = Rows{(size_t)a.c.H * a.c.n * D, (size_t)a.c.n * D, (size_t)D};
-    if (hipError_t e = launch_rows<T, D, F32, float>(RowArgs{{*x}, 1, a.c, plan}, a.stream); e != hipSuccess) return e;
-    if (hipError_t e = sum_heads<T, D>(a.work + lay.states, to, a); e != hipSuccess) return e;
-  }
-  return hipSuccess;
+  float* const parts = a.work + lay.states;
+  RowArgs rows{{{{}, s, 0}, {{}, d, 1}, {{}, d, 1}}, 3, a.c, plan};
+  backward_passes<D>(a, parts, rows.pass[0].p, rows.pass[1].p, rows.pass[2].p);
+  if (hipError_t e = launch_rows<T, D, F32>(rows, a.stream); e != hipSuccess || G == 1) return e;
+  return sum_heads<T, D>(parts, a);
 }
 
 template <typename T, int D, bool F32>
 hipError_t fwd(const Args& a) {
   if (a.c.n > kStepTokens) return chunked_fwd<T, D, F32>(a);
-  const int G = a.c.H / a.HK;
-  Pass p{{a.q, a.qr, 1}, {a.k, a.kr, G}, {a.v, a.kr, G}, a.o, a.qr, a.state, a.state_out, 0, 0, 1.f, a.scale};
-  return launch_step<T, T, D>(p, a.c, a.stream);
+  const int G = a.c.group;
+  return launch_step<T, D>(Pass{{a.q, a.qr, 1}, {a.k, a.kr, G}, {a.v, a.kr, G}, a.o, a.qr, 0, a.state, a.state_out, 0, 0, 1.f, a.scale}, a.c, a.stream);
 }
 
 template <typename T, int D, bool F32>
 hipError_t bwd(const Args& a) {
   if (a.c.n > kStepTokens) return chunked_bwd<T, D, F32>(a);
-  const int G = a.c.H / a.HK;
-  const Role q{a.q, a.qr, 1}, k{a.k, a.kr, G}, v{a.v, a.kr, G}, dout{a.dout, a.qr, 1};
   Common of_items = a.c;      // dS_out and dS_in are by item
   of_items.slots = nullptr;
   of_items.states = a.c.B;
-  hipError_t e = launch_step<T, T, D>(Pass{dout, v, k, a.dq, a.qr, a.state, nullptr, 1, 0, 1.f, a.scale}, a.c, a.stream);
-  if (e != hipSuccess) return e;
-  Pass dv{k, q, dout, a.dv, a.kr, a.dstate, a.dstate_in, 0, 1, a.scale, 1.f}, dk{v, dout, q, a.dk, a.kr, a.dstate, nullptr, 1, 1, a.scale, 1.f};
-  if (G == 1) {
-    e = launch_step<T, T, D>(dv, of_items, a.stream);
-    return e != hipSuccess ? e : launch_step<T, T, D>(dk, of_items, a.stream);
-  }
-  for (Pass* p : {&dv, &dk}) {
-    void* to = p->o;
-    p->o = a.work;
-    p->orow = Rows{(size_t)a.c.H * a.c.n * D, (size_t)a.c.n * D, (size_t)D};
-    if ((e = launch_step<T, float, D>(*p, of_items, a.stream)) != hipSuccess) return e;
-    if ((e = sum_heads<T, D>(a.work, to, a)) != hipSuccess) return e;
-  }
-  return e;
+  Pass dq, dv, dk;
+  backward_passes<D>(a, a.work, dq, dv, dk);
+  hipError_t e = launch_step<T, D>(dq, a.c, a.stream);
+  if (e == hipSuccess) e = launch_step<T, D>(dv, of_items, a.stream);
+  if (e == hipSuccess) e = launch_step<T, D>(dk, of_items, a.stream);
+  return e != hipSuccess || a.c.group == 1 ? e : sum_heads<T, D>(a.work, a);
 }
 
 }  // namespace

@@ -51,8 +51,9 @@ __global__ __launch_bounds__(2 * D) void decay_sum_f32_kernel(SumArgs a) {
   constexpr int FB = D / 32, WORDS = Tile_::WORDS;
   extern __shared__ __align__(16) float tiles[];
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
-  const int pass = blockIdx.x % a.passes, at = blockIdx.x / a.passes, seg = at % a.plan.segs, bh = at / a.plan.segs, b = bh / a.c.H, h = bh % a.c.H;
-  const SumPass& p = a.pass[pass];
+  const Place at = place_of(a.c, blockIdx.x, a.plan.segs, a.passes);
+  const SumPass& p = a.pass[at.pass];
+  const int pass = at.pass, b = at.b, h = at.h, bh = b * a.c.H + h, seg = p.back ? a.plan.segs - 1 - at.seg : at.seg;
   const int len = length_of(a.c, b), i0 = seg * a.plan.tokens, i1 = min(len, i0 + a.plan.tokens);
   if (i0 >= i1) return;
   const float decay = log_decay_of(a.c, h);
@@ -89,19 +90,20 @@ __global__ __launch_bounds__(2 * D) void decay_sum_f32_kernel(SumArgs a) {
 
 // Rows of a segment, as decay_rows_kernel: every wavefront takes 32 channels of the scores a_i . b_j of all pairs, and their sum through LDS gives it all of them, where the product with c_j
 // wants them.
-template <typename T, int D, typename O>
+template <typename T, int D>
 __global__ __launch_bounds__(2 * D, 1) void decay_rows_f32_kernel(RowArgs a) {
   using Tile_ = TileF32<T, D>;
   constexpr int NW = D / 32, FB = D / 32, WORDS = Tile_::WORDS;
   extern __shared__ __align__(16) float tiles[];
   float4* const parts = reinterpret_cast<float4*>(tiles + 6 * WORDS);      // [wavefront][4][64]: four registers
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
-  const int pass = blockIdx.x % a.passes, at = blockIdx.x / a.passes, seg = at % a.plan.segs, bh = at / a.plan.segs, b = bh / a.c.H, h = bh % a.c.H;
-  const RowPass& rp = a.pass[pass];
+  const Place at = place_of(a.c, blockIdx.x, a.plan.segs, a.passes);
+  const RowPass& rp = a.pass[at.pass];
   const Pass& p = rp.p;
+  const int b = at.b, h = at.h, bh = b * a.c.H + h, seg = p.back ? a.plan.segs - 1 - at.seg : at.seg;
   const int len = length_of(a.c, b), i0 = seg * a.plan.tokens, all = min(a.c.n, i0 + a.plan.tokens), i1 = min(len, all);
-  O* const out = static_cast<O*>(p.o) + (size_t)b * p.orow.sb + (size_t)h * p.orow.sh;
-  zero_rows<D, 2 * D>(out, p.orow.sn, max(i0, i1), all);
+  const Results<T> out(p, b, h);
+  zero_rows<D, 2 * D>(out, max(i0, i1), all);
   if (i0 >= i1) return;
 
   Tile_ ta, tb, tc;
@@ -204,12 +206,13 @@ __global__ __launch_bounds__(2 * D, 1) void decay_rows_f32_kernel(RowArgs a) {
       }
     }
     if (i + m < i1) {
-      O* to = out + (size_t)token_at(i + m, len, p.back) * p.orow.sn + 32 * w + 4 * g;
+      const int token = token_at(i + m, len, p.back);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
+        const int ch = 32 * w + 4 * g + 8 * q;
         const float4 v = make_float4(o[4 * q] * p.out_scale, o[4 * q + 1] * p.out_scale, o[4 * q + 2] * p.out_scale, o[4 * q + 3] * p.out_scale);
-        if constexpr (sizeof(O) == 2) *reinterpret_cast<uint2*>(to + 8 * q) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
-        else *reinterpret_cast<float4*>(to + 8 * q) = v;
+        if (sizeof(T) == 4 || out.part) *reinterpret_cast<float4*>(out.part_row(token, ch)) = v;
+        else *reinterpret_cast<uint2*>(out.row(token, ch)) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
       }
     }
     if (more) {

@@ -144,8 +144,9 @@ __global__ __launch_bounds__(256, 2) void decay_sum_kernel(SumArgs a) {
   constexpr int CB = D / 32, BLOCKS = CB * CB / 4, KS = kChunk / 16, TILE = Tile<D, false>::BYTES;
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
-  const int pass = blockIdx.x % a.passes, at = blockIdx.x / a.passes, seg = at % a.plan.segs, bh = at / a.plan.segs, b = bh / a.c.H, h = bh % a.c.H;
-  const SumPass& p = a.pass[pass];
+  const Place at = place_of(a.c, blockIdx.x, a.plan.segs, a.passes);
+  const SumPass& p = a.pass[at.pass];
+  const int pass = at.pass, b = at.b, h = at.h, bh = b * a.c.H + h, seg = p.back ? a.plan.segs - 1 - at.seg : at.seg;
   const int len = __builtin_amdgcn_readfirstlane(length_of(a.c, b)), i0 = seg * a.plan.tokens, i1 = min(len, i0 + a.plan.tokens);
   if (i0 >= i1) return;
   const float decay = log_decay_of(a.c, h);
@@ -285,13 +286,28 @@ struct RowArgs {
   Plan plan;
 };
 
+// A head's results, in the tensors' type or as fp32 parts: eight (fp32 tensors: four) adjacent channels of a token.
+template <typename T>
+struct Results {
+  void* base;
+  size_t pitch;
+  bool part;
+  __device__ __forceinline__ Results(const Pass& p, int b, int h) : pitch(p.orow.sn), part(p.part) {
+    const size_t at = (size_t)b * p.orow.sb + (size_t)h * p.orow.sh;
+    base = part ? (void*)(static_cast<float*>(p.o) + at) : (void*)(static_cast<T*>(p.o) + at);
+  }
+  __device__ __forceinline__ float* part_row(int token, int c) const { return static_cast<float*>(base) + (size_t)token * pitch + c; }
+  __device__ __forceinline__ T* row(int token, int c) const { return static_cast<T*>(base) + (size_t)token * pitch + c; }
+};
+
 // Rows from..to-1 of a head's results: zeros, for padding.
-template <int D, int NT, typename O>
-__device__ __forceinline__ void zero_rows(O* out, size_t pitch, int from, int to) {
+template <int D, int NT, typename T>
+__device__ __forceinline__ void zero_rows(const Results<T>& out, int from, int to) {
   for (int i = from + threadIdx.x / (D / 8); i < to; i += NT / (D / 8)) {
-    uint4* z = reinterpret_cast<uint4*>(out + (size_t)i * pitch + threadIdx.x % (D / 8) * 8);
+    const int c = threadIdx.x % (D / 8) * 8;
+    uint4* z = reinterpret_cast<uint4*>(out.part ? (void*)out.part_row(i, c) : (void*)out.row(i, c));
     z[0] = make_uint4(0, 0, 0, 0);
-    if constexpr (sizeof(O) == 4) z[1] = make_uint4(0, 0, 0, 0);
+    if (sizeof(T) == 4 || out.part) z[1] = make_uint4(0, 0, 0, 0);
   }
 }
 
@@ -316,19 +332,18 @@ constexpr int kUpdatePieces = 2, kAhead = 6;      // kAhead: operands that are r
 
 // Rows of a segment, chunk by chunk.  A wavefront has 32 columns of the state X in its accumulators, where they are the left operand of a_i X as they lie (rounded to bf16); the
 // chunk's weights P, on the lanes as S^T = B A^T gives them, are made by three of the wavefronts and go round through LDS.
-template <int D, typename O>
+template <int D>
 __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
   constexpr int CB = D / 32, FB = D / 32, KS = D / 16, JS = kChunk / 16, IW = 4 / CB, IB = 2 / IW, TILE = Tile<D, false>::BYTES;
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
-  const int pass = blockIdx.x % a.passes, at = blockIdx.x / a.passes, bh = at / a.plan.segs, b = bh / a.c.H, h = bh % a.c.H;
-  const RowPass& rp = a.pass[pass];
+  const Place at = place_of(a.c, blockIdx.x, a.plan.segs, a.passes);
+  const RowPass& rp = a.pass[at.pass];
   const Pass& p = rp.p;
-  const int seg = at % a.plan.segs;
+  const int b = at.b, h = at.h, bh = b * a.c.H + h, seg = p.back ? a.plan.segs - 1 - at.seg : at.seg;
   const int len = __builtin_amdgcn_readfirstlane(length_of(a.c, b)), i0 = seg * a.plan.tokens, all = min(a.c.n, i0 + a.plan.tokens), i1 = min(len, all);
-  O* const out = static_cast<O*>(p.o) + (size_t)b * p.orow.sb + (size_t)h * p.orow.sh;
-
-  zero_rows<D, 256>(out, p.orow.sn, max(i0, i1), all);
+  const Results<uint16_t> out(p, b, h);
+  zero_rows<D, 256>(out, max(i0, i1), all);
   if (i0 >= i1) return;
 
   Tile<D, false> ta, tb, tc;
@@ -487,14 +502,14 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
     for (int y = 0; y < IB; ++y) {
       const int place = i + 32 * (ib0 + y) + m;
       if (place >= i1) continue;
-      O* to = out + (size_t)token_at(place, len, p.back) * p.orow.sn + 32 * cb + 8 * g;
+      const int token = token_at(place, len, p.back);
 #pragma unroll
       for (int hh = 0; hh < 2; ++hh) {
-        if constexpr (sizeof(O) == 2) *reinterpret_cast<bf16x8*>(to + 16 * hh) = pack8(o[y], hh);
-        else {
-          *reinterpret_cast<float4*>(to + 16 * hh) = make_float4(o[y][8 * hh], o[y][8 * hh + 1], o[y][8 * hh + 2], o[y][8 * hh + 3]);
-          *reinterpret_cast<float4*>(to + 16 * hh + 4) = make_float4(o[y][8 * hh + 4], o[y][8 * hh + 5], o[y][8 * hh + 6], o[y][8 * hh + 7]);
-        }
+        const int ch = 32 * cb + 8 * g + 16 * hh;
+        if (!out.part) *reinterpret_cast<bf16x8*>(out.row(token, ch)) = pack8(o[y], hh);
+        else
+#pragma unroll
+          for (int e = 0; e < 8; e += 4) *reinterpret_cast<f32x4*>(out.part_row(token, ch + e)) = f32x4{o[y][8 * hh + e], o[y][8 * hh + e + 1], o[y][8 * hh + e + 2], o[y][8 * hh + e + 3]};
       }
     }
 

@@ -31,7 +31,7 @@ __device__ __forceinline__ void load_run(const T* p, float (&f)[N]) {
 
 // A workgroup has COLS columns of a state: a thread four of them, in ROWS rows.  The rows' products are summed over the lanes that share columns, then over the
 // four wavefronts through LDS.
-template <typename T, typename O, int D, int COLS>
+template <typename T, int D, int COLS>
 __global__ __launch_bounds__(256) void decay_step_kernel(Pass p, Common com) {
   constexpr int CG = COLS / 4, RG = 256 / CG, ROWS = D / RG;
   __shared__ __align__(16) float red[2][4][COLS];
@@ -43,7 +43,12 @@ __global__ __launch_bounds__(256) void decay_step_kernel(Pass p, Common com) {
   const T* pa = static_cast<const T*>(p.a.p) + (size_t)b * p.a.r.sb + (size_t)(h / p.a.group) * p.a.r.sh + f0;
   const T* pb = static_cast<const T*>(p.b.p) + (size_t)b * p.b.r.sb + (size_t)(h / p.b.group) * p.b.r.sh + f0;
   const T* pc = static_cast<const T*>(p.c.p) + (size_t)b * p.c.r.sb + (size_t)(h / p.c.group) * p.c.r.sh + c0 + 4 * cg;
-  O* po = static_cast<O*>(p.o) + (size_t)b * p.orow.sb + (size_t)h * p.orow.sh + c0;
+  const size_t po = (size_t)b * p.orow.sb + (size_t)h * p.orow.sh + c0;
+  auto put = [&](int t, float v) {
+    const size_t i = po + (size_t)t * p.orow.sn + tid;
+    if (p.part) static_cast<float*>(p.o)[i] = v;
+    else f32::stf(static_cast<T*>(p.o), i, v);
+  };
 
   float s[ROWS][4];
   if (p.in && at >= 0) {
@@ -66,11 +71,11 @@ __global__ __launch_bounds__(256) void decay_step_kernel(Pass p, Common com) {
   }
 
   for (int i = 0; i < len; ++i) {
-    const size_t t = p.back ? len - 1 - i : i;
+    const int t = p.back ? len - 1 - i : i;
     float fa[ROWS], fb[ROWS], fc[4], o[4] = {0.f, 0.f, 0.f, 0.f};
-    load_run<ROWS>(pa + t * p.a.r.sn, fa);
-    load_run<ROWS>(pb + t * p.b.r.sn, fb);
-    load_run<4>(pc + t * p.c.r.sn, fc);
+    load_run<ROWS>(pa + (size_t)t * p.a.r.sn, fa);
+    load_run<ROWS>(pb + (size_t)t * p.b.r.sn, fb);
+    load_run<4>(pc + (size_t)t * p.c.r.sn, fc);
     const float decay = p.back && i == 0 ? 1.f : lambda;
 #pragma unroll
     for (int r = 0; r < ROWS; ++r)
@@ -85,10 +90,10 @@ __global__ __launch_bounds__(256) void decay_step_kernel(Pass p, Common com) {
       for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], x);
     if (lane < CG) *reinterpret_cast<float4*>(&red[i % 2][w][4 * cg]) = make_float4(o[0], o[1], o[2], o[3]);
     __syncthreads();
-    if (tid < COLS) f32::stf(po + t * p.orow.sn, tid, p.out_scale * ((red[i % 2][0][tid] + red[i % 2][1][tid]) + (red[i % 2][2][tid] + red[i % 2][3][tid])));
+    if (tid < COLS) put(t, p.out_scale * ((red[i % 2][0][tid] + red[i % 2][1][tid]) + (red[i % 2][2][tid] + red[i % 2][3][tid])));
   }
   for (int t = len; t < com.n; ++t)
-    if (tid < COLS) f32::stf(po + (size_t)t * p.orow.sn, tid, 0.f);
+    if (tid < COLS) put(t, 0.f);
 
   if (p.out && at >= 0) {
     const float last = p.back && len > 0 ? lambda : 1.f;
@@ -99,10 +104,10 @@ __global__ __launch_bounds__(256) void decay_step_kernel(Pass p, Common com) {
   }
 }
 
-template <typename T, typename O, int D>
+template <typename T, int D>
 hipError_t launch_step(const Pass& p, const Common& c, hipStream_t s) {
-  if ((long long)c.B * c.H >= 2 * kCUs) decay_step_kernel<T, O, D, D><<<dim3(c.H, c.B), 256, 0, s>>>(p, c);
-  else decay_step_kernel<T, O, D, 32><<<dim3(c.H * (D / 32), c.B), 256, 0, s>>>(p, c);
+  if ((long long)c.B * c.H >= 2 * kCUs) decay_step_kernel<T, D, D><<<dim3(c.H, c.B), 256, 0, s>>>(p, c);
+  else decay_step_kernel<T, D, 32><<<dim3(c.H * (D / 32), c.B), 256, 0, s>>>(p, c);
   return hipGetLastError();
 }
 
