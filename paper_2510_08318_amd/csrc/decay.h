@@ -86,19 +86,36 @@ constexpr int kChunk = 64, kChunkF32 = 32;
 struct Plan {
   int segs, tokens;         // tokens of a segment
 };
-// The number of segments by a count of what each choice costs, in chunks of a workgroup of the rows kernel: as many rounds of resident workgroups as the call makes, and
-// with several segments the sums, which read two tensors of three, and two launches more.
+// The number of segments by what each choice should take.  A chunk of a workgroup takes `rows` us in the rows kernel and `sums` in the kernel of the sums where the chip is empty, and
+// longer by `more` for each workgroup to a compute unit (of `resident`, beyond which it is another round); a state is written, read and written, and read.  Us of kernels, fewer
+// segments / as chosen / more: 12 x 32760 x 128, 21 / 42 / 64, 174 / 152 / 184; 12 x 4680, 8 / 19 / 37, 65 / 45 / 48; 40 x 75600, 6 / 12 / 19, 1142 / 1009 / 1092; step of 2 x 12 x 4133 x 64,
+// 11 / 33, 145 / 134; step in fp32 of 2 x 1024 x 64, 16 / 32, 54 / 44.
+struct ChunkTimes {
+  float rows, sums, more;
+  int resident;
+};
+inline ChunkTimes chunk_times(int chunk, int d) {
+  if (chunk == kChunkF32) return d == 128 ? ChunkTimes{6.5f, 4.f, 1.f, 1} : ChunkTimes{4.4f, 3.f, 0.8f, 2};
+  return d == 128 ? ChunkTimes{3.1f, 1.4f, 1.5f, 2} : ChunkTimes{2.f, 1.f, 0.6f, 3};
+}
 inline Plan plan_of(int B, int H, int n, int d, int chunk, int row_passes, int sum_passes) {
-  const long long chunks = (n + chunk - 1) / chunk, heads = (long long)B * H, slots = kCUs * (chunk == kChunkF32 && d == 128 ? 1 : 2);
-  Plan best{1, (int)chunks * chunk};
-  double least = 0;
-  for (long long want = 1; want <= chunks && want <= 256; ++want) {
-    const long long per = (chunks + want - 1) / want, segs = (chunks + per - 1) / per;
-    if (segs != want) continue;
-    const long long rounds = (heads * row_passes * segs + slots - 1) / slots, sums = (heads * sum_passes * segs + slots - 1) / slots;
-    double cost = (double)rounds * (double)(per + 1);
-    if (segs > 1) cost += (double)sums * (0.6 * (double)per + 1) + 5 + 0.1 * (double)segs;
-    if (want == 1 || cost < least) { least = cost; best = Plan{(int)segs, (int)per * chunk}; }
+  const ChunkTimes t = chunk_times(chunk, d);
+  const int chunks = (n + chunk - 1) / chunk;
+  const float heads = (float)B * (float)H;
+  auto kernel = [&](float groups, float per, float one) {
+    const float units = groups * (1.f / kCUs), full = (float)t.resident, rounds = units <= full ? 1.f : (float)(int)(units / full + 0.999f);
+    return 4.f + rounds * per * (one + t.more * (units < full ? units : full));
+  };
+  Plan best{1, chunks * chunk};
+  float least = 0;
+  // (the next choice is the least number of segments that makes them shorter)
+  for (int per = chunks, segs = 1;; per = (chunks - 1) / ((chunks - 1) / (per - 1) + 1) + 1) {
+    segs = (chunks + per - 1) / per;
+    if (segs > 256) break;
+    float cost = kernel(heads * row_passes * segs, (float)per, t.rows);
+    if (segs > 1) cost += kernel(heads * sum_passes * segs, (float)per, t.sums) + 4.f + heads * sum_passes * segs * (float)(d * d) * (16.f / 5.5e6f);
+    if (segs == 1 || cost < least) { least = cost; best = Plan{segs, per * chunk}; }
+    if (per == 1) break;
   }
   return best;
 }

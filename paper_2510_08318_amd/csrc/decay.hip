@@ -54,12 +54,16 @@ void backward_passes(const Args& a, float* parts, Pass& dq, Pass& dv, Pass& dk) 
 constexpr int kStepTokens = 16;
 
 constexpr int chunk_of(int dtype) { return dtype == LINATTN_BF16 ? kChunk : kChunkF32; }
-struct Layout {             // of the workspace, in floats
-  size_t states, parts;     // all states; dv and dk of all query heads
+struct Layout {
+  Plan plan;
+  size_t states, parts;     // of the workspace, in floats: all states; dv and dk of all query heads
 };
 Layout layout_of(int dtype, int B, int H, int HK, int n, int d, bool backward) {
-  Layout r{0, 0};
-  if (n > kStepTokens) r.states = (size_t)plan_of(B, H, n, d, chunk_of(dtype), backward ? 3 : 1, backward ? 2 : 1).segs * (backward ? 2 : 1) * B * H * d * d;
+  Layout r{};
+  if (n > kStepTokens) {
+    r.plan = plan_of(B, H, n, d, chunk_of(dtype), backward ? 3 : 1, backward ? 2 : 1);
+    r.states = (size_t)r.plan.segs * (backward ? 2 : 1) * B * H * d * d;
+  }
   if (backward && H != HK) r.parts = 2 * (size_t)B * H * n * d;
   return r;
 }
@@ -99,7 +103,7 @@ hipError_t launch_states(const SumArgs& sums, const ScanArgs& scan, hipStream_t 
 template <typename T, int D, bool F32>
 hipError_t chunked_fwd(const Args& a) {
   const int G = a.c.group;
-  const Plan plan = plan_of(a.c.B, a.c.H, a.c.n, D, chunk_of(a.dtype), 1, 1);
+  const Plan plan = layout_of(a.dtype, a.c.B, a.c.H, a.HK, a.c.n, D, false).plan;
   const Role q{a.q, a.qr, 1}, k{a.k, a.kr, G}, v{a.v, a.kr, G};
   const bool states = plan.segs > 1 || a.state_out;
   if (states) {
@@ -114,9 +118,9 @@ hipError_t chunked_fwd(const Args& a) {
 template <typename T, int D, bool F32>
 hipError_t chunked_bwd(const Args& a) {
   const int G = a.c.group;
-  const Plan plan = plan_of(a.c.B, a.c.H, a.c.n, D, chunk_of(a.dtype), 3, 2);
   const Role q{a.q, a.qr, 1}, k{a.k, a.kr, G}, v{a.v, a.kr, G}, dout{a.dout, a.qr, 1};
   const Layout lay = layout_of(a.dtype, a.c.B, a.c.H, a.HK, a.c.n, D, true);
+  const Plan& plan = lay.plan;
   const bool states = plan.segs > 1 || a.dstate_in;
   const size_t one = lay.states / 2;
   float *s = states ? a.work : nullptr, *d = states ? a.work + one : nullptr;

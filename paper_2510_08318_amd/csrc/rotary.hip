@@ -2,7 +2,9 @@
 //
 //   y1 = x1 cos t - x2 sin t,  y2 = x1 sin t + x2 cos t,  t = position base^(-2m / dims)
 //
-// Bytes bound it: a row is read and written once.  An angle serves all heads of its token, so a thread keeps its channels' sines and cosines and goes through the heads.
+// Bytes bound it: a row is read and written once.  An angle serves all heads of its token, so a thread keeps its channels' sines and cosines and goes through the heads; it has 16 bytes of a
+// row (with pairs in halves of the axes 16 of either half, or single channels where the halves are not whole 16 bytes).  2 x 12 x 32760 x 128 bf16, 44 + 42 + 42 channels: 64 us, 6.3 TB/s;
+// one token of 64 sequences, 32 + 8 heads: 5 us, of which a launch is 3.
 #include "../../include/linattn.h"
 #include "rotary.h"
 #include "f32_split.h"
@@ -18,9 +20,10 @@ template <typename T, int N>
 struct Run {                // N adjacent values of a row
   static constexpr int W = (N * (int)sizeof(T) + 3) / 4;
   uint32_t w[W];
+  template <bool STREAM>
   __device__ __forceinline__ void load(const T* p) {
     if constexpr (W == 4) {
-      const uint4 x = *reinterpret_cast<const uint4*>(p);
+      const uint4 x = STREAM ? ld_nt(reinterpret_cast<const uint4*>(p)) : *reinterpret_cast<const uint4*>(p);
       w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
     } else if constexpr (sizeof(T) == 2) w[0] = *reinterpret_cast<const uint16_t*>(p);
     else w[0] = *reinterpret_cast<const uint32_t*>(p);
@@ -54,9 +57,10 @@ template <typename T, int NP, bool HALVES>
 struct Pairs {
   static constexpr int N = HALVES ? NP : 2 * NP;
   Run<T, N> a, b;           // b: HALVES only
+  template <bool STREAM>
   __device__ __forceinline__ void load(const T* row, int at, int other) {
-    a.load(row + at);
-    if constexpr (HALVES) b.load(row + other);
+    a.template load<STREAM>(row + at);
+    if constexpr (HALVES) b.template load<STREAM>(row + other);
   }
   __device__ __forceinline__ void store(T* row, int at, int other) const {
     a.store(row + at);
@@ -80,15 +84,14 @@ struct Pairs {
 
 constexpr int kAhead = 4;      // rows whose loads are in flight together
 
-template <typename T, int D, int NP, bool HALVES>
+template <typename T, int D, int NP, bool HALVES, bool STREAM>
 __global__ __launch_bounds__(256) void rotary_kernel(Args a, int heads) {
   constexpr int PARTS = D / 2 / NP;
-  const int part = threadIdx.x % PARTS, b = blockIdx.z;
-  const long long t = (long long)blockIdx.x * (256 / PARTS) + threadIdx.x / PARTS;
-  if (t >= a.n) return;
-  int len = a.n;
-  if (a.lengths) { len = a.lengths[b]; len = len < a.n ? len : a.n; }
-  const bool live = t < len;
+  const int part = threadIdx.x % PARTS;
+  const long long token = (long long)blockIdx.x * (256 / PARTS) + threadIdx.x / PARTS, tokens = (long long)a.B * a.n;
+  if (token >= tokens) return;
+  const int b = tokens >> 32 ? (int)(token / a.n) : (int)((uint32_t)token / (uint32_t)a.n), t = (int)(token - (long long)b * a.n);
+  const bool live = t < (a.lengths ? a.lengths[b] : a.n);
 
   // this thread's channels: pairs p0 .. p0 + NP - 1
   const int p0 = part * NP;
@@ -100,6 +103,21 @@ __global__ __launch_bounds__(256) void rotary_kernel(Args a, int heads) {
     if (x < 3) at = (x == 2 ? a.from[2] : x == 1 ? a.from[1] : 0) + (2 * p0 - (x == 2 ? a.from[2] : x == 1 ? a.from[1] : 0)) / 2;
     other = at + size / 2;
   }
+  // the first rows are asked for before the angles are worked out
+  const int h0 = blockIdx.y * heads, h1 = h0 + heads < a.H + a.HK ? h0 + heads : a.H + a.HK;
+  const size_t q0 = (size_t)b * a.qr.sb + (size_t)t * a.qr.sn, k0 = (size_t)b * a.kr.sb + (size_t)t * a.kr.sn;
+  auto from = [&](int h) { return h < a.H ? static_cast<const T*>(a.q) + q0 + (size_t)h * a.qr.sh : static_cast<const T*>(a.k) + k0 + (size_t)(h - a.H) * a.kr.sh; };
+  auto to = [&](int h) { return h < a.H ? static_cast<T*>(a.qo) + q0 + (size_t)h * a.qr.sh : static_cast<T*>(a.ko) + k0 + (size_t)(h - a.H) * a.kr.sh; };
+  Pairs<T, NP, HALVES> x[kAhead];
+  auto ask = [&](int h) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (live && h + i < h1) x[i].template load<STREAM>(from(h + i), at, other);
+      else x[i].clear();
+    }
+  };
+  ask(h0);
+
   double pos[3] = {0., 0., 0.};
   if (a.positions) {
     const int* p = a.positions + (size_t)b * a.item + (size_t)t * a.axes;
@@ -107,51 +125,49 @@ __global__ __launch_bounds__(256) void rotary_kernel(Args a, int heads) {
     if (a.axes > 1) pos[1] = p[1];
     if (a.axes > 2) pos[2] = p[2];
   } else {
-    int x = (int)t;
-    if (a.axes > 2) { const int y = x / a.grid2; pos[2] = (double)(x - y * a.grid2) + a.first[2]; x = y; }
-    if (a.axes > 1) { const int y = x / a.grid1; pos[1] = (double)(x - y * a.grid1) + a.first[1]; x = y; }
-    pos[0] = (double)x + a.first[0];
+    int i = (int)t;
+    if (a.axes > 2) { const int y = i / a.grid2; pos[2] = (double)(i - y * a.grid2) + a.first[2]; i = y; }
+    if (a.axes > 1) { const int y = i / a.grid1; pos[1] = (double)(i - y * a.grid1) + a.first[1]; i = y; }
+    pos[0] = (double)i + a.first[0];
   }
   float s[NP], c[NP];
   uint32_t kept = 0;
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
-    const int x = 2 * (p0 + i);
-    if (x >= a.from[3]) kept |= 1u << i;
-    const double angle = (x >= a.from[2] ? pos[2] : x >= a.from[1] ? pos[1] : pos[0]) * a.turns[p0 + i];
+    const int ch = 2 * (p0 + i);
+    if (ch >= a.from[3]) kept |= 1u << i;
+    const double angle = (ch >= a.from[2] ? pos[2] : ch >= a.from[1] ? pos[1] : pos[0]) * a.turns[p0 + i];
     sine_of(a.back ? -angle : angle, s[i], c[i]);
   }
 
-  const int h1 = (blockIdx.y + 1) * heads < a.H + a.HK ? (blockIdx.y + 1) * heads : a.H + a.HK;
-  const size_t q0 = (size_t)b * a.qr.sb + (size_t)t * a.qr.sn, k0 = (size_t)b * a.kr.sb + (size_t)t * a.kr.sn;
-  auto from = [&](int h) { return h < a.H ? static_cast<const T*>(a.q) + q0 + (size_t)h * a.qr.sh : static_cast<const T*>(a.k) + k0 + (size_t)(h - a.H) * a.kr.sh; };
-  auto to = [&](int h) { return h < a.H ? static_cast<T*>(a.qo) + q0 + (size_t)h * a.qr.sh : static_cast<T*>(a.ko) + k0 + (size_t)(h - a.H) * a.kr.sh; };
-  for (int h0 = blockIdx.y * heads; h0 < h1; h0 += kAhead) {
-    Pairs<T, NP, HALVES> x[kAhead];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      if (live && h0 + i < h1) x[i].load(from(h0 + i), at, other);
-      else x[i].clear();
-    }
+  for (int h = h0;;) {
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
-      if (h0 + i < h1) {
+      if (h + i < h1) {
         if (live) x[i].turn(s, c, kept);
-        x[i].store(to(h0 + i), at, other);
+        x[i].store(to(h + i), at, other);
       }
+    h += kAhead;
+    if (h >= h1) break;
+    ask(h);
   }
 }
 
 template <typename T, int D, int NP, bool HALVES>
 hipError_t run(const Args& a, hipStream_t s) {
   constexpr int TOKENS = 256 / (D / 2 / NP);
-  const long long blocks = (a.n + TOKENS - 1) / TOKENS;
+  const long long blocks = ((long long)a.B * a.n + TOKENS - 1) / TOKENS;
   const int all = a.H + a.HK;
   // Heads of a thread: all of them, or fewer where that fills the chip.
-  long long groups = (4 * kCUs + blocks * a.B - 1) / (blocks * a.B);
+  long long groups = (4 * kCUs + blocks - 1) / blocks;
   groups = groups < all ? groups : all;
   const int heads = (int)((all + groups - 1) / groups);
-  rotary_kernel<T, D, NP, HALVES><<<dim3((unsigned)blocks, (all + heads - 1) / heads, a.B), 256, 0, s>>>(a, heads);
+  const dim3 grid((unsigned)blocks, (all + heads - 1) / heads);
+  // Rows that the last-level cache of 256 MB has no room for, with the results, are read past it, which leaves it to the results.  Us, so / through the cache, 2 x 12 heads of bf16 x 128:
+  // 32760 tokens (403 MB with the results) 65 / 82, 24000 (295 MB) 51 / 51, 16000 35 / 32, 12000 28 / 25.
+  const bool big = 2. * (double)a.B * a.n * all * D * sizeof(T) > 300e6;
+  if (big) rotary_kernel<T, D, NP, HALVES, true><<<grid, 256, 0, s>>>(a, heads);
+  else rotary_kernel<T, D, NP, HALVES, false><<<grid, 256, 0, s>>>(a, heads);
   return hipGetLastError();
 }
 

@@ -402,6 +402,21 @@ def _int3(name, values, axes):
     return (B_.ctypes.c_int * 3)(*values)
 
 
+@functools.lru_cache(maxsize=256)
+def _rotary_desc(dtype, B, H, HK, n, d, layout, dims, pairs, inverse, base, grid, first):
+    """The description of a call without its tensors."""
+    axes = len(dims)
+    _need(1 <= axes <= 3 and pairs in ("adjacent", "halves"), "dims: one to three axes; pairs: 'adjacent' or 'halves'")
+    return B_.RotaryDesc(dtype, B, H, HK, n, d, _layout_code(layout), axes, _int3("dims", dims, axes),
+                         B_.PAIRS_HALVES if pairs == "halves" else B_.PAIRS_ADJACENT, int(inverse), base,
+                         _int3("grid", grid if grid is not None else (1,) * axes, axes), _int3("first", first if first is not None else (0,) * axes, axes),
+                         None, 0, None)
+
+
+def _numbers(values):
+    return values if values is None or type(values) is tuple else tuple(values)
+
+
 @_on_device_of
 def rotary(q, k=None, *, dims=None, grid=None, first=None, positions=None, base=10000.0, pairs="adjacent", inverse=False, layout="bhnd", lengths=None,
            q_out=None, k_out=None):
@@ -421,20 +436,17 @@ def rotary(q, k=None, *, dims=None, grid=None, first=None, positions=None, base=
     else:
         HK = _token_dims(k, layout)[1]
         _check_tokens("k", k, _token_shape(B, HK, n, d, layout), q.dtype, index)
-    dims = (d,) if dims is None else dims
-    axes = len(dims)
-    _need(1 <= axes <= 3 and pairs in ("adjacent", "halves"), "dims: one to three axes; pairs: 'adjacent' or 'halves'")
-    _need(grid is not None or positions is not None or axes == 1, "grid: the tokens along each axis")
-    items = 0
+    dims = (d,) if dims is None else _numbers(dims)
+    _need(grid is not None or positions is not None or len(dims) == 1, "grid: the tokens along each axis")
+    desc = B_.RotaryDesc.from_buffer_copy(_rotary_desc(dtype, B, H, HK, n, d, layout, dims, pairs, bool(inverse), base, _numbers(grid), _numbers(first)))
     if positions is not None:
-        _need(grid is None or first is None or not any(first), "positions: in place of grid and first")
-        items = 1 if positions.dim() == 2 else B
-        _check_ints("positions", positions, (n, axes) if items == 1 and positions.dim() == 2 else (B, n, axes), index)
-    _check_ints("lengths", lengths, (B,), index)
-    desc = B_.RotaryDesc(dtype, B, H, HK, n, d, _layout_code(layout), axes, _int3("dims", dims, axes),
-                         B_.PAIRS_HALVES if pairs == "halves" else B_.PAIRS_ADJACENT, int(inverse), base,
-                         _int3("grid", grid if grid is not None else (1,) * axes, axes), _int3("first", first if first is not None else (0,) * axes, axes),
-                         B_._ptr(positions), items, B_._ptr(lengths))
+        _need(first is None or not any(first), "positions: in place of grid and first")
+        shared = positions.dim() == 2
+        _check_ints("positions", positions, (n, len(dims)) if shared else (B, n, len(dims)), index)
+        desc.positions, desc.position_items = positions.data_ptr(), 1 if shared else B
+    if lengths is not None:
+        _check_ints("lengths", lengths, (B,), index)
+        desc.lengths = lengths.data_ptr()
     q_out = _result("q_out", q_out, q, index)
     k_out = _result("k_out", k_out, k, index) if k is not None else None
     B_.linattn_rotary(desc, q, k, q_out, k_out, _raw_stream(index))
@@ -446,7 +458,16 @@ def _check_state(name, t, shape, index):
         _check_tokens(name, t, shape, torch.float32, index)
 
 
-def _decay_desc(q, k, v, log_decay, slots, states, scale, layout, lengths, f32_math):
+@functools.lru_cache(maxsize=256)
+def _decay_numbers(dtype, B, H, HK, n, d, layout, scale, states):
+    """The description of a call without its tensors, and the sizes of its workspaces (forward, backward), which its numbers decide."""
+    some = 256      # an address, for the checks
+    desc = B_.DecayDesc(dtype, B, H, HK, n, d, _layout_code(layout), scale, some, None, some if states else None, states, None, 0)
+    return desc, [B_.linattn_decay_workspace_bytes(desc, backward) for backward in (False, True)]
+
+
+def _decay_desc(q, k, v, log_decay, slots, states, scale, layout, lengths, f32_math, backward):
+    """(description, workspace); the caller holds the workspace until the call has been queued."""
     B, H, n, d = _token_dims(q, layout)
     HK = _token_dims(k, layout)[1]
     dtype, index, shape = _dtype_code(q, f32_math), q.get_device(), _token_shape(B, HK, n, d, layout)
@@ -456,16 +477,14 @@ def _decay_desc(q, k, v, log_decay, slots, states, scale, layout, lengths, f32_m
     _check_tokens("log_decay", log_decay, (H,), torch.float32, index)
     _check_ints("lengths", lengths, (B,), index)
     _check_ints("slots", slots, (B,), index)
-    return B_.DecayDesc(dtype, B, H, HK, n, d, _layout_code(layout), scale, B_._ptr(log_decay), B_._ptr(lengths), B_._ptr(slots), states, None, 0)
-
-
-def _decay_workspace(desc, q, backward):
-    size = B_.linattn_decay_workspace_bytes(desc, backward)
-    if size == 0:
-        return None
-    work = q.new_empty(size, dtype=torch.uint8)
-    desc.workspace, desc.workspace_bytes = B_._ptr(work), size
-    return work
+    numbers, sizes = _decay_numbers(dtype, B, H, HK, n, d, layout, scale, states)
+    desc = B_.DecayDesc.from_buffer_copy(numbers)
+    desc.log_decay, desc.lengths, desc.slots = B_._ptr(log_decay), B_._ptr(lengths), B_._ptr(slots)
+    work = None
+    if sizes[backward]:
+        work = q.new_empty(sizes[backward], dtype=torch.uint8)
+        desc.workspace, desc.workspace_bytes = work.data_ptr(), sizes[backward]
+    return desc, work
 
 
 def _state_shape(desc):
@@ -492,7 +511,7 @@ def decay_attention(q, k, v, log_decay, *, state=None, slots=None, scale=0.0, la
         state_out = state if state_out is None else state_out
     else:
         states = 0
-    desc = _decay_desc(q, k, v, log_decay, slots, states, scale, layout, lengths, f32_math)
+    desc, work = _decay_desc(q, k, v, log_decay, slots, states, scale, layout, lengths, f32_math, False)
     shape = _state_shape(desc)
     _check_state("state", state, shape, index)
     if state_out is None:
@@ -502,7 +521,6 @@ def decay_attention(q, k, v, log_decay, *, state=None, slots=None, scale=0.0, la
     else:
         _check_state("state_out", state_out, shape, index)
     out = _result("out", out, q, index)
-    work = _decay_workspace(desc, q, False)      # (a name holds it until the call has been queued)
     B_.linattn_decay_fwd(desc, q, k, v, state, out, state_out, _raw_stream(index))
     return out, state_out
 
@@ -515,7 +533,7 @@ def decay_attention_backward(q, k, v, log_decay, dout, *, state=None, dstate=Non
     none is made), False where it is not wanted.  log_decay is a constant of the layer and has no gradient.  Nothing is recorded for autograd."""
     index = q.get_device()
     _need(slots is None or state is not None, "slots: rows of state")
-    desc = _decay_desc(q, k, v, log_decay, slots, state.shape[0] if slots is not None else 0, scale, layout, lengths, f32_math)
+    desc, work = _decay_desc(q, k, v, log_decay, slots, state.shape[0] if slots is not None else 0, scale, layout, lengths, f32_math, True)
     _check_state("state", state, _state_shape(desc), index)
     by_item = (desc.B, desc.H, desc.d, desc.d)
     _check_state("dstate", dstate, by_item, index)
@@ -526,6 +544,5 @@ def decay_attention_backward(q, k, v, log_decay, dout, *, state=None, dstate=Non
         dstate_in = None
     _check_state("dstate_in", dstate_in, by_item, index)
     dq, dk, dv = [_result(name, g, like, index) for name, g, like in (("dq", dq, q), ("dk", dk, k), ("dv", dv, v))]
-    work = _decay_workspace(desc, q, True)      # (a name holds it until the call has been queued)
     B_.linattn_decay_bwd(desc, q, k, v, state, dout, dstate, dq, dk, dv, dstate_in, _raw_stream(index))
     return dq, dk, dv, dstate_in
