@@ -498,18 +498,24 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
           for (int r = 0; r < 16; ++r) o[y][r] = fmaf(wt, f32::ldf(from, 16 * (r / 8) + r % 8), o[y][r]);
         }
     }
+    // A lane has channels 8 g .. + 7 and 16 + 8 g .. + 7 of the wavefront's 32 of row m.  Exchanged with the lane 16 further, an instruction has 64 bytes of 16 rows, not 32 of 32.
 #pragma unroll
     for (int y = 0; y < IB; ++y) {
-      const int place = i + 32 * (ib0 + y) + m;
-      if (place >= i1) continue;
-      const int token = token_at(place, len, p.back);
+      const int from = i + 32 * (ib0 + y);
+      if (!out.part) {
+        u32x4 first = __builtin_bit_cast(u32x4, pack8(o[y], 0)), second = __builtin_bit_cast(u32x4, pack8(o[y], 1));
 #pragma unroll
-      for (int hh = 0; hh < 2; ++hh) {
-        const int ch = 32 * cb + 8 * g + 16 * hh;
-        if (!out.part) *reinterpret_cast<bf16x8*>(out.row(token, ch)) = pack8(o[y], hh);
-        else
+        for (int e = 0; e < 4; ++e) {
+          const auto r = __builtin_amdgcn_permlane16_swap(first[e], second[e], false, false);
+          first[e] = r[0]; second[e] = r[1];
+        }
+        const int ch = 32 * cb + 8 * g + (m & 16), place = from + m % 16;
+        if (place < i1) *reinterpret_cast<u32x4*>(out.row(token_at(place, len, p.back), ch)) = first;
+        if (place + 16 < i1) *reinterpret_cast<u32x4*>(out.row(token_at(place + 16, len, p.back), ch)) = second;
+      } else if (from + m < i1) {
+        float* to = out.part_row(token_at(from + m, len, p.back), 32 * cb + 8 * g);
 #pragma unroll
-          for (int e = 0; e < 8; e += 4) *reinterpret_cast<f32x4*>(out.part_row(token, ch + e)) = f32x4{o[y][8 * hh + e], o[y][8 * hh + e + 1], o[y][8 * hh + e + 2], o[y][8 * hh + e + 3]};
+        for (int r = 0; r < 16; r += 4) *reinterpret_cast<f32x4*>(to + 16 * (r / 8) + r % 8) = f32x4{o[y][r], o[y][r + 1], o[y][r + 2], o[y][r + 3]};
       }
     }
 
