@@ -88,8 +88,8 @@ hipError_t launch_states(const SumArgs& sums, const ScanArgs& scan, hipStream_t 
   if constexpr (F32) e = launch<&decay_sum_f32_kernel<T, D>>(sums, sums.c, sums.plan, sums.passes, 2 * D, sum_f32_lds<D>(), s);
   else {
     auto go = [&](auto pieces, auto stream) { return launch<&decay_sum_kernel<D, decltype(pieces)::value, decltype(stream)::value>>(sums, sums.c, sums.plan, sums.passes, 256, sum_lds<D>(), s); };
-    // What it reads is read again by the rows kernel, from the last-level cache of 256 MB as far as it has room.  Us, all kernels, loads that stay / that do not: 12 x 32760 x 128 (201 MB)
-    // 155 / 157, 40 x 75600 x 128 (1550 MB) 1070 / 1035.
+    // What it reads is read again by the rows kernel, from the last-level cache of 256 MB as far as it has room.  Us of both, loads that stay there / that do not: 12 x 32760 x 128 (201 MB)
+    // 154 / 154, 40 x 75600 x 128 (1550 MB) 940 / 905.
     const bool big = (double)sums.c.B * sums.c.n * D * 4. * (sums.passes * (sums.c.H / sums.pass[0].b.group + sums.c.H / sums.pass[0].c.group) / 2) > 256e6;
     using std::integral_constant;
     if (handed_out) e = big ? go(integral_constant<int, 3>{}, std::true_type{}) : go(integral_constant<int, 3>{}, std::false_type{});

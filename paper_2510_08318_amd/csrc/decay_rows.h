@@ -346,7 +346,8 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
   zero_rows<D, 256>(out, max(i0, i1), all);
   if (i0 >= i1) return;
 
-  Tile<D, false> ta, tb, tc;
+  Tile<D, true> ta;         // (read once; b and c again by the neighbours of this workgroup, or just now by the sums' kernel)
+  Tile<D, false> tb, tc;
   ta.of(p.a, b, h, p.back, w, lane);
   tb.of(p.b, b, h, p.back, w, lane);
   tc.of(p.c, b, h, p.back, w, lane);
@@ -414,6 +415,9 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
     const bool more = i + kChunk < i1;
     if (more) tb.load(i + kChunk, i1, len, p.back, b_tile(buffer ^ 1), w, lane);
 
+    // The rows of a chunk go before the state behind it: the other workgroup of the compute unit is in another phase, and its products fill the waits of this one's (12 x 32760 x 128
+    // 95 us with one priority, 89 so; raised for the state instead 90).
+    __builtin_amdgcn_s_setprio(1);
     // weights of block w: (0, 0), (1, 0), (1, 1) of rows and tokens
     if (w < 3) {
       f32x16 s = zero16();
@@ -498,6 +502,7 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
           for (int r = 0; r < 16; ++r) o[y][r] = fmaf(wt, f32::ldf(from, 16 * (r / 8) + r % 8), o[y][r]);
         }
     }
+    __builtin_amdgcn_s_setprio(0);
     // A lane has channels 8 g .. + 7 and 16 + 8 g .. + 7 of the wavefront's 32 of row m.  Exchanged with the lane 16 further, an instruction has 64 bytes of 16 rows, not 32 of 32.
 #pragma unroll
     for (int y = 0; y < IB; ++y) {
