@@ -141,6 +141,55 @@ def test_longer_sequences(mode, n):
     _check(mode, 1, 3, 1, n, 128 if mode == "bf16" else 64, g=__import__("torch").tensor([0.0, -0.003, -0.2], device="cuda"))
 
 
+@pytest.mark.parametrize("mode,d", [("f32", 128), ("f32math", 128), ("f32math", 64), ("bf16", 64)])
+def test_longer_sequences_other_types(mode, d):
+    _check(mode, 1, 2, 2, 900, d, "bnhd", g=__import__("torch").tensor([-0.0004, -0.05], device="cuda"))
+
+
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("d", [64, 128])
+def test_padded_batch_over_segments(mode, d):
+    """Items that end in a segment, at its end, before the last ones; shared key heads."""
+    n, lengths = 1000, [1000, 512, 513, 63, 960, 0]
+
+    def edit(q, k, v, do):
+        for t in (q, k, v, do):
+            for b, length in enumerate(lengths):
+                t[b, length:] = float("inf")
+    _check(mode, 6, 2, 1, n, d, "bnhd", lengths=lengths, edit=edit, g=__import__("torch").tensor([-0.002, -0.1], device="cuda"))
+
+
+def test_full_size():
+    """A layer's size at 832x480 and more heads than the last-level cache has room for: rows of a few heads, here and there, and their states, against the definition in 64 bits."""
+    import torch
+    from paper_2510_08318_amd import torch_glue as G
+    H, n, d = 18, 32760, 128
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    q, k, v, do = [torch.randn((1, H, n, d), generator=gen, device="cuda").to(torch.bfloat16) for _ in range(4)]
+    g = -torch.exp2(-8.0 * torch.arange(1, H + 1, device="cuda") / H)
+    out, end = G.decay_attention(q, k, v, g)
+    dq, dk, dv, _ = G.decay_attention_backward(q, k, v, g, do)
+    rows = torch.tensor([0, 1, 63, 64, 127, 831, 832, 5000, 16383, 16384, 20001, 32700, 32759], device="cuda")
+    for h in (0, 7, 16, 17):
+        Q, K, V, D = [x[0, h].double() for x in (q, k, v, do)]
+        i, c, gh = torch.arange(n, device="cuda").double(), d ** -0.5, float(g[h].double())
+
+        def near(name, got, a, b, x, back):
+            gap = (i[None] - i[rows, None]) * (1 if back else -1)
+            w = torch.where(gap >= 0, torch.exp(gh * gap.clamp(min=0)), 0.0)
+            want, mass = c * (((a[rows] @ b.T) * w) @ x), c * (((a[rows].abs() @ b.T.abs()) * w) @ x.abs())
+            err = FACTOR["bf16"] * 2.01 + (2 * n + d + 128 + 110) * O.FP32
+            over = (got[0, h, rows].double() - want).abs() - err * mass - STORE["bf16"] * want.abs()
+            assert (over <= 0).all(), (name, h, over.max())
+        near("out", out, Q, K, V, False)
+        near("dq", dq, D, V, K, False)
+        near("dk", dk, V, D, Q, True)
+        near("dv", dv, K, Q, D, True)
+        w = torch.exp(gh * (n - 1 - i))[:, None]
+        over = (end[0, h].double() - (w * K).T @ V).abs() - (2 * n + d + 128 + 110) * O.FP32 * ((w * K.abs()).T @ V.abs())
+        assert (over <= 0).all(), (h, over.max())
+
+
 @pytest.mark.parametrize("mode", ["bf16", "f32"])
 def test_many_heads(mode):
     """As many heads as fill the chip: a workgroup takes all of a head's tokens."""

@@ -113,6 +113,24 @@ def test_rows_behind_32_bits():
     assert not got[0, 0, : 1000].any() and not got[0, 0, -1000: -3].any()
 
 
+@pytest.mark.parametrize("kind,layout", [("adjacent", "bnhd"), ("halves", "bhnd")])
+def test_full_size(kind, layout):
+    """A layer's size at 832x480, more than the last-level cache has room for: tokens here and there."""
+    import torch
+    from paper_2510_08318_amd import torch_glue as G
+    H, n, d, dims, grid = 12, 32760, 128, (44, 42, 42), (21, 30, 52)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    q, k = [torch.randn((1, n, H, d) if layout == "bnhd" else (1, H, n, d), generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2)]
+    got = G.rotary(q, k, dims=dims, grid=grid, pairs=kind, layout=layout)
+    rows = np.array([0, 1, 51, 52, 1559, 1560, 20000, 32759])
+    at = torch.tensor(rows, device="cuda")
+    pos = np.stack((rows // 1560, rows // 52 % 30, rows % 52), 1)
+    for x, y in zip((q, k), got):
+        x, y = [G.to_host_f64(t[0, at].transpose(0, 1) if layout == "bnhd" else t[0][:, at]) for t in (x, y)]
+        want, err = O.rotary(x, pos, dims, kind, 10000.0, False)
+        assert (np.abs(y - want) <= err + U["bf16"] * np.abs(want)).all()
+
+
 def test_gradient_by_differences():
     """The inverse of an upstream gradient is the gradient of the sum that it weighs."""
     import torch
