@@ -50,8 +50,9 @@ void backward_passes(const Args& a, float* parts, Pass& dq, Pass& dv, Pass& dk) 
   dv.orow = dk.orow = Rows{(size_t)a.c.H * a.c.n * D, (size_t)a.c.n * D, (size_t)D};
 }
 
-// Tokens up to which the recurrence is taken token by token.
-constexpr int kStepTokens = 16;
+// Tokens up to which the recurrence is taken token by token.  Us a call, so / in chunks: bf16, 4 x 32 states of 128 x 128, 8 tokens 12.7 / 14.2, 16 17.9 / 13.3; 32 x 32 states, 8 tokens
+// 44.8 / 41.6, 16 63 / 43; fp32, 4 x 32 states, 8 12.8 / 18.3, 16 17.9 / 18.9, 24 24 / 19.1.
+constexpr int step_tokens(int dtype) { return dtype == LINATTN_BF16 ? 8 : 16; }
 
 constexpr int chunk_of(int dtype) { return dtype == LINATTN_BF16 ? kChunk : kChunkF32; }
 struct Layout {
@@ -60,9 +61,9 @@ struct Layout {
 };
 Layout layout_of(int dtype, int B, int H, int HK, int n, int d, bool backward) {
   Layout r{};
-  if (n > kStepTokens) {
+  if (n > step_tokens(dtype)) {
     r.plan = plan_of(B, H, n, d, chunk_of(dtype), backward ? 3 : 1, backward ? 2 : 1);
-    r.states = (size_t)r.plan.segs * (backward ? 2 : 1) * B * H * d * d;
+    if (r.plan.segs > 1) r.states = (size_t)r.plan.segs * (backward ? 2 : 1) * B * H * d * d;
   }
   if (backward && H != HK) r.parts = 2 * (size_t)B * H * n * d;
   return r;
@@ -78,7 +79,12 @@ hipError_t launch(const A& args, const Common& c, const Plan& plan, int passes, 
 template <typename T, int D, bool F32>
 hipError_t launch_rows(const RowArgs& r, hipStream_t s) {
   if constexpr (F32) return launch<&decay_rows_f32_kernel<T, D>>(r, r.c, r.plan, r.passes, 2 * D, rows_f32_lds<D>(), s);
-  else return launch<&decay_rows_kernel<D>>(r, r.c, r.plan, r.passes, 256, rows_lds<D>(), s);
+  else {
+    bool state = false;
+    for (int i = 0; i < r.passes; ++i) state |= r.pass[i].p.out != nullptr && r.plan.segs == 1;
+    return state ? launch<&decay_rows_kernel<D, true>>(r, r.c, r.plan, r.passes, 256, rows_lds<D>(), s)
+                 : launch<&decay_rows_kernel<D, false>>(r, r.c, r.plan, r.passes, 256, rows_lds<D>(), s);
+  }
 }
 template <typename T, int D, bool F32>
 hipError_t launch_states(const SumArgs& sums, const ScanArgs& scan, hipStream_t s) {
@@ -105,13 +111,13 @@ hipError_t chunked_fwd(const Args& a) {
   const int G = a.c.group;
   const Plan plan = layout_of(a.dtype, a.c.B, a.c.H, a.HK, a.c.n, D, false).plan;
   const Role q{a.q, a.qr, 1}, k{a.k, a.kr, G}, v{a.v, a.kr, G};
-  const bool states = plan.segs > 1 || a.state_out;
+  const bool states = plan.segs > 1;
   if (states) {
     const SumArgs sums{{{k, v, 0}}, 1, a.c, plan, a.work};
     const ScanArgs scan{{{a.state, a.state_out, 0, 1.f, 0}}, 1, a.c, plan, a.work, D * D};
     if (hipError_t e = launch_states<T, D, F32>(sums, scan, a.stream); e != hipSuccess) return e;
   }
-  const RowArgs rows{{{Pass{q, k, v, a.o, a.qr, 0, a.state, nullptr, 0, 0, 1.f, a.scale}, states ? a.work : nullptr, 0}}, 1, a.c, plan};
+  const RowArgs rows{{{Pass{q, k, v, a.o, a.qr, 0, a.state, a.state_out, 0, 0, 1.f, a.scale}, states ? a.work : nullptr, 0}}, 1, a.c, plan};
   return launch_rows<T, D, F32>(rows, a.stream);
 }
 
@@ -121,7 +127,7 @@ hipError_t chunked_bwd(const Args& a) {
   const Role q{a.q, a.qr, 1}, k{a.k, a.kr, G}, v{a.v, a.kr, G}, dout{a.dout, a.qr, 1};
   const Layout lay = layout_of(a.dtype, a.c.B, a.c.H, a.HK, a.c.n, D, true);
   const Plan& plan = lay.plan;
-  const bool states = plan.segs > 1 || a.dstate_in;
+  const bool states = plan.segs > 1;
   const size_t one = lay.states / 2;
   float *s = states ? a.work : nullptr, *d = states ? a.work + one : nullptr;
   if (states) {
@@ -138,14 +144,14 @@ hipError_t chunked_bwd(const Args& a) {
 
 template <typename T, int D, bool F32>
 hipError_t fwd(const Args& a) {
-  if (a.c.n > kStepTokens) return chunked_fwd<T, D, F32>(a);
+  if (a.c.n > step_tokens(a.dtype)) return chunked_fwd<T, D, F32>(a);
   const int G = a.c.group;
   return launch_step<T, D>(Pass{{a.q, a.qr, 1}, {a.k, a.kr, G}, {a.v, a.kr, G}, a.o, a.qr, 0, a.state, a.state_out, 0, 0, 1.f, a.scale}, a.c, a.stream);
 }
 
 template <typename T, int D, bool F32>
 hipError_t bwd(const Args& a) {
-  if (a.c.n > kStepTokens) return chunked_bwd<T, D, F32>(a);
+  if (a.c.n > step_tokens(a.dtype)) return chunked_bwd<T, D, F32>(a);
   Common of_items = a.c;      // dS_out and dS_in are by item
   of_items.slots = nullptr;
   of_items.states = a.c.B;

@@ -104,7 +104,11 @@ __global__ __launch_bounds__(2 * D, 1) void decay_rows_f32_kernel(RowArgs a) {
   const int len = length_of(a.c, b), i0 = seg * a.plan.tokens, all = min(a.c.n, i0 + a.plan.tokens), i1 = min(len, all);
   const Results<T> out(p, b, h);
   zero_rows<D, 2 * D>(out, max(i0, i1), all);
-  if (i0 >= i1) return;
+  float* const state_out = a.plan.segs == 1 ? state_out_of<D>(a, rp, b, h) : nullptr;      // (with several segments the scan writes it)
+  if (i0 >= i1) {
+    if (state_out) copy_state<D, 2 * D>(a, rp, b, h, state_out);
+    return;
+  }
 
   Tile_ ta, tb, tc;
   ta.of(p.a, b, h);
@@ -215,19 +219,30 @@ __global__ __launch_bounds__(2 * D, 1) void decay_rows_f32_kernel(RowArgs a) {
         else *reinterpret_cast<uint2*>(out.row(token, ch)) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
       }
     }
-    if (more) {
+    if (more || state_out) {
+      // the last chunk's tokens: see decay_rows_kernel
+      const int last = i1 - i - (p.back ? 0 : 1);
+      float fade = hi, fade_lo = lo;
+      if (!more) power_of(decay, last, fade, fade_lo);
 #pragma unroll
       for (int f = 0; f < FB; ++f)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) x[f][r] = fmaf(x[f][r], hi, x[f][r] * lo);
+        for (int r = 0; r < 16; ++r) x[f][r] = fmaf(x[f][r], fade, x[f][r] * fade_lo);
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const float cw = c[r] * keep[r];
+        const int j = row_of_reg(r, g);
+        const float cw = more ? c[r] * keep[r] : i + j < i1 ? c[r] * (expf(decay * (float)(last - j)) * p.in_scale) : 0.f;
 #pragma unroll
-        for (int f = 0; f < FB; ++f) x[f] = mfma_f32(lb[Tile_::word(row_of_reg(r, g), 32 * f + m)], cw, x[f]);
+        for (int f = 0; f < FB; ++f) x[f] = mfma_f32(lb[Tile_::word(j, 32 * f + m)], cw, x[f]);
       }
-      put(buffer ^ 1);
+      if (more) put(buffer ^ 1);
     }
+  }
+  if (state_out) {
+#pragma unroll
+    for (int f = 0; f < FB; ++f)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) state_out[(32 * f + row_of_reg(r, g)) * D + 32 * w + m] = x[f][r];
   }
 }
 

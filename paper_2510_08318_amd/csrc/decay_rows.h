@@ -330,11 +330,28 @@ __device__ __forceinline__ void load_state(const RowArgs& a, const RowPass& rp, 
 
 constexpr int kUpdatePieces = 2, kAhead = 6;      // kAhead: operands that are requested ahead of their products
 
+// Where a pass's state goes, null where nowhere; of a sequence without tokens it is the state that it came with.
+template <int D>
+__device__ __forceinline__ float* state_out_of(const RowArgs& a, const RowPass& rp, int b, int h) {
+  if (!rp.p.out) return nullptr;
+  Common com = a.c;
+  if (rp.by_item) { com.slots = nullptr; com.states = com.B; }
+  const long long row = state_row(com, b, h);
+  return row >= 0 ? rp.p.out + row * D * D : nullptr;
+}
+template <int D, int NT>
+__device__ __forceinline__ void copy_state(const RowArgs& a, const RowPass& rp, int b, int h, float* to) {
+  const float* from = rp.p.in ? rp.p.in + (to - rp.p.out) : nullptr;      // (the same row of the tensor)
+  for (int i = threadIdx.x * 4; i < D * D; i += NT * 4)
+    *reinterpret_cast<float4*>(to + i) = from ? *reinterpret_cast<const float4*>(from + i) : make_float4(0.f, 0.f, 0.f, 0.f);
+}
+
+// STATE, of a call with one segment: the state behind the last token is handed out, so the rows c_j enter it whole, as three pieces, and lambda^chunk is a sum of two numbers.
 // Rows of a segment, chunk by chunk.  A wavefront has 32 columns of the state X in its accumulators, where they are the left operand of a_i X as they lie (rounded to bf16); the
 // chunk's weights P, on the lanes as S^T = B A^T gives them, are made by three of the wavefronts and go round through LDS.
-template <int D>
+template <int D, bool STATE>
 __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
-  constexpr int CB = D / 32, FB = D / 32, KS = D / 16, JS = kChunk / 16, IW = 4 / CB, IB = 2 / IW, TILE = Tile<D, false>::BYTES;
+  constexpr int CB = D / 32, FB = D / 32, KS = D / 16, JS = kChunk / 16, IW = 4 / CB, IB = 2 / IW, TILE = Tile<D, false>::BYTES, PIECES = STATE ? 3 : kUpdatePieces;
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
   const Place at = place_of(a.c, blockIdx.x, a.plan.segs, a.passes);
@@ -344,7 +361,11 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
   const int len = __builtin_amdgcn_readfirstlane(length_of(a.c, b)), i0 = seg * a.plan.tokens, all = min(a.c.n, i0 + a.plan.tokens), i1 = min(len, all);
   const Results<uint16_t> out(p, b, h);
   zero_rows<D, 256>(out, max(i0, i1), all);
-  if (i0 >= i1) return;
+  float* const state_out = STATE ? state_out_of<D>(a, rp, b, h) : nullptr;
+  if (i0 >= i1) {
+    if (STATE && state_out) copy_state<D, 256>(a, rp, b, h, state_out);
+    return;
+  }
 
   Tile<D, true> ta;         // (read once; b and c again by the neighbours of this workgroup, or just now by the sums' kernel)
   Tile<D, false> tb, tc;
@@ -378,13 +399,15 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
     const int gap = m - row_of(r % 8, g) - 16 * (r / 8) + (w == 1 ? 32 : 0);
     pairs[r] = gap >= 0 ? expf(decay * (float)gap) * pair_scale : 0.f;
   }
-  if (threadIdx.x < kChunk) {      // [k-step][g][8]
-    const int ks = threadIdx.x / 16, gg = threadIdx.x / 8 % 2, e = threadIdx.x % 8;
-    *(__attribute__((address_space(3))) float*)(kept + 4 * threadIdx.x) = expf(decay * (float)(kChunk - 16 * ks - row_of(e, gg))) * p.in_scale;
-  }
+  auto keep_weights = [&](int from, int tokens) {      // lambda^(from - j) of token j, [k-step][g][8], by a wavefront
+    const int j = 16 * (lane / 16) + row_of(lane % 8, lane / 8 % 2);
+    *(__attribute__((address_space(3))) float*)(kept + 4 * (uint32_t)lane) = j < tokens ? expf(decay * (float)(from - j)) * p.in_scale : 0.f;
+  };
+  if (w == 3 && (!STATE || i0 + kChunk < i1)) keep_weights(kChunk, kChunk);
 #pragma unroll
   for (int i = 0; i < IB; ++i) mine[i] = expf(decay * (float)(32 * (ib0 + i) + m)) * p.out_scale;
-  const float over = expf(decay * (float)kChunk);
+  float over, over_lo;
+  power_of(decay, kChunk, over, over_lo);
 
   // Addresses in the tile of a, and so, with constants that fit an instruction, in the others: 16-byte pieces 2 ks + g of row m; first and second 8 rows of a block's columns, transposed.
   uint32_t rows_at[KS], columns_at[FB][2], c_at[2], weights_at = weights + 16 * (uint32_t)lane, kept_at = kept + 32 * (uint32_t)g;
@@ -437,6 +460,9 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
 #pragma unroll
       for (int hh = 0; hh < 2; ++hh) *(__attribute__((address_space(3))) bf16x8*)(weights_at + (uint32_t)((2 * w + hh) * 1024)) = pack8(s, hh);
     }
+
+    // Behind the last token (see decay_scan_kernel) weights go by the chunk's tokens; those that are not there have none.
+    if (STATE && w == 3 && !more) keep_weights(i1 - i - (p.back ? 0 : 1), i1 - i);
 
     // a_i X, and what lies before the chunk fades
     f32x16 o[IB];
@@ -524,14 +550,16 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
       }
     }
 
-    if (more) {
+    if (more || (STATE && state_out)) {
+      float fade = over, fade_lo = over_lo;
+      if (STATE && !more) power_of(decay, i1 - i - (p.back ? 0 : 1), fade, fade_lo);
 #pragma unroll
       for (int f = 0; f < FB; ++f)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) x[f][r] *= over;
+        for (int r = 0; r < 16; ++r) x[f][r] = STATE ? fmaf(x[f][r], fade, x[f][r] * fade_lo) : x[f][r] * fade;
 #pragma unroll
       for (int ks = 0; ks < JS; ++ks) {
-        bf16x8 cw[kUpdatePieces];
+        bf16x8 cw[PIECES];
         float keep[8];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -539,12 +567,12 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) keep[4 * half + e] = four[e];
         }
-        weigh<kUpdatePieces>(c[ks], keep, cw);
+        weigh<PIECES>(c[ks], keep, cw);
 #pragma unroll
         for (int f = 0; f < FB; ++f) {
           const bf16x8 r = turned_at2(columns_at[f][0] + lb + (uint32_t)(16 * ks * D * 2), columns_at[f][1] + lb + (uint32_t)((16 * ks + 8) * D * 2));
 #pragma unroll
-          for (int j = kUpdatePieces - 1; j >= 0; --j) x[f] = mfma(r, cw[j], x[f]);
+          for (int j = PIECES - 1; j >= 0; --j) x[f] = mfma(r, cw[j], x[f]);
         }
       }
     }
@@ -552,6 +580,12 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
   for (int i = i0; i < i1; i += 2 * kChunk) {
     chunk(i, std::integral_constant<int, 0>{});
     if (i + kChunk < i1) chunk(i + kChunk, std::integral_constant<int, 1>{});
+  }
+  if (STATE && state_out && (IB == 2 || ib0 == 0)) {
+#pragma unroll
+    for (int f = 0; f < FB; ++f)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) state_out[(32 * f + 16 * (r / 8) + 8 * g + r % 8) * D + column] = x[f][r];
   }
 }
 
