@@ -353,7 +353,7 @@ typedef struct linattn_rotary_desc {
   int grid[3];            /* tokens along each axis, the last fastest: token i has the coordinates of i in the grid (the first is not looked at, and
                              has no end), plus */
   int first[3];           /* these */
-  const int* positions;   /* optional device [position_items, n, axes], in place of grid and first */
+  const int* positions;   /* optional device [position_items, n, axes]; grid and first are then not looked at */
   int position_items;     /* 1 (the same for all items) or B */
   const int* lengths;     /* optional device [B]: tokens of each item.  Padding is not read; its rows of the results are zeros.  NULL: n each. */
 } linattn_rotary_desc;

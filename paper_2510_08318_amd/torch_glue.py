@@ -423,7 +423,7 @@ def rotary(q, k=None, *, dims=None, grid=None, first=None, positions=None, base=
     """q and k with each token's rows turned by its position along up to three axes (linattn_rotary).  q, k: bf16 or fp32, [B, heads, n, d] ("bhnd") or
     [B, n, heads, d] ("bnhd").  dims: channels of each axis, one after the other (None: (d,)); channels behind the last stay as they are.  pairs: "adjacent"
     channels of an axis, or of its "halves".  Positions: token i has the coordinates of i in `grid` (tokens along each axis, the last fastest; not needed
-    with one axis), plus `first`; or int32 `positions` [n, axes] or [B, n, axes].  inverse: turned back, which is also the gradient: rotary(dq, dk, ...,
+    with one axis), plus `first`; or int32 `positions` [n, axes] or [B, n, axes], in place of both.  inverse: turned back, which is also the gradient: rotary(dq, dk, ...,
     inverse=True).  lengths: int32 [B], the tokens of each item; the rest is padding.  q_out, k_out may be q and k.  Returns (q_out, k_out), or
     (q_out, None) without k.  Nothing is recorded for autograd."""
     B, H, n, d = _token_dims(q, layout)
@@ -440,7 +440,6 @@ def rotary(q, k=None, *, dims=None, grid=None, first=None, positions=None, base=
     _need(grid is not None or positions is not None or len(dims) == 1, "grid: the tokens along each axis")
     desc = B_.RotaryDesc.from_buffer_copy(_rotary_desc(dtype, B, H, HK, n, d, layout, dims, pairs, bool(inverse), base, _numbers(grid), _numbers(first)))
     if positions is not None:
-        _need(first is None or not any(first), "positions: in place of grid and first")
         shared = positions.dim() == 2
         _check_ints("positions", positions, (n, len(dims)) if shared else (B, n, len(dims)), index)
         desc.positions, desc.position_items = positions.data_ptr(), 1 if shared else B

@@ -77,7 +77,8 @@ def test_explicit_positions(mode, kind, shared):
     rng = np.random.default_rng(3)
     pos = rng.integers(-1000, 1 << 20, (2, 40, 2))
     pos[:, 0], pos[:, 1] = (1 << 31) - 1, -(1 << 31)
-    _check(mode, 2, 3, 1, 40, 64, (32, 32), kind, "bhnd", positions=(pos[0] if shared else pos).tolist(), base=500.0)
+    _check(mode, 2, 3, 1, 40, 64, (32, 32), kind, "bhnd", positions=(pos[0] if shared else pos).tolist(), base=500.0,
+           grid=(1, 3) if shared else None, first=(7, 9))      # (not looked at)
 
 
 @pytest.mark.parametrize("mode", ["bf16", "f32"])
