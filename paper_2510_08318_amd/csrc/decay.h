@@ -92,14 +92,15 @@ struct Plan {
 // 11 / 33, 145 / 134; step in fp32 of 2 x 1024 x 64, 16 / 32, 54 / 44.
 struct ChunkTimes {
   float rows, sums, more;
-  int resident;
+  int resident, chunk;
 };
-inline ChunkTimes chunk_times(int chunk, int d) {
-  if (chunk == kChunkF32) return d == 128 ? ChunkTimes{6.5f, 4.f, 1.f, 1} : ChunkTimes{4.4f, 3.f, 0.8f, 2};
-  return d == 128 ? ChunkTimes{3.1f, 1.4f, 1.5f, 2} : ChunkTimes{2.f, 1.f, 0.6f, 3};
+inline ChunkTimes chunk_times(bool f32, bool whole, int d) {      // of fp32 tensors; of bf16 tensors in fp32 arithmetic
+  if (f32) return d == 128 ? ChunkTimes{6.5f, 4.f, 1.f, 1, kChunkF32} : ChunkTimes{4.4f, 3.f, 0.8f, 2, kChunkF32};
+  if (whole) return d == 128 ? ChunkTimes{5.f, 1.6f, 1.5f, 1, kChunk} : ChunkTimes{3.f, 1.1f, 0.6f, 2, kChunk};
+  return d == 128 ? ChunkTimes{3.1f, 1.4f, 1.5f, 2, kChunk} : ChunkTimes{2.f, 1.f, 0.6f, 3, kChunk};
 }
-inline Plan plan_of(int B, int H, int n, int d, int chunk, int row_passes, int sum_passes) {
-  const ChunkTimes t = chunk_times(chunk, d);
+inline Plan plan_of(int B, int H, int n, const ChunkTimes& t, int d, int row_passes, int sum_passes) {
+  const int chunk = t.chunk;
   const int chunks = (n + chunk - 1) / chunk;
   const float heads = (float)B * (float)H;
   auto kernel = [&](float groups, float per, float one) {

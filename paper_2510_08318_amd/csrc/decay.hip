@@ -54,7 +54,6 @@ void backward_passes(const Args& a, float* parts, Pass& dq, Pass& dv, Pass& dk) 
 // 44.8 / 41.6, 16 63 / 43; fp32, 4 x 32 states, 8 12.8 / 18.3, 16 17.9 / 18.9, 24 24 / 19.1.
 constexpr int step_tokens(int dtype) { return dtype == LINATTN_BF16 ? 8 : 16; }
 
-constexpr int chunk_of(int dtype) { return dtype == LINATTN_BF16 ? kChunk : kChunkF32; }
 struct Layout {
   Plan plan;
   size_t states, parts;     // of the workspace, in floats: all states; dv and dk of all query heads
@@ -62,7 +61,7 @@ struct Layout {
 Layout layout_of(int dtype, int B, int H, int HK, int n, int d, bool backward) {
   Layout r{};
   if (n > step_tokens(dtype)) {
-    r.plan = plan_of(B, H, n, d, chunk_of(dtype), backward ? 3 : 1, backward ? 2 : 1);
+    r.plan = plan_of(B, H, n, chunk_times(dtype == LINATTN_F32, dtype == LINATTN_BF16_F32MATH, d), d, backward ? 3 : 1, backward ? 2 : 1);
     if (r.plan.segs > 1) r.states = (size_t)r.plan.segs * (backward ? 2 : 1) * B * H * d * d;
   }
   if (backward && H != HK) r.parts = 2 * (size_t)B * H * n * d;
@@ -78,27 +77,27 @@ hipError_t launch(const A& args, const Common& c, const Plan& plan, int passes, 
 // T: the tensors' type; F32: fp32 arithmetic
 template <typename T, int D, bool F32>
 hipError_t launch_rows(const RowArgs& r, hipStream_t s) {
-  if constexpr (F32) return launch<&decay_rows_f32_kernel<T, D>>(r, r.c, r.plan, r.passes, 2 * D, rows_f32_lds<D>(), s);
+  if constexpr (sizeof(T) == 4) return launch<&decay_rows_f32_kernel<D>>(r, r.c, r.plan, r.passes, 2 * D, rows_f32_lds<D>(), s);
   else {
     bool state = false;
     for (int i = 0; i < r.passes; ++i) state |= r.pass[i].p.out != nullptr && r.plan.segs == 1;
-    return state ? launch<&decay_rows_kernel<D, true>>(r, r.c, r.plan, r.passes, 256, rows_lds<D>(), s)
-                 : launch<&decay_rows_kernel<D, false>>(r, r.c, r.plan, r.passes, 256, rows_lds<D>(), s);
+    return state ? launch<&decay_rows_kernel<D, true, F32>>(r, r.c, r.plan, r.passes, 256, rows_lds<D, F32>(), s)
+                 : launch<&decay_rows_kernel<D, false, F32>>(r, r.c, r.plan, r.passes, 256, rows_lds<D, F32>(), s);
   }
 }
 template <typename T, int D, bool F32>
 hipError_t launch_states(const SumArgs& sums, const ScanArgs& scan, hipStream_t s) {
-  bool handed_out = false;
-  for (int i = 0; i < scan.passes; ++i) handed_out |= scan.pass[i].out != nullptr;
+  bool whole = F32;         // the sums have to be those of fp32
+  for (int i = 0; i < scan.passes; ++i) whole |= scan.pass[i].out != nullptr;
   hipError_t e;
-  if constexpr (F32) e = launch<&decay_sum_f32_kernel<T, D>>(sums, sums.c, sums.plan, sums.passes, 2 * D, sum_f32_lds<D>(), s);
+  if constexpr (sizeof(T) == 4) e = launch<&decay_sum_f32_kernel<D>>(sums, sums.c, sums.plan, sums.passes, 2 * D, sum_f32_lds<D>(), s);
   else {
     auto go = [&](auto pieces, auto stream) { return launch<&decay_sum_kernel<D, decltype(pieces)::value, decltype(stream)::value>>(sums, sums.c, sums.plan, sums.passes, 256, sum_lds<D>(), s); };
     // What it reads is read again by the rows kernel, from the last-level cache of 256 MB as far as it has room.  Us of both, loads that stay there / that do not: 12 x 32760 x 128 (201 MB)
     // 154 / 154, 40 x 75600 x 128 (1550 MB) 940 / 905.
     const bool big = (double)sums.c.B * sums.c.n * D * 4. * (sums.passes * (sums.c.H / sums.pass[0].b.group + sums.c.H / sums.pass[0].c.group) / 2) > 256e6;
     using std::integral_constant;
-    if (handed_out) e = big ? go(integral_constant<int, 3>{}, std::true_type{}) : go(integral_constant<int, 3>{}, std::false_type{});
+    if (whole) e = big ? go(integral_constant<int, 3>{}, std::true_type{}) : go(integral_constant<int, 3>{}, std::false_type{});
     else e = big ? go(integral_constant<int, kUpdatePieces>{}, std::true_type{}) : go(integral_constant<int, kUpdatePieces>{}, std::false_type{});
   }
   if (e != hipSuccess) return e;

@@ -1,5 +1,4 @@
-// The passes of decay.h in fp32 arithmetic, on v_mfma_f32_32x32x2_f32: fp32 tensors, and bf16 tensors widened on their way into LDS.  Chunks of kChunkF32 tokens; a wavefront has 32
-// columns of the state.
+// The passes of decay.h for fp32 tensors, on v_mfma_f32_32x32x2_f32.  Chunks of kChunkF32 tokens; a wavefront has 32 columns of the state.
 //   lane l = (m, g), m = l % 32, g = l / 32.  A: A[m][g], B: B[g][m], D: rows 8 (r / 4) + 4 g + r % 4 of column m
 // so register r of an accumulator is, as it lies, the operand of a step over rows 8 (r / 4) + r % 4 and that + 4.
 #pragma once
@@ -11,14 +10,14 @@ namespace decay {
 __device__ __forceinline__ f32x16 mfma_f32(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
 
 // Rows of a token tensor into an fp32 LDS tile [32][D], its 16-byte pieces swizzled by row, through registers: ask requests, put writes.  Rows from `end` on are row end - 1 again.
-template <typename T, int D>
+template <int D>
 struct TileF32 {
-  static constexpr int NT = 2 * D, V = 16 / (int)sizeof(T), N = kChunkF32 * D / V / NT, WORDS = kChunkF32 * D;
-  const T* base;
+  static constexpr int NT = 2 * D, V = 4, N = kChunkF32 * D / V / NT, WORDS = kChunkF32 * D;
+  const float* base;
   size_t pitch;
   uint4 x[N];
   __device__ __forceinline__ void of(const Role& r, int b, int h) {
-    base = static_cast<const T*>(r.p) + (size_t)b * r.r.sb + (size_t)(h / r.group) * r.r.sh;
+    base = static_cast<const float*>(r.p) + (size_t)b * r.r.sb + (size_t)(h / r.group) * r.r.sh;
     pitch = r.r.sn;
   }
   __device__ __forceinline__ void ask(int i0, int end, int len, bool back) {
@@ -33,11 +32,7 @@ struct TileF32 {
 #pragma unroll
     for (int y = 0; y < N; ++y) {
       const int item = y * NT + threadIdx.x, row = item / (D / V), c = item % (D / V) * V;
-      float f[V];
-      if constexpr (V == 8) unpack_bf16x8(x[y], f);
-      else f32::unpack_f32x4(x[y], f);
-#pragma unroll
-      for (int e = 0; e < V; e += 4) *reinterpret_cast<float4*>(tile + word(row, c + e)) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+      *reinterpret_cast<uint4*>(tile + word(row, c)) = x[y];
     }
   }
 };
@@ -45,9 +40,9 @@ struct TileF32 {
 __device__ __forceinline__ int row_of_reg(int r, int g) { return 8 * (r / 4) + 4 * g + r % 4; }
 
 // A segment's own sum, as decay_sum_kernel.
-template <typename T, int D>
+template <int D>
 __global__ __launch_bounds__(2 * D) void decay_sum_f32_kernel(SumArgs a) {
-  using Tile_ = TileF32<T, D>;
+  using Tile_ = TileF32<D>;
   constexpr int FB = D / 32, WORDS = Tile_::WORDS;
   extern __shared__ __align__(16) float tiles[];
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
@@ -90,9 +85,9 @@ __global__ __launch_bounds__(2 * D) void decay_sum_f32_kernel(SumArgs a) {
 
 // Rows of a segment, as decay_rows_kernel: every wavefront takes 32 channels of the scores a_i . b_j of all pairs, and their sum through LDS gives it all of them, where the product with c_j
 // wants them.
-template <typename T, int D>
+template <int D>
 __global__ __launch_bounds__(2 * D, 1) void decay_rows_f32_kernel(RowArgs a) {
-  using Tile_ = TileF32<T, D>;
+  using Tile_ = TileF32<D>;
   constexpr int NW = D / 32, FB = D / 32, WORDS = Tile_::WORDS;
   extern __shared__ __align__(16) float tiles[];
   float4* const parts = reinterpret_cast<float4*>(tiles + 6 * WORDS);      // [wavefront][4][64]: four registers
@@ -102,7 +97,7 @@ __global__ __launch_bounds__(2 * D, 1) void decay_rows_f32_kernel(RowArgs a) {
   const Pass& p = rp.p;
   const int b = at.b, h = at.h, bh = b * a.c.H + h, seg = p.back ? a.plan.segs - 1 - at.seg : at.seg;
   const int len = length_of(a.c, b), i0 = seg * a.plan.tokens, all = min(a.c.n, i0 + a.plan.tokens), i1 = min(len, all);
-  const Results<T> out(p, b, h);
+  const Results<float> out(p, b, h);
   zero_rows<D, 2 * D>(out, max(i0, i1), all);
   float* const state_out = a.plan.segs == 1 ? state_out_of<D>(a, rp, b, h) : nullptr;      // (with several segments the scan writes it)
   if (i0 >= i1) {
@@ -215,8 +210,7 @@ __global__ __launch_bounds__(2 * D, 1) void decay_rows_f32_kernel(RowArgs a) {
       for (int q = 0; q < 4; ++q) {
         const int ch = 32 * w + 4 * g + 8 * q;
         const float4 v = make_float4(o[4 * q] * p.out_scale, o[4 * q + 1] * p.out_scale, o[4 * q + 2] * p.out_scale, o[4 * q + 3] * p.out_scale);
-        if (sizeof(T) == 4 || out.part) *reinterpret_cast<float4*>(out.part_row(token, ch)) = v;
-        else *reinterpret_cast<uint2*>(out.row(token, ch)) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+        *reinterpret_cast<float4*>(out.row(token, ch)) = v;      // (parts have the same type)
       }
     }
     if (more || state_out) {

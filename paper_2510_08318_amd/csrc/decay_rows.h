@@ -105,14 +105,14 @@ __device__ __forceinline__ bf16x8 turned_at2(uint32_t lo, uint32_t hi) { return 
 // Row of a k-step's element e in lane group g, as the transposing reads give them.
 __device__ __forceinline__ constexpr int row_of(int e, int g) { return 8 * (e / 4) + 4 * g + e % 4; }
 
-// Rows times their weights, as the sum of PIECES bf16 numbers.
-template <int PIECES>
-__device__ __forceinline__ void weigh(bf16x8 x, const float* w, bf16x8 (&p)[PIECES]) {
-  const u32x4 in = __builtin_bit_cast(u32x4, x);
+// Eight numbers, by pairs, as the sum of PIECES bf16 numbers each (three hold fp32 whole).
+template <int PIECES, typename Two>
+__device__ __forceinline__ void split(Two two, bf16x8 (&p)[PIECES]) {
   u32x4 out[PIECES];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    float a = f32::lo_f32(in[i]) * w[2 * i], b = f32::hi_f32(in[i]) * w[2 * i + 1];
+    float a, b;
+    two(i, a, b);
 #pragma unroll
     for (int j = 0; j < PIECES; ++j) {
       out[j][i] = pack_bf16x2(a, b);
@@ -121,6 +121,24 @@ __device__ __forceinline__ void weigh(bf16x8 x, const float* w, bf16x8 (&p)[PIEC
   }
 #pragma unroll
   for (int j = 0; j < PIECES; ++j) p[j] = __builtin_bit_cast(bf16x8, out[j]);
+}
+// Rows times their weights.
+template <int PIECES>
+__device__ __forceinline__ void weigh(bf16x8 x, const float* w, bf16x8 (&p)[PIECES]) {
+  const u32x4 in = __builtin_bit_cast(u32x4, x);
+  split([&](int i, float& a, float& b) { a = f32::lo_f32(in[i]) * w[2 * i]; b = f32::hi_f32(in[i]) * w[2 * i + 1]; }, p);
+}
+// Registers 8 h .. 8 h + 7 of an accumulator.
+template <int PIECES>
+__device__ __forceinline__ void split8(const f32x16& e, int h, bf16x8 (&p)[PIECES]) {
+  split([&](int i, float& a, float& b) { a = e[8 * h + 2 * i]; b = e[8 * h + 2 * i + 1]; }, p);
+}
+// acc += a p, the smallest piece first
+template <int PIECES>
+__device__ __forceinline__ f32x16 mfma_pieces(bf16x8 a, const bf16x8 (&p)[PIECES], f32x16 acc) {
+#pragma unroll
+  for (int j = PIECES - 1; j >= 0; --j) acc = mfma(a, p[j], acc);
+  return acc;
 }
 
 // ---- a segment's own sum --------------------------------------------------------------------------------------------
@@ -196,9 +214,7 @@ __global__ __launch_bounds__(256, 2) void decay_sum_kernel(SumArgs a) {
       weigh<PIECES>(x, wt, c);
 #pragma unroll
       for (int y = 0; y < BLOCKS; ++y) {
-        const bf16x8 r = turned<D>(from + tile, fb0 + y, 16 * ks);
-#pragma unroll
-        for (int j = PIECES - 1; j >= 0; --j) sum[y] = mfma(r, c[j], sum[y]);
+        sum[y] = mfma_pieces(turned<D>(from + tile, fb0 + y, 16 * ks), c, sum[y]);
       }
     }
   }
@@ -346,12 +362,13 @@ __device__ __forceinline__ void copy_state(const RowArgs& a, const RowPass& rp, 
     *reinterpret_cast<float4*>(to + i) = from ? *reinterpret_cast<const float4*>(from + i) : make_float4(0.f, 0.f, 0.f, 0.f);
 }
 
+// WHOLE, fp32 arithmetic on bf16 tensors: weights, states and weighted rows enter as three pieces each, so that every product is that of fp32 numbers (a_i . b_j is one of bf16 as it is).
 // STATE, of a call with one segment: the state behind the last token is handed out, so the rows c_j enter it whole, as three pieces, and lambda^chunk is a sum of two numbers.
 // Rows of a segment, chunk by chunk.  A wavefront has 32 columns of the state X in its accumulators, where they are the left operand of a_i X as they lie (rounded to bf16); the
 // chunk's weights P, on the lanes as S^T = B A^T gives them, are made by three of the wavefronts and go round through LDS.
-template <int D, bool STATE>
-__global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
-  constexpr int CB = D / 32, FB = D / 32, KS = D / 16, JS = kChunk / 16, IW = 4 / CB, IB = 2 / IW, TILE = Tile<D, false>::BYTES, PIECES = STATE ? 3 : kUpdatePieces;
+template <int D, bool STATE, bool WHOLE>
+__global__ __launch_bounds__(256, WHOLE ? 1 : 2) void decay_rows_kernel(RowArgs a) {
+  constexpr int CB = D / 32, FB = D / 32, KS = D / 16, JS = kChunk / 16, IW = 4 / CB, IB = 2 / IW, TILE = Tile<D, false>::BYTES, ONE = WHOLE ? 3 : 1, PIECES = WHOLE || STATE ? 3 : kUpdatePieces;
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
   const Place at = place_of(a.c, blockIdx.x, a.plan.segs, a.passes);
@@ -373,7 +390,7 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
   tb.of(p.b, b, h, p.back, w, lane);
   tc.of(p.c, b, h, p.back, w, lane);
   // in LDS: a chunk's a, its c, two of b; its pairs' weights; the weights that tokens have in the state behind a chunk
-  const uint32_t lds = lds_address(smem), la = lds, lc = lds + TILE, weights = lds + 4 * TILE, kept = weights + 6 * 1024;
+  const uint32_t lds = lds_address(smem), la = lds, lc = lds + TILE, weights = lds + 4 * TILE, kept = weights + ONE * 6 * 1024;
   auto b_tile = [&](int buffer) { return lds + (uint32_t)(2 + buffer) * TILE; };
   auto ask_ac = [&](int i) {
     ta.load(i, i1, len, p.back, la, w, lane);
@@ -458,7 +475,12 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = w == 1 || row_of(r % 8, g) + 16 * (r / 8) <= m ? s[r] * pairs[r] : 0.f;
 #pragma unroll
-      for (int hh = 0; hh < 2; ++hh) *(__attribute__((address_space(3))) bf16x8*)(weights_at + (uint32_t)((2 * w + hh) * 1024)) = pack8(s, hh);
+      for (int hh = 0; hh < 2; ++hh) {
+        bf16x8 piece[ONE];
+        split8(s, hh, piece);
+#pragma unroll
+        for (int j = 0; j < ONE; ++j) *(__attribute__((address_space(3))) bf16x8*)(weights_at + (uint32_t)((6 * j + 2 * w + hh) * 1024)) = piece[j];
+      }
     }
 
     // Behind the last token (see decay_scan_kernel) weights go by the chunk's tokens; those that are not there have none.
@@ -469,7 +491,7 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
     {
 #pragma unroll
       for (int y = 0; y < IB; ++y) o[y] = zero16();
-      bf16x8 op[KS * IB], xs;
+      bf16x8 op[KS * IB], xs[ONE];
       auto get = [&](int i) { op[i] = operand_at(rows_at[i / IB] + (uint32_t)((ib0 + i % IB) * 32 * D * 2)); };
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) get(i);
@@ -477,8 +499,9 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
       for (int i = 0; i < KS * IB; ++i) {
         if (i + kAhead < KS * IB) get(i + kAhead);
         __builtin_amdgcn_sched_barrier(0);
-        if (i % IB == 0) xs = pack8(x[i / IB / 2], i / IB % 2);
-        o[i % IB] = mfma(xs, op[i], o[i % IB]);
+        if (i % IB == 0) split8(x[i / IB / 2], i / IB % 2, xs);
+#pragma unroll
+        for (int j = ONE - 1; j >= 0; --j) o[i % IB] = mfma(xs[j], op[i], o[i % IB]);
         __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
@@ -505,15 +528,19 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
     if (more) ask_ac(i + kChunk);
 
     if (!one_by_one) {
-      auto weight_block = [&](int blk, int hh) { return operand_at(weights_at + (uint32_t)((2 * blk + hh) * 1024)); };
+      auto pairs_of = [&](f32x16& acc, int blk, int block) {
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+          bf16x8 piece[ONE];
+#pragma unroll
+          for (int j = 0; j < ONE; ++j) piece[j] = operand_at(weights_at + (uint32_t)((6 * j + 2 * blk + hh) * 1024));
+          acc = mfma_pieces(c[2 * block + hh], piece, acc);
+        }
+      };
 #pragma unroll
       for (int y = 0; y < IB; ++y) {
-        const int ib = ib0 + y;
-#pragma unroll
-        for (int hh = 0; hh < 2; ++hh) o[y] = mfma(c[hh], weight_block(ib, hh), o[y]);
-        if (ib)
-#pragma unroll
-          for (int hh = 0; hh < 2; ++hh) o[y] = mfma(c[2 + hh], weight_block(2, hh), o[y]);
+        pairs_of(o[y], ib0 + y, 0);
+        if (ib0 + y) pairs_of(o[y], 2, 1);
       }
     } else {
 #pragma unroll
@@ -522,7 +549,10 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
           const int jj = j % 16, src = 32 * ((jj / 4) % 2) + m, elem = jj / 8 * 4 + jj % 4;
           const int blk = ib0 + y == 0 ? 0 : j < 32 ? 1 : 2;
           const uint32_t pw = weights + (uint32_t)((2 * blk + j % 32 / 16) * 1024 + 16 * src + 2 * elem);
-          const float wt = __builtin_bit_cast(float, (uint32_t)*(__attribute__((address_space(3))) const uint16_t*)pw << 16);
+          float wt = 0.f;
+#pragma unroll
+          for (int piece = ONE - 1; piece >= 0; --piece)
+            wt += __builtin_bit_cast(float, (uint32_t)*(__attribute__((address_space(3))) const uint16_t*)(pw + (uint32_t)(piece * 6 * 1024)) << 16);
           const uint16_t* from = reinterpret_cast<const uint16_t*>(tc.base + (size_t)token_at(min(i + j, i1 - 1), len, p.back) * tc.pitch) + 32 * cb + 8 * g;
 #pragma unroll
           for (int r = 0; r < 16; ++r) o[y][r] = fmaf(wt, f32::ldf(from, 16 * (r / 8) + r % 8), o[y][r]);
@@ -556,7 +586,7 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
 #pragma unroll
       for (int f = 0; f < FB; ++f)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) x[f][r] = STATE ? fmaf(x[f][r], fade, x[f][r] * fade_lo) : x[f][r] * fade;
+        for (int r = 0; r < 16; ++r) x[f][r] = WHOLE || STATE ? fmaf(x[f][r], fade, x[f][r] * fade_lo) : x[f][r] * fade;
 #pragma unroll
       for (int ks = 0; ks < JS; ++ks) {
         bf16x8 cw[PIECES];
@@ -570,9 +600,7 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
         weigh<PIECES>(c[ks], keep, cw);
 #pragma unroll
         for (int f = 0; f < FB; ++f) {
-          const bf16x8 r = turned_at2(columns_at[f][0] + lb + (uint32_t)(16 * ks * D * 2), columns_at[f][1] + lb + (uint32_t)((16 * ks + 8) * D * 2));
-#pragma unroll
-          for (int j = PIECES - 1; j >= 0; --j) x[f] = mfma(r, cw[j], x[f]);
+          x[f] = mfma_pieces(turned_at2(columns_at[f][0] + lb + (uint32_t)(16 * ks * D * 2), columns_at[f][1] + lb + (uint32_t)((16 * ks + 8) * D * 2)), cw, x[f]);
         }
       }
     }
@@ -589,8 +617,8 @@ __global__ __launch_bounds__(256, 2) void decay_rows_kernel(RowArgs a) {
   }
 }
 
-template <int D>
-constexpr int rows_lds() { return 4 * Tile<D, false>::BYTES + 6 * 1024 + kChunk * 4; }
+template <int D, bool WHOLE>
+constexpr int rows_lds() { return 4 * Tile<D, false>::BYTES + (WHOLE ? 18 : 6) * 1024 + kChunk * 4; }
 template <int D>
 constexpr int sum_lds() { return 4 * Tile<D, false>::BYTES; }
 
