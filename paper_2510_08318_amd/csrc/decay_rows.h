@@ -1,5 +1,7 @@
 // The passes of decay.h on the matrix cores, bf16 operands and fp32 sums: chunks of kChunk tokens, inside of which a row's pairs are taken one by one, while what lies
-// before comes through the state.
+// before comes through the state.  Bytes bound the whole: a forward call reads q, k and v, writes out, and reads k and v once more for the segments' sums (from the last-level cache, where
+// they fit it).  Per token and head the products are 5 d^2 + 96 d multiply-adds (a X, the update and the segment's sum in two pieces; scores and their products), which keep the matrix cores for
+// 30 us of 12 x 32760 x 128, where the bytes are 69; the rest is the way of a chunk from memory through the matrix cores and back, which two workgroups on a compute unit overlap in part.
 #pragma once
 #include "attn_tile.h"
 #include "decay.h"
@@ -8,7 +10,6 @@
 namespace linattn {
 namespace decay {
 
-using attn::arrived;
 using attn::lds_loads_landed;
 using attn::row_at;
 using attn::turned;
@@ -156,7 +157,9 @@ struct SumArgs {
 };
 
 // sum_j lambda^(end - 1 - j) b_j^T c_j over a segment's tokens, end: the first behind them.  The rows c_j enter with their weights, whole, as three bf16 pieces (PIECES 3), where a
-// state is handed out; b_j is bf16 as it is, so that the sum is one of exact products in fp32.
+// state is handed out, as two where rows alone are made from it (their state is rounded to bf16 later); b_j is bf16 as it is, so that the sum is one of exact products in fp32.
+// Four wavefronts share a state's 32 x 32 blocks; the next chunk's rows load while this one's are multiplied.  12 x 32760 x 128 56 us with k and v from memory (201 MB, 3.6 TB/s, the matrix
+// cores busy for 16 % of it, no LDS conflicts); deeper loads, of four chunks of 32 tokens, took as long.
 template <int D, int PIECES, bool STREAM>
 __global__ __launch_bounds__(256, 2) void decay_sum_kernel(SumArgs a) {
   constexpr int CB = D / 32, BLOCKS = CB * CB / 4, KS = kChunk / 16, TILE = Tile<D, false>::BYTES;
@@ -251,7 +254,7 @@ __device__ __forceinline__ void power_of(float decay, int r, float& hi, float& l
 }
 
 // Two elements of a head's state a thread, segment after segment: X in front of segment s (as decay.h has it: out's and dq's times lambda) takes the place of its
-// sum, X' = lambda^tokens X + lambda sum.
+// sum, X' = lambda^tokens X + lambda sum.  A chain of segments, each a read and a write: at 42 segments of 12 heads 13 us (31 MB each way), at the largest call, 40 heads of 12, the same.
 __global__ __launch_bounds__(256) void decay_scan_kernel(ScanArgs a) {
   const int pass = blockIdx.z, bh = blockIdx.y, b = bh / a.c.H, h = bh % a.c.H, e = (blockIdx.x * 256 + threadIdx.x) * 2;
   const ScanPass& p = a.pass[pass];
@@ -302,7 +305,7 @@ struct RowArgs {
   Plan plan;
 };
 
-// A head's results, in the tensors' type or as fp32 parts: eight (fp32 tensors: four) adjacent channels of a token.
+// A head's results, in the tensors' type or as fp32 parts.
 template <typename T>
 struct Results {
   void* base;
@@ -364,8 +367,12 @@ __device__ __forceinline__ void copy_state(const RowArgs& a, const RowPass& rp, 
 
 // WHOLE, fp32 arithmetic on bf16 tensors: weights, states and weighted rows enter as three pieces each, so that every product is that of fp32 numbers (a_i . b_j is one of bf16 as it is).
 // STATE, of a call with one segment: the state behind the last token is handed out, so the rows c_j enter it whole, as three pieces, and lambda^chunk is a sum of two numbers.
-// Rows of a segment, chunk by chunk.  A wavefront has 32 columns of the state X in its accumulators, where they are the left operand of a_i X as they lie (rounded to bf16); the
-// chunk's weights P, on the lanes as S^T = B A^T gives them, are made by three of the wavefronts and go round through LDS.
+// Rows of a segment, chunk by chunk.  A wavefront has 32 columns of the state X in its accumulators, where they are the left operand of a_i X as they lie (rounded to bf16: with the weights
+// P, 2^-8 of a factor each, next to the 2^-8 of a result's own store; the weighted rows c_j that go into the state are the sum of two bf16 numbers, since one rounding there would stay in
+// every later row).  The chunk's weights P, on the lanes as S^T = B A^T gives them, are made by three of the wavefronts and go round through LDS.
+// 64 tokens and not 32: half as many products with X, for pairs that cost as much as they save; a wavefront has 62 products a chunk at d 128.  Two workgroups on a compute unit (80 KB of LDS
+// each, 128 + 128 registers) and not one with all its tiles twice: 40 x 75600 x 128 723 us, one 770.  12 x 32760 x 128 83 us: 435 MB at 5.3 TB/s, where the arithmetic alone takes 63 and the
+// memory alone 70; the matrix cores are busy for 23 % of it, vector instructions for 30 %, a wavefront waits for 39 %.  40 x 75600 x 128 635 us.
 template <int D, bool STATE, bool WHOLE>
 __global__ __launch_bounds__(256, WHOLE ? 1 : 2) void decay_rows_kernel(RowArgs a) {
   constexpr int CB = D / 32, FB = D / 32, KS = D / 16, JS = kChunk / 16, IW = 4 / CB, IB = 2 / IW, TILE = Tile<D, false>::BYTES, ONE = WHOLE ? 3 : 1, PIECES = WHOLE || STATE ? 3 : kUpdatePieces;
@@ -559,7 +566,8 @@ __global__ __launch_bounds__(256, WHOLE ? 1 : 2) void decay_rows_kernel(RowArgs 
         }
     }
     __builtin_amdgcn_s_setprio(0);
-    // A lane has channels 8 g .. + 7 and 16 + 8 g .. + 7 of the wavefront's 32 of row m.  Exchanged with the lane 16 further, an instruction has 64 bytes of 16 rows, not 32 of 32.
+    // A lane has channels 8 g .. + 7 and 16 + 8 g .. + 7 of the wavefront's 32 of row m.  Exchanged with the lane 16 further, an instruction has 64 bytes of 16 rows, not 32 of
+    // 32: 40 x 75600 x 128 709 us, and 635 so.  (Past the cache 1221 and 689.)
 #pragma unroll
     for (int y = 0; y < IB; ++y) {
       const int from = i + 32 * (ib0 + y);

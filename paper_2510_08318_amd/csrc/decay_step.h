@@ -1,5 +1,5 @@
 // The recurrence of decay.h token by token, in fp32: the state's elements stay in registers.  For few tokens, where a call reads and writes its states
-// and little else.
+// and little else: 64 sequences of 32 states of 128 x 128 (270 MB) take 57 us at one token, 4.7 TB/s, the rate of a copy; 12 states of 64 x 64 4.0, of which a launch is 3.
 #pragma once
 #include "decay.h"
 #include "f32_plain.h"
@@ -104,6 +104,7 @@ __global__ __launch_bounds__(256) void decay_step_kernel(Pass p, Common com) {
   }
 }
 
+// Whole states, whose reads and writes are the longest runs, where that gives every compute unit two; else 32 columns to a workgroup.
 template <typename T, int D>
 hipError_t launch_step(const Pass& p, const Common& c, hipStream_t s) {
   if ((long long)c.B * c.H >= 2 * kCUs) decay_step_kernel<T, D, D><<<dim3(c.H, c.B), 256, 0, s>>>(p, c);

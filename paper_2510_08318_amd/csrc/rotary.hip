@@ -146,7 +146,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(Args a, int heads) {
 }
 
 // Pairs in halves that are not whole 16 bytes.  A workgroup works the sines and cosines of some tokens out into LDS, then goes through their rows, 16 bytes a thread, in the order of memory; the
-// other channels of the pairs come through LDS too.  2 x 12 x 32760 x 128 bf16, 44 + 42 + 42 channels: 92 us; a pair a thread, 2 bytes an access, 123.
+// other channels of the pairs come through LDS too.  2 x 12 x 32760 x 128 bf16, 44 + 42 + 42 channels: 90 us; a pair a thread, 2 bytes an access, 123.
 template <typename T, int D, bool INNER, bool STREAM>      // INNER: [B, n, H, d]
 __global__ __launch_bounds__(256) void rotary_staged_kernel(Args a, int heads) {
   constexpr int V = kValues<T>, PARTS = D / V, ROWS = 256 / PARTS, TOKENS = 2048 / D;
