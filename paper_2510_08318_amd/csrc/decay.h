@@ -89,13 +89,13 @@ struct Plan {
 // The number of segments by what each choice should take.  A chunk of a workgroup takes `rows` us in the rows kernel and `sums` in the kernel of the sums where the chip is empty, and
 // longer by `more` for each workgroup to a compute unit (of `resident`, beyond which it is another round); a state is written, read and written, and read.  Us of kernels, fewer
 // segments / as chosen / more: 12 x 32760 x 128, 21 / 42 / 64, 174 / 152 / 184; 12 x 4680, 8 / 19 / 37, 65 / 45 / 48; 40 x 75600, 6 / 12 / 19, 1142 / 1009 / 1092; step of 2 x 12 x 4133 x 64,
-// 11 / 33, 145 / 134; step in fp32 of 2 x 1024 x 64, 16 / 32, 54 / 44.
+// 11 / 33, 145 / 134; step in fp32 of 2 x 1024 x 64, 16 / 32, 54 / 44; fp32, 12 x 32760 x 128, 21 / 42, 595 / 551, 24 x 4133 x 64, 21 / 42, 93 / 71.
 struct ChunkTimes {
   float rows, sums, more;
   int resident, chunk;
 };
 inline ChunkTimes chunk_times(bool f32, bool whole, int d) {      // of fp32 tensors; of bf16 tensors in fp32 arithmetic
-  if (f32) return d == 128 ? ChunkTimes{6.5f, 4.f, 1.f, 1, kChunkF32} : ChunkTimes{4.4f, 3.f, 0.8f, 2, kChunkF32};
+  if (f32) return d == 128 ? ChunkTimes{6.5f, 4.f, 2.f, 2, kChunkF32} : ChunkTimes{4.4f, 3.f, 0.8f, 4, kChunkF32};
   if (whole) return d == 128 ? ChunkTimes{5.f, 1.6f, 1.5f, 1, kChunk} : ChunkTimes{3.f, 1.1f, 0.6f, 2, kChunk};
   return d == 128 ? ChunkTimes{3.1f, 1.4f, 1.5f, 2, kChunk} : ChunkTimes{2.f, 1.f, 0.6f, 3, kChunk};
 }

@@ -52,8 +52,9 @@ void backward_passes(const Args& a, float* parts, Pass& dq, Pass& dv, Pass& dk) 
 }
 
 // Tokens up to which the recurrence is taken token by token.  Us a call, so / in chunks: bf16, 4 x 32 states of 128 x 128, 8 tokens 12.7 / 14.2, 16 17.9 / 13.3; 32 x 32 states, 8 tokens
-// 44.8 / 41.6, 16 63 / 43; fp32, 4 x 32 states, 8 12.8 / 18.3, 16 17.9 / 18.9, 24 24 / 19.1.
-constexpr int step_tokens(int dtype) { return dtype == LINATTN_BF16 ? 8 : 16; }
+// 44.8 / 41.6, 16 63 / 43; fp32, 4 x 32 states, 8 13.2 / -, 12 15.2 / -, 16 18.5 / 16.7, 24 24 / 16.4; bf16 in fp32 arithmetic as fp32,
+// with chunks that take longer.
+constexpr int step_tokens(int dtype) { return dtype == LINATTN_BF16 ? 8 : dtype == LINATTN_F32 ? 12 : 16; }
 
 struct Layout {
   Plan plan;
