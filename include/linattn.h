@@ -371,9 +371,9 @@ int linattn_rotary(const linattn_rotary_desc* desc, const void* q, const void* k
  * with no feature map and no denominator (a map of q and k, and a norm of o, are the caller's).  H query heads share HK key heads as in
  * linattn_window_fwd; every query head has its own decay and state.  The decay is a constant of the layer: there is no gradient for it.
  *
- * Numeric domain: states and sums are fp32, and so are all weights lambda^r.  LINATTN_BF16: the products (q . k) lambda^r and the state's entries enter the matrix cores as bf16 where they
- * make a row of out, dq, dk or dv, with fp32 sums (a rounding of at most 2^-8 relative to the factor each; with the store of the result two roundings, 1.7e-3 rms each); the rows that go
- * into a state have their weights to 2^-16, and states that are handed out (state_out, dstate_in) are products and sums in fp32.  Calls of up to 8 tokens are in fp32 throughout.
+ * Numeric domain: states and sums are fp32, and so are all weights lambda^r.  LINATTN_BF16: the products (q . k) lambda^r and the state's entries enter the matrix cores as the sum of two bf16 numbers
+ * each where they make a row of out, dq, dk or dv (2^-16 relative to the factor), with fp32 sums, so that the store of the result is the one rounding that counts (1.7e-3 rms); the rows that
+ * go into a state have their weights to 2^-16, and states that are handed out (state_out, dstate_in) are products and sums in fp32.  Calls of up to 8 tokens are in fp32 throughout.
  * LINATTN_F32, LINATTN_BF16_F32MATH: fp32 arithmetic throughout.  Of a sequence's tokens a row depends on those that it sees alone: an infinity or NaN in a later token (earlier, for
  * dk and dv), or in the padding, does not reach it.  What one does reach is not finite, NaN where arithmetic might have left an infinity, also where its weight is 0 (log_decay = -inf
  * does not keep it out).  Sums of magnitudes, a factor `scale` in them, have to stay below 2^127; magnitudes below 2^-100 may count as zero. */

@@ -100,7 +100,7 @@ hipError_t launch_states(const SumArgs& sums, const ScanArgs& scan, hipStream_t 
     const bool big = (double)sums.c.B * sums.c.n * D * 4. * (sums.passes * (sums.c.H / sums.pass[0].b.group + sums.c.H / sums.pass[0].c.group) / 2) > 256e6;
     using std::integral_constant;
     if (whole) e = big ? go(integral_constant<int, 3>{}, std::true_type{}) : go(integral_constant<int, 3>{}, std::false_type{});
-    else e = big ? go(integral_constant<int, kUpdatePieces>{}, std::true_type{}) : go(integral_constant<int, kUpdatePieces>{}, std::false_type{});
+    else e = big ? go(integral_constant<int, kPieces>{}, std::true_type{}) : go(integral_constant<int, kPieces>{}, std::false_type{});
   }
   if (e != hipSuccess) return e;
   decay_scan_kernel<<<dim3(D * D / 512, scan.c.B * scan.c.H, scan.passes), 256, 0, s>>>(scan);

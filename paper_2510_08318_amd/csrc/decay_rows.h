@@ -1,7 +1,7 @@
 // The passes of decay.h on the matrix cores, bf16 operands and fp32 sums: chunks of kChunk tokens, inside of which a row's pairs are taken one by one, while what lies
 // before comes through the state.  Bytes bound the whole: a forward call reads q, k and v, writes out, and reads k and v once more for the segments' sums (from the last-level cache, where
-// they fit it).  Per token and head the products are 5 d^2 + 96 d multiply-adds (a X, the update and the segment's sum in two pieces; scores and their products), which keep the matrix cores for
-// 30 us of 12 x 32760 x 128, where the bytes are 69; the rest is the way of a chunk from memory through the matrix cores and back, which two workgroups on a compute unit overlap in part.
+// they fit it).  Per token and head the products are 6 d^2 + 144 d multiply-adds (a X, the update, the segment's sum and the weights' products in two pieces; scores), which keep the matrix cores
+// for 37 us of 12 x 32760 x 128, where the bytes are 69; the rest is the way of a chunk from memory through the matrix cores and back, which two workgroups on a compute unit overlap in part.
 #pragma once
 #include "attn_tile.h"
 #include "decay.h"
@@ -157,7 +157,7 @@ struct SumArgs {
 };
 
 // sum_j lambda^(end - 1 - j) b_j^T c_j over a segment's tokens, end: the first behind them.  The rows c_j enter with their weights, whole, as three bf16 pieces (PIECES 3), where a
-// state is handed out, as two where rows alone are made from it (their state is rounded to bf16 later); b_j is bf16 as it is, so that the sum is one of exact products in fp32.
+// state is handed out, as two where rows alone are made from it (their state enters them as two); b_j is bf16 as it is, so that the sum is one of exact products in fp32.
 // Four wavefronts share a state's 32 x 32 blocks; the next chunk's rows load while this one's are multiplied.  12 x 32760 x 128 56 us with k and v from memory (201 MB, 3.6 TB/s, the matrix
 // cores busy for 16 % of it, no LDS conflicts); deeper loads, of four chunks of 32 tokens, took as long.
 template <int D, int PIECES, bool STREAM>
@@ -347,7 +347,7 @@ __device__ __forceinline__ void load_state(const RowArgs& a, const RowPass& rp, 
   else take([&](int row, int column) { return from[row * D + column] * factor; });
 }
 
-constexpr int kUpdatePieces = 2, kAhead = 6;      // kAhead: operands that are requested ahead of their products
+constexpr int kPieces = 2, kAhead = 6;      // kPieces: bf16 numbers to a factor of products that make rows; kAhead: operands that are requested ahead of their products
 
 // Where a pass's state goes, null where nowhere; of a sequence without tokens it is the state that it came with.
 template <int D>
@@ -366,16 +366,17 @@ __device__ __forceinline__ void copy_state(const RowArgs& a, const RowPass& rp, 
 }
 
 // WHOLE, fp32 arithmetic on bf16 tensors: weights, states and weighted rows enter as three pieces each, so that every product is that of fp32 numbers (a_i . b_j is one of bf16 as it is).
-// STATE, of a call with one segment: the state behind the last token is handed out, so the rows c_j enter it whole, as three pieces, and lambda^chunk is a sum of two numbers.
-// Rows of a segment, chunk by chunk.  A wavefront has 32 columns of the state X in its accumulators, where they are the left operand of a_i X as they lie (rounded to bf16: with the weights
-// P, 2^-8 of a factor each, next to the 2^-8 of a result's own store; the weighted rows c_j that go into the state are the sum of two bf16 numbers, since one rounding there would stay in
-// every later row).  The chunk's weights P, on the lanes as S^T = B A^T gives them, are made by three of the wavefronts and go round through LDS.
-// 64 tokens and not 32: half as many products with X, for pairs that cost as much as they save; a wavefront has 62 products a chunk at d 128.  Two workgroups on a compute unit (80 KB of LDS
+// STATE, of a call with one segment: the state behind the last token is handed out, so the rows c_j enter it whole, as three pieces, and lambda^chunk is a sum of two numbers.  (Else it
+// is one, off by 2^-25: after k chunks of a segment, k 2^-25 of what came before them, at most as much as a piece's rounding over the 100 chunks of the longest segments of several.)
+// Rows of a segment, chunk by chunk.  A wavefront has 32 columns of the state X in its accumulators, where they are the left operand of a_i X as they lie.  X, the weights P and
+// the weighted rows c_j that go into the state are the sum of two bf16 numbers each, 2^-16 of a factor next to the 2^-8 of a result's own store, so that a result is as good as the store
+// (1.66e-3 of its 2-norm; with X and P rounded to one bf16 number 2.35e-3, and a forward call 148 us at 12 x 32760 x 128 where it takes 156).  The chunk's weights P, on the lanes as S^T = B A^T gives them, are made by three of the wavefronts and go round through LDS.
+// 64 tokens and not 32: half as many products with X, for pairs that cost as much as they save; a wavefront has 84 products a chunk at d 128.  Two workgroups on a compute unit (80 KB of LDS
 // each, 128 + 128 registers) and not one with all its tiles twice: 40 x 75600 x 128 723 us, one 770.  12 x 32760 x 128 83 us: 435 MB at 5.3 TB/s, where the arithmetic alone takes 63 and the
 // memory alone 70; the matrix cores are busy for 23 % of it, vector instructions for 30 %, a wavefront waits for 39 %.  40 x 75600 x 128 635 us.
 template <int D, bool STATE, bool WHOLE>
 __global__ __launch_bounds__(256, WHOLE ? 1 : 2) void decay_rows_kernel(RowArgs a) {
-  constexpr int CB = D / 32, FB = D / 32, KS = D / 16, JS = kChunk / 16, IW = 4 / CB, IB = 2 / IW, TILE = Tile<D, false>::BYTES, ONE = WHOLE ? 3 : 1, PIECES = WHOLE || STATE ? 3 : kUpdatePieces;
+  constexpr int CB = D / 32, FB = D / 32, KS = D / 16, JS = kChunk / 16, IW = 4 / CB, IB = 2 / IW, TILE = Tile<D, false>::BYTES, ONE = WHOLE ? 3 : kPieces, PIECES = WHOLE || STATE ? 3 : kPieces;
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 32, g = lane / 32;
   const Place at = place_of(a.c, blockIdx.x, a.plan.segs, a.passes);
@@ -626,7 +627,7 @@ __global__ __launch_bounds__(256, WHOLE ? 1 : 2) void decay_rows_kernel(RowArgs 
 }
 
 template <int D, bool WHOLE>
-constexpr int rows_lds() { return 4 * Tile<D, false>::BYTES + (WHOLE ? 18 : 6) * 1024 + kChunk * 4; }
+constexpr int rows_lds() { return 4 * Tile<D, false>::BYTES + (WHOLE ? 3 : kPieces) * 6 * 1024 + kChunk * 4; }
 template <int D>
 constexpr int sum_lds() { return 4 * Tile<D, false>::BYTES; }
 
