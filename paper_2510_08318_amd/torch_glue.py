@@ -396,25 +396,42 @@ def _result(name, out, like, index):
     return out
 
 
+# Numbers as a call's description is kept by: Python's own, taken from the caller's objects at every call, since a tensor's value may change while its identity does not.
+
+
+def _whole(name, x):
+    try:
+        i = int(x)
+    except (TypeError, ValueError, OverflowError):
+        i = None
+    _need(i is not None and i == x, f"{name}: whole numbers, got {x!r}")
+    return i
+
+
+def _ints(name, values):
+    if values is None or type(values) is tuple and all([type(x) is int for x in values]):
+        return values
+    return tuple([_whole(name, x) for x in values])
+
+
+def _float(x):
+    return x if type(x) is float else float(x.detach() if isinstance(x, torch.Tensor) else x)
+
+
 def _int3(name, values, axes):
-    values = [int(x) for x in values]
     _need(len(values) == axes and all(-(1 << 31) <= x < 1 << 31 for x in values), f"{name}: a 32-bit number for each axis")
     return (B_.ctypes.c_int * 3)(*values)
 
 
 @functools.lru_cache(maxsize=256)
 def _rotary_desc(dtype, B, H, HK, n, d, layout, dims, pairs, inverse, base, grid, first):
-    """The description of a call without its tensors."""
+    """The description of a call without its tensors, from plain numbers."""
     axes = len(dims)
     _need(1 <= axes <= 3 and pairs in ("adjacent", "halves"), "dims: one to three axes; pairs: 'adjacent' or 'halves'")
     return B_.RotaryDesc(dtype, B, H, HK, n, d, _layout_code(layout), axes, _int3("dims", dims, axes),
                          B_.PAIRS_HALVES if pairs == "halves" else B_.PAIRS_ADJACENT, int(inverse), base,
                          _int3("grid", grid if grid is not None else (1,) * axes, axes), _int3("first", first if first is not None else (0,) * axes, axes),
                          None, 0, None)
-
-
-def _numbers(values):
-    return values if values is None or type(values) is tuple else tuple(values)
 
 
 @_on_device_of
@@ -436,9 +453,10 @@ def rotary(q, k=None, *, dims=None, grid=None, first=None, positions=None, base=
     else:
         HK = _token_dims(k, layout)[1]
         _check_tokens("k", k, _token_shape(B, HK, n, d, layout), q.dtype, index)
-    dims = (d,) if dims is None else _numbers(dims)
+    dims = (d,) if dims is None else _ints("dims", dims)
     _need(grid is not None or positions is not None or len(dims) == 1, "grid: the tokens along each axis")
-    desc = B_.RotaryDesc.from_buffer_copy(_rotary_desc(dtype, B, H, HK, n, d, layout, dims, pairs, bool(inverse), base, _numbers(grid), _numbers(first)))
+    desc = B_.RotaryDesc.from_buffer_copy(_rotary_desc(dtype, B, H, HK, n, d, layout, dims, pairs, bool(inverse), _float(base), _ints("grid", grid),
+                                                          _ints("first", first)))
     if positions is not None:
         shared = positions.dim() == 2
         _check_ints("positions", positions, (n, len(dims)) if shared else (B, n, len(dims)), index)
@@ -459,7 +477,7 @@ def _check_state(name, t, shape, index):
 
 @functools.lru_cache(maxsize=256)
 def _decay_numbers(dtype, B, H, HK, n, d, layout, scale, states):
-    """The description of a call without its tensors, and the sizes of its workspaces (forward, backward), which its numbers decide."""
+    """The description of a call without its tensors, and the sizes of its workspaces (forward, backward), which its numbers, plain ones, decide."""
     some = 256      # an address, for the checks
     desc = B_.DecayDesc(dtype, B, H, HK, n, d, _layout_code(layout), scale, some, None, some if states else None, states, None, 0)
     return desc, [B_.linattn_decay_workspace_bytes(desc, backward) for backward in (False, True)]
@@ -476,7 +494,7 @@ def _decay_desc(q, k, v, log_decay, slots, states, scale, layout, lengths, f32_m
     _check_tokens("log_decay", log_decay, (H,), torch.float32, index)
     _check_ints("lengths", lengths, (B,), index)
     _check_ints("slots", slots, (B,), index)
-    numbers, sizes = _decay_numbers(dtype, B, H, HK, n, d, layout, scale, states)
+    numbers, sizes = _decay_numbers(dtype, B, H, HK, n, d, layout, _float(scale), states)
     desc = B_.DecayDesc.from_buffer_copy(numbers)
     desc.log_decay, desc.lengths, desc.slots = B_._ptr(log_decay), B_._ptr(lengths), B_._ptr(slots)
     work = None
