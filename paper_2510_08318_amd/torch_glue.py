@@ -396,6 +396,13 @@ def _result(name, out, like, index):
     return out
 
 
+def _overwritten(*given):
+    """Counts a write in tensors that the caller gave for results: autograd then refuses a backward pass that needs what was in them."""
+    tensors = [t for t in given if isinstance(t, torch.Tensor)]
+    if tensors:
+        torch.autograd.graph.increment_version(tensors)
+
+
 # Numbers as a call's description is kept by: Python's own, taken from the caller's objects at every call, since a tensor's value may change while its identity does not.
 
 
@@ -442,7 +449,7 @@ def rotary(q, k=None, *, dims=None, grid=None, first=None, positions=None, base=
     channels of an axis, or of its "halves".  Positions: token i has the coordinates of i in `grid` (tokens along each axis, the last fastest; not needed
     with one axis), plus `first`; or int32 `positions` [n, axes] or [B, n, axes], in place of both.  inverse: turned back, which is also the gradient: rotary(dq, dk, ...,
     inverse=True).  lengths: int32 [B], the tokens of each item; the rest is padding.  q_out, k_out may be q and k.  Returns (q_out, k_out), or
-    (q_out, None) without k.  Nothing is recorded for autograd."""
+    (q_out, None) without k.  Nothing is recorded for autograd; tensors that are given for results count as changed in place."""
     B, H, n, d = _token_dims(q, layout)
     index = q.get_device()
     dtype = _dtype_code(q, False)
@@ -464,9 +471,11 @@ def rotary(q, k=None, *, dims=None, grid=None, first=None, positions=None, base=
     if lengths is not None:
         _check_ints("lengths", lengths, (B,), index)
         desc.lengths = lengths.data_ptr()
+    given = q_out, k_out
     q_out = _result("q_out", q_out, q, index)
     k_out = _result("k_out", k_out, k, index) if k is not None else None
     B_.linattn_rotary(desc, q, k, q_out, k_out, _raw_stream(index))
+    _overwritten(*given)
     return q_out, k_out
 
 
@@ -519,7 +528,7 @@ def decay_attention(q, k, v, log_decay, *, state=None, slots=None, scale=0.0, la
     itself.  slots: int32 [B], the items' rows of `state` and state_out, which then are [any, H, d, d] and of which one is given at least (state_out=None then stands for
     `state` itself).  lengths: int32 [B], the tokens of each item; the rest is padding.  scale: 0 for 1/sqrt(d).  f32_math: fp32 arithmetic on bf16 tensors.  n = 1 is the step of
     generation token by token.  Returns (out, state_out), or (out, None).  Nothing is recorded for autograd, also where inputs require a gradient:
-    decay_attention_backward gives it, and a torch.autograd.Function around the two has it recorded."""
+    decay_attention_backward gives it, and a torch.autograd.Function around the two has it recorded.  Tensors that are given for results count as changed in place."""
     index = q.get_device()
     if slots is not None:
         pool = state if state is not None else state_out
@@ -528,6 +537,7 @@ def decay_attention(q, k, v, log_decay, *, state=None, slots=None, scale=0.0, la
         state_out = state if state_out is None else state_out
     else:
         states = 0
+    given = out, state_out
     desc, work = _decay_desc(q, k, v, log_decay, slots, states, scale, layout, lengths, f32_math, False)
     shape = _state_shape(desc)
     _check_state("state", state, shape, index)
@@ -539,6 +549,7 @@ def decay_attention(q, k, v, log_decay, *, state=None, slots=None, scale=0.0, la
         _check_state("state_out", state_out, shape, index)
     out = _result("out", out, q, index)
     B_.linattn_decay_fwd(desc, q, k, v, state, out, state_out, _raw_stream(index))
+    _overwritten(*given)
     return out, state_out
 
 
@@ -548,7 +559,7 @@ def decay_attention_backward(q, k, v, log_decay, dout, *, state=None, dstate=Non
     """Gradients (dq, dk, dv, dstate_in) of decay_attention (same keyword arguments) for the upstream gradients dout and dstate (of state_out; fp32 [B, H, d, d],
     None: zeros).  dstate_in, the gradient of `state`, is by item, [B, H, d, d], also where states go by slots: None for a new tensor where a state was given (else
     none is made), False where it is not wanted.  log_decay is a constant of the layer and has no gradient.  Nothing is recorded for autograd."""
-    index = q.get_device()
+    index, given = q.get_device(), (dq, dk, dv, dstate_in)
     _need(slots is None or state is not None, "slots: rows of state")
     desc, work = _decay_desc(q, k, v, log_decay, slots, state.shape[0] if slots is not None else 0, scale, layout, lengths, f32_math, True)
     _check_state("state", state, _state_shape(desc), index)
@@ -562,4 +573,5 @@ def decay_attention_backward(q, k, v, log_decay, dout, *, state=None, dstate=Non
     _check_state("dstate_in", dstate_in, by_item, index)
     dq, dk, dv = [_result(name, g, like, index) for name, g, like in (("dq", dq, q), ("dk", dk, k), ("dv", dv, v))]
     B_.linattn_decay_bwd(desc, q, k, v, state, dout, dstate, dq, dk, dv, dstate_in, _raw_stream(index))
+    _overwritten(*given)
     return dq, dk, dv, dstate_in

@@ -113,3 +113,54 @@ def test_numbers_that_are_refused(calls, kw):
     with pytest.raises(ValueError):
         _rotary(**kw)
     assert not calls
+
+
+def _saved(x):
+    """A graph that holds x as it is now."""
+    w = torch.ones(x.shape, dtype=x.dtype, requires_grad=True)
+    return (w * torch.Tensor.as_subclass(x, torch.Tensor)).sum()
+
+
+def _refused(graph):
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        graph.backward()
+
+
+def test_autograd_sees_what_rotary_overwrites(calls):
+    q, k = tensor(1, 2, 12, 64), tensor(1, 2, 12, 64)
+    a, b = _saved(q), _saved(k)
+    G.rotary(q, k)
+    a.backward(retain_graph=True)                       # (results of their own leave q and k alone)
+    G.rotary(q, k, q_out=q, k_out=k)
+    _refused(a), _refused(b)
+
+
+def test_autograd_sees_the_states_and_results_that_decay_attention_overwrites(calls):
+    q, g = tensor(1, 2, 5, 64), tensor(2, dtype=torch.float32)
+    for kw in (dict(), dict(slots=tensor(1, dtype=torch.int32))):
+        state = tensor(1, 2, 64, 64, dtype=torch.float32)
+        kept = _saved(state)
+        G.decay_attention(q, q, q, g, state=state, state_out=False, **kw)
+        kept.backward(retain_graph=True)
+        G.decay_attention(q, q, q, g, state=state, **(kw or dict(state_out=state)))      # (with slots, in place without a word)
+        _refused(kept)
+    out = tensor(1, 2, 5, 64)
+    kept = _saved(out)
+    G.decay_attention(q, q, q, g, out=out)
+    _refused(kept)
+
+
+def test_autograd_sees_the_gradients_that_are_overwritten(calls):
+    q, g, state = tensor(1, 2, 5, 64), tensor(2, dtype=torch.float32), tensor(1, 2, 64, 64, dtype=torch.float32)
+    outs = dict(dq=tensor(1, 2, 5, 64), dk=tensor(1, 2, 5, 64), dv=tensor(1, 2, 5, 64), dstate_in=tensor(1, 2, 64, 64, dtype=torch.float32))
+    kept = [_saved(x) for x in outs.values()]
+    G.decay_attention_backward(q, q, q, g, q, state=state, **outs)
+    for x in kept:
+        _refused(x)
+
+
+def test_tensors_of_inference_mode_have_no_count(calls):
+    with torch.inference_mode():
+        q = tensor(1, 2, 12, 64)
+        assert G.rotary(q, q_out=q)[0] is q
+    assert G.rotary(q, q_out=q)[0] is q
