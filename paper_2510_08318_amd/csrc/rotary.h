@@ -20,6 +20,15 @@ struct Args {
   double turns[64];         // of pair p, in the order of the axes: turns for each position, base^(-2m / dims) / (2 pi)
 };
 
+// Workgroups of the tokens, `blocks` in all, in grid.x and grid.z (the last of z has ones behind the end), the groups of heads in grid.y.  A launch holds fewer than 2^32 threads in grid.x,
+// 2^24 workgroups; 2^27 tokens of fp32 x 128, 64 GB with one head, are as many.  The most blocks, 2^35 tokens in eights, are 2^12 in grid.z.
+constexpr unsigned kGridX = 1u << 20;
+inline dim3 grid_of(long long blocks, int groups) {
+  const unsigned x = blocks < kGridX ? (unsigned)blocks : kGridX;
+  return dim3(x, (unsigned)groups, (unsigned)((blocks + x - 1) / x));
+}
+__device__ __forceinline__ long long block_of() { return (long long)blockIdx.z * gridDim.x + blockIdx.x; }
+
 hipError_t launch(const Args& a, bool f32, hipStream_t s);
 
 }  // namespace rotary

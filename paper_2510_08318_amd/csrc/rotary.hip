@@ -80,7 +80,7 @@ template <typename T, int D, bool HALVES, bool STREAM>
 __global__ __launch_bounds__(256) void rotary_kernel(Args a, int heads) {
   constexpr int NP = Pairs<T, HALVES>::NP, PARTS = D / 2 / NP;
   const int part = threadIdx.x % PARTS;
-  const long long token = (long long)blockIdx.x * (256 / PARTS) + threadIdx.x / PARTS, tokens = (long long)a.B * a.n;
+  const long long token = block_of() * (256 / PARTS) + threadIdx.x / PARTS, tokens = (long long)a.B * a.n;
   if (token >= tokens) return;
   const int b = tokens >> 32 ? (int)(token / a.n) : (int)((uint32_t)token / (uint32_t)a.n), t = (int)(token - (long long)b * a.n);
   const bool live = t < (a.lengths ? a.lengths[b] : a.n);
@@ -154,7 +154,8 @@ __global__ __launch_bounds__(256) void rotary_staged_kernel(Args a, int heads) {
   __shared__ size_t first[TOKENS][2];                  // element of the token's row of head 0 of q, of k
   __shared__ int live[TOKENS];
   __shared__ uint4 staged[256];
-  const long long token0 = (long long)blockIdx.x * TOKENS, tokens = (long long)a.B * a.n;
+  const long long token0 = block_of() * TOKENS, tokens = (long long)a.B * a.n;
+  if (token0 >= tokens) return;
   const int count = tokens - token0 < TOKENS ? (int)(tokens - token0) : TOKENS;
   for (int i = threadIdx.x; i < count * (D / 2); i += 256) {
     const int x = i / (D / 2), pair = i % (D / 2), ch = 2 * pair;
@@ -267,7 +268,7 @@ hipError_t run(const Args& a, hipStream_t s) {
   const int tokens = whole ? 256 / (a.halves ? D / 2 / V : D / V) : 2048 / D, all = a.H + a.HK;
   const long long blocks = ((long long)a.B * a.n + tokens - 1) / tokens;
   const int heads = heads_of(all, blocks);
-  const dim3 grid((unsigned)blocks, (all + heads - 1) / heads);
+  const dim3 grid = grid_of(blocks, (all + heads - 1) / heads);
   // Rows that the last-level cache of 256 MB has no room for, with the results, go past it.  Us, so / through the cache, with rows that are not in it, 2 x 12 heads of bf16 x 128: 32760 tokens (403
   // MB with the results) 77 / 82, [B, H, n, d] 73 / 78; 16000 (197 MB) 39 / 43, 35 / 41, where the results are left for what reads them next.
   const bool big = 2. * (double)a.B * a.n * all * D * sizeof(T) > 300e6;
