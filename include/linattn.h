@@ -343,7 +343,7 @@ int linattn_cache_attn(const linattn_cache_desc* desc, const linattn_sight* sigh
 
 typedef struct linattn_rotary_desc {
   int dtype;              /* LINATTN_BF16 (LINATTN_BF16_F32MATH is the same here) or LINATTN_F32 */
-  int B, H, HK, n, d;     /* heads of q and of k, any numbers (HK is not looked at without k); d 64 or 128 */
+  int B, H, HK, n, d;     /* heads of q and of k, each any number (HK is not looked at without k); d 64 or 128; B * H and B * HK up to 65535, n up to 2^30, B * n * heads up to 2^35 */
   int layout;
   int axes;               /* 1 to 3 */
   int dims[3];            /* channels of each axis: even, together at most d */
@@ -379,7 +379,7 @@ int linattn_rotary(const linattn_rotary_desc* desc, const void* q, const void* k
  * does not keep it out).  Sums of magnitudes, a factor `scale` in them, have to stay below 2^127; magnitudes below 2^-100 may count as zero. */
 typedef struct linattn_decay_desc {
   int dtype;              /* LINATTN_BF16, LINATTN_F32 or LINATTN_BF16_F32MATH: type of q, k, v, out, dout, dq, dk, dv */
-  int B, H, HK, n, d;     /* H a multiple of HK, d 64 or 128 */
+  int B, H, HK, n, d;     /* H a multiple of HK, d 64 or 128; B * H up to 65535, n up to 2^30, B * n * H up to 2^35 */
   int layout;
   float scale;            /* 2^-100 to 2^100; 0: 1 / sqrt(d) */
   const float* log_decay; /* device [H], at most 0 (what is above, or NaN, counts as 0; -inf: a token sees itself alone) */

@@ -1,12 +1,36 @@
-"""Launches of linattn_rotary and linattn_decay_* that hold every size that linattn.h allows."""
+"""The sizes that linattn.h allows for linattn_rotary and linattn_decay_*: the last of them is taken, the next refused; and grids that hold them."""
 import os
 import shutil
 import subprocess
 
 import pytest
 
+from paper_2510_08318_amd import binding as L
+from tests.test_seq_host import _decay, _rotary
+
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
+
+
+# (a call without tensors is refused for them, once its sizes are taken)
+@pytest.mark.parametrize("size,status", [
+    (dict(B=2047, H=32, HK=32, n=1), "E_NULL"), (dict(B=2048, H=32, HK=32, n=1), "E_SHAPE"), (dict(B=1, H=65535, HK=1, n=1), "E_NULL"),
+    (dict(B=1, H=65536, HK=1, n=1), "E_SHAPE"), (dict(B=1, H=1, HK=1, n=1 << 30), "E_NULL"), (dict(B=1, H=1, HK=1, n=(1 << 30) + 1), "E_SHAPE"),
+    (dict(B=32, H=1, HK=1, n=1 << 30), "E_NULL"), (dict(B=33, H=1, HK=1, n=1 << 30), "E_SHAPE"), (dict(B=1, H=32, HK=1, n=1 << 30), "E_NULL"),
+    (dict(B=1, H=33, HK=1, n=1 << 30), "E_SHAPE")])
+def test_sizes_at_the_limits(size, status):
+    assert L.linattn_rotary(_rotary(**size), None, None, None, None, check=False) == getattr(L, status)
+    assert L.linattn_decay_fwd(_decay(**size), *[None] * 6, check=False) == getattr(L, status)
+    assert L.linattn_decay_bwd(_decay(**size), *[None] * 10, check=False) == getattr(L, status)
+
+
+def test_rotary_s_key_heads_have_the_same_limit():
+    P = 1 << 40
+    call = lambda HK: L.linattn_rotary(_rotary(B=1, H=1, HK=HK, n=1, dims=(32, 16, 0x7ffe)), P, P, P, P, check=False)
+    assert call(65536) == L.E_SHAPE
+    assert L.linattn_rotary(_rotary(B=1, H=1, HK=65535, n=1), None, P, None, P, check=False) == L.E_NULL
+    assert L.linattn_rotary(_rotary(B=1, H=1, HK=65536, n=1), None, P, None, P, check=False) == L.E_SHAPE
+    assert L.linattn_rotary(_rotary(B=1, H=1, HK=65536, n=1), None, None, None, None, check=False) == L.E_NULL
 
 
 PROGRAM = r"""
