@@ -7,6 +7,9 @@ results in the tensors' type: the error of the definition's own result after its
     channels of many pairs, so that the sum is off by a fraction of 2^-16 |y|, and e = 2^-13 leaves a factor of eight and more.  fp32: e = 2^-18, below.
 sums in fp32: an element is a sum over 64 or 128 channels, 32 or 64 tokens of a chunk, and the chunks and segments before it: at most 400 roundings in a row in the sizes here, each at most
     2^-24 of a partial sum that is at most a few times the result in the 2-norm; sqrt(400) 2^-24 = 2^-19.7, and 2^-18 leaves a factor of three.
+|y| is the 2-norm of the result or, where that is larger, of the root of the sum of its terms' squares.  Partial sums are as large as the latter, whatever is left of them: of one token without a
+    state, out = scale (q . k) v, where q . k of 64 or 128 products with random signs is as often as not below two thirds of the root of the sum of their squares, in one of a hundred below an
+    eightieth, and its roundings are those of the partial sums.  The terms' squares are the same sums of squared numbers, the decay twice as fast.
 states that are handed out are such sums, of bf16 tensors too.
 """
 import pytest
@@ -72,12 +75,12 @@ def _dstate(q, do, g, c, ds):
     return x if ds is None else x + math.exp(g * len(q)) * ds
 
 
-def _near(name, mode, got, want, dtype, before):
-    """Blocks of 64 rows; want in 64 bits."""
+def _near(name, mode, got, want, squares, dtype, before):
+    """Blocks of 64 rows; want, and the sums of its terms' squares, in 64 bits."""
     s = (want.to(dtype).double() - want)
     for r in range(0, len(want), 64):
         e = slice(r, r + 64)
-        err, tol = (got[e].double() - want[e]).norm(), 1.03 * s[e].norm() + before * want[e].norm()
+        err, tol = (got[e].double() - want[e]).norm(), 1.03 * s[e].norm() + before * max(want[e].norm(), squares[e].sum().sqrt())
         assert err <= tol, (name, mode, r, (err / want[e].norm()).item(), (tol / want[e].norm()).item())
 
 
@@ -106,22 +109,24 @@ def check(mode, B, H, HK, n, d, layout="bhnd", lengths=None, state=True, train=T
         for j in range(HK):
             if heads is not None and (b, j) not in heads:
                 continue
-            dk = dv = 0.0
+            dk = dv = dk2 = dv2 = 0.0
             for h in range(j * R, j * R + R):
-                w = _definition(q[b, h, :m].double(), k[b, j, :m].double(), v[b, j, :m].double(), do[b, h, :m].double(), float(g[h].double()), d ** -0.5,
-                                None if s0 is None else s0[b, h].double(), None if ds1 is None else ds1[b, h].double())
-                _near(f"out {b} {h}", mode, got["out"][b, h, :m], w[0], out.dtype, BEFORE[mode])
-                _near(f"out alone {b} {h}", mode, got["only"][b, h, :m], w[0], out.dtype, BEFORE[mode])
-                _near(f"state {b} {h}", mode, end[b, h], w[1], torch.float32, SUMS)
+                x = [None if t is None else t.double() for t in (q[b, h, :m], k[b, j, :m], v[b, j, :m], do[b, h, :m], None if s0 is None else s0[b, h],
+                                                                 None if ds1 is None else ds1[b, h])]
+                w = _definition(*x[:4], float(g[h].double()), d ** -0.5, *x[4:])
+                z = _definition(*[t * t for t in x[:4]], 2 * float(g[h].double()), 1 / d, *[None if t is None else t * t for t in x[4:]])
+                _near(f"out {b} {h}", mode, got["out"][b, h, :m], w[0], z[0], out.dtype, BEFORE[mode])
+                _near(f"out alone {b} {h}", mode, got["only"][b, h, :m], w[0], z[0], out.dtype, BEFORE[mode])
+                _near(f"state {b} {h}", mode, end[b, h], w[1], z[1], torch.float32, SUMS)
                 assert not got["out"][b, h, m:].any() and not got["only"][b, h, m:].any()
                 if train:
-                    _near(f"dq {b} {h}", mode, got["dq"][b, h, :m], w[2], out.dtype, BEFORE[mode])
-                    dk, dv = dk + w[3], dv + w[4]
+                    _near(f"dq {b} {h}", mode, got["dq"][b, h, :m], w[2], z[2], out.dtype, BEFORE[mode])
+                    dk, dv, dk2, dv2 = dk + w[3], dv + w[4], dk2 + z[3], dv2 + z[4]
                     if state:
-                        _near(f"dstate {b} {h}", mode, dstate[b, h], w[5], torch.float32, SUMS)
+                        _near(f"dstate {b} {h}", mode, dstate[b, h], w[5], z[5], torch.float32, SUMS)
             if train:
-                for name, x in (("dk", dk), ("dv", dv)):
-                    _near(f"{name} {b} {j}", mode, got[name][b, j, :m], x, out.dtype, BEFORE[mode])
+                for name, x, x2 in (("dk", dk, dk2), ("dv", dv, dv2)):
+                    _near(f"{name} {b} {j}", mode, got[name][b, j, :m], x, x2, out.dtype, BEFORE[mode])
                     assert not got[name][b, j, m:].any()
 
 
