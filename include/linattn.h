@@ -403,7 +403,8 @@ int linattn_decay_fwd(const linattn_decay_desc* desc, const void* q, const void*
                       void* stream);
 
 /* Backward for L with dL/dout = dout and dL/dstate_out = dstate_out; writes dq, dk, dv (dk and dv summed over the query heads of a group) and dstate_in = dL/dstate_in.
- * state_in: the forward's.  dstate_out, dstate_in: optional device fp32 [B, H, d, d], by item also where the forward went by slots.
+ * state_in: the forward's.  dstate_out, dstate_in: optional device fp32 [B, H, d, d], by item also where the forward went by slots; an
+ * item without a slot has zeros for state_in, and its dstate_out counts as any other's (zeros belong there: its state went nowhere).
  * Errors: as above. */
 int linattn_decay_bwd(const linattn_decay_desc* desc, const void* q, const void* k, const void* v, const float* state_in, const void* dout,
                       const float* dstate_out, void* dq, void* dk, void* dv, float* dstate_in, void* stream);

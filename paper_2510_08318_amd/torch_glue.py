@@ -557,8 +557,8 @@ def decay_attention(q, k, v, log_decay, *, state=None, slots=None, scale=0.0, la
 def decay_attention_backward(q, k, v, log_decay, dout, *, state=None, dstate=None, slots=None, scale=0.0, layout="bhnd", lengths=None, f32_math=False,
                              dq=None, dk=None, dv=None, dstate_in=None):
     """Gradients (dq, dk, dv, dstate_in) of decay_attention (same keyword arguments) for the upstream gradients dout and dstate (of state_out; fp32 [B, H, d, d],
-    None: zeros).  dstate_in, the gradient of `state`, is by item, [B, H, d, d], also where states go by slots: None for a new tensor where a state was given (else
-    none is made), False where it is not wanted.  log_decay is a constant of the layer and has no gradient.  Nothing is recorded for autograd."""
+    None: zeros).  dstate_in, the gradient of `state`, is by item, [B, H, d, d], also where states go by slots (dstate of an item without one is
+    used as it is: zeros belong there): None for a new tensor where a state was given (else none is made), False where it is not wanted.  log_decay is a constant of the layer and has no gradient.  Nothing is recorded for autograd."""
     index, given = q.get_device(), (dq, dk, dv, dstate_in)
     _need(slots is None or state is not None, "slots: rows of state")
     desc, work = _decay_desc(q, k, v, log_decay, slots, state.shape[0] if slots is not None else 0, scale, layout, lengths, f32_math, True)
