@@ -398,9 +398,9 @@ def _result(name, out, like, index):
 
 def _overwritten(*given):
     """Counts a write in tensors that the caller gave for results: autograd then refuses a backward pass that needs what was in them."""
-    tensors = [t for t in given if isinstance(t, torch.Tensor)]
-    if tensors:
-        torch.autograd.graph.increment_version(tensors)
+    for t in given:
+        if t is not None and t is not False:
+            torch.autograd.graph.increment_version(t)
 
 
 # Numbers as a call's description is kept by: Python's own, taken from the caller's objects at every call, since a tensor's value may change while its identity does not.
@@ -416,8 +416,14 @@ def _whole(name, x):
 
 
 def _ints(name, values):
-    if values is None or type(values) is tuple and all([type(x) is int for x in values]):
-        return values
+    if values is None:
+        return None
+    if type(values) is tuple:
+        for x in values:
+            if type(x) is not int:
+                break
+        else:
+            return values
     return tuple([_whole(name, x) for x in values])
 
 
