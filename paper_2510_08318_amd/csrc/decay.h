@@ -41,7 +41,8 @@ struct Common {
   int states, B, H, group, n;      // group: query heads to a key head
 };
 
-// A head's decay as the kernels use it: what is above 0, or NaN, counts as 0, and -inf as a number whose products with distances stay finite.
+// A head's decay as the kernels use it: what is above 0, or NaN, counts as 0, and -inf as a number whose product with a distance of 0 is 0.  (Products with far distances may be -inf; exp
+// gives 0 for them.)
 __device__ __forceinline__ float log_decay_of(const Common& c, int h) { return fmaxf(fminf(c.log_decay[h], 0.f), -1e30f); }
 __host__ __device__ inline int length_of(const Common& c, int b) {
   if (!c.lengths) return c.n;
@@ -88,8 +89,9 @@ struct Plan {
 };
 // The number of segments by what each choice should take.  A chunk of a workgroup takes `rows` us in the rows kernel and `sums` in the kernel of the sums where the chip is empty, and
 // longer by `more` for each workgroup to a compute unit (of `resident`, beyond which it is another round); a state is written, read and written, and read.  Us of kernels, fewer
-// segments / as chosen / more: 12 x 32760 x 128, 21 / 42 / 64, 174 / 152 / 184; 12 x 4680, 8 / 19 / 37, 65 / 45 / 48; 40 x 75600, 6 / 12 / 19, 1142 / 1009 / 1092; step of 2 x 12 x 4133 x 64,
-// 11 / 33, 145 / 134; step in fp32 of 2 x 1024 x 64, 16 / 32, 54 / 44; fp32, 12 x 32760 x 128, 21 / 42, 595 / 551, 24 x 4133 x 64, 21 / 42, 93 / 71.
+// segments / as chosen / more: 12 x 32760 x 128, 21 / 40 / 64, 195 / 172 / 200; 12 x 4680, with its state, 13 / 25 / 37, 56.4 / 52.1 / 51.9; 40 x 75600, 6 / 12 / 19, 1176 / 998 / 1099;
+// prompts, 4 x 32 x 2048, 2 / 4 / 8, 127 / 107 / 132; step of 12 x 32760 x 128, 21 both ways / 40 forward and 14 backward / 40 both ways, 614 / 580 / 623; step of 2 x 12 x 4133 x 64, 10 both
+// ways / 22 and 10 / 33 both ways, 114 / 108 / 123; fp32, 12 x 32760 x 128, 21 / 41 / 64, 630 / 551 / 590; 24 x 4133 x 64, 21 / 33 / 64, 94 / 71 / 83; step of 2 x 1024 x 64, 16 / 32, 53 / 41.
 struct ChunkTimes {
   float rows, sums, more;
   int resident, chunk;

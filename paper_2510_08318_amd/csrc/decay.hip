@@ -51,9 +51,8 @@ void backward_passes(const Args& a, float* parts, Pass& dq, Pass& dv, Pass& dk) 
   dv.orow = dk.orow = Rows{(size_t)a.c.H * a.c.n * D, (size_t)a.c.n * D, (size_t)D};
 }
 
-// Tokens up to which the recurrence is taken token by token.  Us a call, so / in chunks: bf16, 4 x 32 states of 128 x 128, 8 tokens 12.7 / 14.2, 16 17.9 / 13.3; 32 x 32 states, 8 tokens
-// 44.8 / 41.6, 16 63 / 43; fp32, 4 x 32 states, 8 13.2 / -, 12 15.2 / -, 16 18.5 / 16.7, 24 24 / 16.4; bf16 in fp32 arithmetic as fp32,
-// with chunks that take longer.
+// Tokens up to which the recurrence is taken token by token.  Us of kernels, so / in chunks: bf16, 4 x 32 states of 128 x 128, 8 tokens 12.3 / 14.1, 16 18.7 / 14.4; 32 x 32 states, 8
+// tokens 45.2 / 43.7, 16 65 / 45; fp32, 4 x 32 states, 8 12.2 / 16.8, 12 15.3 / 16.1, 16 18.1 / 17.1, 24 24.7 / 16.9; bf16 in fp32 arithmetic as fp32, with chunks that take longer.
 constexpr int step_tokens(int dtype) { return dtype == LINATTN_BF16 ? 8 : dtype == LINATTN_F32 ? 12 : 16; }
 
 struct Layout {
@@ -96,7 +95,7 @@ hipError_t launch_states(const SumArgs& sums, const ScanArgs& scan, hipStream_t 
   else {
     auto go = [&](auto pieces, auto stream) { return launch<&decay_sum_kernel<D, decltype(pieces)::value, decltype(stream)::value>>(sums, sums.c, sums.plan, sums.passes, 256, sum_lds<D>(), s); };
     // What it reads is read again by the rows kernel, from the last-level cache of 256 MB as far as it has room.  Us of both, loads that stay there / that do not: 12 x 32760 x 128 (201 MB)
-    // 154 / 154, 40 x 75600 x 128 (1550 MB) 940 / 905.
+    // 157 to 164 / 158 to 162, a step of 30 x 17550 x 64 (135 MB forward) 365 / 372, 40 x 75600 x 128 (1550 MB) 1009 / 983.
     const bool big = (double)sums.c.B * sums.c.n * D * 4. * (sums.passes * (sums.c.H / sums.pass[0].b.group + sums.c.H / sums.pass[0].c.group) / 2) > 256e6;
     using std::integral_constant;
     if (whole) e = big ? go(integral_constant<int, 3>{}, std::true_type{}) : go(integral_constant<int, 3>{}, std::false_type{});

@@ -1,8 +1,9 @@
 // The passes of decay.h for fp32 tensors, on v_mfma_f32_32x32x2_f32.  Chunks of kChunkF32 tokens; a wavefront has 32 columns of the state.
 //   lane l = (m, g), m = l % 32, g = l / 32.  A: A[m][g], B: B[g][m], D: rows 8 (r / 4) + 4 g + r % 4 of column m
 // so register r of an accumulator is, as it lies, the operand of a step over rows 8 (r / 4) + r % 4 and that + 4.
-// These instructions bound it: 12 x 32760 x 128 takes 551 us where they take 290 and the bytes 137, a step of 2 x 1024 x 64 41 (rows 8, sums 6, states between 6.5, twice).  (bf16 tensors in
-// fp32 arithmetic are on the bf16 instructions, three pieces to an fp32 number, in 245; of fp32 tensors both factors of a product would be three, six products to one.)
+// 12 x 32760 x 128 takes 557 us: these instructions alone 290, the bytes 137, and the rest is waits of a chunk between its barriers (loads, the scores' sum through LDS) that the other
+// workgroups of the compute unit do not fill.  A step of 2 x 1024 x 64 41 (rows 8, sums 6, states between 6, twice).  (bf16 tensors in fp32 arithmetic are on the bf16 instructions, three
+// pieces to an fp32 number, in 250; of fp32 tensors both factors of a product would be three, six products to one.)
 #pragma once
 #include "decay_rows.h"
 
@@ -124,7 +125,7 @@ __global__ __launch_bounds__(2 * D) void decay_sum_f32_kernel(SumArgs a) {
 // Rows of a segment, as decay_rows_kernel: every wavefront takes 32 channels of the scores a_i . b_j of all pairs, and their sum through LDS gives it all of them, where the product with c_j
 // wants them.  Tiles once, the next chunk's in registers on the way, and weights from a table in LDS, so that two workgroups fit a compute unit at d 128 and four at 64, and fill each
 // other's waits: 12 x 32760 x 128 419 us with one, 386 with two.  (A workgroup of d 64 has two wavefronts; two such workgroups on a compute unit may share two of its four SIMDs: 2 x 12 x 4133
-// x 64 60 us with as many segments as that fills, 42 with twice as many.)
+// x 64 60 us with as many segments as that fills, 42 with half as many again.)  At d 128 one vector register is spilled.
 template <int D>
 __global__ __launch_bounds__(2 * D, 2) void decay_rows_f32_kernel(RowArgs a) {
   using Tile_ = TileF32<D>;

